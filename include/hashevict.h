@@ -178,6 +178,97 @@ size_t he_workspace_bytes(const he_config* cfg, int32_t max_prompt_len);
  */
 int he_attend(const he_config* cfg, const he_cache* cache, const void* q, float* out, void* stream);
 
+/*
+ * Rotary positions. he_prefill_compress and he_decode_step take queries and keys that have been rotated by their positions;
+ * these calls rotate them. The first `channels` (r) channels of a row form r/2 pairs, (i, i + r/2) or, with `interleaved`,
+ * (2i, 2i + 1); the pair (a, c) of a row at position p becomes
+ *   amplitude * (a cos(p f_i) - c sin(p f_i), c cos(p f_i) + a sin(p f_i)),
+ * the channels from r on are copied. Frequencies are held as turns per position in 64-bit fixed point, so p f_i is reduced
+ * modulo one turn exactly for every int32 position (fp32 angles would be off by 6e-8 of up to 2^31 radians); the rotation is
+ * computed in fp32 and rounded once. The struct holds no pointers: fill it once, keep it where it suits, pass it by address.
+ */
+#define HE_ROTARY_MAX_PAIRS 128
+typedef struct he_rotary {
+  int32_t channels;                    /* r: even, 2..head_dim */
+  int32_t interleaved;                 /* 0: pairs (i, i + r/2), 1: pairs (2i, 2i + 1) */
+  float amplitude;                     /* factor on both components of a rotated pair */
+  int32_t reserved;                    /* 0 */
+  uint64_t turns[HE_ROTARY_MAX_PAIRS]; /* f_i / (2 pi) modulo 1, times 2^64 */
+} he_rotary;
+
+/* How the frequencies f_i = base^(-2i/r) are stretched for contexts longer than the `length` they were trained for:
+ *   LINEAR  f_i / factor
+ *   NTK     base * factor^(r/(r-2)) in place of base (r > 2)
+ *   YARN    f_i / factor for pairs that make fewer than `low` turns over `length`, f_i for those that make more than `high`, a linear
+ *           ramp over the pair index between them; amplitude 0.1 ln(factor) + 1
+ *   BANDS   with n = length * f_i / (2 pi) turns: f_i / factor for n <= low, f_i for n >= high, a mix linear in n between them
+ */
+enum { HE_ROTARY_PLAIN = 0, HE_ROTARY_LINEAR = 1, HE_ROTARY_NTK = 2, HE_ROTARY_YARN = 3, HE_ROTARY_BANDS = 4 };
+
+/* Fills `out` (host). factor >= 1; length, low, high are read for YARN and BANDS only. he_rotary_init_frequencies takes the r/2
+ * frequencies themselves (host, radians per position, finite) and any finite amplitude. */
+int he_rotary_init(he_rotary* out, int32_t channels, int32_t interleaved, double base, int32_t stretch, double factor, double length,
+                   double low, double high);
+int he_rotary_init_frequencies(he_rotary* out, int32_t channels, int32_t interleaved, const double* frequencies, double amplitude);
+
+/*
+ * he_rotate_prompt - rotates the rows of a batch of prompts: q [B, Hkv*G, N, d] and k [B, Hkv, N, d] in the dtype of cfg, addressed
+ * like those of he_prefill_compress, into q_out and k_out of the same shapes with strides of their own. Row n of sequence s
+ * is rotated by positions[s * max_prompt_len + n] (device int32 [B, max_prompt_len], any value), or by n where positions is NULL.
+ * Rows n >= prompt_len[s] are neither read nor written (prompt_len NULL: every row is taken). An output may be its input
+ * (same address, same strides), not overlap it otherwise. q and q_out may both be NULL, and so may k and k_out.
+ */
+int he_rotate_prompt(const he_config* cfg, const he_rotary* rotary, const void* q, const void* k, const int64_t q_strides[3],
+                     const int64_t k_strides[3], const int32_t* positions, const int32_t* prompt_len, int32_t max_prompt_len, void* q_out,
+                     void* k_out, const int64_t q_out_strides[3], const int64_t k_out_strides[3], void* stream);
+
+/*
+ * he_rotate_step - the same for the one new token per sequence that the next he_decode_step will take: q [B, Hkv*G, d], k [B, Hkv, d]
+ * with element strides (sequence, head), each row rotated by the next_pos of its unit, which the call reads on the device.
+ * Nothing of the cache but next_pos is touched.
+ */
+int he_rotate_step(const he_config* cfg, const he_rotary* rotary, const he_cache* cache, const void* q, const void* k,
+                   const int64_t q_strides[2], const int64_t k_strides[2], void* q_out, void* k_out, const int64_t q_out_strides[2],
+                   const int64_t k_out_strides[2], void* stream);
+
+/*
+ * What the scores of an attention call go through before the softmax. A query at position t gives the key at position p
+ *   x = q . k * scale;   cap > 0: x <- cap * tanh(x / cap);   slopes: x <- x - slopes[h * G + g] * |t - p|
+ * and does not see it at all where a mask hides it. A query that sees no key gives zeros.
+ */
+typedef struct he_score_mod {
+  float scale;         /* > 0, or 0 for 1 / sqrt(d) */
+  float cap;           /* > 0, or 0 for none */
+  int32_t window;      /* w > 0: positions p <= t - w are hidden; 0 for none */
+  int32_t reserved;    /* 0 */
+  const float* slopes; /* device fp32 [Hkv*G], or NULL for none */
+} he_score_mod;
+
+/*
+ * he_attend_prompt - attention of a batch of prompts over themselves, as a layer computes it next to he_prefill_compress:
+ *   out[s, h*G + g, i, :] = sum_j softmax_j( x_ij ) * V[s, h, j, :],   i, j < N_s = prompt_len[s],
+ * with x_ij as in he_score_mod (positions t = i, p = j). Token i sees the tokens j of one interval:
+ *   max(doc_start[s * max_prompt_len + i], i - w + 1, 0) <= j < min(N_s, max(i + 1, prefix_len[s])),
+ * that is the past and itself, within its document and the window, and every token of the prefix. doc_start (device int32
+ * [B, max_prompt_len]), prefix_len (device int32 [B]) and mod may be NULL; any values are allowed.
+ * q: [B, Hkv*G, N, d], k, v: [B, Hkv, N, d], out: as q, all in the dtype of cfg, with element strides (batch, head, token), channels
+ * contiguous, rows 16-byte aligned. Rows i >= N_s of out are left as they were; rows of q, k, v behind N_s may hold anything. out
+ * may not overlap q, k or v. Sums and the softmax are carried in fp32. bf16 with head_dim <= 128 runs on the tensor cores, where the weights
+ * are rounded to bf16 before they meet V (up to 2^-8 of each weight; their sum is taken before); all else is fp32 throughout.
+ */
+int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
+                     const int64_t kv_strides[3], const int32_t* prompt_len, int32_t max_prompt_len, const int32_t* doc_start,
+                     const int32_t* prefix_len, void* out, const int64_t out_strides[3], void* stream);
+
+/*
+ * he_attend_scored - he_attend with he_score_mod: the single-token form of the same attention over the compressed cache. The query is
+ * at position t = next_pos - 1 of its unit (the token that the last he_decode_step inserted) and slot j at pos[j]; slots with
+ * pos[j] < first_pos[s] (device int32 [B], or NULL; the start of the token's document) are hidden, and so are those that the window
+ * leaves behind. mod NULL: as he_attend. Layouts and precision are those of he_attend.
+ */
+int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out,
+                     void* stream);
+
 /* he_reset - empty every unit: fill = 0, next_pos = 0, pos = -1, codes = 0, scores = 0. K/V are left as they are. */
 int he_reset(const he_config* cfg, const he_cache* cache, void* stream);
 

@@ -35,10 +35,25 @@ class he_cache(ctypes.Structure):
                 ("k_cache", "v_cache", "codes", "scores", "pos", "budget", "fill", "next_pos", "W", "budget_host", "step_scratch")]
 
 
+HE_ROTARY_MAX_PAIRS = 128
+_STRETCH = {"linear": 1, "ntk": 2, "yarn": 3, "bands": 4}  # HE_ROTARY_*
+
+
+class he_rotary(ctypes.Structure):
+    _fields_ = [("channels", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("turns", ctypes.c_uint64 * HE_ROTARY_MAX_PAIRS)]
+
+
+class he_score_mod(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p)]
+
+
 EXPORTS = (
     "he_hash_keys", "he_decode_step", "he_prefill_compress", "he_workspace_bytes", "he_reset",
     "he_decode_staging_bytes", "he_decode_step_host", "he_decode_step_host_enqueue", "he_decode_step_host_block_enqueue", "he_decode_host_block_bytes", "he_prefill_staging_bytes", "he_prefill_compress_host",
     "he_prefill_compress_noalloc", "he_attend", "he_prefill_oneshot", "he_oneshot_workspace_bytes", "he_prefill_oneshot_l2", "he_attention_loss", "he_decode_step_l2", "he_step_scratch_bytes", "he_device_error_count", "he_prefill_phase_events", "he_last_error",
+    "he_rotary_init", "he_rotary_init_frequencies", "he_rotate_prompt", "he_rotate_step", "he_attend_prompt", "he_attend_scored",
 )
 
 _lib = None
@@ -93,6 +108,16 @@ def lib():
     L.he_device_error_count.restype = ctypes.c_int
     L.he_last_error.argtypes = []
     L.he_last_error.restype = ctypes.c_char_p
+    i64p, f64 = ctypes.POINTER(i64), ctypes.c_double
+    rotp, modp = ctypes.POINTER(he_rotary), ctypes.POINTER(he_score_mod)
+    L.he_rotary_init.argtypes = [rotp, i32, i32, f64, i32, f64, f64, f64, f64]
+    L.he_rotary_init_frequencies.argtypes = [rotp, i32, i32, ctypes.POINTER(f64), f64]
+    L.he_rotate_prompt.argtypes = [cfgp, rotp, vp, vp, i64p, i64p, vp, vp, i32, vp, vp, i64p, i64p, vp]
+    L.he_rotate_step.argtypes = [cfgp, rotp, cap, vp, vp, i64p, i64p, vp, vp, i64p, i64p, vp]
+    L.he_attend_prompt.argtypes = [cfgp, modp, vp, vp, vp, i64p, i64p, vp, i32, vp, vp, vp, i64p, vp]
+    L.he_attend_scored.argtypes = [cfgp, cap, modp, vp, vp, vp, vp]
+    for name in ("he_rotary_init", "he_rotary_init_frequencies", "he_rotate_prompt", "he_rotate_step", "he_attend_prompt", "he_attend_scored"):
+        getattr(L, name).restype = ctypes.c_int
     for name in ("he_hash_keys", "he_decode_step", "he_prefill_compress", "he_reset", "he_decode_step_host", "he_decode_step_host_enqueue",
                  "he_prefill_compress_host", "he_prefill_compress_noalloc"):
         getattr(L, name).restype = ctypes.c_int
@@ -160,6 +185,52 @@ def decode_staging_bytes(cfg: he_config) -> int:
 
 def prefill_staging_bytes(cfg: he_config, max_prompt_len: int) -> int:
     return lib().he_prefill_staging_bytes(ctypes.byref(cfg), max_prompt_len)
+
+
+class Rotary:
+    """he_rotary: the frequencies of rotary positions, kept by the caller and passed to rotate_prompt / rotate_step.
+
+    The first `channels` channels of a row (all of `head_dim` by default) are rotated, in pairs (i, i + channels/2) or, interleaved,
+    (2i, 2i + 1), with frequencies base^(-2i/channels). scaling stretches them for long contexts: {"kind": "linear" | "ntk", "factor"},
+    {"kind": "yarn" | "bands", "factor", "length", "low", "high"} (low and high default to 1 and 32 turns for yarn, 1 and 4 for bands).
+    `frequencies` (radians per position, channels/2 of them) and `amplitude` replace base and scaling altogether."""
+
+    def __init__(self, head_dim, channels=None, base=10000.0, interleaved=False, scaling=None, frequencies=None, amplitude=1.0):
+        self.head_dim, self.channels, self.interleaved = int(head_dim), int(head_dim if channels is None else channels), bool(interleaved)
+        if self.channels > self.head_dim:
+            raise HashEvictError(f"rotary channels {self.channels} > head_dim {self.head_dim}")
+        self.raw = he_rotary()
+        if frequencies is not None:
+            if scaling is not None:
+                raise HashEvictError("frequencies are given as they are: no scaling beside them")
+            f = [float(x) for x in frequencies]
+            if 2 * len(f) != self.channels:
+                raise HashEvictError(f"{len(f)} frequencies for {self.channels} rotary channels")
+            _check(lib().he_rotary_init_frequencies(ctypes.byref(self.raw), self.channels, self.interleaved, (ctypes.c_double * len(f))(*f),
+                                                    float(amplitude)))
+            return
+        if float(amplitude) != 1.0:
+            raise HashEvictError("an amplitude goes with frequencies")
+        s = dict(scaling or {})
+        kind = s.pop("kind", None)
+        if kind is not None and kind not in _STRETCH or kind is None and s:
+            raise HashEvictError(f"rotary scaling {scaling!r}: kind is one of {sorted(_STRETCH)}")
+        if set(s) - ({"factor", "length", "low", "high"} if kind in ("yarn", "bands") else {"factor"}) or kind is not None and "factor" not in s:
+            raise HashEvictError(f"rotary scaling {scaling!r}")
+        _check(lib().he_rotary_init(ctypes.byref(self.raw), self.channels, self.interleaved, float(base), _STRETCH.get(kind, 0),
+                                    float(s.get("factor", 1.0)), float(s.get("length", 0.0)), float(s.get("low", 1.0)),
+                                    float(s.get("high", 4.0 if kind == "bands" else 32.0))))
+
+
+class ScoreMod:
+    """he_score_mod: what scores go through before the softmax. scale (0: 1/sqrt(d)), softcap c (x -> c tanh(x / c), 0: none), window w
+    (the newest w positions are seen, 0: all), slopes (device fp32 [H*G]: x - slope * distance). slopes is kept alive here."""
+
+    def __init__(self, scale=0.0, softcap=0.0, window=0, slopes=None):
+        if slopes is not None and not (slopes.is_cuda and slopes.dtype == torch.float32 and slopes.is_contiguous()):
+            raise HashEvictError("slopes must be a contiguous fp32 tensor on the device")
+        self.slopes = slopes
+        self.raw = he_score_mod(float(scale), float(softcap), int(window), 0, _ptr(slopes))
 
 
 class HashEvictCache:
@@ -233,6 +304,114 @@ class HashEvictCache:
         if out is None:
             out = torch.empty((self.B, self.H * self.G, self.d), dtype=torch.float32, device=self.k_cache.device)
         _check(lib().he_attend(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(out), _stream(stream)))
+        return out
+
+    # --- the layer around the cache: rotary positions, attention with modified scores ------------------
+    def _tensor(self, name, t, shape, dtype, rows=False):
+        """A tensor of a call: its device, type and shape; `rows`: any strides but for the channels, else contiguous."""
+        if t.device != self.k_cache.device or t.dtype != dtype or t.shape != shape:
+            raise HashEvictError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, not {tuple(shape)} {dtype} on {self.k_cache.device}")
+        if not (t.stride(-1) == 1 if rows else t.is_contiguous()):
+            raise HashEvictError(f"{name}: " + ("channels must be contiguous" if rows else "must be contiguous"))
+        return t
+
+    def _strides(self, t):
+        """Element strides of all axes but the channels; an axis of one (whose stride says nothing) takes a row's."""
+        n = t.dim() - 1
+        return (ctypes.c_int64 * n)(*[st if sz > 1 else self.d for sz, st in zip(t.shape[:n], t.stride())])
+
+    def _call(self, fn, *args, stream=None):
+        dev = self.k_cache.device
+        if dev.index == torch.cuda.current_device():
+            _check(fn(*args, _stream(stream)))
+        else:  # the library launches on the current device
+            with torch.cuda.device(dev):
+                _check(fn(*args, _stream(stream)))
+
+    def _rotate(self, rotary, q, k, q_out, k_out, tokens):
+        """Checked arguments of a rotation: (q, its strides, its output, the output's strides) and the same of k."""
+        if rotary.head_dim != self.d:
+            raise HashEvictError(f"rotary of head_dim {rotary.head_dim} for rows of {self.d}")
+        sides = []
+        for name, x, out, heads in (("q", q, q_out, self.H * self.G), ("k", k, k_out, self.H)):
+            if x is None:
+                if out is not None:
+                    raise HashEvictError(f"{name}_out without {name}")
+                sides.append((None, None, None, None))
+                continue
+            shape = (self.B, heads) + tokens + (self.d,)
+            self._tensor(name, x, shape, self.dtype, rows=True)
+            if out is None:
+                out = torch.empty(shape, dtype=self.dtype, device=x.device)
+            self._tensor(name + "_out", out, shape, self.dtype, rows=True)
+            sides.append((x, self._strides(x), out, self._strides(out)))
+        return sides
+
+    def rotate_prompt(self, rotary, q, k, prompt_len=None, positions=None, q_out=None, k_out=None, stream=None):
+        """he_rotate_prompt. q [B, H*G, N, d], k [B, H, N, d] (any strides on the first three axes; either may be None), positions
+        int32 [B, N] (None: 0, 1, ...), prompt_len int32 [B] (None: every row). Returns (q_out, k_out); q_out = q works in place.
+        Rows behind a prompt's end are left as they were."""
+        if q is None and k is None:
+            raise HashEvictError("neither q nor k is given")
+        n = (k if q is None else q).shape[2]
+        (q, qs, q_out, qos), (k, ks, k_out, kos) = self._rotate(rotary, q, k, q_out, k_out, (n,))
+        if positions is not None:
+            self._tensor("positions", positions, (self.B, n), torch.int32)
+        if prompt_len is not None:
+            self._tensor("prompt_len", prompt_len, (self.B,), torch.int32)
+        self._call(lib().he_rotate_prompt, ctypes.byref(self.cfg), ctypes.byref(rotary.raw), _ptr(q), _ptr(k), qs, ks, _ptr(positions),
+                   _ptr(prompt_len), n, _ptr(q_out), _ptr(k_out), qos, kos, stream=stream)
+        return q_out, k_out
+
+    def rotate_step(self, rotary, q, k, q_out=None, k_out=None, stream=None):
+        """he_rotate_step: q [B, H*G, d] and k [B, H, d] of the next decode_step, rotated by the cache's next_pos. Returns (q_out, k_out)."""
+        (q, qs, q_out, qos), (k, ks, k_out, kos) = self._rotate(rotary, q, k, q_out, k_out, ())
+        self._call(lib().he_rotate_step, ctypes.byref(self.cfg), ctypes.byref(rotary.raw), ctypes.byref(self.ca), _ptr(q), _ptr(k), qs, ks,
+                   _ptr(q_out), _ptr(k_out), qos, kos, stream=stream)
+        return q_out, k_out
+
+    def _mod(self, mod):
+        if mod is None:
+            return None
+        if mod.slopes is not None:
+            self._tensor("slopes", mod.slopes, (self.H * self.G,), torch.float32)
+        return ctypes.byref(mod.raw)
+
+    def attend_prompt(self, q, k, v, prompt_len, mod=None, doc_start=None, prefix_len=None, out=None, stream=None):
+        """he_attend_prompt: attention of the prompts over themselves. q [B, H*G, N, d], k / v [B, H, N, d] (any strides on the first
+        three axes), prompt_len int32 [B], mod a ScoreMod, doc_start int32 [B, N] (first position of each token's document),
+        prefix_len int32 [B] (tokens that all of a prompt's tokens see). Returns out [B, H*G, N, d] in the dtype of q; rows behind a
+        prompt's end are left as they were (undefined in an `out` that this call makes)."""
+        n = q.shape[2]
+        self._tensor("q", q, (self.B, self.H * self.G, n, self.d), self.dtype, rows=True)
+        self._tensor("k", k, (self.B, self.H, n, self.d), self.dtype, rows=True)
+        self._tensor("v", v, (self.B, self.H, n, self.d), self.dtype, rows=True)
+        ks = self._strides(k)
+        if ks[:] != self._strides(v)[:]:
+            raise HashEvictError("k and v must have the same strides")
+        if out is None:
+            out = torch.empty((self.B, self.H * self.G, n, self.d), dtype=self.dtype, device=q.device)
+        self._tensor("out", out, q.shape, self.dtype, rows=True)
+        self._tensor("prompt_len", prompt_len, (self.B,), torch.int32)
+        if doc_start is not None:
+            self._tensor("doc_start", doc_start, (self.B, n), torch.int32)
+        if prefix_len is not None:
+            self._tensor("prefix_len", prefix_len, (self.B,), torch.int32)
+        self._call(lib().he_attend_prompt, ctypes.byref(self.cfg), self._mod(mod), _ptr(q), _ptr(k), _ptr(v), self._strides(q), ks,
+                   _ptr(prompt_len), n, _ptr(doc_start), _ptr(prefix_len), _ptr(out), self._strides(out), stream=stream)
+        return out
+
+    def attend_scored(self, q, mod=None, first_pos=None, out=None, stream=None):
+        """he_attend_scored: attend with a ScoreMod. q [B, H*G, d] -> fp32 [B, H*G, d]; the query is the token that the last decode_step
+        inserted, first_pos int32 [B] the first position that it sees (the start of its document)."""
+        self._tensor("q", q, (self.B, self.H * self.G, self.d), self.dtype)
+        if out is None:
+            out = torch.empty((self.B, self.H * self.G, self.d), dtype=torch.float32, device=q.device)
+        self._tensor("out", out, q.shape, torch.float32)
+        if first_pos is not None:
+            self._tensor("first_pos", first_pos, (self.B,), torch.int32)
+        self._call(lib().he_attend_scored, ctypes.byref(self.cfg), ctypes.byref(self.ca), self._mod(mod), _ptr(q), _ptr(first_pos), _ptr(out),
+                   stream=stream)
         return out
 
     def workspace(self, max_prompt_len):

@@ -4,6 +4,8 @@ from __future__ import annotations
 import glob
 import os
 import subprocess
+import time
+from concurrent.futures import ThreadPoolExecutor
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
@@ -14,7 +16,7 @@ _HEADERS = sorted(glob.glob(os.path.join(_ROOT, "include", "*.h")) + glob.glob(o
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC",
 ]
 
 
@@ -24,10 +26,28 @@ def nvcc_path() -> str:
 
 
 DEBUG_LIB_PATH = os.path.join(_PKG, "libhashevict_debug.so")
+_OBJ_DIR = os.path.join(_PKG, "build")
+
+
+def _object(source: str, debug: bool, force: bool, verbose: bool) -> str:
+    """One translation unit; compiled again when it or a header that it read the last time is newer than its object."""
+    obj = os.path.join(_OBJ_DIR, os.path.basename(source)[:-3] + ("_debug.o" if debug else ".o"))
+    deps = obj[:-2] + ".d"
+    if not force and os.path.exists(obj) and os.path.exists(deps):
+        read = open(deps).read().replace("\\\n", " ").split(":", 1)[1].split()
+        if all(os.path.exists(p) and os.path.getmtime(p) <= os.path.getmtime(obj) for p in read + [os.path.abspath(__file__)]):
+            return obj
+    os.makedirs(_OBJ_DIR, exist_ok=True)
+    tmp, began = obj + f".tmp{os.getpid()}", time.time()
+    subprocess.run([nvcc_path()] + NVCC_FLAGS + (["-DHE_BOUNDS_CHECK"] if debug else []) + (["-Xptxas", "-v"] if verbose else []) +
+                   ["-I", os.path.join(_ROOT, "include"), "-MD", "-MF", deps, "-MT", "object", "-c", "-o", tmp, source], check=True)
+    os.utime(tmp, (began, began))  # a source edited meanwhile is newer
+    os.replace(tmp, obj)
+    return obj
 
 
 def build_cuda(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    """Compile csrc/*.cu into libhashevict.so; rebuilds only when a source or header is newer.
+    """Compile csrc/*.cu into libhashevict.so, the translation units side by side; rebuilds only when a source or header is newer.
 
     debug=True builds libhashevict_debug.so with -DHE_BOUNDS_CHECK instead: every slot and token index is range-checked
     before it is used as an address, a failed check skips the access and raises he_device_error_count(). The binding
@@ -36,9 +56,11 @@ def build_cuda(force: bool = False, verbose: bool = False, debug: bool = False) 
     deps = _SOURCES + _HEADERS
     if not force and os.path.exists(out) and all(os.path.getmtime(out) >= os.path.getmtime(p) for p in deps):
         return out
+    began = time.time()
+    with ThreadPoolExecutor(len(_SOURCES)) as pool:
+        objects = list(pool.map(lambda s: _object(s, debug, force, verbose), _SOURCES))
     tmp = out + f".tmp{os.getpid()}"
-    cmd = [nvcc_path()] + NVCC_FLAGS + (["-DHE_BOUNDS_CHECK"] if debug else []) + (["-Xptxas", "-v"] if verbose else []) + \
-        ["-I", os.path.join(_ROOT, "include"), "-o", tmp] + _SOURCES
-    subprocess.run(cmd, check=True)
+    subprocess.run([nvcc_path()] + NVCC_FLAGS + ["-shared", "-o", tmp] + objects, check=True)
+    os.utime(tmp, (began, began))
     os.replace(tmp, out)
     return out

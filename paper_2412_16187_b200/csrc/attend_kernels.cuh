@@ -16,11 +16,20 @@
 
 namespace he {
 
+// he_score_mod on the device (he_attend_scored): scores in log2 units, cap = 0 and window = 0 for none.
+struct AttendMod {
+  float scale_log2, cap_log2, inv_cap;  // x = scale_log2 * q.k, or cap_log2 * tanh(inv_cap * q.k)
+  int window;
+  const float* slopes;       // [Hkv*G] or null
+  const int32_t* first_pos;  // [B] or null
+};
+
 struct AttendArgs {
   he_config cfg;
   he_cache ca;
   const void* q;  // [B, Hkv*G, d]
   float* out;     // [B, Hkv*G, d] fp32
+  AttendMod mod;  // read by the kernels with MOD only
 };
 
 constexpr int kAttendThreads = 256;
@@ -186,16 +195,20 @@ struct AttendRing {
   static constexpr int kBytes = NW * kBufs * kItemBytes;  // 24 KB per warp
 };
 
-template <int D, int NW>
+// With MOD the scores go through he_score_mod: four more bytes a slot (its position, fetched a group ahead into registers) beside 4 D
+// of K and V, and masked slots' V rows are cleared in the ring, as they may hold anything. d may then be below D: the tensor maps fill the channels
+// from d on with zeros.
+template <int D, int NW, bool MOD>
 __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const AttendArgs a, const int S, const __grid_constant__ CUtensorMap kmap,
                                                                      const __grid_constant__ CUtensorMap vmap) {
   using Ring = AttendRing<D, NW>;
   extern __shared__ __align__(16) unsigned char attend_smem_raw[];
   __shared__ __align__(8) unsigned long long merge_bar, ring_bar[NW][Ring::kBufs];
-  constexpr int d = D, CPR = D / 8;        // 16-byte chunks per row
+  constexpr int CPR = D / 8;               // 16-byte chunks per row in a ring buffer
   constexpr int NC = D / 32, NH = D / 64;  // chunks of a K row per lane, of a V row per lane
   constexpr int NBUF = Ring::kBufs, GRP = kAttendGroup;
   const he_config& cfg = a.cfg;
+  const int d = MOD ? cfg.head_dim : D;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
   const int rank = blockIdx.x % S;
   const int unit = blockIdx.y * cfg.n_kv_heads + blockIdx.x / S;
@@ -232,10 +245,10 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   // with three, which the copy engine has not worked off when the wait returns.
   if (NW == 8 && lane == 0) {
     const int rows = min(min(__ldcg(a.ca.fill + unit), cfg.max_budget) - first, GRP);
-    const size_t at = ((size_t)unit * cfg.max_budget + first) * D * 2;
+    const size_t at = ((size_t)unit * cfg.max_budget + first) * d * 2;
     if (rows > 0) {
-      l2_prefetch_bulk(static_cast<const char*>(a.ca.k_cache) + at, (uint32_t)rows * D * 2);
-      l2_prefetch_bulk(static_cast<const char*>(a.ca.v_cache) + at, (uint32_t)rows * D * 2);
+      l2_prefetch_bulk(static_cast<const char*>(a.ca.k_cache) + at, (uint32_t)rows * d * 2);
+      l2_prefetch_bulk(static_cast<const char*>(a.ca.v_cache) + at, (uint32_t)rows * d * 2);
     }
   }
   griddep_wait();
@@ -263,10 +276,26 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     uint4 t = make_uint4(0u, 0u, 0u, 0u);
-    if (gid < G) t = static_cast<const uint4*>(a.q)[((size_t)unit * G + gid) * CPR + 2 * tig + (c & 1) + 8 * (c >> 1)];
+    const int chunk = 2 * tig + (c & 1) + 8 * (c >> 1);
+    if (gid < G && (!MOD || chunk < d / 8)) t = static_cast<const uint4*>(a.q)[((size_t)unit * G + gid) * (d / 8) + chunk];
     qf[2 * c][0] = t.x, qf[2 * c][1] = t.y, qf[2 * c + 1][0] = t.z, qf[2 * c + 1][1] = t.w;
   }
-  const float scale = rsqrtf((float)d) * kLog2e;
+  const float scale = MOD ? a.mod.scale_log2 : rsqrtf((float)d) * kLog2e;
+  float slope = 0.f;     // MOD: log2 units per position
+  int now = 0, low = 0;  // the query's position, the first one it sees
+  if (MOD) {
+    if (a.mod.slopes != nullptr && gid < G) slope = a.mod.slopes[(unit % cfg.n_kv_heads) * G + gid] * kLog2e;
+    now = __ldcg(a.ca.next_pos + unit) - 1;
+    if (a.mod.window > 0) low = max(low, now - a.mod.window + 1);
+    if (a.mod.first_pos != nullptr) low = max(low, a.mod.first_pos[blockIdx.y]);
+  }
+  const int32_t* slot_pos = a.ca.pos + (size_t)unit * cfg.max_budget + 2 * tig;
+  int2 ahead[4];  // positions of this lane's slots 8 i + 2 tig, + 1 of the next group
+  auto fetch_pos = [&](int g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ahead[i] = g + 8 * i + 2 * tig < fill ? __ldcg(reinterpret_cast<const int2*>(slot_pos + g + 8 * i)) : make_int2(-1, -1);
+  };
+  if (MOD) fetch_pos(first);
   float m = -INFINITY, l = 0.f;
   float o[8 * NH][4];
 #pragma unroll
@@ -316,16 +345,32 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
     // This lane: head gid, slots g0 + 8 i + 2 tig, + 1.
     float x[8];
     float gm = -INFINITY;
+    uint32_t seen = 0u;  // MOD: the group's visible slots
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        x[2 * i + e] = g0 + 8 * i + 2 * tig + e < fill ? (sa[i][e] + sb[i][e]) * scale : -INFINITY;
+        const int j = 8 * i + 2 * tig + e;
+        bool ok_j = g0 + j < fill;
+        float s = (sa[i][e] + sb[i][e]) * scale;
+        if (MOD) {
+          const int p = e ? ahead[i].y : ahead[i].x;
+          if (a.mod.cap_log2 > 0.f) s = a.mod.cap_log2 * tanhf((sa[i][e] + sb[i][e]) * a.mod.inv_cap);
+          s -= slope * (float)abs(now - p);
+          ok_j = ok_j && p >= low;
+          seen |= (uint32_t)ok_j << j;
+        }
+        x[2 * i + e] = ok_j ? s : -INFINITY;
         gm = fmaxf(gm, x[2 * i + e]);
       }
+    if (MOD) {
+      seen = __reduce_or_sync(0xFFFFFFFFu, seen);
+      if (t + 2 < items) fetch_pos(g0 + stride);
+    }
     gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 1));
-    gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 2));  // finite: slot g0 is valid
-    const float mn = fmaxf(m, gm);
+    gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 2));  // without MOD finite: slot g0 is valid
+    const float mx = fmaxf(m, gm);
+    const float mn = MOD && mx == -INFINITY ? 0.f : mx;  // (nothing seen so far: all weights are exp2(-inf))
     const float corr = exp2f(m - mn);
     float p[8], ps = 0.f;
 #pragma unroll
@@ -333,7 +378,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
 #pragma unroll
     for (int k = 0; k < 8; k += 2) ps += p[k] + p[k + 1];
     l = l * corr + ps;
-    m = mn;
+    m = mx;
     uint32_t w[4][2];  // hi and lo halves of the weights of slots 8 i + 2 tig, + 1
 #pragma unroll
     for (int i = 0; i < 4; ++i) split_pair(p[2 * i], p[2 * i + 1], w[i][0], w[i][1]);
@@ -342,9 +387,11 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
       for (int t2 = 0; t2 < 8 * NH; ++t2) o[t2][0] *= corr, o[t2][1] *= corr, o[t2][2] *= corr, o[t2][3] *= corr;
     }
     const uint4* vr = step(t + 1);
-    if (g0 + GRP > fill) {  // rows past the fill level (weighted by zero) hold anything: make them finite
-      for (int i = lane; i < GRP * CPR; i += 32)
-        if (g0 + ((i >> 3) & (GRP - 1)) >= fill) const_cast<uint4*>(vr)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (MOD ? seen != 0xFFFFFFFFu : g0 + GRP > fill) {  // rows past the fill level or masked (weighted by zero) hold anything: make them finite
+      for (int i = lane; i < GRP * CPR; i += 32) {
+        const int row = (i >> 3) & (GRP - 1);
+        if (MOD ? !((seen >> row) & 1u) : g0 + row >= fill) const_cast<uint4*>(vr)[i] = make_uint4(0u, 0u, 0u, 0u);
+      }
       __syncwarp();
     }
 #pragma unroll
@@ -397,8 +444,9 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
 #pragma unroll
     for (int t = 0; t < 8 * NH; ++t) {
       const int h = t >> 3, e = t & 7;
-      part_o[(warp * G + gid) * d + (2 * tig + 8 * h) * 8 + e] = o[t][0] + o[t][2];
-      part_o[(warp * G + gid) * d + (2 * tig + 1 + 8 * h) * 8 + e] = o[t][1] + o[t][3];
+      const int c0 = (2 * tig + 8 * h) * 8 + e, c1 = c0 + 8;
+      if (!MOD || c0 < d) part_o[(warp * G + gid) * d + c0] = o[t][0] + o[t][2];
+      if (!MOD || c1 < d) part_o[(warp * G + gid) * d + c1] = o[t][1] + o[t][3];
     }
   }
   __syncthreads();
@@ -412,6 +460,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
 
 // ------------------------------------------------------------------------------------------------ generic
 
+template <bool MOD>
 __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const AttendArgs a) {
   extern __shared__ __align__(16) float asm_[];  // q as fp32 [G][d], then part_ml [warps][G][2], part_o [warps][G][d]
   const he_config& cfg = a.cfg;
@@ -426,7 +475,14 @@ __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const At
   for (int idx = tid; idx < G * cpr; idx += kAttendThreads)
     stage_chunk(qs + (idx / cpr) * d, static_cast<const char*>(a.q) + ((size_t)unit * G + idx / cpr) * d * es, idx % cpr, cfg.dtype);
   __syncthreads();
-  const float scale = rsqrtf((float)d) * kLog2e;
+  const float scale = MOD ? a.mod.scale_log2 : rsqrtf((float)d) * kLog2e;
+  int now = 0, low = 0;  // MOD: the query's position, the first one it sees
+  if (MOD) {
+    now = a.ca.next_pos[unit] - 1;
+    if (a.mod.window > 0) low = max(low, now - a.mod.window + 1);
+    if (a.mod.first_pos != nullptr) low = max(low, a.mod.first_pos[blockIdx.y]);
+  }
+  const float* slopes = MOD && a.mod.slopes != nullptr ? a.mod.slopes + blockIdx.x * G : nullptr;
   const char* Kb = static_cast<const char*>(a.ca.k_cache) + (size_t)unit * cfg.max_budget * d * es;
   const char* Vb = static_cast<const char*>(a.ca.v_cache) + (size_t)unit * cfg.max_budget * d * es;
   const int per = d / 32 + (d % 32 ? 1 : 0);  // channels per lane (<= 8): c = lane + 32 * i
@@ -443,6 +499,12 @@ __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const At
                                       : reinterpret_cast<const float*>(row)[c];
   };
   for (int j = warp; j < fill; j += kAttendWarps) {
+    float away = 0.f;
+    if (MOD) {
+      const int p = a.ca.pos[(size_t)unit * cfg.max_budget + j];
+      if (p < low) continue;
+      away = (float)abs(now - p) * kLog2e;
+    }
     const char* kr = Kb + (size_t)j * d * es;
     const char* vr = Vb + (size_t)j * d * es;
     float kv[kMaxDim / 32], vv[kMaxDim / 32];
@@ -462,7 +524,11 @@ __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const At
           if (i < per && c < d) dot = fmaf(qs[g * d + c], kv[i], dot);
         }
         for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, off);
-        const float sc = dot * scale;
+        float sc = dot * scale;
+        if (MOD) {
+          if (a.mod.cap_log2 > 0.f) sc = a.mod.cap_log2 * tanhf(dot * a.mod.inv_cap);
+          if (slopes != nullptr) sc -= slopes[g] * away;
+        }
         const float mn = fmaxf(m[g], sc);
         const float corr = exp2f(m[g] - mn), p = exp2f(sc - mn);  // exp2f(-inf) = 0 on the first slot
         l[g] = l[g] * corr + p;
@@ -505,7 +571,7 @@ struct LossArgs {
   float* out;          // [B, Hkv*G]
 };
 
-__global__ void __launch_bounds__(kAttendThreads) attention_loss_kernel(const LossArgs a) {
+static __global__ void __launch_bounds__(kAttendThreads) attention_loss_kernel(const LossArgs a) {
   extern __shared__ __align__(16) float lsm_[];  // q as fp32 [G][d], partials [warps][G][3], bitmap of cached positions
   const he_config& cfg = a.cfg;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -588,7 +654,7 @@ __global__ void __launch_bounds__(kAttendThreads) attention_loss_kernel(const Lo
 // The same for bf16 keys with d = 128 and G <= 8: scores of 16 tokens at a time as warp-level MMAs fed straight from
 // 16-byte global loads (the fragment scheme of attend_bf16_kernel), next group's rows requested before the current
 // group's arithmetic. Dynamic shared memory: partials [warps][G][3] floats, then the bitmap of cached positions.
-__global__ void __launch_bounds__(kAttendThreads) attention_loss_bf16_kernel(const LossArgs a) {
+static __global__ void __launch_bounds__(kAttendThreads) attention_loss_bf16_kernel(const LossArgs a) {
   extern __shared__ __align__(16) float lsm_[];
   constexpr int d = 128;
   const he_config& cfg = a.cfg;

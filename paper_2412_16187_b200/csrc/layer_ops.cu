@@ -1,0 +1,265 @@
+// What a decoder layer does around the compressed cache: rotary positions of the rows that enter it (rotary_kernels.cuh), attention of the
+// prompt over itself (prompt_attend_kernels.cuh) and the scored form of the attention over the cache (attend_kernels.cuh). Host side of these calls.
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstring>
+
+#include "attend_kernels.cuh"
+#include "common.cuh"
+#include "hashevict.h"
+#include "host_common.h"
+#include "prompt_attend_kernels.cuh"
+#include "rotary_kernels.cuh"
+
+using namespace he;
+
+int he::layer_error_count() {
+  int n = 0;
+  return cudaMemcpyFromSymbol(&n, he::g_tc_error, sizeof(int)) == cudaSuccess ? n : -1;
+}
+
+namespace {
+
+constexpr int kMaxTokens = 1 << 24;  // positions and distances are exact in fp32
+
+int check_rotary(const he_rotary* r, int d) {
+  if (r == nullptr) return fail(HE_ERR_INVALID_ARG, "rotary is null");
+  if (r->channels < 2 || r->channels % 2 != 0 || r->channels > 2 * HE_ROTARY_MAX_PAIRS)
+    return fail(HE_ERR_INVALID_ARG, "rotary channels %d are not even and in [2, %d]", r->channels, 2 * HE_ROTARY_MAX_PAIRS);
+  if (d > 0 && r->channels > d) return fail(HE_ERR_INVALID_ARG, "rotary channels %d > head_dim %d", r->channels, d);
+  return HE_OK;
+}
+
+// Element strides of 16-byte aligned rows.
+int check_strides(const char* what, const int64_t* strides, int n, int esize) {
+  if (strides == nullptr) return fail(HE_ERR_INVALID_ARG, "%s strides are null", what);
+  for (int i = 0; i < n; ++i)
+    if (strides[i] < 0 || (strides[i] * esize) % 16 != 0)
+      return fail(HE_ERR_INVALID_ARG, "%s stride %lld does not keep rows 16-byte aligned", what, (long long)strides[i]);
+  return HE_OK;
+}
+
+template <int E, int V, bool INTER>
+int launch_rotate_as(const RotateArgs& a, const he_rotary& r, dim3 grid, cudaStream_t st) {
+  return launch_pdl(rotate_kernel<E, V, INTER>, grid, kRotateThreads, 0, true, st, a, r);
+}
+
+int launch_rotate(RotateArgs a, const he_rotary& r, cudaStream_t st) {
+  const int es = esize_of(a.dtype), v = rotary_piece(r, es);
+  a.units = rotary_units(r, a.d, v);
+  const long long items = (long long)a.batch * a.tokens * a.units, blocks = (items + kRotateThreads - 1) / kRotateThreads;
+  const int all = a.heads[0] + a.heads[1];
+  if (blocks == 0 || all == 0) return HE_OK;
+  if (blocks > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld rows in one call", (long long)a.batch * a.tokens);
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  // Heads are shared out until there are enough CTAs for every SM, but a thread that has worked out its sines keeps at least four rows.
+  const long long shares = (8LL * sms + blocks - 1) / blocks;
+  a.heads_per_thread = (int)((all + shares - 1) / shares);
+  if (a.next_pos == nullptr && a.heads_per_thread < 4) a.heads_per_thread = 4;
+  if (a.heads_per_thread > all) a.heads_per_thread = all;
+  const dim3 grid((unsigned)blocks, (unsigned)((all + a.heads_per_thread - 1) / a.heads_per_thread));
+  if (grid.y > 65535) return fail(HE_ERR_UNSUPPORTED, "%d heads in one call", all);
+  if (es == 2) {
+    if (r.interleaved) return launch_rotate_as<2, 8, true>(a, r, grid, st);
+    switch (v) {
+      case 8: return launch_rotate_as<2, 8, false>(a, r, grid, st);
+      case 4: return launch_rotate_as<2, 4, false>(a, r, grid, st);
+      case 2: return launch_rotate_as<2, 2, false>(a, r, grid, st);
+      default: return launch_rotate_as<2, 1, false>(a, r, grid, st);
+    }
+  }
+  if (r.interleaved) return launch_rotate_as<4, 4, true>(a, r, grid, st);
+  switch (v) {
+    case 4: return launch_rotate_as<4, 4, false>(a, r, grid, st);
+    case 2: return launch_rotate_as<4, 2, false>(a, r, grid, st);
+    default: return launch_rotate_as<4, 1, false>(a, r, grid, st);
+  }
+}
+
+// q and k of a rotation: each given with its output, or not at all.
+int rotate_sides(RotateArgs& a, const he_config* cfg, const void* q, const void* k, void* q_out, void* k_out, const int64_t* const strides[4], int n) {
+  const void* in[2] = {q, k};
+  void* out[2] = {q_out, k_out};
+  const int heads[2] = {cfg->n_kv_heads * cfg->group_size, cfg->n_kv_heads};
+  for (int w = 0; w < 2; ++w) {
+    const char* what = w ? "k" : "q";
+    a.heads[w] = 0;
+    if (in[w] == nullptr && out[w] == nullptr) continue;
+    if (in[w] == nullptr || out[w] == nullptr || !aligned16(in[w]) || !aligned16(out[w]))
+      return fail(HE_ERR_INVALID_ARG, "%s or its output is null or not 16-byte aligned", what);
+    if (int rc = check_strides(what, strides[w], n, esize_of(cfg->dtype))) return rc;
+    if (int rc = check_strides(w ? "k_out" : "q_out", strides[2 + w], n, esize_of(cfg->dtype))) return rc;
+    a.x[w] = in[w], a.y[w] = out[w], a.heads[w] = heads[w];
+    for (int i = 0; i < n; ++i) a.in[w][i] = strides[w][i], a.out[w][i] = strides[2 + w][i];
+    if (in[w] == out[w])
+      for (int i = 0; i < n; ++i)
+        if (a.in[w][i] != a.out[w][i]) return fail(HE_ERR_INVALID_ARG, "%s is rotated in place with other strides", what);
+  }
+  return HE_OK;
+}
+
+// he_score_mod with its defaults filled in: the factor of q.k in log2 units and, with a cap, its two factors.
+int check_mod(const he_score_mod* mod, int d, float* scale_log2, float* cap_log2, float* inv_cap, int* window, const float** slopes) {
+  float scale = 1.0f / std::sqrt((float)d), cap = 0.f;
+  *window = 0, *slopes = nullptr;
+  if (mod != nullptr) {
+    if (!(mod->scale >= 0.f) || std::isinf(mod->scale)) return fail(HE_ERR_INVALID_ARG, "scale %g is not finite and >= 0", (double)mod->scale);
+    if (!(mod->cap >= 0.f) || std::isinf(mod->cap)) return fail(HE_ERR_INVALID_ARG, "cap %g is not finite and >= 0", (double)mod->cap);
+    if (mod->window < 0) return fail(HE_ERR_INVALID_ARG, "window %d < 0", mod->window);
+    if (mod->scale > 0.f) scale = mod->scale;
+    cap = mod->cap, *window = mod->window, *slopes = mod->slopes;
+  }
+  *scale_log2 = scale * kLog2e, *cap_log2 = cap * kLog2e, *inv_cap = cap > 0.f ? scale / cap : 0.f;
+  if (!std::isfinite(*scale_log2) || !std::isfinite(*cap_log2) || !std::isfinite(*inv_cap))
+    return fail(HE_ERR_INVALID_ARG, "scale %g with cap %g leaves fp32", (double)scale, (double)cap);
+  return HE_OK;
+}
+
+template <int NQ>
+int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
+  const int tiles = (a.tokens + kPromptRows - 1) / kPromptRows;
+  const long long ctas = (long long)tiles * a.batch * a.n_kv_heads * a.group;
+  if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld tiles in one call", ctas);
+  const size_t smem = prompt_fp32_smem(a.d);
+  if (int rc = set_smem(prompt_fp32_kernel<NQ>, smem)) return rc;
+  return launch_pdl(prompt_fp32_kernel<NQ>, dim3((unsigned)ctas), kPromptThreads, smem, true, st, a, tiles);
+}
+
+}  // namespace
+
+extern "C" {
+
+int he_rotary_init_frequencies(he_rotary* out, int32_t channels, int32_t interleaved, const double* frequencies, double amplitude) {
+  if (out == nullptr || frequencies == nullptr) return fail(HE_ERR_INVALID_ARG, "out or frequencies is null");
+  he_rotary r{};
+  r.channels = channels, r.interleaved = interleaved != 0;
+  if (int rc = check_rotary(&r, 0)) return rc;
+  if (!std::isfinite(amplitude) || !std::isfinite((float)amplitude)) return fail(HE_ERR_INVALID_ARG, "amplitude %g is not finite", amplitude);
+  r.amplitude = (float)amplitude;
+  const long double two_pi = 8.0L * atanl(1.0L);
+  for (int i = 0; i < channels / 2; ++i) {
+    if (!std::isfinite(frequencies[i])) return fail(HE_ERR_INVALID_ARG, "frequency %d is not finite", i);
+    long double t = (long double)frequencies[i] / two_pi;
+    t -= floorl(t);                            // turns modulo 1
+    const long double scaled = ldexpl(t, 64);  // (a turn that rounds up to 2^64 is none)
+    r.turns[i] = scaled >= 18446744073709551615.0L ? 0ull : (uint64_t)(scaled + 0.5L);
+  }
+  *out = r;
+  return HE_OK;
+}
+
+int he_rotary_init(he_rotary* out, int32_t channels, int32_t interleaved, double base, int32_t stretch, double factor, double length,
+                   double low, double high) {
+  he_rotary r{};
+  r.channels = channels;
+  if (int rc = check_rotary(&r, 0)) return rc;
+  if (!(base > 1.0) || !std::isfinite(base)) return fail(HE_ERR_INVALID_ARG, "base %g is not finite and > 1", base);
+  if (stretch < HE_ROTARY_PLAIN || stretch > HE_ROTARY_BANDS) return fail(HE_ERR_INVALID_ARG, "stretch %d is unknown", stretch);
+  if (stretch != HE_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return fail(HE_ERR_INVALID_ARG, "factor %g is not finite and >= 1", factor);
+  if (stretch >= HE_ROTARY_YARN && (!(length > 0.0) || !std::isfinite(length) || !(low > 0.0) || !(high > low) || !std::isfinite(high)))
+    return fail(HE_ERR_INVALID_ARG, "length %g, low %g, high %g: 0 < length and 0 < low < high are needed", length, low, high);
+  if (stretch == HE_ROTARY_NTK && channels == 2) return fail(HE_ERR_INVALID_ARG, "NTK needs more than one pair");
+  const double two_pi = 2.0 * M_PI, rd = channels;
+  double f[HE_ROTARY_MAX_PAIRS], amplitude = 1.0;
+  if (stretch == HE_ROTARY_NTK) base *= std::pow(factor, rd / (rd - 2.0));
+  // YARN: the pair index at which a pair makes n turns over `length` (a real number)
+  auto pair_of = [&](double n) { return rd * std::log(length / (n * two_pi)) / (2.0 * std::log(base)); };
+  const double first = stretch == HE_ROTARY_YARN ? std::fmax(std::floor(pair_of(high)), 0.0) : 0.0;
+  const double last = stretch == HE_ROTARY_YARN ? std::fmin(std::ceil(pair_of(low)), rd - 1.0) : 0.0;
+  for (int i = 0; i < channels / 2; ++i) {
+    f[i] = std::pow(base, -2.0 * i / rd);
+    double keep = 1.0;  // share of the frequency that is not stretched
+    if (stretch == HE_ROTARY_LINEAR) keep = 0.0;
+    if (stretch == HE_ROTARY_YARN) keep = 1.0 - std::fmin(std::fmax((i - first) / std::fmax(last - first, 0.001), 0.0), 1.0);
+    if (stretch == HE_ROTARY_BANDS) keep = std::fmin(std::fmax((length * f[i] / two_pi - low) / (high - low), 0.0), 1.0);
+    f[i] = keep * f[i] + (keep < 1.0 ? (1.0 - keep) * f[i] / factor : 0.0);
+  }
+  if (stretch == HE_ROTARY_YARN) amplitude = 0.1 * std::log(factor) + 1.0;
+  return he_rotary_init_frequencies(out, channels, interleaved, f, amplitude);
+}
+
+int he_rotate_prompt(const he_config* cfg, const he_rotary* rotary, const void* q, const void* k, const int64_t q_strides[3],
+                     const int64_t k_strides[3], const int32_t* positions, const int32_t* prompt_len, int32_t max_prompt_len, void* q_out,
+                     void* k_out, const int64_t q_out_strides[3], const int64_t k_out_strides[3], void* stream) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (int rc = check_rotary(rotary, cfg->head_dim)) return rc;
+  if (max_prompt_len < 0) return fail(HE_ERR_INVALID_ARG, "max_prompt_len %d < 0", max_prompt_len);
+  if (max_prompt_len == 0) return HE_OK;
+  RotateArgs a{};
+  const int64_t* const strides[4] = {q_strides, k_strides, q_out_strides, k_out_strides};
+  if (int rc = rotate_sides(a, cfg, q, k, q_out, k_out, strides, 3)) return rc;
+  a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype;
+  a.batch = cfg->batch, a.tokens = max_prompt_len, a.positions = positions, a.lens = prompt_len;
+  return launch_rotate(a, *rotary, static_cast<cudaStream_t>(stream));
+}
+
+int he_rotate_step(const he_config* cfg, const he_rotary* rotary, const he_cache* cache, const void* q, const void* k,
+                   const int64_t q_strides[2], const int64_t k_strides[2], void* q_out, void* k_out, const int64_t q_out_strides[2],
+                   const int64_t k_out_strides[2], void* stream) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (int rc = check_rotary(rotary, cfg->head_dim)) return rc;
+  if (cache == nullptr || cache->next_pos == nullptr) return fail(HE_ERR_INVALID_ARG, "cache or its next_pos is null");
+  RotateArgs a{};
+  const int64_t* const strides[4] = {q_strides, k_strides, q_out_strides, k_out_strides};
+  if (int rc = rotate_sides(a, cfg, q, k, q_out, k_out, strides, 2)) return rc;
+  a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype;
+  a.batch = cfg->batch, a.tokens = 1, a.next_pos = cache->next_pos;
+  return launch_rotate(a, *rotary, static_cast<cudaStream_t>(stream));
+}
+
+int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
+                     const int64_t kv_strides[3], const int32_t* prompt_len, int32_t max_prompt_len, const int32_t* doc_start,
+                     const int32_t* prefix_len, void* out, const int64_t out_strides[3], void* stream) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (max_prompt_len < 0) return fail(HE_ERR_INVALID_ARG, "max_prompt_len %d < 0", max_prompt_len);
+  if (max_prompt_len > kMaxTokens) return fail(HE_ERR_UNSUPPORTED, "max_prompt_len %d > 2^24", max_prompt_len);
+  PromptArgs a{};
+  if (int rc = check_mod(mod, cfg->head_dim, &a.scale_log2, &a.cap_log2, &a.inv_cap, &a.window, &a.slopes)) return rc;
+  if (max_prompt_len == 0) return HE_OK;
+  if (!q || !k || !v || !out || !prompt_len) return fail(HE_ERR_INVALID_ARG, "q, k, v, out or prompt_len is null");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+  const int es = esize_of(cfg->dtype);
+  if (int rc = check_strides("q", q_strides, 3, es)) return rc;
+  if (int rc = check_strides("k / v", kv_strides, 3, es)) return rc;
+  if (int rc = check_strides("out", out_strides, 3, es)) return rc;
+  a.q = q, a.k = k, a.v = v, a.out = out;
+  for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i], a.ks[i] = kv_strides[i], a.os[i] = out_strides[i];
+  a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_prompt_len;
+  a.lens = prompt_len, a.doc_start = doc_start, a.prefix = prefix_len;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  switch ((a.d + 63) / 64) {
+    case 1: return launch_prompt_fp32<1>(a, st);
+    case 2: return launch_prompt_fp32<2>(a, st);
+    case 3: return launch_prompt_fp32<3>(a, st);
+    default: return launch_prompt_fp32<4>(a, st);
+  }
+}
+
+int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out,
+                     void* stream) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (int rc = check_cache(cache)) return rc;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q or out is null or not 16-byte aligned");
+  if (cfg->batch > 65535) return fail(HE_ERR_UNSUPPORTED, "batch %d > 65535 in one call", cfg->batch);
+  AttendArgs a{*cfg, *cache, q, out, {}};
+  const int G = cfg->group_size, d = cfg->head_dim;
+  if (int rc = check_mod(mod, d, &a.mod.scale_log2, &a.mod.cap_log2, &a.mod.inv_cap, &a.mod.window, &a.mod.slopes)) return rc;
+  a.mod.first_pos = first_pos;
+  const dim3 grid((unsigned)cfg->n_kv_heads, (unsigned)cfg->batch);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (cfg->dtype == HE_DTYPE_BF16 && d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr) {
+    const long long rows = (long long)cfg->batch * cfg->n_kv_heads * cfg->max_budget;
+    AttendMaps maps;
+    if (cache_rows_tmap(cache->k_cache, rows, d, &maps.k) && cache_rows_tmap(cache->v_cache, rows, d, &maps.v))
+      return d <= 64 ? launch_attend<64, true>(a, maps, st) : launch_attend<128, true>(a, maps, st);
+  }
+  const size_t smem = ((size_t)G * d + (size_t)kAttendWarps * G * (d + 2)) * sizeof(float);
+  if (int rc = set_smem(attend_generic_kernel<true>, smem)) return rc;
+  attend_generic_kernel<true><<<grid, kAttendThreads, smem, st>>>(a);
+  HE_CUDA_CHECK(cudaGetLastError());
+  return HE_OK;
+}
+
+}  // extern "C"
