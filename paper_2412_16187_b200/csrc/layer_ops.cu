@@ -127,6 +127,53 @@ int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
   return launch_pdl(prompt_fp32_kernel<NQ>, dim3((unsigned)ctas), kPromptThreads, smem, true, st, a, tiles);
 }
 
+// Tensor map of q, k or v: {channel, token, head, sequence} in boxes of 64 channels x 128 tokens, 128-byte swizzle. An axis of one
+// entry may come with any stride, and gets one that the encoder takes.
+bool prompt_tmap(const void* base, const PromptArgs& a, const long long strides[3], int heads, CUtensorMap* out) {
+  const EncodeTiledFn encode = tmap_encoder();
+  if (encode == nullptr || env_flag_set<4>("HE_DISABLE_TMA")) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)a.d, (cuuint64_t)a.tokens, (cuuint64_t)heads, (cuuint64_t)a.batch};
+  cuuint64_t st[3] = {(cuuint64_t)strides[2] * 2, (cuuint64_t)strides[1] * 2, (cuuint64_t)strides[0] * 2};
+  for (int i = 0; i < 3; ++i) {
+    if (dims[i + 1] == 1) st[i] = (cuuint64_t)a.d * 2;
+    if (st[i] == 0 || st[i] % 16 != 0 || st[i] >= (1ull << 40)) return false;
+  }
+  const cuuint32_t box[4] = {64, (cuuint32_t)kPtTile, 1, 1}, estr[4] = {1, 1, 1, 1};
+  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, st, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Whether the kernel was built with as many registers a thread as its warps share out among themselves.
+template <typename K>
+int registers_suffice(K kernel, int* out) {
+  cudaFuncAttributes at;
+  HE_CUDA_CHECK(cudaFuncGetAttributes(&at, kernel));
+  *out = at.numRegs * kPtThreads >= 256 * kPtSoftRegs + 128 * kPtOtherRegs ? 1 : 2;
+  return HE_OK;
+}
+
+// HE_OK, an error, or -1: the caller's other kernel serves.
+template <int D, bool CAP, bool BIAS>
+int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
+  auto kernel = prompt_tc_kernel<D, CAP, BIAS>;
+  static DeviceTable<1> table;
+  int dev = 0, enough = 0;
+  HE_CUDA_CHECK(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return fail(HE_ERR_UNSUPPORTED, "device index %d", dev);
+  if (int rc = table.get(dev, 0, &enough, [&](int* got) { return registers_suffice(kernel, got); })) return rc;
+  if (enough != 1) return -1;
+  const int by_heads = a.group % 2 == 0, rows = by_heads ? kPtTile : 2 * kPtTile, tiles = (a.tokens + rows - 1) / rows;
+  const long long ctas = (long long)tiles * a.batch * a.n_kv_heads * a.group / (by_heads ? 2 : 1);
+  if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld tiles in one call", ctas);
+  if (int rc = set_smem(kernel, PromptTc<D>::kSmem)) return rc;
+  return launch_pdl(kernel, dim3((unsigned)ctas), kPtThreads, PromptTc<D>::kSmem, true, st, a, tiles, by_heads, maps);
+}
+template <int D>
+int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
+  if (a.cap_log2 > 0.f) return a.slopes != nullptr ? launch_prompt_tc<D, true, true>(a, maps, st) : launch_prompt_tc<D, true, false>(a, maps, st);
+  return a.slopes != nullptr ? launch_prompt_tc<D, false, true>(a, maps, st) : launch_prompt_tc<D, false, false>(a, maps, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -229,6 +276,14 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_prompt_len;
   a.lens = prompt_len, a.doc_start = doc_start, a.prefix = prefix_len;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (a.dtype == HE_DTYPE_BF16 && a.d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr) {
+    PromptMaps maps;
+    if (prompt_tmap(q, a, a.qs, a.n_kv_heads * a.group, &maps.q) && prompt_tmap(k, a, a.ks, a.n_kv_heads, &maps.k) &&
+        prompt_tmap(v, a, a.ks, a.n_kv_heads, &maps.v)) {
+      const int rc = a.d <= 64 ? launch_prompt_tc<64>(a, maps, st) : launch_prompt_tc<128>(a, maps, st);
+      if (rc >= 0) return rc;
+    }
+  }
   switch ((a.d + 63) / 64) {
     case 1: return launch_prompt_fp32<1>(a, st);
     case 2: return launch_prompt_fp32<2>(a, st);
