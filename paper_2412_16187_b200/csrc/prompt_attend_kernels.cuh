@@ -52,7 +52,8 @@ __device__ __forceinline__ void prompt_store(void* p, long long at, int dtype, f
 }
 
 // One row by one warp, over its visible keys alone.
-static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s, int head, int i, int n) {
+// `beat`: raised now and then for those who wait meanwhile.
+static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s, int head, int i, int n, volatile int* beat = nullptr) {
   const int lane = threadIdx.x & 31, kv = head / a.group;
   int lo, hi;
   prompt_interval(a, s, i, n, lo, hi);
@@ -62,6 +63,7 @@ static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s,
 #pragma unroll
   for (int c = 0; c < kMaxDim / 32; ++c) q[c] = lane + 32 * c < a.d ? prompt_element(a.q, q0 + lane + 32 * c, a.dtype) : 0.f, o[c] = 0.f;
   for (int j = lo; j < hi; ++j) {
+    if (beat != nullptr && (j & 1023) == 0 && lane == 0) *beat = *beat + 1;
     float dot = 0.f;
 #pragma unroll
     for (int c = 0; c < kMaxDim / 32; ++c)
@@ -91,7 +93,7 @@ constexpr int kPromptRows = 64, kPromptThreads = 256, kPromptPitch = 68;
 inline size_t prompt_fp32_smem(int d) { return sizeof(float) * (2 * (size_t)d * kPromptPitch + 64 * (size_t)d + 64 * (size_t)kPromptPitch); }
 
 template <int NQ>  // groups of 64 channels
-__global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const PromptArgs a, const int tiles) {
+__global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __grid_constant__ PromptArgs a, const int tiles) {
   extern __shared__ __align__(16) float psm_[];
   const int d = a.d, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
   const int heads = a.n_kv_heads * a.group;
@@ -220,7 +222,8 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const Promp
 
 // ------------------------------------------------------------------------------------------------ tensor cores
 //
-// A CTA works on two tiles of 128 rows that walk over the same blocks of 128 keys: two query heads of one KV head (the same tokens) where the
+// A work item is two tiles of 128 rows that walk over the same blocks of 128 keys, the last first (a bias by distance then lets the
+// running maximum stand, and no output is rescaled): two query heads of one KV head (the same tokens) where the
 // group is even, else 256 tokens of one head. Per block and tile S = Q K^T (128 x 128, fp32 in tensor memory), the softmax's weights P, and
 // O += P V (128 x D, fp32 in tensor memory) with P read from tensor memory, where it takes the place of S. While one tile's softmax runs, the
 // tensor cores work for the other tile.
@@ -229,42 +232,81 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const Promp
 //                    only when a row's maximum has grown by more than 2^8 since the last time (weights up to 256 lose nothing in fp32 or bf16).
 //   warp 8           issues the products: S of the next block of a tile right behind O += P V of this one
 //   warp 9           copies Q, then K and V block by block through a ring of TMA tiles (128-byte swizzle)
+//   warp 10          fetches work: one CTA per SM is resident, takes over the grid's waiting CTAs one after another (cluster launch control)
+//                    and works out which blocks each needs while the others are busy with the item before
+//
+// The items come with the prompts' last tokens first, as those see the most keys. The roles run on from item to item: the next one's Q, K
+// and first S are under way while the rows of this one are written.
 //
 // Registers: 384 threads are launched with 168 each (64,512); warps 0-7 take 208, warps 8-11 keep 80: 256 * 208 + 128 * 80 = 63,488.
 // Channels from d up to D are filled with zeros by the tensor maps.
-constexpr int kPtThreads = 384, kPtTile = 128, kPtMmaWarp = 8, kPtLoadWarp = 9;
-constexpr int kPtSoftRegs = 208, kPtOtherRegs = 80;
-constexpr float kPtSlack = 8.f;  // log2 of how far weights may exceed 1 before the output is rescaled
+constexpr int kPtThreads = 384, kPtTile = 128, kPtMmaWarp = 8, kPtLoadWarp = 9, kPtWorkWarp = 10;
+constexpr int kPtSoftRegs = 224, kPtOtherRegs = 56;
+constexpr int kPtAsk = 2;           // steps of an item that are still to be asked for when the next item is fetched
+constexpr int kPtParts = 1;          // parts of a block's weights that are handed to the products one by one
+constexpr int kPtReaders = 10;       // warps that read an item: softmax, products, copies
+constexpr float kPtSlack = 8.f;      // log2 of how far weights may exceed 1 before the output is rescaled
+constexpr float kPtTanhEnd = 7.f;    // see pt_tanh
+constexpr float kPtNearEnd = 0.7f;   // see pt_tanh_near
+constexpr float kPtNearInv = 1e-5f;  // the powers of a smaller factor leave fp32
 
 template <int D>
 struct PromptTc {
   static constexpr int kTileBytes = kPtTile * D * 2;
-  static constexpr int kStages = D == 128 ? 4 : 8;  // K or V tiles in flight
-  static constexpr size_t kSmem = 1024 + (size_t)(2 + kStages) * kTileBytes;
+  static constexpr int kStages = D == 128 ? 2 : 4;  // places of the ring: K of a block and V of the block before
+  static constexpr size_t kSmem = 1024 + (size_t)(2 + 2 * kStages) * kTileBytes;
 };
 
 struct PromptMaps {
   alignas(64) CUtensorMap q, k, v;
 };
 
+// An item: its rows, and per tile the blocks of keys [jb, je) that it needs and the keys [all_lo, all_hi) that all of its rows see.
+struct PtItem {
+  int some, s, n, p, tok0;
+  int jb[2], je[2], all_lo[2], all_hi[2];
+};
+
+// One product, issued by one lane of a converged warp: the election is part of the instruction, so that descriptors stay in uniform registers.
+__device__ __forceinline__ void pt_mma_ss(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "elect.sync _|q, 0xFFFFFFFF;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
 __device__ __forceinline__ void pt_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      "elect.sync _|q, 0xFFFFFFFF;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
       : "memory");
 }
-// 32 columns of this thread's tensor-memory lane
-__device__ __forceinline__ void pt_st32(uint32_t taddr, const uint32_t (&v)[32]) {
+__device__ __forceinline__ void pt_commit(uint32_t bar) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      "{\n\t.reg .pred q;\n\t"
+      "elect.sync _|q, 0xFFFFFFFF;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+      : "memory");
+}
+// 16 columns of this thread's tensor-memory lane
+__device__ __forceinline__ void pt_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
       ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
-      "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]),
-      "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]),
-      "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
+      "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void pt_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
       : "memory");
 }
 __device__ __forceinline__ void pt_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -283,6 +325,145 @@ __device__ __forceinline__ uint32_t pt_pack(float x, float y) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
   return r;
 }
+// Maximum and minimum that hand a NaN on.
+__device__ __forceinline__ float pt_max(float x, float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float pt_max3(float x, float y, float z) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+__device__ __forceinline__ float pt_max3_abs(float x, float y, float z) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+__device__ __forceinline__ float pt_min(float x, float y) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+// Pairs of fp32 values, two to an instruction.
+struct pt2 {
+  unsigned long long v;
+  __device__ __forceinline__ pt2() {}
+  __device__ __forceinline__ pt2(float x, float y) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y)); }
+  __device__ __forceinline__ void get(float& x, float& y) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+};
+__device__ __forceinline__ pt2 pt_fma(pt2 a, pt2 b, pt2 c) {
+  pt2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ pt2 pt_mul(pt2 a, pt2 b) {
+  pt2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ pt2 pt_add(pt2 a, pt2 b) {
+  pt2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
+// 2^x of N pairs on the FMA pipe, for x <= 100; below -125 it is 2^-125. x = k + f with k the nearest integer, 2^f on [-1/2, 1/2] by the cubic
+// with the least largest relative error (7.5e-5, fitted by reweighted least squares), k added to the exponent. The weights are then rounded to bf16 (up to
+// 3.9e-3), and their sum is taken of the same values. The pairs go through it side by side: one alone is a chain of ten dependent steps.
+template <int N>
+__device__ __forceinline__ void pt_ex2_fma(const pt2* x, float* y) {
+  const pt2 magic(12582912.f, 12582912.f), back(-12582912.f, -12582912.f), minus(-1.f, -1.f);
+  pt2 k[N], f[N], r[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float a, b;
+    x[i].get(a, b);
+    f[i] = pt2(pt_max(a, -125.f), pt_max(b, -125.f));
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) k[i] = pt_add(f[i], magic);  // the low bits hold the integer
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = pt_add(k[i], back);
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = pt_fma(r[i], minus, f[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = pt_fma(f[i], pt2(0.05517166480422020f, 0.05517166480422020f), pt2(0.2426111400127411f, 0.2426111400127411f));
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = pt_fma(r[i], f[i], pt2(0.6932609677314758f, 0.6932609677314758f));
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = pt_fma(r[i], f[i], pt2(0.9999280571937561f, 0.9999280571937561f));
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float r0, r1, k0, k1;
+    r[i].get(r0, r1), k[i].get(k0, k1);
+    y[2 * i] = __int_as_float(__float_as_int(r0) + (__float_as_int(k0) << 23));
+    y[2 * i + 1] = __int_as_float(__float_as_int(r1) + (__float_as_int(k1) << 23));
+  }
+}
+
+// tanh(inv x) / inv of N pairs, |inv x| <= 0.7: x P(x^2), the cubic P(inv^2 x^2) with the least largest relative error (6.7e-6, fitted by reweighted
+// least squares) and the powers of inv in its coefficients.
+struct PtNear {
+  float c0, c1, c2, c3;
+};
+__device__ __forceinline__ PtNear pt_near(float inv) {
+  const float i2 = inv * inv;
+  return {0.9999933242797852f, -0.33289045095443726f * i2, 0.12864211201667786f * i2 * i2, -0.03729049488902092f * i2 * i2 * i2};
+}
+template <int N>
+__device__ __forceinline__ void pt_tanh_near(pt2* x, const PtNear& c) {
+  pt2 w[N], r[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = pt_mul(x[i], x[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = pt_fma(w[i], pt2(c.c3, c.c3), pt2(c.c2, c.c2));
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = pt_fma(r[i], w[i], pt2(c.c1, c.c1));
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = pt_fma(r[i], w[i], pt2(c.c0, c.c0));
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = pt_mul(r[i], x[i]);
+}
+
+// tanh of N pairs, any z: z N(z^2) / D(z^2) with cubics N and D, both 1 at 0, fitted for the least largest error on [-7, 7] (1.4e-6, relative for |z| < 1), where
+// tanh 7 = 1 - 1.7e-6 stands for all beyond. One reciprocal serves a pair: D is at most 91. (By exponentials it takes two special-function
+// operations an element, beside the softmax's own one the pipe that bounds the kernel.)
+template <int N>
+__device__ __forceinline__ void pt_tanh(pt2* z) {
+  const pt2 one(1.f, 1.f);
+  pt2 w[N], nu[N], de[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float a, b;
+    z[i].get(a, b);
+    z[i] = pt2(pt_min(pt_max(a, -kPtTanhEnd), kPtTanhEnd), pt_min(pt_max(b, -kPtTanhEnd), kPtTanhEnd));
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = pt_mul(z[i], z[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) de[i] = pt_fma(w[i], pt2(0.00014415701319693802f, 0.00014415701319693802f), pt2(0.02116040722518346f, 0.02116040722518346f));
+#pragma unroll
+  for (int i = 0; i < N; ++i) nu[i] = pt_fma(w[i], pt2(4.0026867816318985e-06f, 4.0026867816318985e-06f), pt2(0.0022948283489213545f, 0.0022948283489213545f));
+#pragma unroll
+  for (int i = 0; i < N; ++i) de[i] = pt_fma(de[i], w[i], pt2(0.4565702597687332f, 0.4565702597687332f));
+#pragma unroll
+  for (int i = 0; i < N; ++i) nu[i] = pt_fma(nu[i], w[i], pt2(0.1232431128784306f, 0.1232431128784306f));
+#pragma unroll
+  for (int i = 0; i < N; ++i) de[i] = pt_fma(de[i], w[i], one);
+#pragma unroll
+  for (int i = 0; i < N; ++i) nu[i] = pt_fma(nu[i], w[i], one);
+#pragma unroll
+  for (int i = 0; i < N; ++i) nu[i] = pt_mul(nu[i], z[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float d0, d1;
+    de[i].get(d0, d1);
+    const float r = pt_rcp(d0 * d1);
+    z[i] = pt_mul(nu[i], pt_mul(pt2(r, r), pt2(d1, d0)));
+  }
+}
 
 // Shared-memory matrix descriptor of V as the B operand: rows are the products' K index, channels contiguous (MN-major), 128-byte
 // swizzle: 8-row groups 1024 bytes apart, groups of 64 channels a box (128 rows) apart.
@@ -290,153 +471,281 @@ __device__ __forceinline__ uint64_t pt_desc_mn128(uint32_t saddr) {
   return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)((kPtTile * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
+// Bounded wait of a whole warp on another role's work, which may take as long as a row of the longest prompt: the limit counts from the last
+// sign of life (`beat`, raised by the softmax warps every few blocks) on.
+__device__ __forceinline__ bool pt_wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
+  bool got = false;
+  for (int seen = *beat;;) {
+    for (uint32_t i = 0; i < kTcSpinLimit && !got; ++i) {
+      got = mbar_try_wait(bar, parity);
+      if (*abort_flag) break;
+    }
+    if (got || *abort_flag) break;
+    const int now = *beat;
+    if (now == seen) {
+      *abort_flag = 1;
+      break;
+    }
+    seen = now;
+  }
+  return __all_sync(0xFFFFFFFFu, got);
+}
+__device__ __forceinline__ bool pt_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
+  if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)), 1)) return true;
+  return pt_wait_on(bar, parity, abort_flag, beat);
+}
+
+// The grid's next waiting CTA, cancelled and taken over: asked for by one lane, answered in 16 bytes of shared memory.
+__device__ __forceinline__ void pt_ask_work(uint32_t answer, uint32_t bar) {
+  fence_proxy_async();
+  mbar_arrive_expect_tx(bar, 16u);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool pt_read_work(uint32_t answer, int& cta) {
+  uint32_t some, x;
+  asm volatile(
+      "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t"
+      "ld.shared.b128 r, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+      : "=r"(some), "=r"(x)
+      : "r"(answer)
+      : "memory");
+  cta = (int)x;
+  return some != 0;
+}
+
+// EMU of a row's 64 pairs of weights are computed on the FMA pipe: the special-function pipe (16 a cycle and SM) takes 2048 cycles for a block's
+// 2 x 128 x 128 weights, as long as the block's products at D = 128 and twice as long at D = 64.
 template <int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const PromptArgs a, const int tiles, const int by_heads, const __grid_constant__ PromptMaps maps) {
+__global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_constant__ PromptArgs a, const int tiles, const int by_heads,
+                                                                   const __grid_constant__ PromptMaps maps) {
   using T = PromptTc<D>;
-  constexpr int NS = T::kStages, NH = D / 64, BOX = kPtTile * 128;
+  constexpr int NS = T::kStages, NH = D / 64, BOX = kPtTile * 128, EMU = CAP || BIAS ? 8 : 12;
   extern __shared__ __align__(16) unsigned char pt_smem_raw[];
-  __shared__ __align__(8) unsigned long long full_s[NS], empty_s[NS], qfull_s[2], sfull_s[2], pfull_s[2], odone_s[2], drain_s;
-  __shared__ int run_s[2][4];  // per tile: first key seen, end of the keys seen, first and end of the keys that all rows see
+  __shared__ __align__(16) uint4 answer_s;
+  __shared__ __align__(8) unsigned long long full_s[NS], empty_s[NS], qfull_s[2], qempty_s[2], sfull_s[2], pfull_s[2][kPtParts], odone_s[2], ifull_s[2], iempty_s[2], ask_s, work_s, drain_s;
+  __shared__ PtItem item_s[2];
   __shared__ uint32_t tmem_s;
-  __shared__ int abort_s;
+  __shared__ int abort_s, beat_s;
   griddep_launch_dependents();
-  griddep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int heads = a.n_kv_heads * a.group, per = by_heads ? heads / 2 : heads;
-  const int p_idx = blockIdx.x % per, s = (blockIdx.x / per) % a.batch, tile = tiles - 1 - (int)(blockIdx.x / per / a.batch);
-  const int n = min(max(a.lens[s], 0), a.tokens);
-  const int tok0 = by_heads ? tile * kPtTile : tile * 2 * kPtTile;
-  if (tok0 >= n) return;
-  auto head_of = [&](int t) { return by_heads ? 2 * p_idx + t : p_idx; };
-  auto tok_of = [&](int t) { return by_heads ? tok0 : tok0 + t * kPtTile; };
   const uint32_t smem0 = (smem_u32(pt_smem_raw) + 1023u) & ~1023u;
   const uint32_t q_smem = smem0, ring = smem0 + 2 * T::kTileBytes;
-  volatile int* abort_flag = &abort_s;
+  volatile int *abort_flag = &abort_s, *beat = &beat_s;
 
   if (tid == 0) {
 #pragma unroll
     for (int i = 0; i < NS; ++i) mbar_init(smem_u32(&full_s[i]), 1), mbar_init(smem_u32(&empty_s[i]), 1);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&qfull_s[t]), 1), mbar_init(smem_u32(&sfull_s[t]), 1), mbar_init(smem_u32(&odone_s[t]), 1);
-      mbar_init(smem_u32(&pfull_s[t]), kPtTile);
-      run_s[t][0] = 0x7FFFFFFF, run_s[t][1] = 0, run_s[t][2] = 0, run_s[t][3] = 0x7FFFFFFF;
+      mbar_init(smem_u32(&qfull_s[t]), 1), mbar_init(smem_u32(&qempty_s[t]), 1), mbar_init(smem_u32(&sfull_s[t]), 1), mbar_init(smem_u32(&odone_s[t]), 1);
+      for (int q = 0; q < kPtParts; ++q) mbar_init(smem_u32(&pfull_s[t][q]), kPtTile);
+      mbar_init(smem_u32(&ifull_s[t]), 1), mbar_init(smem_u32(&iempty_s[t]), kPtReaders);
     }
-    mbar_init(smem_u32(&drain_s), 1);
-    abort_s = 0;
+    mbar_init(smem_u32(&ask_s), 1), mbar_init(smem_u32(&work_s), 1), mbar_init(smem_u32(&drain_s), 1);
+    abort_s = 0, beat_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kPtMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  __syncthreads();
-  int lo = 0, hi = 0;
-  if (warp < 8) {
-    const int t = warp >> 2, i = tok_of(t) + (tid & (kPtTile - 1));
-    prompt_interval(a, s, i, n, lo, hi);
-    const bool some = lo < hi;
-    const int first = __reduce_min_sync(0xFFFFFFFFu, some ? lo : 0x7FFFFFFF), end = __reduce_max_sync(0xFFFFFFFFu, some ? hi : 0);
-    const int all_lo = __reduce_max_sync(0xFFFFFFFFu, i >= n ? 0 : some ? lo : 0x7FFFFFFF), all_hi = __reduce_min_sync(0xFFFFFFFFu, i >= n ? 0x7FFFFFFF : hi);
-    if (lane == 0) atomicMin(&run_s[t][0], first), atomicMax(&run_s[t][1], end), atomicMax(&run_s[t][2], all_lo), atomicMin(&run_s[t][3], all_hi);
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_s;
-  // blocks of keys [begin, end) of each tile and of both
-  int jb[2], je[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const bool some = run_s[t][1] > 0;
-    jb[t] = some ? run_s[t][0] / kPtTile : 0, je[t] = some ? (run_s[t][1] + kPtTile - 1) / kPtTile : 0;
-  }
-  const int j_begin = jb[0] == je[0] ? jb[1] : jb[1] == je[1] ? jb[0] : min(jb[0], jb[1]), j_end = max(je[0], je[1]);
+  griddep_wait();
+  auto head_of = [&](const PtItem& w, int t) { return by_heads ? 2 * w.p + t : w.p; };
+  auto tok_of = [&](const PtItem& w, int t) { return by_heads ? w.tok0 : w.tok0 + t * kPtTile; };
+  // Item k for a reader's warp (false: there is none, or the CTA has given up), and the end of the reading.
+  auto take_item = [&](int k) -> bool { return pt_wait(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat) && item_s[k & 1].some != 0; };
+  auto give_item = [&](int k) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&iempty_s[k & 1]));
+  };
+  auto read_item = [&](int k, PtItem& w) -> bool {
+    if (!take_item(k)) return false;
+    w = item_s[k & 1];
+    give_item(k);
+    return true;
+  };
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax and output of tile t
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPtSoftRegs));
-    const int t = warp >> 2, row = tid & (kPtTile - 1), i = tok_of(t) + row, head = head_of(t);
+    const int t = warp >> 2, row = tid & (kPtTile - 1);
     const uint32_t lane_base = tmem + ((uint32_t)(warp & 3) << 21);  // this warp's 32 lanes
     const uint32_t s_t = lane_base + t * kPtTile, o_t = lane_base + 2 * kPtTile + t * D;
-    const int all_lo = run_s[t][2], all_hi = run_s[t][3];
-    const float slope = BIAS ? a.slopes[head] * kPromptLog2e : 0.f;
-    float m = -INFINITY, l = 0.f;
+    uint32_t blocks = 0, outputs = 0;  // done so far, over all items
     bool ok = true;
-    const int steps = je[t] - jb[t];
-    for (int it = 0; it < steps; ++it) {
-      const int j0 = (jb[t] + it) * kPtTile;
-      ok = mbar_wait_warp(smem_u32(&sfull_s[t]), it & 1, abort_flag);
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t raw[4][32];
+    for (int k = 0; ok && take_item(k); ++k) {
+      const PtItem& w = item_s[k & 1];  // (read where it is used: registers are short here)
+      const int i = tok_of(w, t) + row, head = head_of(w, t), steps = w.je[t] - w.jb[t];
+      // blocks of keys from the last to the first; all rows see all keys in those from inner_begin to before inner_end
+      const int inner_begin = w.je[t] - w.all_hi[t] / kPtTile, inner_end = w.je[t] - (int)(((unsigned)w.all_lo[t] + kPtTile - 1) / kPtTile);
+      int lo, hi;
+      prompt_interval(a, w.s, i, w.n, lo, hi);
+      const float slope = BIAS ? a.slopes[head] * kPromptLog2e : 0.f;
+      float m = -INFINITY, l = 0.f;
+      for (int it = 0; it < steps; ++it, ++blocks) {
+        ok = pt_wait(smem_u32(&sfull_s[t]), blocks & 1, abort_flag, beat);
+        if (!ok) break;
+        tc_fence_after();
+        float x[128];
+        {
+          uint32_t raw[4][32];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tc_ld32(s_t + 32 * c, raw[c]);
-      tc_wait_ld();
-      float x[128];
+          for (int c = 0; c < 4; ++c) tc_ld32(s_t + 32 * c, raw[c]);
+          tc_wait_ld();
 #pragma unroll
-      for (int c = 0; c < 128; ++c) x[c] = __uint_as_float(raw[c >> 5][c & 31]);
-      if (CAP) {
-        const float two = a.inv_cap * (2.f * kPromptLog2e), top = a.cap_log2;
-#pragma unroll
-        for (int c = 0; c < 128; ++c) x[c] = fmaf(-2.f * top, pt_rcp(pt_ex2(x[c] * two) + 1.f), top);  // tanh z = 1 - 2 / (e^2z + 1)
-      }
-      if (BIAS) {
-        const float away = (float)(j0 - i);
-#pragma unroll
-        for (int c = 0; c < 128; ++c) {
-          const float y = CAP ? x[c] : x[c] * a.scale_log2;
-          x[c] = fmaf(-slope, fabsf(away + (float)c), y);
+          for (int c = 0; c < 128; ++c) x[c] = __uint_as_float(raw[c >> 5][c & 31]);
         }
-      }
-      if (j0 < all_lo || j0 + kPtTile > all_hi) {
-        const uint32_t from = (uint32_t)(lo - j0), span = (uint32_t)(hi - lo);
-        const bool some = lo < hi;
+        const bool edge = it < inner_begin || it >= inner_end;
+        const int j0 = (w.je[t] - 1 - it) * kPtTile;
+        float scale = a.scale_log2;  // from x to log2 units
+        if (CAP) {  // x <- tanh(inv x) / inv
+          const float inv = a.inv_cap;
+          float far[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < 128; ++c) x[c] = some && (uint32_t)c - from < span ? x[c] : -INFINITY;
-      }
-      float top = fmaxf(x[0], x[1]);
+          for (int c = 0; c < 128; c += 8)
 #pragma unroll
-      for (int c = 2; c < 128; c += 2) top = fmaxf(top, fmaxf(x[c], x[c + 1]));
-      const float scale = CAP || BIAS ? 1.f : a.scale_log2;
-      const float mx = fmaxf(m, top * scale);
-      if (__any_sync(0xFFFFFFFFu, mx > m + kPtSlack)) {  // (m = -inf: the first keys that a row sees)
-        const float corr = mx == -INFINITY ? 1.f : pt_ex2(m - mx);
-        m = mx;
-        l *= corr;
-        if (it > 0) {  // the product of the block before is done: S of this one was issued behind it
+            for (int e = 0; e < 4; ++e) far[e] = pt_max3_abs(far[e], x[c + e], x[c + e + 4]);
+          const float most = pt_max(pt_max(far[0], far[1]), pt_max(far[2], far[3])) * inv;
+          const PtNear near = pt_near(inv);
+          if (__builtin_expect(inv >= kPtNearInv && __all_sync(0xFFFFFFFFu, most <= kPtNearEnd), 1)) {
 #pragma unroll
-          for (int c = 0; c < D; c += 32) {
-            uint32_t o[32];
-            tc_ld32(o_t + c, o);
-            tc_wait_ld();
+            for (int c = 0; c < 128; c += 16) {
+              pt2 z[8];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
-            pt_st32(o_t + c, o);
+              for (int e = 0; e < 8; ++e) z[e] = pt2(x[c + 2 * e], x[c + 2 * e + 1]);
+              pt_tanh_near<8>(z, near);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) z[e].get(x[c + 2 * e], x[c + 2 * e + 1]);
+            }
+          } else {  // which form an element takes goes by itself: no row depends on its neighbours
+            const float back = a.cap_log2 / a.scale_log2;  // 1 / inv
+#pragma unroll
+            for (int c = 0; c < 128; c += 8) {
+              pt2 z[4], y[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) z[e] = pt_mul(pt2(x[c + 2 * e], x[c + 2 * e + 1]), pt2(inv, inv));
+              pt_tanh<4>(z);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] = pt2(x[c + 2 * e], x[c + 2 * e + 1]);
+              pt_tanh_near<4>(y, near);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float z0, z1, y0, y1;
+                pt_mul(z[e], pt2(back, back)).get(z0, z1), y[e].get(y0, y1);
+                const bool n0 = inv >= kPtNearInv && fabsf(x[c + 2 * e] * inv) <= kPtNearEnd, n1 = inv >= kPtNearInv && fabsf(x[c + 2 * e + 1] * inv) <= kPtNearEnd;
+                x[c + 2 * e] = n0 ? y0 : z0, x[c + 2 * e + 1] = n1 ? y1 : z1;
+              }
+            }
           }
         }
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-      uint32_t w[2][32];
+        if (BIAS) {
+          const float away = (float)(j0 - i);
+          const pt2 sc(scale, scale);
+          if (j0 + kPtTile - 1 <= i - row) {  // no key behind any of the tile's rows
+            const pt2 up(8.f * slope, 8.f * slope);
 #pragma unroll
-      for (int c = 0; c < 128; c += 2) {
-        const float p0 = pt_ex2(fmaf(x[c], scale, -ref)), p1 = pt_ex2(fmaf(x[c + 1], scale, -ref));
-        sum[(c >> 1) & 3] += p0 + p1;
-        w[c >> 6][(c >> 1) & 31] = pt_pack(p0, p1);
+            for (int q = 0; q < 128; q += 32) {
+              pt2 bias[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) bias[e] = pt2(slope * (away + (float)(q + 2 * e)), slope * (away + (float)(q + 2 * e + 1)));
+#pragma unroll
+              for (int c = q; c < q + 32; c += 2) {
+                const int e = (c >> 1) & 3;
+                pt_fma(pt2(x[c], x[c + 1]), sc, bias[e]).get(x[c], x[c + 1]);
+                bias[e] = pt_add(bias[e], up);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 128; ++c) x[c] = fmaf(x[c], scale, -slope * fabsf(away + (float)c));
+          }
+          scale = 1.f;
+        }
+        if (edge) {
+          const uint32_t from = (uint32_t)(lo - j0), span = lo < hi ? (uint32_t)(hi - lo) : 0u;
+#pragma unroll
+          for (int c = 0; c < 128; ++c) x[c] = (uint32_t)c - from < span ? x[c] : -INFINITY;
+        }
+        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 128; c += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tops[e] = pt_max3(tops[e], x[c + e], x[c + e + 4]);
+        const float top = pt_max(pt_max(tops[0], tops[1]), pt_max(tops[2], tops[3])) * scale;
+        const float mx = pt_max(m, top);
+        const bool grown = !(mx <= m + kPtSlack);  // (also m = -inf, the first keys that a row sees, and a NaN)
+        if (__any_sync(0xFFFFFFFFu, grown)) {
+          const float corr = grown ? pt_ex2(m - mx) : 1.f;  // (a row does not depend on its neighbours)
+          if (grown) m = mx;
+          l *= corr;
+          if (it > 0) {  // the product of the block before is done: S of this one was issued behind it
+#pragma unroll
+            for (int c = 0; c < D; c += 16) {
+              uint32_t o[16];
+              pt_ld16(o_t + c, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
+              pt_st16(o_t + c, o);
+            }
+          }
+        }
+        const float ref = m == -INFINITY ? 0.f : m + (m - m);  // (an infinite score: NaN, as inf - inf)
+        const pt2 sc(scale, scale), off(-ref, -ref);
+        pt2 sum[2] = {pt2(0.f, 0.f), pt2(0.f, 0.f)};
+        float p[128] = {};
+        uint32_t packed[4][16];
+        auto stored = [&](int part) {
+          pt_wait_st();
+          tc_fence_before();
+          mbar_arrive(smem_u32(&pfull_s[t][part]));
+        };
+        // Pair e: into the sum, rounded, and every 16 pairs to tensor memory. A part is handed over when the pairs behind it are under way.
+        auto finish = [&](int e) {
+          sum[e & 1] = pt_add(sum[e & 1], pt2(p[2 * e], p[2 * e + 1]));
+          packed[e >> 4][e & 15] = pt_pack(p[2 * e], p[2 * e + 1]);
+          if ((e & 15) == 15) pt_st16(s_t + 16 * (e >> 4), packed[e >> 4]);
+          if (e % (64 / kPtParts) == 7 && e > 8) stored(e / (64 / kPtParts) - 1);
+        };
+        // The special-function pipe takes the pairs in a row, sums and rounding follow eight pairs behind; the last EMU pairs go to the FMA pipe.
+#pragma unroll
+        for (int e = 0; e < 64 - EMU; ++e) {
+          pt_fma(pt2(x[2 * e], x[2 * e + 1]), sc, off).get(p[2 * e], p[2 * e + 1]);
+          p[2 * e] = pt_ex2(p[2 * e]), p[2 * e + 1] = pt_ex2(p[2 * e + 1]);
+          if (e >= 8) finish(e - 8);
+        }
+        if (EMU > 0) {
+          pt2 y[EMU];
+#pragma unroll
+          for (int e = 0; e < EMU; ++e) y[e] = pt_fma(pt2(x[128 - 2 * EMU + 2 * e], x[128 - 2 * EMU + 2 * e + 1]), sc, off);
+          pt_ex2_fma<EMU>(y, p + 128 - 2 * EMU);
+          if (edge) {  // (hidden keys weigh exactly nothing)
+#pragma unroll
+            for (int e = 128 - 2 * EMU; e < 128; ++e) p[e] = x[e] == -INFINITY ? 0.f : p[e];
+          }
+        }
+#pragma unroll
+        for (int e = 56 - EMU; e < 64; ++e) finish(e);
+        stored(kPtParts - 1);
+        float s0, s1;
+        pt_add(sum[0], sum[1]).get(s0, s1);
+        l += s0 + s1;
+        if ((it & 63) == 63 && lane == 0) *beat = *beat + 1;
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      pt_st32(s_t, w[0]);
-      pt_st32(s_t + 32, w[1]);
-      pt_wait_st();
-      tc_fence_before();
-      mbar_arrive(smem_u32(&pfull_s[t]));
-    }
-    if (ok && steps > 0) ok = mbar_wait_warp(smem_u32(&odone_s[t]), 0, abort_flag);
-    if (ok) {
+      if (ok && steps > 0) ok = pt_wait(smem_u32(&odone_s[t]), outputs++ & 1, abort_flag, beat);
+      if (!ok) break;
       tc_fence_after();
       const float inv = l != 0.f ? 1.f / l : 0.f;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (s * a.os[0] + head * a.os[1] + i * a.os[2]);
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (w.s * a.os[0] + head * a.os[1] + i * a.os[2]);
       bool bad = false;
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
@@ -453,120 +762,184 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const PromptAr
             f[u] = steps > 0 && inv != 0.f ? __uint_as_float(o[e + u]) * inv : 0.f;
             bad |= c + e < a.d && f[u] != f[u];
           }
-          if (i < n && c + e < a.d)
+          if (i < w.n && c + e < a.d)
             *reinterpret_cast<uint4*>(out + c + e) = make_uint4(pt_pack(f[0], f[1]), pt_pack(f[2], f[3]), pt_pack(f[4], f[5]), pt_pack(f[6], f[7]));
         }
       }
-      uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < n);
+      uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
       __syncwarp();
-      for (; again != 0u; again &= again - 1u) prompt_row_again(a, s, head, i - lane + __ffs(again) - 1, n);
+      for (; again != 0u; again &= again - 1u) prompt_row_again(a, w.s, head, i - lane + __ffs(again) - 1, w.n, beat);
+      tc_fence_before();
+      give_item(k);
     }
-    tc_fence_before();
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPtOtherRegs));
     if (warp == kPtLoadWarp) {
       // ---------------------------------------------------------------- copies
-      int slot = 0, used = 0;  // ring place of the next tile, tiles asked for so far
-      if (lane == 0) {
+      uint32_t used = 0, queries[2] = {0, 0};  // K or V tiles and Q tiles asked for so far
+      bool ok = true;
+      PtItem w;
+      for (int k = 0; ok && read_item(k, w); ++k) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          if (je[t] > jb[t]) {
-            const uint32_t bar = smem_u32(&qfull_s[t]);
-            mbar_arrive_expect_tx(bar, T::kTileBytes);
+          if (ok && w.je[t] > w.jb[t]) {
+            if (queries[t] > 0) ok = pt_wait(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
+            if (!ok) break;
+            if (lane == 0) {
+              const uint32_t bar = smem_u32(&qfull_s[t]);
+              mbar_arrive_expect_tx(bar, T::kTileBytes);
 #pragma unroll
-            for (int h = 0; h < NH; ++h) tma_load_4d(q_smem + t * T::kTileBytes + h * BOX, &maps.q, 64 * h, tok_of(t), head_of(t), s, bar);
+              for (int h = 0; h < NH; ++h) tma_load_4d(q_smem + t * T::kTileBytes + h * BOX, &maps.q, 64 * h, tok_of(w, t), head_of(w, t), w.s, bar);
+            }
+            ++queries[t];
           }
-      }
-      const int kv = head_of(0) / a.group;
-      for (int item = 0; item < 2 * (j_end - j_begin); ++item) {
-        if (used >= NS && !mbar_wait_warp(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag)) break;
-        if (lane == 0) {
-          const uint32_t bar = smem_u32(&full_s[slot]);
-          mbar_arrive_expect_tx(bar, T::kTileBytes);
+        const int j_begin = w.jb[0] == w.je[0] ? w.jb[1] : w.jb[1] == w.je[1] ? w.jb[0] : min(w.jb[0], w.jb[1]), j_end = max(w.je[0], w.je[1]);
+        const int kv = head_of(w, 0) / a.group;
+        const int blocks = j_end - j_begin, ask = max(blocks + 1 - kPtAsk, 0);
+        if (ok && lane == 0 && blocks == 0) mbar_arrive(smem_u32(&ask_s));
+        for (int step = 0; ok && blocks > 0 && step <= blocks; ++step) {
+          if (lane == 0 && step == ask) mbar_arrive(smem_u32(&ask_s));
+          const uint32_t slot = used % NS;
+          if (used >= NS) ok = pt_wait(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
+          if (!ok) break;
+          if (lane == 0) {
+            const uint32_t bar = smem_u32(&full_s[slot]), at = ring + slot * 2 * T::kTileBytes;
+            mbar_arrive_expect_tx(bar, (step > 0 && step < blocks ? 2u : 1u) * T::kTileBytes);
 #pragma unroll
-          for (int h = 0; h < NH; ++h)
-            tma_load_4d(ring + slot * T::kTileBytes + h * BOX, (item & 1) ? &maps.v : &maps.k, 64 * h, (j_begin + (item >> 1)) * kPtTile, kv, s, bar);
+            for (int h = 0; h < NH; ++h) {
+              if (step > 0) tma_load_4d(at + T::kTileBytes + h * BOX, &maps.v, 64 * h, (j_end - step) * kPtTile, kv, w.s, bar);
+              if (step < blocks) tma_load_4d(at + h * BOX, &maps.k, 64 * h, (j_end - 1 - step) * kPtTile, kv, w.s, bar);
+            }
+          }
+          ++used;
         }
-        ++used;
-        slot = slot + 1 == NS ? 0 : slot + 1;
       }
       __syncwarp();
       if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) {  // let what is in flight land before shared memory is given up
         for (int t = 0; t < 2; ++t)
-          if (je[t] > jb[t]) mbar_drain(smem_u32(&qfull_s[t]), 0);
-        for (int u = max(0, used - NS); u < used; ++u) mbar_drain(smem_u32(&full_s[u % NS]), (u / NS) & 1);
+          if (queries[t] > 0) mbar_drain(smem_u32(&qfull_s[t]), (queries[t] - 1) & 1);
+        for (uint32_t u = used > (uint32_t)NS ? used - NS : 0; u < used; ++u) mbar_drain(smem_u32(&full_s[u % NS]), (u / NS) & 1);
       }
     } else if (warp == kPtMmaWarp) {
-      // ---------------------------------------------------------------- products (issued by one elected lane)
+      // ---------------------------------------------------------------- products
+      // This warp shares its scheduler's instruction cache with softmax code that is many times larger, and fetches what it runs once a step
+      // anew: few instructions count. Hence the elections inside the instructions, the tiles in a loop, one wait and one release a step.
       constexpr uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((kPtTile / 8) << 17) | ((kPtTile / 16) << 24);
       constexpr uint32_t idesc_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) /* B is MN-major */ | ((D / 8) << 17) | ((kPtTile / 16) << 24);
+      const uint64_t qdesc = umma_desc_k128(q_smem), kdesc = umma_desc_k128(ring), vdesc = pt_desc_mn128(ring + T::kTileBytes);
+      uint32_t slot = 0, lap = 0, taken = 0, queries = 0;  // ring place of the next step, the parity of its use; parities of the blocks of P and of the Q tiles, a bit a tile
       bool ok = true;
-      auto slot_of = [&](int item) { return item % NS; };
-      auto landed = [&](int item) { ok = ok && mbar_wait_warp(smem_u32(&full_s[slot_of(item)]), (item / NS) & 1, abort_flag); };
-      auto qk = [&](int t, int item) {
-        if (!ok) return;
-        const uint64_t ad = umma_desc_k128(q_smem + t * T::kTileBytes), bd = umma_desc_k128(ring + slot_of(item) * T::kTileBytes);
-        if (tc_elect()) {
-#pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint64_t at = (uint64_t)(((ks >> 2) * BOX + (ks & 3) * 32) >> 4);
-            tc_mma_bf16(tmem + t * kPtTile, ad + at, bd + at, idesc_qk, ks != 0);
-          }
-          tc_commit(smem_u32(&sfull_s[t]));
-        }
-        __syncwarp();
-      };
-      auto pv = [&](int t, int item, int it, bool last) {
-        ok = ok && mbar_wait_warp(smem_u32(&pfull_s[t]), it & 1, abort_flag);
-        if (!ok) return;
-        tc_fence_after();
-        const uint64_t bd = pt_desc_mn128(ring + slot_of(item) * T::kTileBytes);
-        if (tc_elect()) {
-#pragma unroll
-          for (int ks = 0; ks < kPtTile / 16; ++ks)
-            pt_mma_ts(tmem + 2 * kPtTile + t * D, tmem + t * kPtTile + 8 * ks, bd + (uint64_t)((ks * 16 * 128) >> 4), idesc_pv, it > 0 || ks != 0);
-          if (last) tc_commit(smem_u32(&odone_s[t]));
-        }
-        __syncwarp();
-      };
-      auto release = [&](int item) {
-        if (ok && tc_elect()) tc_commit(smem_u32(&empty_s[slot_of(item)]));
-        __syncwarp();
-      };
-      auto active = [&](int t, int j) { return j >= jb[t] && j < je[t]; };
-      for (int j = j_begin - 1; j < j_end && ok; ++j) {
-        // O += P V of block j, S of block j + 1, tile by tile
-        const int item = 2 * (j - j_begin);  // block j's K; its V is the next, block j + 1's K the one after
-        if (j >= j_begin) {
-          landed(item + 1);
-          const int rows = n - j * kPtTile;
-          if (ok && rows < kPtTile) {  // V rows behind the prompt's end hold anything: zeros
-            for (int u = lane; u < (kPtTile - rows) * 8 * NH; u += 32) {
-              const int h = u / ((kPtTile - rows) * 8), at = u % ((kPtTile - rows) * 8);
-              asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + slot_of(item + 1) * T::kTileBytes + h * BOX + rows * 128 + at * 16), "r"(0) : "memory");
-            }
+      PtItem w;
+      for (int k = 0; ok && read_item(k, w); ++k) {
+        const int j_begin = w.jb[0] == w.je[0] ? w.jb[1] : w.jb[1] == w.je[1] ? w.jb[0] : min(w.jb[0], w.jb[1]), j_end = max(w.je[0], w.je[1]);
+        if (j_begin == j_end) continue;
+#pragma unroll 1
+        for (int j = j_end; j >= j_begin; --j) {
+          // O += P V of block j, S of block j - 1, tile by tile
+          ok = pt_wait(smem_u32(&full_s[slot]), lap, abort_flag, beat);
+          if (!ok) break;
+          const int rows = w.n - j * kPtTile;
+          if (__builtin_expect(j < j_end && rows < kPtTile, 0)) {  // V rows behind the prompt's end hold anything: zeros
+            const int chunks = (kPtTile - rows) * 8;
+            for (int c = lane; c < chunks * NH; c += 32)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + (2 * slot + 1) * T::kTileBytes + (c / chunks) * BOX + rows * 128 + (c % chunks) * 16), "r"(0) : "memory");
             fence_proxy_async();
             __syncwarp();
           }
-        }
-        if (j + 1 < j_end) landed(item + 2);
+          const uint64_t at = (uint64_t)(slot * (2 * T::kTileBytes >> 4));
+#pragma unroll 1
+          for (int t = 0; t < 2; ++t) {
+            const int t_begin = t ? w.jb[1] : w.jb[0], t_end = t ? w.je[1] : w.je[0];
+            const uint32_t s_at = tmem + t * kPtTile;
+            if (j >= t_begin && j < t_end) {
+              ok = pt_wait(smem_u32(&pfull_s[t][0]), (taken >> t) & 1, abort_flag, beat);
+              if (!ok) break;
+              taken ^= 1u << t;
+              tc_fence_after();
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (j >= j_begin && active(t, j)) pv(t, item + 1, j - jb[t], j + 1 == je[t]);
-          if (j + 1 < j_end && active(t, j + 1)) {
-            if (j + 1 == jb[t]) ok = ok && mbar_wait_warp(smem_u32(&qfull_s[t]), 0, abort_flag);
-            qk(t, item + 2);
+              for (int ks = 0; ks < kPtTile / 16; ++ks)
+                pt_mma_ts(tmem + 2 * kPtTile + t * D, s_at + 8 * ks, vdesc + at + (uint64_t)((ks * 16 * 128) >> 4), idesc_pv, ks != 0 || j + 1 != t_end);
+              if (j == t_begin) pt_commit(smem_u32(&odone_s[t]));
+            }
+            if (j > t_begin && j <= t_end) {
+              if (j == t_end) {
+                ok = pt_wait(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
+                if (!ok) break;
+                queries ^= 1u << t;
+              }
+              const uint64_t ad = qdesc + (uint64_t)(t * (T::kTileBytes >> 4));
+#pragma unroll
+              for (int ks = 0; ks < D / 16; ++ks) {
+                const uint64_t of = (uint64_t)(((ks >> 2) * BOX + (ks & 3) * 32) >> 4);
+                pt_mma_ss(s_at, ad + of, kdesc + at + of, idesc_qk, ks != 0);
+              }
+              pt_commit(smem_u32(&sfull_s[t]));
+              if (j - 1 == t_begin) pt_commit(smem_u32(&qempty_s[t]));
+            }
           }
+          if (!ok) break;
+          pt_commit(smem_u32(&empty_s[slot]));
+          if (++slot == NS) slot = 0, lap ^= 1u;
         }
-        if (j >= j_begin) release(item + 1);
-        if (j + 1 < j_end) release(item + 2);
       }
-      const bool gave_up = __any_sync(0xFFFFFFFFu, *abort_flag != 0);
-      if (gave_up) {  // products in flight end before tensor memory is given up
-        if (tc_elect()) tc_commit(smem_u32(&drain_s));
-        __syncwarp();
+      if (!ok || __any_sync(0xFFFFFFFFu, *abort_flag != 0)) {  // products in flight end before tensor memory is given up
+        pt_commit(smem_u32(&drain_s));
         mbar_drain(smem_u32(&drain_s), 0);
       }
+    } else if (warp == kPtWorkWarp) {
+      // ---------------------------------------------------------------- work
+      const uint32_t answer = smem_u32(&answer_s);
+      int cta = blockIdx.x, k = 0;
+      uint32_t asked = 0;
+      bool ok = true;
+      auto hand_over = [&](const PtItem& w) {
+        if (k >= 2) ok = ok && pt_wait(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
+        if (!ok) return;
+        if (lane == 0) {
+          item_s[k & 1] = w;
+          mbar_arrive(smem_u32(&ifull_s[k & 1]));
+        }
+        __syncwarp();
+        ++k;
+      };
+      PtItem w;
+      while (ok) {
+        w.some = 1, w.p = cta % per, w.s = (cta / per) % a.batch;
+        const int tile = tiles - 1 - cta / per / a.batch;
+        w.tok0 = by_heads ? tile * kPtTile : tile * 2 * kPtTile;
+        w.n = min(max(a.lens[w.s], 0), a.tokens);
+        if (w.tok0 < w.n) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            int first = 0x7FFFFFFF, end = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
+#pragma unroll
+            for (int r = 0; r < kPtTile / 32; ++r) {
+              const int i = tok_of(w, t) + 32 * r + lane;
+              int lo, hi;
+              prompt_interval(a, w.s, i, w.n, lo, hi);
+              if (lo < hi) first = min(first, lo), end = max(end, hi);
+              if (i < w.n) all_lo = max(all_lo, lo < hi ? lo : 0x7FFFFFFF), all_hi = min(all_hi, hi);
+            }
+            first = __reduce_min_sync(0xFFFFFFFFu, first), end = __reduce_max_sync(0xFFFFFFFFu, end);
+            w.all_lo[t] = __reduce_max_sync(0xFFFFFFFFu, all_lo), w.all_hi[t] = __reduce_min_sync(0xFFFFFFFFu, all_hi);
+            w.jb[t] = end > 0 ? first / kPtTile : 0, w.je[t] = end > 0 ? (end + kPtTile - 1) / kPtTile : 0;
+          }
+          hand_over(w);
+          // not before this item is nearly done: a CTA that took the next one at once would be bound to it however long this one lasts
+          ok = ok && pt_wait(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
+        }
+        if (!ok) break;
+        if (lane == 0) pt_ask_work(answer, smem_u32(&work_s));
+        ++asked;
+        if (!pt_wait(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
+        const bool more = pt_read_work(answer, cta);
+        if (!more) {
+          w.some = 0;
+          hand_over(w);
+          break;
+        }
+      }
+      if (asked > 0 && __any_sync(0xFFFFFFFFu, *abort_flag != 0)) mbar_drain(smem_u32(&work_s), (asked - 1) & 1);
     }
     __syncwarp();
   }
