@@ -157,8 +157,20 @@ def _stream(stream=None) -> int:
         return torch.cuda.current_stream().cuda_stream
 
 
+def _current_device() -> int:
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _layout(t):
+    """All that the checks of a call look at in a tensor."""
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.device)
 
 
 def hash_keys(x: torch.Tensor, W: torch.Tensor, hash_bits: int | None = None, stream=None) -> torch.Tensor:
@@ -200,6 +212,7 @@ class Rotary:
         if self.channels > self.head_dim:
             raise HashEvictError(f"rotary channels {self.channels} > head_dim {self.head_dim}")
         self.raw = he_rotary()
+        self.pointer = ctypes.pointer(self.raw)
         if frequencies is not None:
             if scaling is not None:
                 raise HashEvictError("frequencies are given as they are: no scaling beside them")
@@ -231,6 +244,7 @@ class ScoreMod:
             raise HashEvictError("slopes must be a contiguous fp32 tensor on the device")
         self.slopes = slopes
         self.raw = he_score_mod(float(scale), float(softcap), int(window), 0, _ptr(slopes))
+        self.pointer = ctypes.pointer(self.raw)
 
 
 class HashEvictCache:
@@ -276,6 +290,7 @@ class HashEvictCache:
         self.step_scratch = torch.empty(lib().he_step_scratch_bytes(ctypes.byref(self.cfg)), dtype=torch.uint8, device=dev)
         self.ca.step_scratch = _ptr(self.step_scratch)
         self._ws = None
+        self._cfg_p, self._ca_p, self._layouts = ctypes.pointer(self.cfg), ctypes.pointer(self.ca), {}
 
     @property
     def codes(self):
@@ -307,45 +322,58 @@ class HashEvictCache:
         return out
 
     # --- the layer around the cache: rotary positions, attention with modified scores ------------------
+    # A decode loop makes these calls with tensors of the same layout at every token. What the checks of a call find - that every tensor has
+    # its device, type, shape and contiguous channels - and the strides that the library takes are kept by layout (never by address).
+    def _rows(self, name, t, shape, dtype):
+        """Element strides (as the library takes them) of a tensor with any strides but for its channels. An axis of one entry, whose stride
+        says nothing, takes a row's."""
+        self._tensor(name, t, shape, dtype, rows=True)
+        n = t.dim() - 1
+        arr = (ctypes.c_int64 * n)(*[st if sz > 1 else self.d for sz, st in zip(t.shape[:n], t.stride())])
+        return ctypes.cast(arr, ctypes.POINTER(ctypes.c_int64))
+
     def _tensor(self, name, t, shape, dtype, rows=False):
         """A tensor of a call: its device, type and shape; `rows`: any strides but for the channels, else contiguous."""
         if t.device != self.k_cache.device or t.dtype != dtype or t.shape != shape:
             raise HashEvictError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, not {tuple(shape)} {dtype} on {self.k_cache.device}")
         if not (t.stride(-1) == 1 if rows else t.is_contiguous()):
             raise HashEvictError(f"{name}: " + ("channels must be contiguous" if rows else "must be contiguous"))
-        return t
 
-    def _strides(self, t):
-        """Element strides of all axes but the channels; an axis of one (whose stride says nothing) takes a row's."""
-        n = t.dim() - 1
-        return (ctypes.c_int64 * n)(*[st if sz > 1 else self.d for sz, st in zip(t.shape[:n], t.stride())])
+    def _known(self, key, make):
+        found = self._layouts.get(key)
+        if found is None:
+            found = make()
+            if len(self._layouts) >= 1024:
+                self._layouts.clear()
+            self._layouts[key] = found
+        return found
 
-    def _call(self, fn, *args, stream=None):
+    def _call(self, fn, stream, *args):
         dev = self.k_cache.device
-        if dev.index == torch.cuda.current_device():
+        if dev.index == _current_device():
             _check(fn(*args, _stream(stream)))
         else:  # the library launches on the current device
             with torch.cuda.device(dev):
                 _check(fn(*args, _stream(stream)))
 
-    def _rotate(self, rotary, q, k, q_out, k_out, tokens):
-        """Checked arguments of a rotation: (q, its strides, its output, the output's strides) and the same of k."""
-        if rotary.head_dim != self.d:
-            raise HashEvictError(f"rotary of head_dim {rotary.head_dim} for rows of {self.d}")
-        sides = []
+    def _rotation(self, head_dim, q, k, q_out, k_out, tokens):
+        if head_dim != self.d:
+            raise HashEvictError(f"rotary of head_dim {head_dim} for rows of {self.d}")
+        found = []
         for name, x, out, heads in (("q", q, q_out, self.H * self.G), ("k", k, k_out, self.H)):
-            if x is None:
-                if out is not None:
-                    raise HashEvictError(f"{name}_out without {name}")
-                sides.append((None, None, None, None))
-                continue
             shape = (self.B, heads) + tokens + (self.d,)
-            self._tensor(name, x, shape, self.dtype, rows=True)
-            if out is None:
-                out = torch.empty(shape, dtype=self.dtype, device=x.device)
-            self._tensor(name + "_out", out, shape, self.dtype, rows=True)
-            sides.append((x, self._strides(x), out, self._strides(out)))
-        return sides
+            found += (None, None) if x is None else (self._rows(name, x, shape, self.dtype), self._rows(name + "_out", out, shape, self.dtype))
+        return found
+
+    def _outputs(self, q, k, q_out, k_out):
+        """Outputs of a rotation, made where they are missing."""
+        if q is None and q_out is not None or k is None and k_out is not None:
+            raise HashEvictError("an output without its input")
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        return q_out, k_out
 
     def rotate_prompt(self, rotary, q, k, prompt_len=None, positions=None, q_out=None, k_out=None, stream=None):
         """he_rotate_prompt. q [B, H*G, N, d], k [B, H, N, d] (any strides on the first three axes; either may be None), positions
@@ -354,64 +382,72 @@ class HashEvictCache:
         if q is None and k is None:
             raise HashEvictError("neither q nor k is given")
         n = (k if q is None else q).shape[2]
-        (q, qs, q_out, qos), (k, ks, k_out, kos) = self._rotate(rotary, q, k, q_out, k_out, (n,))
+        q_out, k_out = self._outputs(q, k, q_out, k_out)
+        qs, qos, ks, kos = self._known(("rotate", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
+                                       lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, (n,)))
         if positions is not None:
             self._tensor("positions", positions, (self.B, n), torch.int32)
         if prompt_len is not None:
             self._tensor("prompt_len", prompt_len, (self.B,), torch.int32)
-        self._call(lib().he_rotate_prompt, ctypes.byref(self.cfg), ctypes.byref(rotary.raw), _ptr(q), _ptr(k), qs, ks, _ptr(positions),
-                   _ptr(prompt_len), n, _ptr(q_out), _ptr(k_out), qos, kos, stream=stream)
+        self._call(lib().he_rotate_prompt, stream, self._cfg_p, rotary.pointer, _ptr(q), _ptr(k), qs, ks, _ptr(positions), _ptr(prompt_len), n,
+                   _ptr(q_out), _ptr(k_out), qos, kos)
         return q_out, k_out
 
     def rotate_step(self, rotary, q, k, q_out=None, k_out=None, stream=None):
         """he_rotate_step: q [B, H*G, d] and k [B, H, d] of the next decode_step, rotated by the cache's next_pos. Returns (q_out, k_out)."""
-        (q, qs, q_out, qos), (k, ks, k_out, kos) = self._rotate(rotary, q, k, q_out, k_out, ())
-        self._call(lib().he_rotate_step, ctypes.byref(self.cfg), ctypes.byref(rotary.raw), ctypes.byref(self.ca), _ptr(q), _ptr(k), qs, ks,
-                   _ptr(q_out), _ptr(k_out), qos, kos, stream=stream)
+        q_out, k_out = self._outputs(q, k, q_out, k_out)
+        qs, qos, ks, kos = self._known(("step", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
+                                       lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, ()))
+        self._call(lib().he_rotate_step, stream, self._cfg_p, rotary.pointer, self._ca_p, _ptr(q), _ptr(k), qs, ks, _ptr(q_out), _ptr(k_out), qos, kos)
         return q_out, k_out
 
     def _mod(self, mod):
         if mod is None:
             return None
-        if mod.slopes is not None:
-            self._tensor("slopes", mod.slopes, (self.H * self.G,), torch.float32)
-        return ctypes.byref(mod.raw)
+        if mod.slopes is not None and (mod.slopes.shape[0] != self.H * self.G or mod.slopes.dim() != 1 or mod.slopes.device != self.k_cache.device):
+            raise HashEvictError(f"slopes: {tuple(mod.slopes.shape)} on {mod.slopes.device}, not {(self.H * self.G,)} on {self.k_cache.device}")
+        return mod.pointer
+
+    def _prompt(self, q, k, v, out, prompt_len, doc_start, prefix_len):
+        n = q.shape[2]
+        ks, vs = self._rows("k", k, (self.B, self.H, n, self.d), self.dtype), self._rows("v", v, (self.B, self.H, n, self.d), self.dtype)
+        if ks[:3] != vs[:3]:
+            raise HashEvictError("k and v must have the same strides")
+        self._tensor("prompt_len", prompt_len, (self.B,), torch.int32)
+        if doc_start is not None:
+            self._tensor("doc_start", doc_start, (self.B, n), torch.int32)
+        if prefix_len is not None:
+            self._tensor("prefix_len", prefix_len, (self.B,), torch.int32)
+        qs = self._rows("q", q, (self.B, self.H * self.G, n, self.d), self.dtype)
+        return qs, ks, self._rows("out", out, q.shape, self.dtype)
 
     def attend_prompt(self, q, k, v, prompt_len, mod=None, doc_start=None, prefix_len=None, out=None, stream=None):
         """he_attend_prompt: attention of the prompts over themselves. q [B, H*G, N, d], k / v [B, H, N, d] (any strides on the first
         three axes), prompt_len int32 [B], mod a ScoreMod, doc_start int32 [B, N] (first position of each token's document),
         prefix_len int32 [B] (tokens that all of a prompt's tokens see). Returns out [B, H*G, N, d] in the dtype of q; rows behind a
         prompt's end are left as they were (undefined in an `out` that this call makes)."""
-        n = q.shape[2]
-        self._tensor("q", q, (self.B, self.H * self.G, n, self.d), self.dtype, rows=True)
-        self._tensor("k", k, (self.B, self.H, n, self.d), self.dtype, rows=True)
-        self._tensor("v", v, (self.B, self.H, n, self.d), self.dtype, rows=True)
-        ks = self._strides(k)
-        if ks[:] != self._strides(v)[:]:
-            raise HashEvictError("k and v must have the same strides")
         if out is None:
-            out = torch.empty((self.B, self.H * self.G, n, self.d), dtype=self.dtype, device=q.device)
-        self._tensor("out", out, q.shape, self.dtype, rows=True)
-        self._tensor("prompt_len", prompt_len, (self.B,), torch.int32)
-        if doc_start is not None:
-            self._tensor("doc_start", doc_start, (self.B, n), torch.int32)
-        if prefix_len is not None:
-            self._tensor("prefix_len", prefix_len, (self.B,), torch.int32)
-        self._call(lib().he_attend_prompt, ctypes.byref(self.cfg), self._mod(mod), _ptr(q), _ptr(k), _ptr(v), self._strides(q), ks,
-                   _ptr(prompt_len), n, _ptr(doc_start), _ptr(prefix_len), _ptr(out), self._strides(out), stream=stream)
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qs, ks, os_ = self._known(("prompt", _layout(q), _layout(k), _layout(v), _layout(out), _layout(prompt_len), _layout(doc_start), _layout(prefix_len)),
+                                  lambda: self._prompt(q, k, v, out, prompt_len, doc_start, prefix_len))
+        self._call(lib().he_attend_prompt, stream, self._cfg_p, self._mod(mod), _ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(prompt_len), q.shape[2],
+                   _ptr(doc_start), _ptr(prefix_len), _ptr(out), os_)
         return out
+
+    def _scored(self, q, first_pos, out):
+        self._tensor("q", q, (self.B, self.H * self.G, self.d), self.dtype)
+        self._tensor("out", out, q.shape, torch.float32)
+        if first_pos is not None:
+            self._tensor("first_pos", first_pos, (self.B,), torch.int32)
+        return True
 
     def attend_scored(self, q, mod=None, first_pos=None, out=None, stream=None):
         """he_attend_scored: attend with a ScoreMod. q [B, H*G, d] -> fp32 [B, H*G, d]; the query is the token that the last decode_step
         inserted, first_pos int32 [B] the first position that it sees (the start of its document)."""
-        self._tensor("q", q, (self.B, self.H * self.G, self.d), self.dtype)
         if out is None:
-            out = torch.empty((self.B, self.H * self.G, self.d), dtype=torch.float32, device=q.device)
-        self._tensor("out", out, q.shape, torch.float32)
-        if first_pos is not None:
-            self._tensor("first_pos", first_pos, (self.B,), torch.int32)
-        self._call(lib().he_attend_scored, ctypes.byref(self.cfg), ctypes.byref(self.ca), self._mod(mod), _ptr(q), _ptr(first_pos), _ptr(out),
-                   stream=stream)
+            out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        self._known(("scored", _layout(q), _layout(out), _layout(first_pos)), lambda: self._scored(q, first_pos, out))
+        self._call(lib().he_attend_scored, stream, self._cfg_p, self._ca_p, self._mod(mod), _ptr(q), _ptr(first_pos), _ptr(out))
         return out
 
     def workspace(self, max_prompt_len):

@@ -253,6 +253,13 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   }
   griddep_wait();
   const int fill = __ldcg(a.ca.fill + unit);
+  float slope = 0.f;              // MOD: log2 units per position
+  int now = 0, low = 0;           // MOD: the query's position, the first one it sees
+  if (MOD) {                      // (asked for together with `fill`, looked at behind the first copies)
+    now = __ldcg(a.ca.next_pos + unit) - 1;
+    if (a.mod.first_pos != nullptr) low = a.mod.first_pos[blockIdx.y];
+    if (a.mod.slopes != nullptr && gid < G) slope = a.mod.slopes[(unit % cfg.n_kv_heads) * G + gid] * kLog2e;
+  }
   const int items = first < fill ? 2 * ((fill - first + stride - 1) / stride) : 0;
   const int row_base = unit * cfg.max_budget;
   // Item t (K rows of group t / 2, or its V rows) into buffer b.
@@ -281,21 +288,16 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
     qf[2 * c][0] = t.x, qf[2 * c][1] = t.y, qf[2 * c + 1][0] = t.z, qf[2 * c + 1][1] = t.w;
   }
   const float scale = MOD ? a.mod.scale_log2 : rsqrtf((float)d) * kLog2e;
-  float slope = 0.f;     // MOD: log2 units per position
-  int now = 0, low = 0;  // the query's position, the first one it sees
-  if (MOD) {
-    if (a.mod.slopes != nullptr && gid < G) slope = a.mod.slopes[(unit % cfg.n_kv_heads) * G + gid] * kLog2e;
-    now = __ldcg(a.ca.next_pos + unit) - 1;
-    if (a.mod.window > 0) low = max(low, now - a.mod.window + 1);
-    if (a.mod.first_pos != nullptr) low = max(low, a.mod.first_pos[blockIdx.y]);
-  }
   const int32_t* slot_pos = a.ca.pos + (size_t)unit * cfg.max_budget + 2 * tig;
   int2 ahead[4];  // positions of this lane's slots 8 i + 2 tig, + 1 of the next group
   auto fetch_pos = [&](int g) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) ahead[i] = g + 8 * i + 2 * tig < fill ? __ldcg(reinterpret_cast<const int2*>(slot_pos + g + 8 * i)) : make_int2(-1, -1);
   };
-  if (MOD) fetch_pos(first);
+  if (MOD) {
+    fetch_pos(first);
+    low = max(low, a.mod.window > 0 ? max(0, now - a.mod.window + 1) : 0);
+  }
   float m = -INFINITY, l = 0.f;
   float o[8 * NH][4];
 #pragma unroll
@@ -382,16 +384,33 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
     uint32_t w[4][2];  // hi and lo halves of the weights of slots 8 i + 2 tig, + 1
 #pragma unroll
     for (int i = 0; i < 4; ++i) split_pair(p[2 * i], p[2 * i + 1], w[i][0], w[i][1]);
+    uint32_t third[4];  // MOD: what two terms leave of a weight (2^-17 of it) as a third, in products of its own: a few slots' weights are then as exact as fp32's
+#pragma unroll
+    for (int i = 0; MOD && i < 4; ++i)
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n"
+          : "=r"(third[i])
+          : "f"(p[2 * i + 1] - __uint_as_float(w[i][0] & 0xFFFF0000u) - __uint_as_float(w[i][1] & 0xFFFF0000u)),
+            "f"(p[2 * i] - __uint_as_float(w[i][0] << 16) - __uint_as_float(w[i][1] << 16)));
     if (__any_sync(0xFFFFFFFFu, corr != 1.f)) {
 #pragma unroll
       for (int t2 = 0; t2 < 8 * NH; ++t2) o[t2][0] *= corr, o[t2][1] *= corr, o[t2][2] *= corr, o[t2][3] *= corr;
     }
     const uint4* vr = step(t + 1);
-    if (MOD ? seen != 0xFFFFFFFFu : g0 + GRP > fill) {  // rows past the fill level or masked (weighted by zero) hold anything: make them finite
-      for (int i = lane; i < GRP * CPR; i += 32) {
-        const int row = (i >> 3) & (GRP - 1);
-        if (MOD ? !((seen >> row) & 1u) : g0 + row >= fill) const_cast<uint4*>(vr)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (MOD) {  // hidden rows (weighted by zero) hold anything: make them finite, 32 / CPR of them at a time
+      for (uint32_t hidden = ~seen; hidden != 0u;) {
+        int row = __ffs(hidden) - 1;
+        hidden &= hidden - 1u;
+#pragma unroll
+        for (int more = 1; more < 32 / CPR; ++more) {
+          if (lane >= more * CPR && hidden != 0u) row = __ffs(hidden) - 1;
+          hidden &= hidden - 1u;
+        }
+        const_cast<uint4*>(vr)[(lane % CPR / 8) * GRP * 8 + row * 8 + lane % 8] = make_uint4(0u, 0u, 0u, 0u);
       }
+      __syncwarp();
+    } else if (g0 + GRP > fill) {  // rows past the fill level (weighted by zero) hold anything: make them finite
+      for (int i = lane; i < GRP * CPR; i += 32)
+        if (g0 + ((i >> 3) & (GRP - 1)) >= fill) const_cast<uint4*>(vr)[i] = make_uint4(0u, 0u, 0u, 0u);
       __syncwarp();
     }
 #pragma unroll
@@ -414,6 +433,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
           const uint32_t b0 = __byte_perm(w0[e >> 1], w1[e >> 1], sel);
           const uint32_t b1 = __byte_perm(w2[e >> 1], w3[e >> 1], sel);
           mma_bf16_m16n8k16(o[8 * h + e], w[2 * hf][0], w[2 * hf][1], w[2 * hf + 1][0], w[2 * hf + 1][1], b0, b1);
+          if (MOD) mma_bf16_m16n8k16(o[8 * h + e], third[2 * hf], 0u, third[2 * hf + 1], 0u, b0, b1);
         }
       }
   }
@@ -460,8 +480,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
 
 // ------------------------------------------------------------------------------------------------ generic
 
-template <bool MOD>
-__global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const AttendArgs a) {
+static __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const AttendArgs a) {
   extern __shared__ __align__(16) float asm_[];  // q as fp32 [G][d], then part_ml [warps][G][2], part_o [warps][G][d]
   const he_config& cfg = a.cfg;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -475,14 +494,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const At
   for (int idx = tid; idx < G * cpr; idx += kAttendThreads)
     stage_chunk(qs + (idx / cpr) * d, static_cast<const char*>(a.q) + ((size_t)unit * G + idx / cpr) * d * es, idx % cpr, cfg.dtype);
   __syncthreads();
-  const float scale = MOD ? a.mod.scale_log2 : rsqrtf((float)d) * kLog2e;
-  int now = 0, low = 0;  // MOD: the query's position, the first one it sees
-  if (MOD) {
-    now = a.ca.next_pos[unit] - 1;
-    if (a.mod.window > 0) low = max(low, now - a.mod.window + 1);
-    if (a.mod.first_pos != nullptr) low = max(low, a.mod.first_pos[blockIdx.y]);
-  }
-  const float* slopes = MOD && a.mod.slopes != nullptr ? a.mod.slopes + blockIdx.x * G : nullptr;
+  const float scale = rsqrtf((float)d) * kLog2e;
   const char* Kb = static_cast<const char*>(a.ca.k_cache) + (size_t)unit * cfg.max_budget * d * es;
   const char* Vb = static_cast<const char*>(a.ca.v_cache) + (size_t)unit * cfg.max_budget * d * es;
   const int per = d / 32 + (d % 32 ? 1 : 0);  // channels per lane (<= 8): c = lane + 32 * i
@@ -499,12 +511,6 @@ __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const At
                                       : reinterpret_cast<const float*>(row)[c];
   };
   for (int j = warp; j < fill; j += kAttendWarps) {
-    float away = 0.f;
-    if (MOD) {
-      const int p = a.ca.pos[(size_t)unit * cfg.max_budget + j];
-      if (p < low) continue;
-      away = (float)abs(now - p) * kLog2e;
-    }
     const char* kr = Kb + (size_t)j * d * es;
     const char* vr = Vb + (size_t)j * d * es;
     float kv[kMaxDim / 32], vv[kMaxDim / 32];
@@ -524,11 +530,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const At
           if (i < per && c < d) dot = fmaf(qs[g * d + c], kv[i], dot);
         }
         for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, off);
-        float sc = dot * scale;
-        if (MOD) {
-          if (a.mod.cap_log2 > 0.f) sc = a.mod.cap_log2 * tanhf(dot * a.mod.inv_cap);
-          if (slopes != nullptr) sc -= slopes[g] * away;
-        }
+        const float sc = dot * scale;
         const float mn = fmaxf(m[g], sc);
         const float corr = exp2f(m[g] - mn), p = exp2f(sc - mn);  // exp2f(-inf) = 0 on the first slot
         l[g] = l[g] * corr + p;
@@ -554,6 +556,180 @@ __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(const At
   }
   __syncthreads();
   attend_merge<kAttendWarps>(part_ml, part_o, G, d, a.out + (size_t)unit * G * d);
+}
+
+// ------------------------------------------------------------------------------------------------ he_attend_scored, any dtype and d
+//
+// 64 slots at a time in shared memory as fp32, K rows padded so that lanes that read neighbouring rows meet every bank once. Scores: a warp
+// works for one query head (8 / GP warps share a head's slots, GP the group rounded up to a power of two), a lane for one or more slots.
+// Output: warp w adds up slots 8 w .. 8 w + 7 of the tile for all heads, a lane for four channels of every 128. A cluster of S CTAs shares a
+// unit as in attend_bf16_kernel. Bound by HBM where the grid fills the SMs (three CTAs of 70 KB each at d = 128), else by what an SM pulls.
+// Hidden slots are not read at all: their rows are zeros.
+constexpr int kScoredSlots = 64;
+inline size_t scored_smem(int S, int G, int d) {
+  const size_t tiles = (size_t)kScoredSlots * (2 * d + 4), merge = (size_t)8 * G * (d + 2);
+  return sizeof(float) * ((size_t)G * d + (tiles > merge ? tiles : merge) + kScoredSlots * 8 + 64 + (S > 1 ? (size_t)S * G * (d + 2) : 0));
+}
+
+template <int E, int GP>
+__global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const AttendArgs a, const int S) {
+  extern __shared__ __align__(16) float asm_[];
+  __shared__ __align__(8) unsigned long long merge_bar;
+  const he_config& cfg = a.cfg;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = blockIdx.x % S, head = blockIdx.x / S, unit = blockIdx.y * cfg.n_kv_heads + head;
+  const int d = cfg.head_dim, G = cfg.group_size, pitch = d + 4;
+  float* qs = asm_;                                  // [G][d]
+  float* ks = qs + G * d;                            // [64][d + 4], then vs [64][d]; at the end part_ml, part_o
+  float* vs = ks + kScoredSlots * pitch;
+  const int tiles_floats = kScoredSlots * (2 * d + 4), merge_floats = 8 * G * (d + 2);
+  float* ps = ks + max(tiles_floats, merge_floats);  // [64 slots][8] weights
+  float* stat = ps + kScoredSlots * 8;               // [8] factors of the output, [8][2] maxima by warp (see below)
+  float* gather = stat + 64;
+  const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&merge_bar);
+  griddep_launch_dependents();
+  if (S > 1) {
+    if (rank == 0 && tid == 0) {
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory");
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)((S - 1) * G * (d + 2) * 4)) : "memory");
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // waited for before the first remote store
+  }
+  griddep_wait();
+  const int fill = __ldcg(a.ca.fill + unit), now = __ldcg(a.ca.next_pos + unit) - 1;
+  int low = a.mod.first_pos != nullptr ? max(0, a.mod.first_pos[blockIdx.y]) : 0;
+  if (a.mod.window > 0) low = max(low, now - a.mod.window + 1);
+  const int cpr = d * E / 16;
+  for (int i = tid; i < G * cpr; i += kAttendThreads) stage_chunk(qs + (i / cpr) * d, static_cast<const char*>(a.q) + ((size_t)unit * G + i / cpr) * d * E, i % cpr, cfg.dtype);
+  const char* Kb = static_cast<const char*>(a.ca.k_cache) + (size_t)unit * cfg.max_budget * d * E;
+  const char* Vb = static_cast<const char*>(a.ca.v_cache) + (size_t)unit * cfg.max_budget * d * E;
+  const int32_t* pos = a.ca.pos + (size_t)unit * cfg.max_budget;
+  constexpr int WPH = 8 / GP, MINE = kScoredSlots / (32 * WPH) > 0 ? kScoredSlots / (32 * WPH) : 1;  // warps of a head, slots of a lane
+  constexpr int LANES = kScoredSlots / (WPH * MINE);                                                   // lanes of a warp with slots
+  const int g = warp / WPH, part = warp % WPH;
+  const float slope = a.mod.slopes != nullptr && g < G ? a.mod.slopes[head * G + g] * kLog2e : 0.f;
+  float m = -INFINITY, l = 0.f;  // of head g; l of this lane's slots
+  float o[8][8];                 // [head][channel 4 lane + e, 128 + 4 lane + e]
+#pragma unroll
+  for (int h = 0; h < 8; ++h)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[h][e] = 0.f;
+  for (int j0 = kScoredSlots * rank; j0 < fill; j0 += kScoredSlots * S) {
+    __syncthreads();  // the last tile has been read (and q written)
+    for (int i = tid; i < kScoredSlots * cpr; i += kAttendThreads) {
+      const int r = i / cpr, c = i % cpr;
+      const bool seen = j0 + r < fill && __ldcg(pos + j0 + r) >= low;
+      uint4 k4 = make_uint4(0u, 0u, 0u, 0u), v4 = k4;
+      if (seen) {
+        k4 = ldg_stream16(reinterpret_cast<const uint4*>(Kb + (size_t)(j0 + r) * d * E) + c);
+        v4 = ldg_stream16(reinterpret_cast<const uint4*>(Vb + (size_t)(j0 + r) * d * E) + c);
+      }
+      store_chunk(ks + r * pitch, k4, c, E == 2 ? HE_DTYPE_BF16 : HE_DTYPE_F32);
+      store_chunk(vs + r * d, v4, c, E == 2 ? HE_DTYPE_BF16 : HE_DTYPE_F32);
+    }
+    int p[MINE];
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) {
+      const int r = part * LANES * MINE + u * LANES + lane % LANES;
+      p[u] = j0 + r < fill ? __ldcg(pos + j0 + r) : -1;
+    }
+    __syncthreads();
+    // scores of head g
+    float x[MINE], top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) {
+      const int r = part * LANES * MINE + u * LANES + lane % LANES;
+      float s4[4] = {0.f, 0.f, 0.f, 0.f};
+      if (g < G)
+        for (int c = 0; c < d; c += 4) {
+          const float4 k4 = *reinterpret_cast<const float4*>(ks + r * pitch + c), q4 = *reinterpret_cast<const float4*>(qs + g * d + c);
+          s4[0] = fmaf(k4.x, q4.x, s4[0]), s4[1] = fmaf(k4.y, q4.y, s4[1]), s4[2] = fmaf(k4.z, q4.z, s4[2]), s4[3] = fmaf(k4.w, q4.w, s4[3]);
+        }
+      const float dot = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+      float y = a.mod.cap_log2 > 0.f ? a.mod.cap_log2 * tanhf(dot * a.mod.inv_cap) : dot * a.mod.scale_log2;
+      y -= slope * (float)abs(now - p[u]);
+      x[u] = p[u] >= low ? y : -INFINITY;
+      top = fmaxf(top, x[u]);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, off));
+    if (WPH > 1) {  // a head's warps agree on the maximum
+      if (lane == 0) stat[8 + warp] = top;
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < WPH; ++u) top = fmaxf(top, stat[8 + g * WPH + u]);
+    }
+    const float mx = fmaxf(m, top), mn = mx == -INFINITY ? 0.f : mx, corr = exp2f(m - mn);
+    m = mx;
+    l *= corr;
+#pragma unroll
+    for (int u = 0; u < MINE; ++u) {
+      const int r = part * LANES * MINE + u * LANES + lane % LANES;
+      const float w = exp2f(x[u] - mn);
+      if (lane < LANES) l += w, ps[r * 8 + g] = w;
+    }
+    if (part == 0 && lane == 0) stat[g] = corr;
+    __syncthreads();
+    // output: this warp's slots
+    float f[8];
+    *reinterpret_cast<float4*>(f) = *reinterpret_cast<const float4*>(stat);
+    if (GP > 4) *reinterpret_cast<float4*>(f + 4) = *reinterpret_cast<const float4*>(stat + 4);
+#pragma unroll
+    for (int h = 0; h < GP; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[h][e] *= f[h];
+#pragma unroll 2
+    for (int r = 8 * warp; r < 8 * warp + 8; ++r) {
+      float w[8];
+      *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(ps + r * 8);
+      if (GP > 4) *reinterpret_cast<float4*>(w + 4) = *reinterpret_cast<const float4*>(ps + r * 8 + 4);
+#pragma unroll
+      for (int part_c = 0; part_c < 2; ++part_c) {
+        const int c = 128 * part_c + 4 * lane;
+        if (c < d) {
+          const float4 v4 = *reinterpret_cast<const float4*>(vs + r * d + c);
+#pragma unroll
+          for (int h = 0; h < GP; ++h) {
+            o[h][4 * part_c] = fmaf(w[h], v4.x, o[h][4 * part_c]), o[h][4 * part_c + 1] = fmaf(w[h], v4.y, o[h][4 * part_c + 1]);
+            o[h][4 * part_c + 2] = fmaf(w[h], v4.z, o[h][4 * part_c + 2]), o[h][4 * part_c + 3] = fmaf(w[h], v4.w, o[h][4 * part_c + 3]);
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  // every warp's share of the output, the sums by the warps that hold them
+  float* part_ml = ks;
+  float* part_o = ks + 8 * G * 2;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, off);
+  if (lane == 0) stat[16 + warp] = m, stat[24 + warp] = l;
+  __syncthreads();
+  for (int h = lane; h < G; h += 32) {
+    float lw = 0.f;  // (counted once: by warp 0)
+    if (warp == 0)
+      for (int u = 0; u < WPH; ++u) lw += stat[24 + h * WPH + u];
+    part_ml[(warp * G + h) * 2] = stat[16 + h * WPH], part_ml[(warp * G + h) * 2 + 1] = lw;
+  }
+#pragma unroll
+  for (int h = 0; h < GP; ++h)
+    if (h < G)
+#pragma unroll
+      for (int part_c = 0; part_c < 2; ++part_c) {
+        const int c = 128 * part_c + 4 * lane;
+        if (c < d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) part_o[(warp * G + h) * d + c + e] = o[h][4 * part_c + e];
+      }
+  __syncthreads();
+  if (S == 1) {
+    attend_merge<8>(part_ml, part_o, G, d, a.out + (size_t)unit * G * d);
+    return;
+  }
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  attend_merge_cluster<8>(part_ml, part_o, gather, bar, G, d, S, rank, a.out + (size_t)unit * G * d);
 }
 
 // ------------------------------------------------------------------------------------------------ attention loss

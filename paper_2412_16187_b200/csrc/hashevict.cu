@@ -876,8 +876,8 @@ int he_attend(const he_config* cfg, const he_cache* cache, const void* q, float*
       return d == 64 ? launch_attend<64, false>(a, maps, st) : launch_attend<128, false>(a, maps, st);
   }
   const size_t smem = ((size_t)G * d + (size_t)kAttendWarps * G * (d + 2)) * sizeof(float);
-  if (int rc = set_smem(attend_generic_kernel<false>, smem)) return rc;
-  attend_generic_kernel<false><<<grid, kAttendThreads, smem, st>>>(a);
+  if (int rc = set_smem(attend_generic_kernel, smem)) return rc;
+  attend_generic_kernel<<<grid, kAttendThreads, smem, st>>>(a);
   HE_CUDA_CHECK(cudaGetLastError());
   return HE_OK;
 }

@@ -117,14 +117,23 @@ int check_mod(const he_score_mod* mod, int d, float* scale_log2, float* cap_log2
   return HE_OK;
 }
 
-template <int NQ>
+template <int NQ, int R>
 int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
-  const int tiles = (a.tokens + kPromptRows - 1) / kPromptRows;
+  const int tiles = (a.tokens + 16 * R - 1) / (16 * R);
   const long long ctas = (long long)tiles * a.batch * a.n_kv_heads * a.group;
   if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld tiles in one call", ctas);
-  const size_t smem = prompt_fp32_smem(a.d);
-  if (int rc = set_smem(prompt_fp32_kernel<NQ>, smem)) return rc;
-  return launch_pdl(prompt_fp32_kernel<NQ>, dim3((unsigned)ctas), kPromptThreads, smem, true, st, a, tiles);
+  const size_t smem = prompt_fp32_smem<R>(a.d);
+  auto kernel = prompt_fp32_kernel<NQ, R>;
+  if (int rc = set_smem(kernel, smem)) return rc;
+  return launch_pdl(kernel, dim3((unsigned)ctas), kPromptThreads, smem, true, st, a, tiles);
+}
+// Tiles of 64 rows once there is one for every SM, else of 16.
+template <int NQ>
+int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  const long long large = (long long)((a.tokens + 63) / 64) * a.batch * a.n_kv_heads * a.group;
+  return large >= sms ? launch_prompt_fp32<NQ, 4>(a, st) : launch_prompt_fp32<NQ, 1>(a, st);
 }
 
 // Tensor map of q, k or v: {channel, token, head, sequence} in boxes of 64 channels x 128 tokens, 128-byte swizzle. An axis of one
@@ -172,6 +181,34 @@ template <int D>
 int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
   if (a.cap_log2 > 0.f) return a.slopes != nullptr ? launch_prompt_tc<D, true, true>(a, maps, st) : launch_prompt_tc<D, true, false>(a, maps, st);
   return a.slopes != nullptr ? launch_prompt_tc<D, false, true>(a, maps, st) : launch_prompt_tc<D, false, false>(a, maps, st);
+}
+
+// As many CTAs per unit as keep the grid within two per SM, at most 8 (a cluster of any device) and no fewer than two tiles of slots for each.
+template <int E, int GP>
+int launch_scored(const AttendArgs& a, cudaStream_t st) {
+  const long long units = (long long)a.cfg.batch * a.cfg.n_kv_heads;
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  int S = 1;
+  while (S < 8 && 2 * S * units <= 2 * sms && 2 * S * 2 * kScoredSlots <= a.cfg.max_budget) S *= 2;
+  const size_t smem = scored_smem(S, a.cfg.group_size, a.cfg.head_dim);
+  auto kernel = attend_scored_kernel<E, GP>;
+  if (int rc = set_smem(kernel, smem)) return rc;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3((unsigned)(a.cfg.n_kv_heads * S), (unsigned)a.cfg.batch);
+  lc.blockDim = dim3(kAttendThreads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)S;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = S > 1 ? 2 : 1;
+  HE_CUDA_CHECK(cudaLaunchKernelEx(&lc, kernel, a, S));
+  return HE_OK;
 }
 
 }  // namespace
@@ -302,7 +339,6 @@ int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score
   const int G = cfg->group_size, d = cfg->head_dim;
   if (int rc = check_mod(mod, d, &a.mod.scale_log2, &a.mod.cap_log2, &a.mod.inv_cap, &a.mod.window, &a.mod.slopes)) return rc;
   a.mod.first_pos = first_pos;
-  const dim3 grid((unsigned)cfg->n_kv_heads, (unsigned)cfg->batch);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (cfg->dtype == HE_DTYPE_BF16 && d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr) {
     const long long rows = (long long)cfg->batch * cfg->n_kv_heads * cfg->max_budget;
@@ -310,11 +346,10 @@ int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score
     if (cache_rows_tmap(cache->k_cache, rows, d, &maps.k) && cache_rows_tmap(cache->v_cache, rows, d, &maps.v))
       return d <= 64 ? launch_attend<64, true>(a, maps, st) : launch_attend<128, true>(a, maps, st);
   }
-  const size_t smem = ((size_t)G * d + (size_t)kAttendWarps * G * (d + 2)) * sizeof(float);
-  if (int rc = set_smem(attend_generic_kernel<true>, smem)) return rc;
-  attend_generic_kernel<true><<<grid, kAttendThreads, smem, st>>>(a);
-  HE_CUDA_CHECK(cudaGetLastError());
-  return HE_OK;
+  if (G == 1) return cfg->dtype == HE_DTYPE_BF16 ? launch_scored<2, 1>(a, st) : launch_scored<4, 1>(a, st);
+  if (G == 2) return cfg->dtype == HE_DTYPE_BF16 ? launch_scored<2, 2>(a, st) : launch_scored<4, 2>(a, st);
+  if (G <= 4) return cfg->dtype == HE_DTYPE_BF16 ? launch_scored<2, 4>(a, st) : launch_scored<4, 4>(a, st);
+  return cfg->dtype == HE_DTYPE_BF16 ? launch_scored<2, 8>(a, st) : launch_scored<4, 8>(a, st);
 }
 
 }  // extern "C"

@@ -4,7 +4,7 @@
 // All kernels keep the running maximum, the sum of the weights and the unnormalised output of a row in fp32, in log2 units.
 //
 //   prompt_tc_kernel      bf16, head sizes up to 128: two tiles of 128 rows x 128 keys at a time on the tensor cores (tcgen05).
-//   prompt_fp32_kernel    any dtype and head size: 64 rows x 64 keys at a time on the CUDA cores.
+//   prompt_fp32_kernel    any dtype and head size: 64 or 16 rows x 64 keys at a time on the CUDA cores.
 //
 // Values in hidden places. Hidden keys get a weight of zero by selection, whatever their score is; a hidden V row that holds an infinity or a
 // NaN would still turn the product 0 * V into NaN. V rows behind the prompt's end are therefore read as zeros, and a
@@ -86,46 +86,57 @@ static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s,
 
 // ------------------------------------------------------------------------------------------------ CUDA cores
 //
-// 64 rows of one query head per CTA, 64 keys at a time. Thread (ty, tx) of 16 x 16 holds the scores of rows 4 ty .. + 3 and keys
-// 4 tx .. + 3, and of the output the same rows and channels 4 tx .. + 3 of every 64. Q and K lie in shared memory channel by channel, so that
-// both are read as four values at a time; the weights go through shared memory key by key.
-constexpr int kPromptRows = 64, kPromptThreads = 256, kPromptPitch = 68;
-inline size_t prompt_fp32_smem(int d) { return sizeof(float) * (2 * (size_t)d * kPromptPitch + 64 * (size_t)d + 64 * (size_t)kPromptPitch); }
+// 16 R rows of one query head per CTA, 64 keys at a time. Thread (ty, tx) of 16 x 16 holds the scores of rows R ty .. + R - 1 and keys
+// tx, tx + 16, tx + 32, tx + 48, and of the output the same rows and channels 4 tx .. + 3 of every 64. Q and K lie in shared memory row by row, four
+// floats longer than the row, so that the 16 threads that read neighbouring keys meet every bank once; the weights go through shared memory key by key.
+// Bound by the FMA pipe and the loads that feed it (R = 4: 8 loads of 16 bytes for 64 products). R = 1 for calls that would leave SMs idle.
+constexpr int kPromptThreads = 256;
+template <int R>
+constexpr int kPromptPitch = 16 * R + 4;  // of the weights
+template <int R>
+inline size_t prompt_fp32_smem(int d) {
+  return sizeof(float) * ((size_t)(16 * R + 64) * (d + 4) + 64 * (size_t)d + 64 * (size_t)kPromptPitch<R>);
+}
 
-template <int NQ>  // groups of 64 channels
+template <int NQ, int R>  // groups of 64 channels, rows of a thread
 __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __grid_constant__ PromptArgs a, const int tiles) {
   extern __shared__ __align__(16) float psm_[];
-  const int d = a.d, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
+  constexpr int PP = kPromptPitch<R>;
+  const int d = a.d, pitch = d + 4, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
   const int heads = a.n_kv_heads * a.group;
   const int head = blockIdx.x % heads, s = (blockIdx.x / heads) % a.batch, tile = tiles - 1 - blockIdx.x / heads / a.batch;
-  const int kv = head / a.group, i0 = tile * kPromptRows;
-  float* qt = psm_;                   // [d][68]
-  float* kt = qt + d * kPromptPitch;  // [d][68]
-  float* vs = kt + d * kPromptPitch;  // [64][d]
-  float* pt = vs + 64 * d;            // [64 keys][68]
+  const int kv = head / a.group, i0 = tile * 16 * R;
+  float* qs = psm_;                // [16 R][d + 4]
+  float* ks = qs + 16 * R * pitch; // [64][d + 4]
+  float* vs = ks + 64 * pitch;     // [64][d]
+  float* pt = vs + 64 * d;         // [64 keys][16 R + 4]
   __shared__ int run[2];
   griddep_launch_dependents();
   griddep_wait();
   const int n = min(max(a.lens[s], 0), a.tokens);
   if (i0 >= n) return;
   if (tid == 0) run[0] = 0x7FFFFFFF, run[1] = 0;
-  int lo[4], hi[4];
+  int lo[R], hi[R];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) prompt_interval(a, s, i0 + 4 * ty + r, n, lo[r], hi[r]);
+  for (int r = 0; r < R; ++r) prompt_interval(a, s, i0 + R * ty + r, n, lo[r], hi[r]);
   __syncthreads();
   if (tx == 0)
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < R; ++r)
       if (lo[r] < hi[r]) atomicMin(&run[0], lo[r]), atomicMax(&run[1], hi[r]);
   const long long q0 = s * a.qs[0] + head * a.qs[1], k0 = s * a.ks[0] + kv * a.ks[1];
-  for (int idx = tid; idx < 64 * d; idx += kPromptThreads) {
-    const int r = idx / d, c = idx % d;
-    qt[c * kPromptPitch + r] = i0 + r < n ? prompt_element(a.q, q0 + (i0 + r) * a.qs[2] + c, a.dtype) : 0.f;
+  const int es = esize_of(a.dtype), cpr = d * es / 16;  // 16-byte chunks of a row
+  auto chunk = [&](const void* p, long long row_at, int c) {
+    return __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p) + row_at * es) + c);
+  };
+  for (int idx = tid; idx < 16 * R * cpr; idx += kPromptThreads) {
+    const int r = idx / cpr, c = idx % cpr;
+    store_chunk(qs + r * pitch, i0 + r < n ? chunk(a.q, q0 + (i0 + r) * a.qs[2], c) : make_uint4(0u, 0u, 0u, 0u), c, a.dtype);
   }
   const float slope = a.slopes != nullptr ? a.slopes[head] * kPromptLog2e : 0.f;
-  float m[4], l[4], o[4][4 * NQ];
+  float m[R], l[R], o[R][4 * NQ];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
+  for (int r = 0; r < R; ++r) {
     m[r] = -INFINITY, l[r] = 0.f;
 #pragma unroll
     for (int c = 0; c < 4 * NQ; ++c) o[r][c] = 0.f;
@@ -134,32 +145,40 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
   const int j_begin = run[0] / 64 * 64, j_end = run[1];
   for (int j0 = j_begin; j0 < j_end; j0 += 64) {
     __syncthreads();  // the last tile has been read
-    for (int idx = tid; idx < 64 * d; idx += kPromptThreads) {
-      const int r = idx / d, c = idx % d, j = j0 + r;
-      kt[c * kPromptPitch + r] = j < n ? prompt_element(a.k, k0 + j * a.ks[2] + c, a.dtype) : 0.f;
-      vs[idx] = j < n ? prompt_element(a.v, k0 + j * a.ks[2] + c, a.dtype) : 0.f;
+#pragma unroll 4
+    for (int idx = tid; idx < 64 * cpr; idx += kPromptThreads) {
+      const int r = idx / cpr, c = idx % cpr, j = j0 + r;
+      uint4 k4 = make_uint4(0u, 0u, 0u, 0u), v4 = k4;
+      if (j < n) k4 = chunk(a.k, k0 + j * a.ks[2], c), v4 = chunk(a.v, k0 + j * a.ks[2], c);
+      store_chunk(ks + r * pitch, k4, c, a.dtype);
+      store_chunk(vs + r * d, v4, c, a.dtype);
     }
     __syncthreads();
-    float x[4][4];
+    float x[R][4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[r][e] = 0.f;
-    for (int c = 0; c < d; ++c) {
-      const float4 q4 = *reinterpret_cast<const float4*>(qt + c * kPromptPitch + 4 * ty), k4 = *reinterpret_cast<const float4*>(kt + c * kPromptPitch + 4 * tx);
-      const float qv[4] = {q4.x, q4.y, q4.z, q4.w}, kv4[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll 2
+    for (int c = 0; c < d; c += 4) {
+      float4 q4[R], k4[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(qs + (R * ty + r) * pitch + c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[r][e] = fmaf(qv[r], kv4[e], x[r][e]);
+      for (int e = 0; e < 4; ++e) k4[e] = *reinterpret_cast<const float4*>(ks + (tx + 16 * e) * pitch + c);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[r][e] = fmaf(q4[r].w, k4[e].w, fmaf(q4[r].z, k4[e].z, fmaf(q4[r].y, k4[e].y, fmaf(q4[r].x, k4[e].x, x[r][e]))));
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = i0 + 4 * ty + r;
+    for (int r = 0; r < R; ++r) {
+      const int i = i0 + R * ty + r;
       float top = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int j = j0 + 4 * tx + e;
+        const int j = j0 + tx + 16 * e;
         float y = a.cap_log2 > 0.f ? a.cap_log2 * tanhf(x[r][e] * a.inv_cap) : x[r][e] * a.scale_log2;
         y -= slope * (float)abs(i - j);
         x[r][e] = j >= lo[r] && j < hi[r] ? y : -INFINITY;
@@ -180,11 +199,14 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<float4*>(pt + (4 * tx + e) * kPromptPitch + 4 * ty) = make_float4(x[0][e], x[1][e], x[2][e], x[3][e]);
-    __syncwarp();  // rows 4 ty .. + 3 are written and read by the same half warp
+#pragma unroll
+      for (int r = 0; r < R; ++r) pt[(tx + 16 * e) * PP + R * ty + r] = x[r][e];
+    __syncwarp();  // a row's weights are written and read by the same half warp
+#pragma unroll 2
     for (int j = 0; j < 64; ++j) {
-      const float4 p4 = *reinterpret_cast<const float4*>(pt + j * kPromptPitch + 4 * ty);
-      const float pv[4] = {p4.x, p4.y, p4.z, p4.w};
+      float pv[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) pv[r] = pt[j * PP + R * ty + r];
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const int c = 64 * q + 4 * tx;
@@ -192,7 +214,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
           const float4 v4 = *reinterpret_cast<const float4*>(vs + j * d + c);
           const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
+          for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[r][4 * q + e] = fmaf(pv[r], vv[e], o[r][4 * q + e]);
         }
@@ -200,8 +222,8 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
     }
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int i = i0 + 4 * ty + r;
+  for (int r = 0; r < R; ++r) {
+    const int i = i0 + R * ty + r;
     const long long o0 = s * a.os[0] + head * a.os[1] + i * a.os[2];
     bool bad = false;
 #pragma unroll
@@ -216,7 +238,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
     __syncwarp();
 #pragma unroll
     for (int w = 0; w < 2; ++w)  // the rows of this warp's two ty
-      if ((again >> (16 * w)) & 0xFFFFu) prompt_row_again(a, s, head, i0 + 4 * ((tid - lane) / 16 + w) + r, n);
+      if ((again >> (16 * w)) & 0xFFFFu) prompt_row_again(a, s, head, i0 + R * ((tid - lane) / 16 + w) + r, n);
   }
 }
 
