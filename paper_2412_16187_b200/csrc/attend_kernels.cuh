@@ -198,6 +198,10 @@ struct AttendRing {
 // With MOD the scores go through he_score_mod: four more bytes a slot (its position, fetched a group ahead into registers) beside 4 D
 // of K and V, and masked slots' V rows are cleared in the ring, as they may hold anything. d may then be below D: the tensor maps fill the channels
 // from d on with zeros.
+// Exactness: weights of few slots show the 2^-18 that two bf16 terms leave of each (1.3e-6 of the output at 20 slots), sums over many slots the truncation
+// of the MMA's accumulator (1.7e-6 at 8000). With MOD a weight has a third term and each group's products start from zero and are added with rounding: 2e-7 and
+// 6e-7. Groups of up to 4 heads hold the third terms in the rows that they leave empty (rows 4..7 repeat the heads of rows 0..3), larger
+// ones take products of their own.
 template <int D, int NW, bool MOD>
 __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const AttendArgs a, const int S, const __grid_constant__ CUtensorMap kmap,
                                                                      const __grid_constant__ CUtensorMap vmap) {
@@ -253,12 +257,14 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   }
   griddep_wait();
   const int fill = __ldcg(a.ca.fill + unit);
+  const bool fold = MOD && G <= 4;                // third terms in rows 4..7
+  const int my_head = fold ? gid & 3 : gid;
   float slope = 0.f;              // MOD: log2 units per position
   int now = 0, low = 0;           // MOD: the query's position, the first one it sees
   if (MOD) {                      // (asked for together with `fill`, looked at behind the first copies)
     now = __ldcg(a.ca.next_pos + unit) - 1;
     if (a.mod.first_pos != nullptr) low = a.mod.first_pos[blockIdx.y];
-    if (a.mod.slopes != nullptr && gid < G) slope = a.mod.slopes[(unit % cfg.n_kv_heads) * G + gid] * kLog2e;
+    if (a.mod.slopes != nullptr && my_head < G) slope = a.mod.slopes[(unit % cfg.n_kv_heads) * G + my_head] * kLog2e;
   }
   const int items = first < fill ? 2 * ((fill - first + stride - 1) / stride) : 0;
   const int row_base = unit * cfg.max_budget;
@@ -284,7 +290,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   for (int c = 0; c < NC; ++c) {
     uint4 t = make_uint4(0u, 0u, 0u, 0u);
     const int chunk = 2 * tig + (c & 1) + 8 * (c >> 1);
-    if (gid < G && (!MOD || chunk < d / 8)) t = static_cast<const uint4*>(a.q)[((size_t)unit * G + gid) * (d / 8) + chunk];
+    if (my_head < G && (!MOD || chunk < d / 8)) t = static_cast<const uint4*>(a.q)[((size_t)unit * G + my_head) * (d / 8) + chunk];
     qf[2 * c][0] = t.x, qf[2 * c][1] = t.y, qf[2 * c + 1][0] = t.z, qf[2 * c + 1][1] = t.w;
   }
   const float scale = MOD ? a.mod.scale_log2 : rsqrtf((float)d) * kLog2e;
@@ -384,13 +390,15 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
     uint32_t w[4][2];  // hi and lo halves of the weights of slots 8 i + 2 tig, + 1
 #pragma unroll
     for (int i = 0; i < 4; ++i) split_pair(p[2 * i], p[2 * i + 1], w[i][0], w[i][1]);
-    uint32_t third[4];  // MOD: what two terms leave of a weight (2^-17 of it) as a third, in products of its own: a few slots' weights are then as exact as fp32's
+    uint32_t third[4];  // MOD: what two terms leave of a weight
 #pragma unroll
-    for (int i = 0; MOD && i < 4; ++i)
+    for (int i = 0; MOD && i < 4; ++i) {
       asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n"
           : "=r"(third[i])
           : "f"(p[2 * i + 1] - __uint_as_float(w[i][0] & 0xFFFF0000u) - __uint_as_float(w[i][1] & 0xFFFF0000u)),
             "f"(p[2 * i] - __uint_as_float(w[i][0] << 16) - __uint_as_float(w[i][1] << 16)));
+      if (fold && gid >= 4) w[i][0] = third[i], w[i][1] = 0u;
+    }
     if (__any_sync(0xFFFFFFFFu, corr != 1.f)) {
 #pragma unroll
       for (int t2 = 0; t2 < 8 * NH; ++t2) o[t2][0] *= corr, o[t2][1] *= corr, o[t2][2] *= corr, o[t2][3] *= corr;
@@ -413,29 +421,56 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
         if (g0 + ((i >> 3) & (GRP - 1)) >= fill) const_cast<uint4*>(vr)[i] = make_uint4(0u, 0u, 0u, 0u);
       __syncwarp();
     }
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)  // 16 slots per MMA
+    if constexpr (MOD) {
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
-        uint4 vb[4];
+        uint4 vb[2][4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const int row = 16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1);
-          vb[s] = vr[h * GRP * 8 + row * 8 + (gid ^ (row & 7))];
-        }
-        const uint32_t w0[4] = {vb[0].x, vb[0].y, vb[0].z, vb[0].w};
-        const uint32_t w1[4] = {vb[1].x, vb[1].y, vb[1].z, vb[1].w};
-        const uint32_t w2[4] = {vb[2].x, vb[2].y, vb[2].z, vb[2].w};
-        const uint32_t w3[4] = {vb[3].x, vb[3].y, vb[3].z, vb[3].w};
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            const int row = 16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1);
+            vb[hf][s] = vr[h * GRP * 8 + row * 8 + (gid ^ (row & 7))];
+          }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint32_t sel = (e & 1) ? 0x7632u : 0x5410u;
-          const uint32_t b0 = __byte_perm(w0[e >> 1], w1[e >> 1], sel);
-          const uint32_t b1 = __byte_perm(w2[e >> 1], w3[e >> 1], sel);
-          mma_bf16_m16n8k16(o[8 * h + e], w[2 * hf][0], w[2 * hf][1], w[2 * hf + 1][0], w[2 * hf + 1][1], b0, b1);
-          if (MOD) mma_bf16_m16n8k16(o[8 * h + e], third[2 * hf], 0u, third[2 * hf + 1], 0u, b0, b1);
+          float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const uint32_t sel = (e & 1) ? 0x7632u : 0x5410u;
+            auto word = [&](const uint4& v) { return (e >> 1) == 0 ? v.x : (e >> 1) == 1 ? v.y : (e >> 1) == 2 ? v.z : v.w; };
+            const uint32_t b0 = __byte_perm(word(vb[hf][0]), word(vb[hf][1]), sel), b1 = __byte_perm(word(vb[hf][2]), word(vb[hf][3]), sel);
+            mma_bf16_m16n8k16(c, w[2 * hf][0], w[2 * hf][1], w[2 * hf + 1][0], w[2 * hf + 1][1], b0, b1);
+            if (!fold) mma_bf16_m16n8k16(c, third[2 * hf], 0u, third[2 * hf + 1], 0u, b0, b1);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[8 * h + e][k] += c[k];
         }
       }
+    } else {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)  // 16 slots per MMA
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+          uint4 vb[4];
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            const int row = 16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1);
+            vb[s] = vr[h * GRP * 8 + row * 8 + (gid ^ (row & 7))];
+          }
+          const uint32_t w0[4] = {vb[0].x, vb[0].y, vb[0].z, vb[0].w};
+          const uint32_t w1[4] = {vb[1].x, vb[1].y, vb[1].z, vb[1].w};
+          const uint32_t w2[4] = {vb[2].x, vb[2].y, vb[2].z, vb[2].w};
+          const uint32_t w3[4] = {vb[3].x, vb[3].y, vb[3].z, vb[3].w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t sel = (e & 1) ? 0x7632u : 0x5410u;
+            const uint32_t b0 = __byte_perm(w0[e >> 1], w1[e >> 1], sel);
+            const uint32_t b1 = __byte_perm(w2[e >> 1], w3[e >> 1], sel);
+            mma_bf16_m16n8k16(o[8 * h + e], w[2 * hf][0], w[2 * hf][1], w[2 * hf + 1][0], w[2 * hf + 1][1], b0, b1);
+          }
+        }
+    }
   }
   if (!ok) {  // gave up on a copy: count it, and let what is in flight land (bounded) before the rings are reused
     if (lane == 0) {
@@ -459,6 +494,12 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   // Per-warp partial result. l is summed over the quad (m and corr were equal across it).
   l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
   l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+  if (fold) {  // the third terms' share
+#pragma unroll
+    for (int t = 0; t < 8 * NH; ++t)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) o[t][k] += __shfl_down_sync(0xFFFFFFFFu, o[t][k], 16);
+  }
   if (gid < G) {
     if (tig == 0) part_ml[(warp * G + gid) * 2] = m, part_ml[(warp * G + gid) * 2 + 1] = l;
 #pragma unroll
