@@ -196,13 +196,13 @@ struct AttendRing {
 };
 
 // With MOD the scores go through he_score_mod: four more bytes a slot (its position, fetched a group ahead into registers) beside 4 D
-// of K and V, and masked slots' V rows are cleared in the ring, as they may hold anything. d may then be below D: the tensor maps fill the channels
+// of K and V, and masked slots' V rows are cleared in registers, as they may hold anything. With BELOW d is below D: the tensor maps fill the channels
 // from d on with zeros.
 // Exactness: weights of few slots show the 2^-18 that two bf16 terms leave of each (1.3e-6 of the output at 20 slots), sums over many slots the truncation
 // of the MMA's accumulator (1.7e-6 at 8000). With MOD a weight has a third term and each group's products start from zero and are added with rounding: 2e-7 and
-// 6e-7. Groups of up to 4 heads hold the third terms in the rows that they leave empty (rows 4..7 repeat the heads of rows 0..3), larger
+// 6e-7. Groups of up to 4 heads (FOLD) hold the third terms in the rows that they leave empty (rows 4..7 repeat the heads of rows 0..3), larger
 // ones take products of their own.
-template <int D, int NW, bool MOD>
+template <int D, int NW, bool MOD, bool CAP = false, bool FOLD = false, bool BELOW = false>
 __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const AttendArgs a, const int S, const __grid_constant__ CUtensorMap kmap,
                                                                      const __grid_constant__ CUtensorMap vmap) {
   using Ring = AttendRing<D, NW>;
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   constexpr int NC = D / 32, NH = D / 64;  // chunks of a K row per lane, of a V row per lane
   constexpr int NBUF = Ring::kBufs, GRP = kAttendGroup;
   const he_config& cfg = a.cfg;
-  const int d = MOD ? cfg.head_dim : D;
+  const int d = BELOW ? cfg.head_dim : D;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
   const int rank = blockIdx.x % S;
   const int unit = blockIdx.y * cfg.n_kv_heads + blockIdx.x / S;
@@ -257,8 +257,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   }
   griddep_wait();
   const int fill = __ldcg(a.ca.fill + unit);
-  const bool fold = MOD && G <= 4;                // third terms in rows 4..7
-  const int my_head = fold ? gid & 3 : gid;
+  const int my_head = FOLD ? gid & 3 : gid;
   float slope = 0.f;              // MOD: log2 units per position
   int now = 0, low = 0;           // MOD: the query's position, the first one it sees
   if (MOD) {                      // (asked for together with `fill`, looked at behind the first copies)
@@ -290,7 +289,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   for (int c = 0; c < NC; ++c) {
     uint4 t = make_uint4(0u, 0u, 0u, 0u);
     const int chunk = 2 * tig + (c & 1) + 8 * (c >> 1);
-    if (my_head < G && (!MOD || chunk < d / 8)) t = static_cast<const uint4*>(a.q)[((size_t)unit * G + my_head) * (d / 8) + chunk];
+    if (my_head < G && (!BELOW || chunk < d / 8)) t = static_cast<const uint4*>(a.q)[((size_t)unit * G + my_head) * (d / 8) + chunk];
     qf[2 * c][0] = t.x, qf[2 * c][1] = t.y, qf[2 * c + 1][0] = t.z, qf[2 * c + 1][1] = t.w;
   }
   const float scale = MOD ? a.mod.scale_log2 : rsqrtf((float)d) * kLog2e;
@@ -363,7 +362,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
         float s = (sa[i][e] + sb[i][e]) * scale;
         if (MOD) {
           const int p = e ? ahead[i].y : ahead[i].x;
-          if (a.mod.cap_log2 > 0.f) s = a.mod.cap_log2 * tanhf((sa[i][e] + sb[i][e]) * a.mod.inv_cap);
+          if (CAP) s = a.mod.cap_log2 * tanhf((sa[i][e] + sb[i][e]) * a.mod.inv_cap);
           s -= slope * (float)abs(now - p);
           ok_j = ok_j && p >= low;
           seen |= (uint32_t)ok_j << j;
@@ -397,26 +396,14 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
           : "=r"(third[i])
           : "f"(p[2 * i + 1] - __uint_as_float(w[i][0] & 0xFFFF0000u) - __uint_as_float(w[i][1] & 0xFFFF0000u)),
             "f"(p[2 * i] - __uint_as_float(w[i][0] << 16) - __uint_as_float(w[i][1] << 16)));
-      if (fold && gid >= 4) w[i][0] = third[i], w[i][1] = 0u;
+      if (FOLD && gid >= 4) w[i][0] = third[i], w[i][1] = 0u;
     }
     if (__any_sync(0xFFFFFFFFu, corr != 1.f)) {
 #pragma unroll
       for (int t2 = 0; t2 < 8 * NH; ++t2) o[t2][0] *= corr, o[t2][1] *= corr, o[t2][2] *= corr, o[t2][3] *= corr;
     }
     const uint4* vr = step(t + 1);
-    if (MOD) {  // hidden rows (weighted by zero) hold anything: make them finite, 32 / CPR of them at a time
-      for (uint32_t hidden = ~seen; hidden != 0u;) {
-        int row = __ffs(hidden) - 1;
-        hidden &= hidden - 1u;
-#pragma unroll
-        for (int more = 1; more < 32 / CPR; ++more) {
-          if (lane >= more * CPR && hidden != 0u) row = __ffs(hidden) - 1;
-          hidden &= hidden - 1u;
-        }
-        const_cast<uint4*>(vr)[(lane % CPR / 8) * GRP * 8 + row * 8 + lane % 8] = make_uint4(0u, 0u, 0u, 0u);
-      }
-      __syncwarp();
-    } else if (g0 + GRP > fill) {  // rows past the fill level (weighted by zero) hold anything: make them finite
+    if (!MOD && g0 + GRP > fill) {  // rows past the fill level (weighted by zero) hold anything: make them finite
       for (int i = lane; i < GRP * CPR; i += 32)
         if (g0 + ((i >> 3) & (GRP - 1)) >= fill) const_cast<uint4*>(vr)[i] = make_uint4(0u, 0u, 0u, 0u);
       __syncwarp();
@@ -432,6 +419,15 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
             const int row = 16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1);
             vb[hf][s] = vr[h * GRP * 8 + row * 8 + (gid ^ (row & 7))];
           }
+        if (seen != 0xFFFFFFFFu) {  // hidden rows (weighted by zero) hold anything: zeros
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+              const uint32_t keep = 0u - ((seen >> (16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1))) & 1u);
+              vb[hf][s].x &= keep, vb[hf][s].y &= keep, vb[hf][s].z &= keep, vb[hf][s].w &= keep;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float c[4] = {0.f, 0.f, 0.f, 0.f};
@@ -441,7 +437,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
             auto word = [&](const uint4& v) { return (e >> 1) == 0 ? v.x : (e >> 1) == 1 ? v.y : (e >> 1) == 2 ? v.z : v.w; };
             const uint32_t b0 = __byte_perm(word(vb[hf][0]), word(vb[hf][1]), sel), b1 = __byte_perm(word(vb[hf][2]), word(vb[hf][3]), sel);
             mma_bf16_m16n8k16(c, w[2 * hf][0], w[2 * hf][1], w[2 * hf + 1][0], w[2 * hf + 1][1], b0, b1);
-            if (!fold) mma_bf16_m16n8k16(c, third[2 * hf], 0u, third[2 * hf + 1], 0u, b0, b1);
+            if (!FOLD) mma_bf16_m16n8k16(c, third[2 * hf], 0u, third[2 * hf + 1], 0u, b0, b1);
           }
 #pragma unroll
           for (int k = 0; k < 4; ++k) o[8 * h + e][k] += c[k];
@@ -494,7 +490,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   // Per-warp partial result. l is summed over the quad (m and corr were equal across it).
   l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
   l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
-  if (fold) {  // the third terms' share
+  if (FOLD) {  // the third terms' share
 #pragma unroll
     for (int t = 0; t < 8 * NH; ++t)
 #pragma unroll
@@ -506,8 +502,8 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
     for (int t = 0; t < 8 * NH; ++t) {
       const int h = t >> 3, e = t & 7;
       const int c0 = (2 * tig + 8 * h) * 8 + e, c1 = c0 + 8;
-      if (!MOD || c0 < d) part_o[(warp * G + gid) * d + c0] = o[t][0] + o[t][2];
-      if (!MOD || c1 < d) part_o[(warp * G + gid) * d + c1] = o[t][1] + o[t][3];
+      if (!BELOW || c0 < d) part_o[(warp * G + gid) * d + c0] = o[t][0] + o[t][2];
+      if (!BELOW || c1 < d) part_o[(warp * G + gid) * d + c1] = o[t][1] + o[t][3];
     }
   }
   __syncthreads();
@@ -605,15 +601,21 @@ static __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(c
 // works for one query head (8 / GP warps share a head's slots, GP the group rounded up to a power of two), a lane for one or more slots.
 // Output: warp w adds up slots 8 w .. 8 w + 7 of the tile for all heads, a lane for four channels of every 128. A cluster of S CTAs shares a
 // unit as in attend_bf16_kernel. Bound by HBM where the grid fills the SMs (three CTAs of 70 KB each at d = 128), else by what an SM pulls.
-// Hidden slots are not read at all: their rows are zeros.
+// Hidden slots are not read at all: their rows are zeros. fp32 rows are copied asynchronously, with `stages` = 2 a tile ahead (calls that leave an SM
+// to one CTA); which slots of a tile are hidden is found out one tile earlier still, so that no copy waits for a position.
 constexpr int kScoredSlots = 64;
-inline size_t scored_smem(int S, int G, int d) {
-  const size_t tiles = (size_t)kScoredSlots * (2 * d + 4), merge = (size_t)8 * G * (d + 2);
+inline size_t scored_smem(int S, int stages, int G, int d) {
+  const size_t tiles = (size_t)stages * kScoredSlots * (2 * d + 4), merge = (size_t)8 * G * (d + 2);
   return sizeof(float) * ((size_t)G * d + (tiles > merge ? tiles : merge) + kScoredSlots * 8 + 64 + (S > 1 ? (size_t)S * G * (d + 2) : 0));
+}
+// 16 bytes into shared memory, or zeros
+__device__ __forceinline__ void cp_async16_or_zero(void* smem_dst, const void* gmem_src, bool some) {
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(smem_dst);
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(gmem_src), "r"(some ? 16u : 0u) : "memory");
 }
 
 template <int E, int GP>
-__global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const AttendArgs a, const int S) {
+__global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const AttendArgs a, const int S, const int stages) {
   extern __shared__ __align__(16) float asm_[];
   __shared__ __align__(8) unsigned long long merge_bar;
   const he_config& cfg = a.cfg;
@@ -622,10 +624,10 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Att
   const int d = cfg.head_dim, G = cfg.group_size, pitch = d + 4;
   float* qs = asm_;                                  // [G][d]
   float* ks = qs + G * d;                            // [64][d + 4], then vs [64][d]; at the end part_ml, part_o
-  float* vs = ks + kScoredSlots * pitch;
-  const int tiles_floats = kScoredSlots * (2 * d + 4), merge_floats = 8 * G * (d + 2);
+  const int stage_floats = kScoredSlots * (2 * d + 4), tiles_floats = stages * stage_floats, merge_floats = 8 * G * (d + 2);
   float* ps = ks + max(tiles_floats, merge_floats);  // [64 slots][8] weights
-  float* stat = ps + kScoredSlots * 8;               // [8] factors of the output, [8][2] maxima by warp (see below)
+  float* stat = ps + kScoredSlots * 8;               // [8] factors of the output, then what warps tell each other (see below)
+  uint32_t* seen_s = reinterpret_cast<uint32_t*>(stat + 32);  // [3][2] visible slots of a tile, by turns
   float* gather = stat + 64;
   const uint32_t bar = (uint32_t)__cvta_generic_to_shared(&merge_bar);
   griddep_launch_dependents();
@@ -657,18 +659,67 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Att
   for (int h = 0; h < 8; ++h)
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[h][e] = 0.f;
-  for (int j0 = kScoredSlots * rank; j0 < fill; j0 += kScoredSlots * S) {
-    __syncthreads();  // the last tile has been read (and q written)
-    for (int i = tid; i < kScoredSlots * cpr; i += kAttendThreads) {
-      const int r = i / cpr, c = i % cpr;
-      const bool seen = j0 + r < fill && __ldcg(pos + j0 + r) >= low;
-      uint4 k4 = make_uint4(0u, 0u, 0u, 0u), v4 = k4;
-      if (seen) {
-        k4 = ldg_stream16(reinterpret_cast<const uint4*>(Kb + (size_t)(j0 + r) * d * E) + c);
-        v4 = ldg_stream16(reinterpret_cast<const uint4*>(Vb + (size_t)(j0 + r) * d * E) + c);
+  const int step = kScoredSlots * S, j_first = kScoredSlots * rank;
+  auto look = [&](int tile) {  // which slots of a tile are visible (warps 0 and 1)
+    if (warp < 2) {
+      const int j = j_first + tile * step + 32 * warp + lane;
+      const uint32_t bits = __ballot_sync(0xFFFFFFFFu, j < fill && __ldcg(pos + j) >= low);
+      if (lane == 0) seen_s[2 * (tile % 3) + warp] = bits;
+    }
+  };
+  const int r_first = tid / cpr, c_first = tid % cpr, r_step = kAttendThreads / cpr, c_step = kAttendThreads % cpr;
+  auto fetch = [&](int tile) {
+    float* kt = ks + (stages == 2 ? tile & 1 : 0) * stage_floats;
+    float* vt = kt + kScoredSlots * pitch;
+    const int j0 = j_first + tile * step;
+    const uint32_t seen[2] = {seen_s[2 * (tile % 3)], seen_s[2 * (tile % 3) + 1]};
+    int r = r_first, c = c_first;
+    auto next = [&]() {
+      r += r_step, c += c_step;
+      if (c >= cpr) c -= cpr, ++r;
+    };
+    auto visible = [&](int row) { return ((row < 32 ? seen[0] : seen[1]) >> (row & 31)) & 1u; };
+    if (E == 4) {
+      for (; r < kScoredSlots; next()) {
+        const bool some = visible(r) != 0u;
+        const size_t at = ((size_t)(some ? j0 + r : 0) * d) * E + 16 * c;
+        cp_async16_or_zero(kt + r * pitch + 4 * c, Kb + at, some);
+        cp_async16_or_zero(vt + r * d + 4 * c, Vb + at, some);
       }
-      store_chunk(ks + r * pitch, k4, c, E == 2 ? HE_DTYPE_BF16 : HE_DTYPE_F32);
-      store_chunk(vs + r * d, v4, c, E == 2 ? HE_DTYPE_BF16 : HE_DTYPE_F32);
+    } else {
+      while (r < kScoredSlots) {  // four rows' chunks at a time in registers
+        uint4 k4[4], v4[4];
+        int rr[4], cc[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u, next()) {
+          rr[u] = r, cc[u] = c;
+          k4[u] = v4[u] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < kScoredSlots && visible(r)) {
+            const size_t at = ((size_t)(j0 + r) * d) * E + 16 * c;
+            k4[u] = ldg_stream16(reinterpret_cast<const uint4*>(Kb + at)), v4[u] = ldg_stream16(reinterpret_cast<const uint4*>(Vb + at));
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (rr[u] < kScoredSlots) store_chunk(kt + rr[u] * pitch, k4[u], cc[u], HE_DTYPE_BF16), store_chunk(vt + rr[u] * d, v4[u], cc[u], HE_DTYPE_BF16);
+      }
+    }
+    cp_async_commit();
+  };
+  const int tiles = j_first < fill ? (fill - j_first + step - 1) / step : 0;
+  look(0), look(1);
+  __syncthreads();
+  if (tiles > 0) fetch(0);
+  for (int tile = 0; tile < tiles; ++tile) {
+    const int j0 = j_first + tile * step;
+    const float* kt = ks + (stages == 2 ? tile & 1 : 0) * stage_floats;
+    const float* vt = kt + kScoredSlots * pitch;
+    look(tile + 2);
+    if (stages == 2 && tile + 1 < tiles) {
+      fetch(tile + 1);
+      cp_async_wait_pending(1);
+    } else {
+      cp_async_wait_all();
     }
     int p[MINE];
 #pragma unroll
@@ -685,7 +736,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Att
       float s4[4] = {0.f, 0.f, 0.f, 0.f};
       if (g < G)
         for (int c = 0; c < d; c += 4) {
-          const float4 k4 = *reinterpret_cast<const float4*>(ks + r * pitch + c), q4 = *reinterpret_cast<const float4*>(qs + g * d + c);
+          const float4 k4 = *reinterpret_cast<const float4*>(kt + r * pitch + c), q4 = *reinterpret_cast<const float4*>(qs + g * d + c);
           s4[0] = fmaf(k4.x, q4.x, s4[0]), s4[1] = fmaf(k4.y, q4.y, s4[1]), s4[2] = fmaf(k4.z, q4.z, s4[2]), s4[3] = fmaf(k4.w, q4.w, s4[3]);
         }
       const float dot = (s4[0] + s4[1]) + (s4[2] + s4[3]);
@@ -730,7 +781,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Att
       for (int part_c = 0; part_c < 2; ++part_c) {
         const int c = 128 * part_c + 4 * lane;
         if (c < d) {
-          const float4 v4 = *reinterpret_cast<const float4*>(vs + r * d + c);
+          const float4 v4 = *reinterpret_cast<const float4*>(vt + r * d + c);
 #pragma unroll
           for (int h = 0; h < GP; ++h) {
             o[h][4 * part_c] = fmaf(w[h], v4.x, o[h][4 * part_c]), o[h][4 * part_c + 1] = fmaf(w[h], v4.y, o[h][4 * part_c + 1]);
@@ -739,6 +790,8 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Att
         }
       }
     }
+    __syncthreads();  // the tile has been read
+    if (stages == 1 && tile + 1 < tiles) fetch(tile + 1);
   }
   __syncthreads();
   // every warp's share of the output, the sums by the warps that hold them

@@ -183,9 +183,9 @@ struct AttendMaps {
   alignas(64) CUtensorMap k, v;
 };
 
-template <int D, int NW, bool MOD>
+template <int D, int NW, bool MOD, bool CAP, bool FOLD, bool BELOW>
 int launch_attend_on(const AttendArgs& a, const AttendMaps& maps, int S, size_t smem, cudaStream_t st) {
-  if (int rc = set_smem(attend_bf16_kernel<D, NW, MOD>, smem)) return rc;
+  if (int rc = set_smem(attend_bf16_kernel<D, NW, MOD, CAP, FOLD, BELOW>, smem)) return rc;
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3((unsigned)(a.cfg.n_kv_heads * S), (unsigned)a.cfg.batch);
   lc.blockDim = dim3(32 * NW);
@@ -199,7 +199,7 @@ int launch_attend_on(const AttendArgs& a, const AttendMaps& maps, int S, size_t 
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   lc.attrs = at;
   lc.numAttrs = S > 1 ? 2 : 1;
-  HE_CUDA_CHECK(cudaLaunchKernelEx(&lc, attend_bf16_kernel<D, NW, MOD>, a, S, maps.k, maps.v));
+  HE_CUDA_CHECK(cudaLaunchKernelEx(&lc, attend_bf16_kernel<D, NW, MOD, CAP, FOLD, BELOW>, a, S, maps.k, maps.v));
   return HE_OK;
 }
 
@@ -216,7 +216,7 @@ constexpr size_t attend_smem(int S, int G) {
 // 90 GB/s, the GPU 6.3 TB/s, so a unit is spread until the grid has one CTA per SM. Measured (us per call in a graph, caches larger
 // than L2; register-fed kernel with clusters of up to 8 before): 8 units of 9830 slots 16.9 -> 10.6, 32 of 2048 8.7 -> 7.9, 128 of
 // 1024 14.6 -> 12.9.
-template <int D, bool MOD>
+template <int D, bool MOD, bool CAP = false, bool FOLD = false, bool BELOW = false>
 int launch_attend(const AttendArgs& a, const AttendMaps& maps, cudaStream_t st) {
   const long long units = (long long)a.cfg.batch * a.cfg.n_kv_heads;
   int sms = 0, dev = 0;
@@ -242,9 +242,9 @@ int launch_attend(const AttendArgs& a, const AttendMaps& maps, cudaStream_t st) 
         at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
         oc.attrs = at;
         oc.numAttrs = 1;
-        if (int rc = set_smem(attend_bf16_kernel<D, 8, MOD>, kAttendMaxSmem)) return rc;
-        if (cudaFuncSetAttribute(attend_bf16_kernel<D, 8, MOD>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(got, attend_bf16_kernel<D, 8, MOD>, &oc) != cudaSuccess || *got < 1) {
+        if (int rc = set_smem(attend_bf16_kernel<D, 8, MOD, CAP, FOLD, BELOW>, kAttendMaxSmem)) return rc;
+        if (cudaFuncSetAttribute(attend_bf16_kernel<D, 8, MOD, CAP, FOLD, BELOW>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(got, attend_bf16_kernel<D, 8, MOD, CAP, FOLD, BELOW>, &oc) != cudaSuccess || *got < 1) {
           (void)cudaGetLastError();
           *got = -1;
         }
@@ -258,8 +258,8 @@ int launch_attend(const AttendArgs& a, const AttendMaps& maps, cudaStream_t st) 
   if (S < 1) S = 1;
   // Two small CTAs per SM once there are more units than SMs, so that one streams while the other starts or merges (512 units
   // of 1000 slots, d = 64: 24.4 against 27.7 us; level at 256 units of 2048 slots).
-  if (units > sms) return launch_attend_on<D, 4, MOD>(a, maps, 1, 1024 + AttendRing<D, 4>::kBytes, st);
-  return launch_attend_on<D, 8, MOD>(a, maps, S, attend_smem<D>(S, a.cfg.group_size), st);
+  if (units > sms) return launch_attend_on<D, 4, MOD, CAP, FOLD, BELOW>(a, maps, 1, 1024 + AttendRing<D, 4>::kBytes, st);
+  return launch_attend_on<D, 8, MOD, CAP, FOLD, BELOW>(a, maps, S, attend_smem<D>(S, a.cfg.group_size), st);
 }
 
 }  // namespace he

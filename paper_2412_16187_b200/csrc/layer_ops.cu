@@ -183,6 +183,15 @@ int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t s
   return a.slopes != nullptr ? launch_prompt_tc<D, false, true>(a, maps, st) : launch_prompt_tc<D, false, false>(a, maps, st);
 }
 
+template <bool CAP, bool FOLD>
+int launch_scored_bf16(const AttendArgs& a, const AttendMaps& maps, cudaStream_t st) {
+  switch (a.cfg.head_dim) {
+    case 64: return launch_attend<64, true, CAP, FOLD, false>(a, maps, st);
+    case 128: return launch_attend<128, true, CAP, FOLD, false>(a, maps, st);
+    default: return a.cfg.head_dim < 64 ? launch_attend<64, true, CAP, FOLD, true>(a, maps, st) : launch_attend<128, true, CAP, FOLD, true>(a, maps, st);
+  }
+}
+
 // As many CTAs per unit as keep the grid within two per SM, at most 8 (a cluster of any device) and no fewer than two tiles of slots for each.
 template <int E, int GP>
 int launch_scored(const AttendArgs& a, cudaStream_t st) {
@@ -191,7 +200,9 @@ int launch_scored(const AttendArgs& a, cudaStream_t st) {
   if (int rc = sm_count(&sms)) return rc;
   int S = 1;
   while (S < 8 && 2 * S * units <= 2 * sms && 2 * S * 2 * kScoredSlots <= a.cfg.max_budget) S *= 2;
-  const size_t smem = scored_smem(S, a.cfg.group_size, a.cfg.head_dim);
+  // a tile ahead where an SM has one CTA and its 227 KB
+  const int stages = E == 4 && S * units <= sms && scored_smem(S, 2, a.cfg.group_size, a.cfg.head_dim) <= kAttendMaxSmem ? 2 : 1;
+  const size_t smem = scored_smem(S, stages, a.cfg.group_size, a.cfg.head_dim);
   auto kernel = attend_scored_kernel<E, GP>;
   if (int rc = set_smem(kernel, smem)) return rc;
   cudaLaunchConfig_t lc{};
@@ -207,7 +218,7 @@ int launch_scored(const AttendArgs& a, cudaStream_t st) {
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   lc.attrs = at;
   lc.numAttrs = S > 1 ? 2 : 1;
-  HE_CUDA_CHECK(cudaLaunchKernelEx(&lc, kernel, a, S));
+  HE_CUDA_CHECK(cudaLaunchKernelEx(&lc, kernel, a, S, stages));
   return HE_OK;
 }
 
@@ -344,7 +355,8 @@ int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score
     const long long rows = (long long)cfg->batch * cfg->n_kv_heads * cfg->max_budget;
     AttendMaps maps;
     if (cache_rows_tmap(cache->k_cache, rows, d, &maps.k) && cache_rows_tmap(cache->v_cache, rows, d, &maps.v))
-      return d <= 64 ? launch_attend<64, true>(a, maps, st) : launch_attend<128, true>(a, maps, st);
+      return a.mod.cap_log2 > 0.f ? (G <= 4 ? launch_scored_bf16<true, true>(a, maps, st) : launch_scored_bf16<true, false>(a, maps, st))
+                                  : (G <= 4 ? launch_scored_bf16<false, true>(a, maps, st) : launch_scored_bf16<false, false>(a, maps, st));
   }
   if (G == 1) return cfg->dtype == HE_DTYPE_BF16 ? launch_scored<2, 1>(a, st) : launch_scored<4, 1>(a, st);
   if (G == 2) return cfg->dtype == HE_DTYPE_BF16 ? launch_scored<2, 2>(a, st) : launch_scored<4, 2>(a, st);
