@@ -40,6 +40,13 @@ int check_strides(const char* what, const int64_t* strides, int n, int esize) {
   return HE_OK;
 }
 
+// The rows of an output do not overlap: an axis of more than one entry is a row or more apart.
+int check_apart(const char* what, const int64_t* strides, const long long* sizes, int n, int d) {
+  for (int i = 0; i < n; ++i)
+    if (sizes[i] > 1 && strides[i] < d) return fail(HE_ERR_INVALID_ARG, "%s stride %lld lets rows of %d overlap", what, (long long)strides[i], d);
+  return HE_OK;
+}
+
 template <int E, int V, bool INTER>
 int launch_rotate_as(const RotateArgs& a, const he_rotary& r, dim3 grid, cudaStream_t st) {
   return launch_pdl(rotate_kernel<E, V, INTER>, grid, kRotateThreads, 0, true, st, a, r);
@@ -57,7 +64,8 @@ int launch_rotate(RotateArgs a, const he_rotary& r, cudaStream_t st) {
   // Heads are shared out until there are enough CTAs for every SM, but a thread that has worked out its sines keeps at least four rows.
   const long long shares = (8LL * sms + blocks - 1) / blocks;
   a.heads_per_thread = (int)((all + shares - 1) / shares);
-  if (a.next_pos == nullptr && a.heads_per_thread < 4) a.heads_per_thread = 4;
+  if (a.heads_per_thread < 4) a.heads_per_thread = 4;
+  if (a.next_pos != nullptr) a.heads_per_thread = 1;  // (each head's unit has a position of its own)
   if (a.heads_per_thread > all) a.heads_per_thread = all;
   const dim3 grid((unsigned)blocks, (unsigned)((all + a.heads_per_thread - 1) / a.heads_per_thread));
   if (grid.y > 65535) return fail(HE_ERR_UNSUPPORTED, "%d heads in one call", all);
@@ -79,7 +87,8 @@ int launch_rotate(RotateArgs a, const he_rotary& r, cudaStream_t st) {
 }
 
 // q and k of a rotation: each given with its output, or not at all.
-int rotate_sides(RotateArgs& a, const he_config* cfg, const void* q, const void* k, void* q_out, void* k_out, const int64_t* const strides[4], int n) {
+int rotate_sides(RotateArgs& a, const he_config* cfg, const void* q, const void* k, void* q_out, void* k_out, const int64_t* const strides[4], int n,
+                 long long tokens) {
   const void* in[2] = {q, k};
   void* out[2] = {q_out, k_out};
   const int heads[2] = {cfg->n_kv_heads * cfg->group_size, cfg->n_kv_heads};
@@ -91,6 +100,8 @@ int rotate_sides(RotateArgs& a, const he_config* cfg, const void* q, const void*
       return fail(HE_ERR_INVALID_ARG, "%s or its output is null or not 16-byte aligned", what);
     if (int rc = check_strides(what, strides[w], n, esize_of(cfg->dtype))) return rc;
     if (int rc = check_strides(w ? "k_out" : "q_out", strides[2 + w], n, esize_of(cfg->dtype))) return rc;
+    const long long sizes[3] = {cfg->batch, heads[w], tokens};
+    if (int rc = check_apart(w ? "k_out" : "q_out", strides[2 + w], sizes, n, cfg->head_dim)) return rc;
     a.x[w] = in[w], a.y[w] = out[w], a.heads[w] = heads[w];
     for (int i = 0; i < n; ++i) a.in[w][i] = strides[w][i], a.out[w][i] = strides[2 + w][i];
     if (in[w] == out[w])
@@ -284,7 +295,7 @@ int he_rotate_prompt(const he_config* cfg, const he_rotary* rotary, const void* 
   if (max_prompt_len == 0) return HE_OK;
   RotateArgs a{};
   const int64_t* const strides[4] = {q_strides, k_strides, q_out_strides, k_out_strides};
-  if (int rc = rotate_sides(a, cfg, q, k, q_out, k_out, strides, 3)) return rc;
+  if (int rc = rotate_sides(a, cfg, q, k, q_out, k_out, strides, 3, max_prompt_len)) return rc;
   a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype;
   a.batch = cfg->batch, a.tokens = max_prompt_len, a.positions = positions, a.lens = prompt_len;
   return launch_rotate(a, *rotary, static_cast<cudaStream_t>(stream));
@@ -298,7 +309,7 @@ int he_rotate_step(const he_config* cfg, const he_rotary* rotary, const he_cache
   if (cache == nullptr || cache->next_pos == nullptr) return fail(HE_ERR_INVALID_ARG, "cache or its next_pos is null");
   RotateArgs a{};
   const int64_t* const strides[4] = {q_strides, k_strides, q_out_strides, k_out_strides};
-  if (int rc = rotate_sides(a, cfg, q, k, q_out, k_out, strides, 2)) return rc;
+  if (int rc = rotate_sides(a, cfg, q, k, q_out, k_out, strides, 2, 1)) return rc;
   a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype;
   a.batch = cfg->batch, a.tokens = 1, a.next_pos = cache->next_pos;
   return launch_rotate(a, *rotary, static_cast<cudaStream_t>(stream));
@@ -319,6 +330,8 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
   if (int rc = check_strides("q", q_strides, 3, es)) return rc;
   if (int rc = check_strides("k / v", kv_strides, 3, es)) return rc;
   if (int rc = check_strides("out", out_strides, 3, es)) return rc;
+  const long long sizes[3] = {cfg->batch, (long long)cfg->n_kv_heads * cfg->group_size, max_prompt_len};
+  if (int rc = check_apart("out", out_strides, sizes, 3, cfg->head_dim)) return rc;
   a.q = q, a.k = k, a.v = v, a.out = out;
   for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i], a.ks[i] = kv_strides[i], a.os[i] = out_strides[i];
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_prompt_len;

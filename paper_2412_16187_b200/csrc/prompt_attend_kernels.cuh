@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
 // Channels from d up to D are filled with zeros by the tensor maps.
 constexpr int kPtThreads = 384, kPtTile = 128, kPtMmaWarp = 8, kPtLoadWarp = 9, kPtWorkWarp = 10;
 constexpr int kPtSoftRegs = 224, kPtOtherRegs = 56;
-constexpr int kPtAsk = 2;           // steps of an item that are still to be asked for when the next item is fetched
+constexpr int kPtAsk = 4;           // steps of an item that are still to be asked for when the next item is fetched
 constexpr int kPtParts = 1;          // parts of a block's weights that are handed to the products one by one
 constexpr int kPtReaders = 10;       // warps that read an item: softmax, products, copies
 constexpr float kPtSlack = 8.f;      // log2 of how far weights may exceed 1 before the output is rescaled
@@ -289,30 +289,31 @@ struct PtItem {
   int jb[2], je[2], all_lo[2], all_hi[2];
 };
 
-// One product, issued by one lane of a converged warp: the election is part of the instruction, so that descriptors stay in uniform registers.
-__device__ __forceinline__ void pt_mma_ss(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+// One product or commit, issued by the lane of a converged warp that has `leader` set: a predicate on the instruction, so that descriptors stay in
+// uniform registers.
+__device__ __forceinline__ void pt_mma_ss(uint32_t leader, uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "elect.sync _|q, 0xFFFFFFFF;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(leader)
       : "memory");
 }
-__device__ __forceinline__ void pt_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+__device__ __forceinline__ void pt_mma_ts(uint32_t leader, uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "elect.sync _|q, 0xFFFFFFFF;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate)
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(leader)
       : "memory");
 }
-__device__ __forceinline__ void pt_commit(uint32_t bar) {
+__device__ __forceinline__ void pt_commit(uint32_t leader, uint32_t bar) {
   asm volatile(
       "{\n\t.reg .pred q;\n\t"
-      "elect.sync _|q, 0xFFFFFFFF;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader)
       : "memory");
 }
 // 16 columns of this thread's tensor-memory lane
@@ -497,7 +498,9 @@ __device__ __forceinline__ uint64_t pt_desc_mn128(uint32_t saddr) {
 // sign of life (`beat`, raised by the softmax warps every few blocks) on.
 __device__ __forceinline__ bool pt_wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   bool got = false;
+#pragma unroll 1
   for (int seen = *beat;;) {
+#pragma unroll 1
     for (uint32_t i = 0; i < kTcSpinLimit && !got; ++i) {
       got = mbar_try_wait(bar, parity);
       if (*abort_flag) break;
@@ -515,6 +518,15 @@ __device__ __forceinline__ bool pt_wait_on(uint32_t bar, uint32_t parity, volati
 __device__ __forceinline__ bool pt_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)), 1)) return true;
   return pt_wait_on(bar, parity, abort_flag, beat);
+}
+
+// The same for the roles beside the softmax, what follows the first poll in one place.
+static __device__ __noinline__ bool pt_wait_far(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
+  return pt_wait_on(bar, parity, abort_flag, beat);
+}
+__device__ __forceinline__ bool pt_wait_small(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
+  if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)), 1)) return true;
+  return pt_wait_far(bar, parity, abort_flag, beat);
 }
 
 // The grid's next waiting CTA, cancelled and taken over: asked for by one lane, answered in 16 bytes of shared memory.
@@ -590,8 +602,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
     if (lane == 0) mbar_arrive(smem_u32(&iempty_s[k & 1]));
   };
   auto read_item = [&](int k, PtItem& w) -> bool {
-    if (!take_item(k)) return false;
+    if (!pt_wait_small(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat)) return false;
     w = item_s[k & 1];
+    if (w.some == 0) return false;
     give_item(k);
     return true;
   };
@@ -636,7 +649,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
           for (int c = 0; c < 128; c += 8)
 #pragma unroll
             for (int e = 0; e < 4; ++e) far[e] = pt_max3_abs(far[e], x[c + e], x[c + e + 4]);
-          const float most = pt_max(pt_max(far[0], far[1]), pt_max(far[2], far[3])) * inv;
+          const float most = i < w.n ? pt_max(pt_max(far[0], far[1]), pt_max(far[2], far[3])) * inv : 0.f;  // (rows behind the end hold anything)
           const PtNear near = pt_near(inv);
           if (__builtin_expect(inv >= kPtNearInv && __all_sync(0xFFFFFFFFu, most <= kPtNearEnd), 1)) {
 #pragma unroll
@@ -704,7 +717,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
           for (int e = 0; e < 4; ++e) tops[e] = pt_max3(tops[e], x[c + e], x[c + e + 4]);
         const float top = pt_max(pt_max(tops[0], tops[1]), pt_max(tops[2], tops[3])) * scale;
         const float mx = pt_max(m, top);
-        const bool grown = !(mx <= m + kPtSlack);  // (also m = -inf, the first keys that a row sees, and a NaN)
+        const bool grown = i < w.n && !(mx <= m + kPtSlack);  // (also m = -inf, the first keys that a row sees, and a NaN)
         if (__any_sync(0xFFFFFFFFu, grown)) {
           const float corr = grown ? pt_ex2(m - mx) : 1.f;  // (a row does not depend on its neighbours)
           if (grown) m = mx;
@@ -768,26 +781,28 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       tc_fence_after();
       const float inv = l != 0.f ? 1.f / l : 0.f;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (w.s * a.os[0] + head * a.os[1] + i * a.os[2]);
-      bool bad = false;
+      const bool none = inv == 0.f;  // (a row that sees nothing: zeros)
+      float nan[2] = {0.f, 0.f};     // NaN once an output is
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
-        uint32_t o[32];
+        uint32_t o[32] = {};
         if (steps > 0) {
           tc_ld32(o_t + c, o);
           tc_wait_ld();
         }
+        uint32_t word[16];
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          float f[8];
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            f[u] = steps > 0 && inv != 0.f ? __uint_as_float(o[e + u]) * inv : 0.f;
-            bad |= c + e < a.d && f[u] != f[u];
-          }
-          if (i < w.n && c + e < a.d)
-            *reinterpret_cast<uint4*>(out + c + e) = make_uint4(pt_pack(f[0], f[1]), pt_pack(f[2], f[3]), pt_pack(f[4], f[5]), pt_pack(f[6], f[7]));
+        for (int e = 0; e < 16; ++e) {
+          float f0, f1;
+          pt_mul(pt2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), pt2(inv, inv)).get(f0, f1);
+          nan[e & 1] = pt_max3(nan[e & 1], f0, f1);
+          word[e] = none ? 0u : pt_pack(f0, f1);
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (i < w.n && c + 8 * e < a.d) *reinterpret_cast<uint4*>(out + c + 8 * e) = make_uint4(word[4 * e], word[4 * e + 1], word[4 * e + 2], word[4 * e + 3]);
       }
+      const bool bad = !none && pt_max(nan[0], nan[1]) != pt_max(nan[0], nan[1]);
       uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
       __syncwarp();
       for (; again != 0u; again &= again - 1u) prompt_row_again(a, w.s, head, i - lane + __ffs(again) - 1, w.n, beat);
@@ -805,7 +820,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           if (ok && w.je[t] > w.jb[t]) {
-            if (queries[t] > 0) ok = pt_wait(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
+            if (queries[t] > 0) ok = pt_wait_small(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
             if (!ok) break;
             if (lane == 0) {
               const uint32_t bar = smem_u32(&qfull_s[t]);
@@ -822,7 +837,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         for (int step = 0; ok && blocks > 0 && step <= blocks; ++step) {
           if (lane == 0 && step == ask) mbar_arrive(smem_u32(&ask_s));
           const uint32_t slot = used % NS;
-          if (used >= NS) ok = pt_wait(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
+          if (used >= NS) ok = pt_wait_small(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
           if (!ok) break;
           if (lane == 0) {
             const uint32_t bar = smem_u32(&full_s[slot]), at = ring + slot * 2 * T::kTileBytes;
@@ -850,6 +865,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       constexpr uint32_t idesc_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) /* B is MN-major */ | ((D / 8) << 17) | ((kPtTile / 16) << 24);
       const uint64_t qdesc = umma_desc_k128(q_smem), kdesc = umma_desc_k128(ring), vdesc = pt_desc_mn128(ring + T::kTileBytes);
       uint32_t slot = 0, lap = 0, taken = 0, queries = 0;  // ring place of the next step, the parity of its use; parities of the blocks of P and of the Q tiles, a bit a tile
+      const uint32_t leader = tc_elect() ? 1u : 0u;
       bool ok = true;
       PtItem w;
       for (int k = 0; ok && read_item(k, w); ++k) {
@@ -858,7 +874,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll 1
         for (int j = j_end; j >= j_begin; --j) {
           // O += P V of block j, S of block j - 1, tile by tile
-          ok = pt_wait(smem_u32(&full_s[slot]), lap, abort_flag, beat);
+          ok = pt_wait_small(smem_u32(&full_s[slot]), lap, abort_flag, beat);
           if (!ok) break;
           const int rows = w.n - j * kPtTile;
           if (__builtin_expect(j < j_end && rows < kPtTile, 0)) {  // V rows behind the prompt's end hold anything: zeros
@@ -874,18 +890,18 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             const int t_begin = t ? w.jb[1] : w.jb[0], t_end = t ? w.je[1] : w.je[0];
             const uint32_t s_at = tmem + t * kPtTile;
             if (j >= t_begin && j < t_end) {
-              ok = pt_wait(smem_u32(&pfull_s[t][0]), (taken >> t) & 1, abort_flag, beat);
+              ok = pt_wait_small(smem_u32(&pfull_s[t][0]), (taken >> t) & 1, abort_flag, beat);
               if (!ok) break;
               taken ^= 1u << t;
               tc_fence_after();
 #pragma unroll
               for (int ks = 0; ks < kPtTile / 16; ++ks)
-                pt_mma_ts(tmem + 2 * kPtTile + t * D, s_at + 8 * ks, vdesc + at + (uint64_t)((ks * 16 * 128) >> 4), idesc_pv, ks != 0 || j + 1 != t_end);
-              if (j == t_begin) pt_commit(smem_u32(&odone_s[t]));
+                pt_mma_ts(leader, tmem + 2 * kPtTile + t * D, s_at + 8 * ks, vdesc + at + (uint64_t)((ks * 16 * 128) >> 4), idesc_pv, ks != 0 || j + 1 != t_end);
+              if (j == t_begin) pt_commit(leader, smem_u32(&odone_s[t]));
             }
             if (j > t_begin && j <= t_end) {
               if (j == t_end) {
-                ok = pt_wait(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
+                ok = pt_wait_small(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
                 if (!ok) break;
                 queries ^= 1u << t;
               }
@@ -893,19 +909,19 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll
               for (int ks = 0; ks < D / 16; ++ks) {
                 const uint64_t of = (uint64_t)(((ks >> 2) * BOX + (ks & 3) * 32) >> 4);
-                pt_mma_ss(s_at, ad + of, kdesc + at + of, idesc_qk, ks != 0);
+                pt_mma_ss(leader, s_at, ad + of, kdesc + at + of, idesc_qk, ks != 0);
               }
-              pt_commit(smem_u32(&sfull_s[t]));
-              if (j - 1 == t_begin) pt_commit(smem_u32(&qempty_s[t]));
+              pt_commit(leader, smem_u32(&sfull_s[t]));
+              if (j - 1 == t_begin) pt_commit(leader, smem_u32(&qempty_s[t]));
             }
           }
           if (!ok) break;
-          pt_commit(smem_u32(&empty_s[slot]));
+          pt_commit(leader, smem_u32(&empty_s[slot]));
           if (++slot == NS) slot = 0, lap ^= 1u;
         }
       }
       if (!ok || __any_sync(0xFFFFFFFFu, *abort_flag != 0)) {  // products in flight end before tensor memory is given up
-        pt_commit(smem_u32(&drain_s));
+        pt_commit(leader, smem_u32(&drain_s));
         mbar_drain(smem_u32(&drain_s), 0);
       }
     } else if (warp == kPtWorkWarp) {
@@ -915,7 +931,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       uint32_t asked = 0;
       bool ok = true;
       auto hand_over = [&](const PtItem& w) {
-        if (k >= 2) ok = ok && pt_wait(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
+        if (k >= 2) ok = ok && pt_wait_small(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
         if (!ok) return;
         if (lane == 0) {
           item_s[k & 1] = w;
@@ -931,10 +947,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         w.tok0 = by_heads ? tile * kPtTile : tile * 2 * kPtTile;
         w.n = min(max(a.lens[w.s], 0), a.tokens);
         if (w.tok0 < w.n) {
-#pragma unroll
           for (int t = 0; t < 2; ++t) {
             int first = 0x7FFFFFFF, end = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
-#pragma unroll
+#pragma unroll 1
             for (int r = 0; r < kPtTile / 32; ++r) {
               const int i = tok_of(w, t) + 32 * r + lane;
               int lo, hi;
@@ -948,12 +963,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
           }
           hand_over(w);
           // not before this item is nearly done: a CTA that took the next one at once would be bound to it however long this one lasts
-          ok = ok && pt_wait(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
+          ok = ok && pt_wait_small(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
         }
         if (!ok) break;
         if (lane == 0) pt_ask_work(answer, smem_u32(&work_s));
         ++asked;
-        if (!pt_wait(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
+        if (!pt_wait_small(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
         const bool more = pt_read_work(answer, cta);
         if (!more) {
           w.some = 0;

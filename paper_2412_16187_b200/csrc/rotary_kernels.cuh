@@ -111,16 +111,14 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_kernel(const RotateArgs
   const int c1 = !INTER && turns ? c0 + half : c0 + V;
   const bool second = c1 < a.d;
   float sn[V], cs[V];
-  int at = 0;
-  auto angles = [&](int pos) {
-    at = pos;
+  // (single tokens: a thread has one head, whose unit says the position)
+  const int unit = h_begin >= a.heads[0] ? h_begin - a.heads[0] : h_begin / a.group;
+  const int pos = a.next_pos != nullptr ? a.next_pos[s * a.n_kv_heads + unit] : a.positions != nullptr ? a.positions[row] : n;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      sn[i] = 0.f, cs[i] = 1.f;
-      if (V * u + i < half) rotary_sincos(rot, V * u + i, pos, sn[i], cs[i]);
-    }
-  };
-  if (a.next_pos == nullptr) angles(a.positions != nullptr ? a.positions[row] : n);
+  for (int i = 0; i < V; ++i) {
+    sn[i] = 0.f, cs[i] = 1.f;
+    if (V * u + i < half) rotary_sincos(rot, V * u + i, pos, sn[i], cs[i]);
+  }
   auto rotate = [&](Piece& p0, Piece& p1) {
     if (!turns) return;
     float x[V], y[V];
@@ -157,10 +155,6 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_kernel(const RotateArgs
     for (int i = 0; i < UNROLL; ++i)
       if (h + i < h_end) {
         const int w = h + i >= a.heads[0] ? 1 : 0, hh = w ? h + i - a.heads[0] : h + i;
-        if (a.next_pos != nullptr) {
-          const int pos = a.next_pos[s * a.n_kv_heads + (w ? hh : hh / a.group)];
-          if (h + i == h_begin || pos != at) angles(pos);
-        }
         rotate(p0[i], p1[i]);
         char* dst = static_cast<char*>(a.y[w]) + (s * a.out[w][0] + hh * a.out[w][1] + n * a.out[w][2]) * E;
         p0[i].store(dst + c0 * E);

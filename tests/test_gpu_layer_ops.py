@@ -214,6 +214,65 @@ def test_attend_prompt_of_broadcast_and_strided_inputs():
     check_prompt(out, q, k, v, [n, 131], {}, {"doc_start": None, "prefix_len": None}, None, g)
 
 
+@pytest.mark.parametrize("opt", ["plain", "all", "prefix"])
+@pytest.mark.parametrize("shape", [(3, 4, 8, 128, BF16, [1100, 700, 3], "tokens"), (2, 20, 1, 64, BF16, [1500, 900], "heads"), (1, 2, 4, 128, BF16, [2700], "heads")])
+def test_more_tiles_than_the_gpu_holds_at_once(shape, opt):
+    """CTAs that go on from item to item: rings, phases and places carry over."""
+    o = OPTIONS[opt]
+    q, k, v, plen, mod, kw, slopes = prompt_case(shape, o, seed=3)
+    out = torch.full_like(q, 7.0)
+    make_cache(*shape[:5]).attend_prompt(q, k, v, plen, mod=mod, out=out, **kw)
+    check_prompt(out, q, k, v, shape[5], o, kw, slopes, shape[2])
+    for s, n in enumerate(shape[5]):
+        assert bool((out[s, :, n:] == 7.0).all())
+
+
+def test_prompts_without_tokens_and_rows_that_see_nothing():
+    cache = make_cache(2, 1, 2, 128, BF16)
+    q, k = torch.randn((2, 2, 300, 128), device="cuda").to(BF16), torch.randn((2, 1, 300, 128), device="cuda").to(BF16)
+    out = torch.full_like(q, 7.0)
+    for lens in ([0, 0], [-5, 0]):
+        cache.attend_prompt(q, k, k, torch.tensor(lens, dtype=torch.int32, device="cuda"), out=out)
+        assert bool((out == 7.0).all())
+    nothing = torch.full((2, 300), 10 ** 9, dtype=torch.int32, device="cuda")
+    cache.attend_prompt(q, k, k, torch.tensor([300, 1000], dtype=torch.int32, device="cuda"), doc_start=nothing, out=out)
+    assert not out.any()
+    empty = cache.attend_prompt(q[:, :, :0], k[:, :, :0], k[:, :, :0], torch.tensor([3, 3], dtype=torch.int32, device="cuda"))
+    assert empty.shape == (2, 2, 0, 128)
+
+
+@pytest.mark.parametrize("cap, scale", [(0.25, 0.0), (1e6, 0.0), (3.0, 4.0), (50.0, 1e-7), (1e-3, 1.0), (2.0, 50.0)])
+@pytest.mark.parametrize("dtype, d", [(BF16, 128), (BF16, 64), (F32, 64)])
+def test_caps_far_from_the_scores(cap, scale, dtype, d):
+    """Scores far inside the cap, about it and far beyond it, where tanh takes its other forms."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    n = 200
+    cache = make_cache(1, 1, 2, d, dtype)
+    q, k, v = rows(gen, 1, 2, n, d, dtype), rows(gen, 1, 1, n, d, dtype), rows(gen, 1, 1, n, d, dtype)
+    out = cache.attend_prompt(q, k, v, torch.tensor([n], dtype=torch.int32, device="cuda"), mod=ScoreMod(scale=scale, softcap=cap))
+    at = torch.arange(n, device="cuda")
+    ref = attend(q[0], k[0, 0], v[0, 0], at, at, prompt_seen(n), scale=scale, cap=cap)
+    # On the tensor cores tanh is within 7e-6 of itself (and 2e-6 absolutely): a score of x is off by at most 7e-6 |x|, with |x| <= min(cap, |raw|), and
+    # fp32 products leave 1e-6 of the raw score. A weight is off by twice that, relatively, an output by as much of the largest |V|.
+    raw = float((q[0].double() @ k[0, 0].double().T).abs().max()) * (scale or d ** -0.5)
+    more = 2 * (7e-6 + 1e-6) * min(cap, raw) * float(v.double().abs().max())
+    assert bool(((out[0].double() - ref).abs() <= tolerance(ref, v.double().abs().max(), dtype, dtype == F32) + more).all())
+
+
+@pytest.mark.parametrize("dtype, d", [(BF16, 128), (BF16, 64), (F32, 64)])
+def test_a_key_that_is_not_a_number_reaches_those_who_see_it(dtype, d):
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    n, bad = 300, 140
+    for mod, prefix in ((None, None), (ScoreMod(softcap=5.0), None), (ScoreMod(window=40), None), (ScoreMod(slopes=torch.ones(2, device="cuda")), 150)):
+        cache = make_cache(1, 1, 2, d, dtype)
+        q, k, v = rows(gen, 1, 2, n, d, dtype), rows(gen, 1, 1, n, d, dtype), rows(gen, 1, 1, n, d, dtype)
+        k[0, 0, bad, 7] = math.nan
+        pl = None if prefix is None else torch.tensor([prefix], dtype=torch.int32, device="cuda")
+        out = cache.attend_prompt(q, k, v, torch.tensor([n], dtype=torch.int32, device="cuda"), mod=mod, prefix_len=pl)
+        sees = prompt_seen(n, 40 if mod is not None and mod.raw.window else 0, None, prefix or 0)[:, bad]
+        assert torch.equal(torch.isnan(out[0]).all(-1), sees.expand(2, -1)) and torch.equal(torch.isnan(out[0]).any(-1), sees.expand(2, -1))
+
+
 # ---------------------------------------------------------------------------------------------- one token over the cache
 def fill_cache(gen, shape, fills, junk=True):
     b, h, g, d, dtype = shape

@@ -92,6 +92,7 @@ def test_calls_refuse_on_the_host():
     assert prompt(ks=i64x3(64, 64, 4)) == 1 and "aligned" in err()
     assert prompt(ks=i64x3(64, -64, 64)) == 1 and "stride" in err()
     assert prompt(qos=i64x3(64, 64 * 16, 64)) == 1 and "in place" in err()
+    assert prompt(kos=i64x3(64 * 16, 64, 0)) == 1 and "overlap" in err()
 
     cache = binding.he_cache()
     step = lambda c: L.he_rotate_step(cfg, rot, c, FAKE, FAKE, ok2, ok2, FAKE, FAKE, ok2, ok2, None)  # noqa: E731
@@ -109,6 +110,7 @@ def test_calls_refuse_on_the_host():
     assert attend(v=FAKE + 8) == 1 and "aligned" in err()
     assert attend(kvs=i64x3(64, 64, 12)) == 1 and "aligned" in err()
     assert attend(os=None) == 1 and "out strides" in err()
+    assert attend(os=i64x3(64 * 16, 0, 64)) == 1 and "overlap" in err()
     for bad, word in ((mod(-1.0, 0, 0, 0, None), "scale"), (mod(float("nan"), 0, 0, 0, None), "scale"), (mod(0, -2.0, 0, 0, None), "cap"),
                       (mod(0, float("inf"), 0, 0, None), "cap"), (mod(0, 0, -1, 0, None), "window"), (mod(3e38, 1e-30, 0, 0, None), "leaves fp32")):
         assert attend(mod=bad) == 1 and word in err(), word
