@@ -133,10 +133,12 @@ int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
   const int tiles = (a.tokens + 16 * R - 1) / (16 * R);
   const long long ctas = (long long)tiles * a.batch * a.n_kv_heads * a.group;
   if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld tiles in one call", ctas);
-  const size_t smem = prompt_fp32_smem<R>(a.d);
+  // a tile of keys ahead where an SM has one CTA and its 227 KB
+  const int stages = R == 1 && a.dtype == HE_DTYPE_F32 && prompt_fp32_smem<R>(a.d, 2) <= kAttendMaxSmem ? 2 : 1;
+  const size_t smem = prompt_fp32_smem<R>(a.d, stages);
   auto kernel = prompt_fp32_kernel<NQ, R>;
   if (int rc = set_smem(kernel, smem)) return rc;
-  return launch_pdl(kernel, dim3((unsigned)ctas), kPromptThreads, smem, true, st, a, tiles);
+  return launch_pdl(kernel, dim3((unsigned)ctas), kPromptThreads, smem, true, st, a, tiles, stages);
 }
 // Tiles of 64 rows once there is one for every SM, else of 16.
 template <int NQ>

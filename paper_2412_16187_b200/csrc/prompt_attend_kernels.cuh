@@ -88,18 +88,25 @@ static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s,
 //
 // 16 R rows of one query head per CTA, 64 keys at a time. Thread (ty, tx) of 16 x 16 holds the scores of rows R ty .. + R - 1 and keys
 // tx, tx + 16, tx + 32, tx + 48, and of the output the same rows and channels 4 tx .. + 3 of every 64. Q and K lie in shared memory row by row, four
-// floats longer than the row, so that the 16 threads that read neighbouring keys meet every bank once; the weights go through shared memory key by key.
+// floats longer than the row, so that the 16 threads that read neighbouring keys meet every bank once; the weights go through shared memory key by key, in the place of K.
 // Bound by the FMA pipe and the loads that feed it (R = 4: 8 loads of 16 bytes for 64 products). R = 1 for calls that would leave SMs idle.
 constexpr int kPromptThreads = 256;
 template <int R>
 constexpr int kPromptPitch = 16 * R + 4;  // of the weights
 template <int R>
-inline size_t prompt_fp32_smem(int d) {
-  return sizeof(float) * ((size_t)(16 * R + 64) * (d + 4) + 64 * (size_t)d + 64 * (size_t)kPromptPitch<R>);
+inline size_t prompt_fp32_smem(int d, int stages) {
+  const size_t keys = 64 * (size_t)(d + 4), weights = 64 * (size_t)kPromptPitch<R>;  // the weights take the place of the K tile
+  return sizeof(float) * ((size_t)16 * R * (d + 4) + (size_t)stages * ((keys > weights ? keys : weights) + 64 * (size_t)d));
+}
+// 16 bytes into shared memory, or zeros
+__device__ __forceinline__ void prompt_copy16(void* smem_dst, const void* gmem_src, bool some) {
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(smem_dst);
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(gmem_src), "r"(some ? 16u : 0u) : "memory");
 }
 
+// fp32 rows are copied asynchronously, with `stages` = 2 a tile of keys ahead (calls that leave an SM to one CTA).
 template <int NQ, int R>  // groups of 64 channels, rows of a thread
-__global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __grid_constant__ PromptArgs a, const int tiles) {
+__global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_kernel(const __grid_constant__ PromptArgs a, const int tiles, const int stages) {
   extern __shared__ __align__(16) float psm_[];
   constexpr int PP = kPromptPitch<R>;
   const int d = a.d, pitch = d + 4, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
@@ -108,8 +115,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
   const int kv = head / a.group, i0 = tile * 16 * R;
   float* qs = psm_;                // [16 R][d + 4]
   float* ks = qs + 16 * R * pitch; // [64][d + 4]
-  float* vs = ks + 64 * pitch;     // [64][d]
-  float* pt = vs + 64 * d;         // [64 keys][16 R + 4]
+  const int keys_floats = 64 * max(pitch, PP), stage_floats = keys_floats + 64 * d;  // K tile (then the weights [64 keys][16 R + 4]), V tile [64][d]
   __shared__ int run[2];
   griddep_launch_dependents();
   griddep_wait();
@@ -143,17 +149,46 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
   }
   __syncthreads();
   const int j_begin = run[0] / 64 * 64, j_end = run[1];
-  for (int j0 = j_begin; j0 < j_end; j0 += 64) {
-    __syncthreads();  // the last tile has been read
+  const int r_first = tid / cpr, c_first = tid % cpr, r_step = kPromptThreads / cpr, c_step = kPromptThreads % cpr;
+  const bool async = a.dtype == HE_DTYPE_F32;
+  auto fetch = [&](int j0, int stage) {
+    float* kt = ks + stage * stage_floats;
+    float* vt = kt + keys_floats;
 #pragma unroll 4
-    for (int idx = tid; idx < 64 * cpr; idx += kPromptThreads) {
-      const int r = idx / cpr, c = idx % cpr, j = j0 + r;
-      uint4 k4 = make_uint4(0u, 0u, 0u, 0u), v4 = k4;
-      if (j < n) k4 = chunk(a.k, k0 + j * a.ks[2], c), v4 = chunk(a.v, k0 + j * a.ks[2], c);
-      store_chunk(ks + r * pitch, k4, c, a.dtype);
-      store_chunk(vs + r * d, v4, c, a.dtype);
+    for (int r = r_first, c = c_first; r < 64;) {
+      const int j = j0 + r;
+      const long long at = k0 + (j < n ? j : 0) * a.ks[2];
+      if (async) {
+        prompt_copy16(kt + r * pitch + 4 * c, static_cast<const float*>(a.k) + at + 4 * c, j < n);
+        prompt_copy16(vt + r * d + 4 * c, static_cast<const float*>(a.v) + at + 4 * c, j < n);
+      } else {
+        uint4 k4 = make_uint4(0u, 0u, 0u, 0u), v4 = k4;
+        if (j < n) k4 = chunk(a.k, at, c), v4 = chunk(a.v, at, c);
+        store_chunk(kt + r * pitch, k4, c, HE_DTYPE_BF16);
+        store_chunk(vt + r * d, v4, c, HE_DTYPE_BF16);
+      }
+      r += r_step, c += c_step;
+      if (c >= cpr) c -= cpr, ++r;
+    }
+    cp_async_commit();
+  };
+  if (stages == 2 && j_begin < j_end) fetch(j_begin, 0);
+  for (int j0 = j_begin, stage = 0; j0 < j_end; j0 += 64, stage ^= stages - 1) {
+    if (stages == 2) {
+      if (j0 + 64 < j_end) {
+        fetch(j0 + 64, stage ^ 1);
+        cp_async_wait_pending(1);
+      } else {
+        cp_async_wait_all();
+      }
+    } else {
+      fetch(j0, 0);
+      cp_async_wait_all();
     }
     __syncthreads();
+    const float* kt = ks + stage * stage_floats;
+    const float* vt = kt + keys_floats;
+    float* pt = ks + stage * stage_floats;
     float x[R][4];
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -165,7 +200,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
 #pragma unroll
       for (int r = 0; r < R; ++r) q4[r] = *reinterpret_cast<const float4*>(qs + (R * ty + r) * pitch + c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) k4[e] = *reinterpret_cast<const float4*>(ks + (tx + 16 * e) * pitch + c);
+      for (int e = 0; e < 4; ++e) k4[e] = *reinterpret_cast<const float4*>(kt + (tx + 16 * e) * pitch + c);
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -197,21 +232,23 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
 #pragma unroll
       for (int c = 0; c < 4 * NQ; ++c) o[r][c] *= corr;
     }
+    __syncthreads();  // K has been read
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int r = 0; r < R; ++r) pt[(tx + 16 * e) * PP + R * ty + r] = x[r][e];
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (R == 4) *reinterpret_cast<float4*>(pt + (tx + 16 * e) * PP + 4 * ty) = make_float4(x[0][e], x[1][e], x[2][e], x[3][e]);
+      else pt[(tx + 16 * e) * PP + ty] = x[0][e];
+    }
     __syncwarp();  // a row's weights are written and read by the same half warp
 #pragma unroll 2
     for (int j = 0; j < 64; ++j) {
-      float pv[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) pv[r] = pt[j * PP + R * ty + r];
+      __align__(16) float pv[R];
+      if constexpr (R == 4) *reinterpret_cast<float4*>(pv) = *reinterpret_cast<const float4*>(pt + j * PP + 4 * ty);
+      else pv[0] = pt[j * PP + ty];
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const int c = 64 * q + 4 * tx;
         if (c < d) {
-          const float4 v4 = *reinterpret_cast<const float4*>(vs + j * d + c);
+          const float4 v4 = *reinterpret_cast<const float4*>(vt + j * d + c);
           const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
           for (int r = 0; r < R; ++r)
@@ -220,6 +257,7 @@ __global__ void __launch_bounds__(kPromptThreads) prompt_fp32_kernel(const __gri
         }
       }
     }
+    __syncthreads();  // the tile has been read
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
