@@ -216,7 +216,8 @@ int he_rotary_init_frequencies(he_rotary* out, int32_t channels, int32_t interle
  * like those of he_prefill_compress, into q_out and k_out of the same shapes with strides of their own. Row n of sequence s
  * is rotated by positions[s * max_prompt_len + n] (device int32 [B, max_prompt_len], any value), or by n where positions is NULL.
  * Rows n >= prompt_len[s] are neither read nor written (prompt_len NULL: every row is taken). An output may be its input
- * (same address, same strides), not overlap it otherwise, and its rows do not overlap each other. q and q_out may both be NULL, and so may k and k_out.
+ * (same address, same strides), not overlap it otherwise, and its rows do not overlap each other: sorted by stride, each axis steps over
+ * all that the ones before it cover. q and q_out may both be NULL, and so may k and k_out.
  */
 int he_rotate_prompt(const he_config* cfg, const he_rotary* rotary, const void* q, const void* k, const int64_t q_strides[3],
                      const int64_t k_strides[3], const int32_t* positions, const int32_t* prompt_len, int32_t max_prompt_len, void* q_out,
@@ -253,7 +254,7 @@ typedef struct he_score_mod {
  * [B, max_prompt_len]), prefix_len (device int32 [B]) and mod may be NULL; any values are allowed.
  * q: [B, Hkv*G, N, d], k, v: [B, Hkv, N, d], out: as q, all in the dtype of cfg, with element strides (batch, head, token), channels
  * contiguous, rows 16-byte aligned. Rows i >= N_s of out are left as they were; rows of q, k, v behind N_s may hold anything. out
- * may not overlap q, k or v. Sums and the softmax are carried in fp32. bf16 with head_dim <= 128 runs on the tensor cores, where the weights
+ * may not overlap q, k or v, nor its rows each other (as in he_rotate_prompt). Sums and the softmax are carried in fp32. bf16 with head_dim <= 128 runs on the tensor cores, where the weights
  * are rounded to bf16 before they meet V (up to 2^-8 of each weight; their sum is taken before); all else is fp32 throughout.
  */
 int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
@@ -264,7 +265,8 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
  * he_attend_scored - he_attend with he_score_mod: the single-token form of the same attention over the compressed cache. The query is
  * at position t = next_pos - 1 of its unit (the token that the last he_decode_step inserted) and slot j at pos[j]; slots with
  * pos[j] < first_pos[s] (device int32 [B], or NULL; the start of the token's document) are hidden, and so are those that the window
- * leaves behind. mod NULL: as he_attend. Layouts and precision are those of he_attend.
+ * leaves behind. mod NULL: as he_attend. Layouts are those of he_attend; results agree with exact arithmetic to about 1e-6 of the largest |V|
+ * entry. Rows of hidden slots may hold anything.
  */
 int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out,
                      void* stream);
@@ -395,7 +397,7 @@ int he_prefill_compress_noalloc(const he_config* cfg, const he_cache* cache, con
  * block that hits one releases what it holds and returns), plus, in the bounds-checking debug build, how many
  * indices were found out of range. A call during which the counter rose has returned HE_OK all the same (calls
  * only enqueue work), but its outputs are undefined: he_hash_keys, he_prefill_compress and its variants,
- * he_attend, and he_decode_step with a step scratch are the calls whose kernels contain such waits. This is the one call of the
+ * he_attend, he_attend_scored, he_attend_prompt (bf16) and he_decode_step with a step scratch are the calls whose kernels contain such waits. This is the one call of the
  * library, besides the *_host variants, that synchronises the device. Returns -1 if the counter cannot be read.
  * Diagnostic only: the paper has no counterpart.
  */

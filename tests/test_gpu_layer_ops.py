@@ -447,6 +447,50 @@ def test_two_streams_and_repeated_calls_give_the_same_bits():
         assert torch.equal(out, first)
 
 
+def test_calls_that_share_tensor_memory_follow_one_another():
+    """The prompt's attention and its compression both take tensor memory: in turn on one stream, and beside each other on two."""
+    b, h, g, d, lens = 4, 4, 4, 128, [300, 700, 513, 64]
+    q, k, v, plen, mod, kw, _ = prompt_case((b, h, g, d, BF16, lens, "heads"), OPTIONS["cap"], seed=5, junk=False)
+    w = torch.randn((d, 16), generator=torch.Generator().manual_seed(3))
+    caches = [HashEvictCache(b, h, g, d, 16, [32] * b, w) for _ in range(3)]
+    n = q.shape[2]
+    work = [c.workspace(n) for c in caches]
+    want = caches[0].attend_prompt(q, k, v, plen, mod=mod, out=torch.zeros_like(q))
+    caches[0].prefill_compress(q, k, v, plen, n, workspace=work[0])
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.zeros_like(q) for _ in range(2)]
+    for _ in range(20):
+        caches[1].attend_prompt(q, k, v, plen, mod=mod, out=outs[0], stream=streams[0])
+        caches[1].prefill_compress(q, k, v, plen, n, workspace=work[1], stream=streams[0])
+        caches[2].prefill_compress(q, k, v, plen, n, workspace=work[2], stream=streams[1])
+        caches[2].attend_prompt(q, k, v, plen, mod=mod, out=outs[1], stream=streams[1])
+    torch.cuda.synchronize()
+    for c, out in zip(caches[1:], outs):
+        assert torch.equal(out, want)
+        assert torch.equal(c.pos, caches[0].pos) and torch.equal(c.k_cache, caches[0].k_cache)
+    assert binding.device_error_count() == 0
+
+
+def test_outputs_between_other_rows():
+    """q, k and v as parts of one projection, outputs into parts of another: what lies between them stays."""
+    b, h, g, d, n = 2, 2, 3, 64, 150
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    fused = torch.randn((b, n, (g + 2) * h, d), generator=gen, device="cuda", dtype=BF16)
+    q, k, v = fused.transpose(1, 2).split((g * h, h, h), dim=1)
+    cache, plen, rot = make_cache(b, h, g, d, BF16), torch.tensor([n, 77], dtype=torch.int32, device="cuda"), Rotary(d)
+    want_q, want_k = cache.rotate_prompt(rot, q.contiguous(), k.contiguous())
+    want = cache.attend_prompt(want_q, want_k, v.contiguous(), plen, out=torch.zeros_like(want_q))
+    before = fused.clone()
+    into = torch.full((b, n, g * h + 1, d), 3.0, device="cuda", dtype=BF16)
+    cache.rotate_prompt(rot, q, k, plen, q_out=q, k_out=k)  # in place
+    out = into.transpose(1, 2)[:, : g * h]
+    assert cache.attend_prompt(q, k, v, plen, out=out) is out
+    for s, m in enumerate(plen.tolist()):
+        assert torch.equal(out[s, :, :m], want[s, :, :m]) and bool((out[s, :, m:] == 3.0).all())
+        assert torch.equal(q[s, :, :m], want_q[s, :, :m]) and torch.equal(fused[s, m:], before[s, m:])
+    assert torch.equal(v, before.transpose(1, 2)[:, (g + 1) * h:]) and bool((into[:, :, g * h] == 3.0).all())
+
+
 def test_offsets_beyond_32_bits():
     """A batch whose last rows lie more than 2^32 elements into q and k."""
     b, h, g, d, n = 2, 1, 1, 128, 300
@@ -478,6 +522,8 @@ def test_the_binding_refuses():
         lambda: cache.attend_prompt(q, k, k, n, mod=ScoreMod(slopes=torch.ones(3, device="cuda"))), lambda: cache.attend_prompt(q, k, k, n, mod=ScoreMod(window=-2)),
         lambda: cache.attend_prompt(q, k, k, n, out=k), lambda: ScoreMod(slopes=torch.ones(4)), lambda: ScoreMod(slopes=torch.ones(8, device="cuda")[::2]),
         lambda: cache.attend_scored(z(2, 4, 32)), lambda: cache.attend_scored(z(2, 4, 64, dtype=F32)), lambda: cache.attend_scored(z(2, 64, 4).transpose(1, 2)),
+        lambda: cache.rotate_prompt(rot, q[0], k[0]), lambda: cache.attend_prompt(q[0], k[0], k[0], n), lambda: cache.rotate_step(rot, None, None),
+        lambda: cache.rotate_prompt(rot, q, k, k_out=torch.empty(2, 1, 10, 64, device="cuda", dtype=BF16).expand(2, 2, 10, 64)),
         lambda: cache.attend_scored(z(2, 4, 64), first_pos=n.long()), lambda: cache.attend_scored(z(2, 4, 64), out=z(2, 4, 64)),
     ]
     for i, call in enumerate(bad):

@@ -74,7 +74,7 @@ FAKE = 0x10000  # never followed: every check below comes before the launch
 def test_calls_refuse_on_the_host():
     L, err = binding.lib(), lambda: binding.lib().he_last_error().decode()
     i64x3, i64x2 = ctypes.c_int64 * 3, ctypes.c_int64 * 2
-    ok3, ok2 = i64x3(64 * 16, 64, 64), i64x2(64, 64)
+    ok3, ok2 = i64x3(8 * 64 * 16, 64 * 16, 64), i64x2(8 * 64, 64)  # [2, up to 8 heads, 16, 64]
     cfg = ctypes.byref(binding.he_config(2, 2, 4, 64, 32, 64, 0, 0, 1, 0))
     rot = ctypes.byref(Rotary(64).raw)
     wide = ctypes.byref(Rotary(128).raw)
@@ -91,8 +91,10 @@ def test_calls_refuse_on_the_host():
     assert prompt(qs=None) == 1 and "strides" in err()
     assert prompt(ks=i64x3(64, 64, 4)) == 1 and "aligned" in err()
     assert prompt(ks=i64x3(64, -64, 64)) == 1 and "stride" in err()
-    assert prompt(qos=i64x3(64, 64 * 16, 64)) == 1 and "in place" in err()
-    assert prompt(kos=i64x3(64 * 16, 64, 0)) == 1 and "overlap" in err()
+    assert prompt(qos=i64x3(9 * 64 * 16, 64 * 16, 64)) == 1 and "in place" in err()
+    for bad in (i64x3(64 * 16, 64, 0), i64x3(64 * 16, 64, 64), i64x3(64, 64 * 16, 64), i64x3(2 * 64 * 16 - 8, 64 * 16, 64)):
+        assert prompt(kos=bad) == 1 and "overlap" in err()
+    assert prompt(n=1, ks=i64x3(128, 64, 0), kos=i64x3(64, 64, 0)) == 1 and "overlap" in err()  # (of one token only its stride says nothing)
 
     cache = binding.he_cache()
     step = lambda c: L.he_rotate_step(cfg, rot, c, FAKE, FAKE, ok2, ok2, FAKE, FAKE, ok2, ok2, None)  # noqa: E731
@@ -111,6 +113,7 @@ def test_calls_refuse_on_the_host():
     assert attend(kvs=i64x3(64, 64, 12)) == 1 and "aligned" in err()
     assert attend(os=None) == 1 and "out strides" in err()
     assert attend(os=i64x3(64 * 16, 0, 64)) == 1 and "overlap" in err()
+    assert attend(os=i64x3(64 * 8, 64, 64)) == 1 and "overlap" in err()
     for bad, word in ((mod(-1.0, 0, 0, 0, None), "scale"), (mod(float("nan"), 0, 0, 0, None), "scale"), (mod(0, -2.0, 0, 0, None), "cap"),
                       (mod(0, float("inf"), 0, 0, None), "cap"), (mod(0, 0, -1, 0, None), "window"), (mod(3e38, 1e-30, 0, 0, None), "leaves fp32")):
         assert attend(mod=bad) == 1 and word in err(), word
