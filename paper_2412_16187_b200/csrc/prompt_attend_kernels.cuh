@@ -92,7 +92,7 @@ static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s,
 // Bound by the FMA pipe and the loads that feed it (R = 4: 8 loads of 16 bytes for 64 products). 4 x 32 heads of 2048 tokens at d = 128 take
 // 4.4 ms: 31 TFLOP/s, of about 70 that the FMA pipe has. With one CTA an SM instead of two it is
 // 6.0 ms there, and 32 heads of 2048 tokens at d = 64 take 1.03 ms beside 0.75.
-// R = 1 for calls that would leave SMs idle: 5 x 311 tokens of one head at d = 128 take 39 us beside 76 with R = 4 (44 without a tile ahead);
+// R = 1 for calls that would leave SMs idle: 5 x 311 tokens of one head at d = 128 take 38 us beside 76 with R = 4 (44 without a tile ahead);
 // 32 heads of 1024 tokens, which fill the SMs, 313 us with R = 4 beside 772.
 constexpr int kPromptThreads = 256;
 template <int R>
@@ -113,6 +113,7 @@ template <int NQ, int R>  // groups of 64 channels, rows of a thread
 __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_kernel(const __grid_constant__ PromptArgs a, const int tiles, const int stages) {
   extern __shared__ __align__(16) float psm_[];
   constexpr int PP = kPromptPitch<R>;
+  constexpr int UNROLL = R == 1 ? 8 : 2;  // one row has few loads in flight otherwise
   const int d = a.d, pitch = d + 4, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
   const int heads = a.n_kv_heads * a.group;
   const int head = blockIdx.x % heads, s = (blockIdx.x / heads) % a.batch, tile = tiles - 1 - blockIdx.x / heads / a.batch;
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[r][e] = 0.f;
-#pragma unroll 2
+#pragma unroll UNROLL
     for (int c = 0; c < d; c += 4) {
       float4 q4[R], k4[4];
 #pragma unroll
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
       else pt[(tx + 16 * e) * PP + ty] = x[0][e];
     }
     __syncwarp();  // a row's weights are written and read by the same half warp
-#pragma unroll 2
+#pragma unroll UNROLL
     for (int j = 0; j < 64; ++j) {
       __align__(16) float pv[R];
       if constexpr (R == 4) *reinterpret_cast<float4*>(pv) = *reinterpret_cast<const float4*>(pt + j * PP + 4 * ty);
