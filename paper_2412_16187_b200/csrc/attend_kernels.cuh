@@ -12,6 +12,8 @@
 #pragma once
 #include <cuda.h>  // CUtensorMap (types only; the encoder is fetched through the runtime)
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace he {
@@ -31,6 +33,12 @@ struct AttendArgs {
   float* out;     // [B, Hkv*G, d] fp32
   AttendMod mod;  // read by the kernels with MOD only
 };
+struct ScoredArgs : AttendArgs {
+  int n_order;  // > 0: the sequences in the order in which their CTAs start, largest budgets first
+  uint8_t order[256];
+};
+template <bool MOD>
+using AttendArgsOf = std::conditional_t<MOD, ScoredArgs, AttendArgs>;
 
 constexpr int kAttendThreads = 256;
 constexpr int kAttendWarps = kAttendThreads / 32;
@@ -202,11 +210,11 @@ struct AttendRing {
 // of the MMA's accumulator (1.7e-6 at 8000). With MOD a weight has a third term and each group's products start from zero and are added with rounding: 2e-7 and
 // 6e-7. Groups of up to 4 heads (FOLD) hold the third terms in the rows that they leave empty (rows 4..7 repeat the heads of rows 0..3), larger
 // ones take products of their own.
-// Measured, d = 128 and G = 4: 512 units of 512 to 4096 slots 94 us without modification (6.1 TB/s; he_attend's two terms take 90), 97 with a cap or a window, 94 with
-// slopes: bound by HBM. 8 units of 9830 slots 11.0 us (he_attend 10.1), 11.9 with a cap: bound by what the 16 CTAs of a cluster pull. Groups of 8 without room
+// Measured, d = 128 and G = 4: 512 units of 512 to 4096 slots 85.6 us without modification (6.6 TB/s), 86.2 with a cap, a window or slopes: bound by
+// HBM (94.5 and 97 with the units in their own order; he_attend 91). 8 units of 9830 slots 11.0 us (he_attend 10.1), 11.9 with a cap: bound by what the 16 CTAs of a cluster pull. Groups of 8 without room
 // for the third terms: 128 units of 2048 slots at d = 64 13.6 us (he_attend 10.8), bound by the issue of MMAs and their operands.
 template <int D, int NW, bool MOD, bool CAP = false, bool FOLD = false, bool BELOW = false>
-__global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const AttendArgs a, const int S, const __grid_constant__ CUtensorMap kmap,
+__global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const AttendArgsOf<MOD> a, const int S, const __grid_constant__ CUtensorMap kmap,
                                                                      const __grid_constant__ CUtensorMap vmap) {
   using Ring = AttendRing<D, NW>;
   extern __shared__ __align__(16) unsigned char attend_smem_raw[];
@@ -218,7 +226,9 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   const int d = BELOW ? cfg.head_dim : D;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
   const int rank = blockIdx.x % S;
-  const int unit = blockIdx.y * cfg.n_kv_heads + blockIdx.x / S;
+  int seq = blockIdx.y;
+  if constexpr (MOD && NW == 4) seq = a.n_order > 0 ? a.order[blockIdx.y] : seq;
+  const int unit = seq * cfg.n_kv_heads + blockIdx.x / S;
   const int G = cfg.group_size;
   // rounded up to 1024 bytes (the swizzle's period) by an offset from the array itself
   float* asm_ = reinterpret_cast<float*>(attend_smem_raw + ((1024u - ((uint32_t)__cvta_generic_to_shared(attend_smem_raw) & 1023u)) & 1023u));
@@ -265,7 +275,7 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
   int now = 0, low = 0;           // MOD: the query's position, the first one it sees
   if (MOD) {                      // (asked for together with `fill`, looked at behind the first copies)
     now = __ldcg(a.ca.next_pos + unit) - 1;
-    if (a.mod.first_pos != nullptr) low = a.mod.first_pos[blockIdx.y];
+    if (a.mod.first_pos != nullptr) low = a.mod.first_pos[seq];
     if (a.mod.slopes != nullptr && my_head < G) slope = a.mod.slopes[(unit % cfg.n_kv_heads) * G + my_head] * kLog2e;
   }
   const int items = first < fill ? 2 * ((fill - first + stride - 1) / stride) : 0;
@@ -620,12 +630,13 @@ __device__ __forceinline__ void cp_async16_or_zero(void* smem_dst, const void* g
 }
 
 template <int E, int GP>
-__global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const AttendArgs a, const int S, const int stages) {
+__global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const ScoredArgs a, const int S, const int stages) {
   extern __shared__ __align__(16) float asm_[];
   __shared__ __align__(8) unsigned long long merge_bar;
   const he_config& cfg = a.cfg;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = blockIdx.x % S, head = blockIdx.x / S, unit = blockIdx.y * cfg.n_kv_heads + head;
+  const int seq = a.n_order > 0 ? a.order[blockIdx.y] : blockIdx.y;
+  const int rank = blockIdx.x % S, head = blockIdx.x / S, unit = seq * cfg.n_kv_heads + head;
   const int d = cfg.head_dim, G = cfg.group_size, pitch = d + 4;
   float* qs = asm_;                                  // [G][d]
   float* ks = qs + G * d;                            // [64][d + 4], then vs [64][d]; at the end part_ml, part_o
@@ -647,7 +658,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Att
   }
   griddep_wait();
   const int fill = __ldcg(a.ca.fill + unit), now = __ldcg(a.ca.next_pos + unit) - 1;
-  int low = a.mod.first_pos != nullptr ? max(0, a.mod.first_pos[blockIdx.y]) : 0;
+  int low = a.mod.first_pos != nullptr ? max(0, a.mod.first_pos[seq]) : 0;
   if (a.mod.window > 0) low = max(low, now - a.mod.window + 1);
   const int cpr = d * E / 16;
   for (int i = tid; i < G * cpr; i += kAttendThreads) stage_chunk(qs + (i / cpr) * d, static_cast<const char*>(a.q) + ((size_t)unit * G + i / cpr) * d * E, i % cpr, cfg.dtype);

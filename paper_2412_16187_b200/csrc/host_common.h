@@ -184,7 +184,7 @@ struct AttendMaps {
 };
 
 template <int D, int NW, bool MOD, bool CAP, bool FOLD, bool BELOW>
-int launch_attend_on(const AttendArgs& a, const AttendMaps& maps, int S, size_t smem, cudaStream_t st) {
+int launch_attend_on(const AttendArgsOf<MOD>& a, const AttendMaps& maps, int S, size_t smem, cudaStream_t st) {
   if (int rc = set_smem(attend_bf16_kernel<D, NW, MOD, CAP, FOLD, BELOW>, smem)) return rc;
   cudaLaunchConfig_t lc{};
   lc.gridDim = dim3((unsigned)(a.cfg.n_kv_heads * S), (unsigned)a.cfg.batch);
@@ -217,7 +217,7 @@ constexpr size_t attend_smem(int S, int G) {
 // than L2; register-fed kernel with clusters of up to 8 before): 8 units of 9830 slots 16.9 -> 10.6, 32 of 2048 8.7 -> 7.9, 128 of
 // 1024 14.6 -> 12.9.
 template <int D, bool MOD, bool CAP = false, bool FOLD = false, bool BELOW = false>
-int launch_attend(const AttendArgs& a, const AttendMaps& maps, cudaStream_t st) {
+int launch_attend(const AttendArgsOf<MOD>& a, const AttendMaps& maps, cudaStream_t st) {
   const long long units = (long long)a.cfg.batch * a.cfg.n_kv_heads;
   int sms = 0, dev = 0;
   if (int rc = sm_count(&sms)) return rc;

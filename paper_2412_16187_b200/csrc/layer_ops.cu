@@ -204,8 +204,34 @@ int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t s
   return a.slopes != nullptr ? launch_prompt_tc<D, false, true>(a, maps, st) : launch_prompt_tc<D, false, false>(a, maps, st);
 }
 
+// Units that do not all run at once (two CTAs an SM) end evenly when the longest start first: 512 of 512 to 4096 slots 94 -> 85 us back to back. Known from the caller's mirror of the budgets; sorted again only when its contents
+// change. A unit's result does not depend on it.
+int order_units(ScoredArgs* a) {
+  const int n = a->cfg.batch;
+  const int32_t* budget = a->ca.budget_host;
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  a->n_order = 0;
+  if (budget == nullptr || n > 256 || (long long)n * a->cfg.n_kv_heads <= 2 * sms) return HE_OK;
+  struct Order {
+    int n = 0;
+    int32_t budget[256];
+    uint8_t order[256];
+  };
+  thread_local Order known;
+  if (known.n != n || memcmp(known.budget, budget, sizeof(int32_t) * n) != 0) {
+    known.n = n;
+    memcpy(known.budget, budget, sizeof(int32_t) * n);
+    for (int i = 0; i < n; ++i) known.order[i] = (uint8_t)i;
+    std::stable_sort(known.order, known.order + n, [&](uint8_t x, uint8_t y) { return known.budget[x] > known.budget[y]; });
+  }
+  a->n_order = n;
+  memcpy(a->order, known.order, n);
+  return HE_OK;
+}
+
 template <bool CAP, bool FOLD>
-int launch_scored_bf16(const AttendArgs& a, const AttendMaps& maps, cudaStream_t st) {
+int launch_scored_bf16(const ScoredArgs& a, const AttendMaps& maps, cudaStream_t st) {
   switch (a.cfg.head_dim) {
     case 64: return launch_attend<64, true, CAP, FOLD, false>(a, maps, st);
     case 128: return launch_attend<128, true, CAP, FOLD, false>(a, maps, st);
@@ -215,7 +241,7 @@ int launch_scored_bf16(const AttendArgs& a, const AttendMaps& maps, cudaStream_t
 
 // As many CTAs per unit as keep the grid within two per SM, at most 8 (a cluster of any device) and no fewer than two tiles of slots for each.
 template <int E, int GP>
-int launch_scored(const AttendArgs& a, cudaStream_t st) {
+int launch_scored(const ScoredArgs& a, cudaStream_t st) {
   const long long units = (long long)a.cfg.batch * a.cfg.n_kv_heads;
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
@@ -369,10 +395,11 @@ int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score
   if (int rc = check_cache(cache)) return rc;
   if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q or out is null or not 16-byte aligned");
   if (cfg->batch > 65535) return fail(HE_ERR_UNSUPPORTED, "batch %d > 65535 in one call", cfg->batch);
-  AttendArgs a{*cfg, *cache, q, out, {}};
+  ScoredArgs a{{*cfg, *cache, q, out, {}}, 0, {}};
   const int G = cfg->group_size, d = cfg->head_dim;
   if (int rc = check_mod(mod, d, &a.mod.scale_log2, &a.mod.cap_log2, &a.mod.inv_cap, &a.mod.window, &a.mod.slopes)) return rc;
   a.mod.first_pos = first_pos;
+  if (int rc = order_units(&a)) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (cfg->dtype == HE_DTYPE_BF16 && d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr) {
     const long long rows = (long long)cfg->batch * cfg->n_kv_heads * cfg->max_budget;

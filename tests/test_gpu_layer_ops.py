@@ -447,6 +447,34 @@ def test_two_streams_and_repeated_calls_give_the_same_bits():
         assert torch.equal(out, first)
 
 
+@pytest.mark.parametrize("b, h, g, d, dtype", [(50, 8, 4, 128, BF16), (90, 4, 8, 64, BF16), (256, 2, 2, 96, BF16), (60, 8, 1, 64, F32), (300, 1, 4, 128, BF16)])
+def test_the_order_of_the_units_changes_nothing(b, h, g, d, dtype):
+    """With a mirror of the budgets the longest units start first; more units than the GPU holds at once, and more sequences than an order has room for."""
+    gen = torch.Generator(device="cuda").manual_seed(b)
+    budgets = torch.randint(1, 200, (b,), generator=torch.Generator().manual_seed(b))
+    caches = [HashEvictCache(b, h, g, d, 16, budgets, torch.zeros((d, 16)), dtype=dtype, host_budget_mirror=m) for m in (False, True)]
+    first, now = torch.randint(0, 150, (b,), generator=gen, device="cuda", dtype=torch.int32), 400
+    k, v = (torch.randn(caches[0].k_cache.shape, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    pos = torch.randint(0, now, caches[0].pos.shape, generator=gen, device="cuda", dtype=torch.int32)
+    q, mod = torch.randn((b, h * g, d), generator=gen, device="cuda").to(dtype), ScoreMod(softcap=10.0, window=350)
+    outs = []
+    for c in caches:
+        c.k_cache.copy_(k), c.v_cache.copy_(v), c.pos.copy_(pos), c.next_pos.fill_(now)
+        c.fill.copy_(budgets.to("cuda", torch.int32)[:, None].expand(b, h))
+        outs.append(c.attend_scored(q, mod, first_pos=first))
+    assert torch.equal(outs[0], outs[1])
+    for s in (0, b // 2, b - 1):  # and against the definition
+        n = int(budgets[s])
+        for u in range(h):
+            at = pos[s, u, :n].long()
+            seen = ((at >= first[s]) & (at > now - 1 - 350))[None].expand(g, n)
+            rows_q = q[s, u * g:(u + 1) * g].double()
+            x = 10.0 * torch.tanh(rows_q @ k[s, u, :n].double().T / math.sqrt(d) / 10.0)
+            w = torch.softmax(x.masked_fill(~seen, -math.inf), -1).nan_to_num(0.0)
+            ref = w @ v[s, u, :n].double()
+            assert float((outs[1][s, u * g:(u + 1) * g].double() - ref).abs().max()) <= 1e-5 * float(v.abs().max()), (s, u)
+
+
 def test_calls_that_share_tensor_memory_follow_one_another():
     """The prompt's attention and its compression both take tensor memory: in turn on one stream, and beside each other on two."""
     b, h, g, d, lens = 4, 4, 4, 128, [300, 700, 513, 64]
