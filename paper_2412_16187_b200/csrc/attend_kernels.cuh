@@ -46,6 +46,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // Merge of the per-warp partial results (m = running max in log2 units, l = running sum, o = unnormalised output).
 // part_ml: [warps][G][2], part_o: [warps][G][d]. Every thread writes some of the G * d outputs.
+// A sum of zero means that nothing was seen. A score that is a NaN or +inf leaves the sum a NaN (the maxima let a NaN pass by), and the output too.
 template <int NW>
 __device__ __forceinline__ void attend_merge(const float* part_ml, const float* part_o, int G, int d, float* out_unit) {
   for (int idx = threadIdx.x; idx < G * d; idx += 32 * NW) {
@@ -61,7 +62,7 @@ __device__ __forceinline__ void attend_merge(const float* part_ml, const float* 
       L += part_ml[(w * G + g) * 2 + 1] * f;
       O += part_o[(w * G + g) * d + c] * f;
     }
-    out_unit[idx] = L > 0.f ? O / L : 0.f;
+    out_unit[idx] = L != 0.f ? O / L : 0.f;
   }
 }
 
@@ -134,7 +135,7 @@ __device__ __forceinline__ void attend_merge_cluster(const float* part_ml, const
       L += gather[r * per + G + g] * f;
       O += gather[r * per + 2 * G + idx] * f;
     }
-    out_unit[idx] = L > 0.f ? O / L : 0.f;
+    out_unit[idx] = L != 0.f ? O / L : 0.f;
   }
 }
 
