@@ -134,8 +134,8 @@ int he_hash_keys(const he_config* cfg, const void* x, int64_t rows, int64_t row_
  * caller promises in exchange that they were completely written before this call was ENQUEUED on the stream's
  * device timeline - by work the host has synchronised with, or by work ordered before everything still pending in
  * the stream (inputs staged ahead of a run of calls, or a captured graph whose inputs are final before it is
- * launched). If the rows are produced by a kernel enqueued shortly before the call, leave the flag off. Results are
- * identical with and without the flag.
+ * launched). If the rows are produced by a kernel enqueued shortly before the call (he_rotate_step's or he_rotate_prompt's, say),
+ * leave the flag off. Results are identical with and without the flag.
  */
 int he_decode_step(const he_config* cfg, const he_cache* cache, const void* q, const void* k, const void* v,
                    int32_t* victim_out, int32_t* evicted_pos_out, uint32_t* qcodes_out, void* stream);
@@ -226,7 +226,8 @@ int he_rotate_prompt(const he_config* cfg, const he_rotary* rotary, const void* 
 /*
  * he_rotate_step - the same for the one new token per sequence that the next he_decode_step will take: q [B, Hkv*G, d], k [B, Hkv, d]
  * with element strides (sequence, head), each row rotated by the next_pos of its unit, which the call reads on the device.
- * Nothing of the cache but next_pos is touched.
+ * Nothing of the cache but next_pos is touched. A cfg with HE_FLAG_EARLY_INPUTS is refused: with that flag the he_decode_step that
+ * follows reads q and k before this call's kernel has written them.
  */
 int he_rotate_step(const he_config* cfg, const he_rotary* rotary, const he_cache* cache, const void* q, const void* k,
                    const int64_t q_strides[2], const int64_t k_strides[2], void* q_out, void* k_out, const int64_t q_out_strides[2],

@@ -394,7 +394,8 @@ class HashEvictCache:
         return q_out, k_out
 
     def rotate_step(self, rotary, q, k, q_out=None, k_out=None, stream=None):
-        """he_rotate_step: q [B, H*G, d] and k [B, H, d] of the next decode_step, rotated by the cache's next_pos. Returns (q_out, k_out)."""
+        """he_rotate_step: q [B, H*G, d] and k [B, H, d] of the next decode_step, rotated by the cache's next_pos. Returns (q_out, k_out).
+        Refused by a cache with early_inputs, whose decode_step would read the rows before they are written."""
         q_out, k_out = self._outputs(q, k, q_out, k_out)
         qs, qos, ks, kos = self._known(("step", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
                                        lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, ()))

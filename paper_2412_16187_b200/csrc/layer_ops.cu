@@ -343,6 +343,9 @@ int he_rotate_step(const he_config* cfg, const he_rotary* rotary, const he_cache
   if (int rc = check_config(cfg, true)) return rc;
   if (int rc = check_rotary(rotary, cfg->head_dim)) return rc;
   if (cache == nullptr || cache->next_pos == nullptr) return fail(HE_ERR_INVALID_ARG, "cache or its next_pos is null");
+  // such a step reads its rows before the kernel ahead of it in the stream, this one, has written them
+  if (cfg->flags & HE_FLAG_EARLY_INPUTS)
+    return fail(HE_ERR_INVALID_ARG, "rows rotated for the next step are written too late for HE_FLAG_EARLY_INPUTS");
   RotateArgs a{};
   const int64_t* const strides[4] = {q_strides, k_strides, q_out_strides, k_out_strides};
   if (int rc = rotate_sides(a, cfg, q, k, q_out, k_out, strides, 2, 1)) return rc;

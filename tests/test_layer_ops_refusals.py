@@ -1,0 +1,19 @@
+"""Calls around the cache that the library and its binding turn down before anything is launched."""
+import ctypes
+
+from paper_2412_16187_b200 import HE_FLAG_EARLY_INPUTS, Rotary, binding
+
+FAKE, FAR = 0x10000, 0x40000000  # never followed: every check below comes before the launch
+
+
+def config(flags=0, dtype=1):
+    return binding.he_config(2, 2, 4, 64, 32, 64, 0, 0, dtype, flags)
+
+
+def test_a_step_that_reads_its_rows_early_is_not_rotated_for():
+    L, cache, two = binding.lib(), binding.he_cache(*([FAKE] * 9), None, None), ctypes.c_int64 * 2
+    q, k = two(8 * 64, 64), two(2 * 64, 64)
+    for flags in (HE_FLAG_EARLY_INPUTS, HE_FLAG_EARLY_INPUTS | 1):
+        cfg = config(flags)
+        assert L.he_rotate_step(ctypes.byref(cfg), Rotary(64).pointer, ctypes.byref(cache), FAKE, FAKE, q, k, FAR, FAR + FAKE, q, k, None) == 1
+        assert b"EARLY_INPUTS" in L.he_last_error()
