@@ -312,7 +312,7 @@ constexpr int kPtReaders = 10;       // warps that read an item: softmax, produc
 constexpr float kPtSlack = 8.f;      // log2 of how far weights may exceed 1 before the output is rescaled
 constexpr float kPtTanhEnd = 7.f;    // see pt_tanh
 constexpr float kPtNearEnd = 0.7f;   // see pt_tanh_near
-constexpr float kPtNearInv = 1e-5f;  // the powers of a smaller factor leave fp32
+constexpr float kPtNearInv = 1e-5f, kPtNearMost = 1e5f;  // the powers of a smaller or larger factor leave fp32
 
 template <int D>
 struct PromptTc {
@@ -698,6 +698,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         float scale = a.scale_log2;  // from x to log2 units
         if (CAP) {  // x <- tanh(inv x) / inv
           const float inv = a.inv_cap;
+          const bool near_holds = inv >= kPtNearInv && inv <= kPtNearMost;
           float far[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int c = 0; c < 128; c += 8)
@@ -705,7 +706,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             for (int e = 0; e < 4; ++e) far[e] = pt_max3_abs(far[e], x[c + e], x[c + e + 4]);
           const float most = i < w.n ? pt_max(pt_max(far[0], far[1]), pt_max(far[2], far[3])) * inv : 0.f;  // (rows behind the end hold anything)
           const PtNear near = pt_near(inv);
-          if (__builtin_expect(inv >= kPtNearInv && __all_sync(0xFFFFFFFFu, most <= kPtNearEnd), 1)) {
+          if (__builtin_expect(near_holds && __all_sync(0xFFFFFFFFu, most <= kPtNearEnd), 1)) {
 #pragma unroll
             for (int c = 0; c < 128; c += 16) {
               pt2 z[8];
@@ -730,7 +731,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
               for (int e = 0; e < 4; ++e) {
                 float z0, z1, y0, y1;
                 pt_mul(z[e], pt2(back, back)).get(z0, z1), y[e].get(y0, y1);
-                const bool n0 = inv >= kPtNearInv && fabsf(x[c + 2 * e] * inv) <= kPtNearEnd, n1 = inv >= kPtNearInv && fabsf(x[c + 2 * e + 1] * inv) <= kPtNearEnd;
+                const bool n0 = near_holds && fabsf(x[c + 2 * e] * inv) <= kPtNearEnd, n1 = near_holds && fabsf(x[c + 2 * e + 1] * inv) <= kPtNearEnd;
                 x[c + 2 * e] = n0 ? y0 : z0, x[c + 2 * e + 1] = n1 ? y1 : z1;
               }
             }
