@@ -240,7 +240,7 @@ int he_rotate_step(const he_config* cfg, const he_rotary* rotary, const he_cache
  */
 typedef struct he_score_mod {
   float scale;         /* > 0, or 0 for 1 / sqrt(d) */
-  float cap;           /* > 0, or 0 for none */
+  float cap;           /* > 0, or 0 for none; scale / cap is refused below 1.2e-38, the least normal fp32 number */
   int32_t window;      /* w > 0: positions p <= t - w are hidden; 0 for none */
   int32_t reserved;    /* 0 */
   const float* slopes; /* device fp32 [Hkv*G], or NULL for none */

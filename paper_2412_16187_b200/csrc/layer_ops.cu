@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -131,7 +132,8 @@ int check_mod(const he_score_mod* mod, int d, float* scale_log2, float* cap_log2
     cap = mod->cap, *window = mod->window, *slopes = mod->slopes;
   }
   *scale_log2 = scale * kLog2e, *cap_log2 = cap * kLog2e, *inv_cap = cap > 0.f ? scale / cap : 0.f;
-  if (!std::isfinite(*scale_log2) || !std::isfinite(*cap_log2) || !std::isfinite(*inv_cap))
+  // (a ratio below the normal numbers would be lost, or its inverse: such a cap is none)
+  if (!std::isfinite(*scale_log2) || !std::isfinite(*cap_log2) || !std::isfinite(*inv_cap) || (cap > 0.f && *inv_cap < FLT_MIN))
     return fail(HE_ERR_INVALID_ARG, "scale %g with cap %g leaves fp32", (double)scale, (double)cap);
   return HE_OK;
 }

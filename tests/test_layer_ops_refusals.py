@@ -17,3 +17,15 @@ def test_a_step_that_reads_its_rows_early_is_not_rotated_for():
         cfg = config(flags)
         assert L.he_rotate_step(ctypes.byref(cfg), Rotary(64).pointer, ctypes.byref(cache), FAKE, FAKE, q, k, FAR, FAR + FAKE, q, k, None) == 1
         assert b"EARLY_INPUTS" in L.he_last_error()
+
+
+def test_a_cap_whose_ratio_to_the_scale_is_no_normal_number_is_refused():
+    L, mod = binding.lib(), binding.he_score_mod
+    cache, three = binding.he_cache(*([FAKE] * 9), None, None), ctypes.c_int64 * 3
+    q, k = three(8 * 64 * 16, 64 * 16, 64), three(2 * 64 * 16, 64 * 16, 64)
+    cfg = config()
+    for bad in (mod(1e-30, 1e30, 0, 0, None), mod(1e-10, 1e35, 0, 0, None), mod(1e-38, 2.0, 0, 0, None)):
+        assert L.he_attend_prompt(ctypes.byref(cfg), ctypes.byref(bad), FAKE, FAKE, FAKE, q, k, FAKE, 16, None, None, FAR, q, None) == 1
+        assert b"leaves fp32" in L.he_last_error()
+        assert L.he_attend_scored(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(bad), FAKE, None, FAR, None) == 1
+        assert b"leaves fp32" in L.he_last_error()
