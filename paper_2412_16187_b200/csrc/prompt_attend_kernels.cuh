@@ -506,7 +506,11 @@ __device__ __forceinline__ void pt_tanh(pt2* z) {
     z[i] = pt2(pt_min(pt_max(a, -kPtTanhEnd), kPtTanhEnd), pt_min(pt_max(b, -kPtTanhEnd), kPtTanhEnd));
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = pt_mul(z[i], z[i]);
+  for (int i = 0; i < N; ++i) {  // a NaN goes on in the numerator alone: the reciprocal is shared with a neighbour that may be seen where this one is hidden
+    float a, b;
+    pt_mul(z[i], z[i]).get(a, b);
+    w[i] = pt2(fminf(a, kPtTanhEnd * kPtTanhEnd), fminf(b, kPtTanhEnd * kPtTanhEnd));
+  }
 #pragma unroll
   for (int i = 0; i < N; ++i) de[i] = pt_fma(w[i], pt2(0.00014415701319693802f, 0.00014415701319693802f), pt2(0.02116040722518346f, 0.02116040722518346f));
 #pragma unroll
