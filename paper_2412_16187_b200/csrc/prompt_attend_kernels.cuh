@@ -7,8 +7,10 @@
 //   prompt_fp32_kernel    any dtype and head size: 64 or 16 rows x 64 keys at a time on the CUDA cores.
 //
 // Values in hidden places. Hidden keys get a weight of zero by selection, whatever their score is; a hidden V row that holds an infinity or a
-// NaN would still turn the product 0 * V into NaN. V rows behind the prompt's end are therefore read as zeros, and a
-// row whose output has come out as NaN is computed once more over its visible keys alone (prompt_row_again), which costs nothing where it does not happen.
+// NaN would still turn the product 0 * V into NaN. V rows behind the prompt's end are therefore read as zeros, and a row whose output has come
+// out as NaN is computed once more over its visible keys alone where what it hides can be the reason (prompt_rows_again). It cannot where the sum of the
+// weights is a NaN (a score that the row sees), where no V row that its tile has multiplied by zero holds anything but numbers, or where
+// V rows that it sees are NaN in the same channels. Looking costs a warp one run over the rows in question for its 32 rows of output.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -43,45 +45,208 @@ __device__ __forceinline__ void prompt_interval(const PromptArgs& a, int s, int 
   hi = min(hi, n);
 }
 
-__device__ __forceinline__ float prompt_element(const void* p, long long at, int dtype) {
-  return dtype == HE_DTYPE_BF16 ? bf16_bits_to_f32(static_cast<const uint16_t*>(p)[at]) : static_cast<const float*>(p)[at];
-}
 __device__ __forceinline__ void prompt_store(void* p, long long at, int dtype, float f) {
   if (dtype == HE_DTYPE_BF16) static_cast<__nv_bfloat16*>(p)[at] = __float2bfloat16_rn(f);
   else static_cast<float*>(p)[at] = f;
 }
 
-// One row by one warp, over its visible keys alone.
-// `beat`: raised now and then for those who wait meanwhile.
-static __device__ __noinline__ void prompt_row_again(const PromptArgs& a, int s, int head, int i, int n, volatile int* beat = nullptr) {
-  const int lane = threadIdx.x & 31, kv = head / a.group;
-  int lo, hi;
-  prompt_interval(a, s, i, n, lo, hi);
-  const long long q0 = s * a.qs[0] + head * a.qs[1] + i * a.qs[2], k0 = s * a.ks[0] + kv * a.ks[1];
+// Elements of a 16-byte chunk as fp32: eight, or four.
+template <int ES>
+__device__ __forceinline__ void prompt_unpack(const uint4& chunk, float (&f)[16 / ES]) {
+  const uint32_t w[4] = {chunk.x, chunk.y, chunk.z, chunk.w};
+#pragma unroll
+  for (int e = 0; e < 16 / ES; ++e) f[e] = ES == 4 ? __uint_as_float(w[e % 4]) : __uint_as_float((e & 1) ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+}
+
+// Up to four rows of a head, row[0] <= row[1] <= ..., by one warp, each over its visible keys alone: 32 keys at a time, a lane for the scores of each, then for
+// the channels of one chunk (of 1 / per of the keys where a row has fewer chunks than there are lanes). `beat`: raised now and then for those
+// who wait meanwhile. Four rows over 2048 keys at d = 128 take 0.6 ms.
+constexpr int kPromptAgain = 4;
+template <int ES>
+static __device__ __noinline__ void prompt_compute_again(const PromptArgs& a, int s, int head, const int (&row)[kPromptAgain], int n, volatile int* beat) {
+  constexpr int EPC = 16 / ES, SLOTS = ES == 4 ? 2 : 1, RB = kPromptAgain;  // elements of a chunk; chunks of a lane (rows have up to 64)
+  const uint32_t all_lanes = 0xFFFFFFFFu;
+  const int lane = threadIdx.x & 31, kv = head / a.group, cpr = a.d / EPC;
+  const int per = cpr < 32 ? 32 / cpr : 1, sub = cpr < 32 ? lane / cpr : 0, c = cpr < 32 ? lane % cpr : lane;
+  auto chunk = [&](const void* p, long long at_row, int at) { return *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + at_row * ES + 16 * at); };
+  const long long q0 = s * a.qs[0] + head * a.qs[1], k0 = s * a.ks[0] + kv * a.ks[1];
   const float slope = a.slopes != nullptr ? a.slopes[head] * kPromptLog2e : 0.f;
-  float q[kMaxDim / 32], o[kMaxDim / 32], m = -INFINITY, l = 0.f;
+  int lo[RB], hi[RB], begin = 0x7FFFFFFF, end = 0;
+  float m[RB], l[RB], o[RB][SLOTS][EPC];  // l: of this lane's keys; o: of this lane's chunks and keys
 #pragma unroll
-  for (int c = 0; c < kMaxDim / 32; ++c) q[c] = lane + 32 * c < a.d ? prompt_element(a.q, q0 + lane + 32 * c, a.dtype) : 0.f, o[c] = 0.f;
-  for (int j = lo; j < hi; ++j) {
-    if (beat != nullptr && (j & 1023) == 0 && lane == 0) *beat = *beat + 1;
-    float dot = 0.f;
+  for (int b = 0; b < RB; ++b) {
+    prompt_interval(a, s, row[b], n, lo[b], hi[b]);
+    begin = min(begin, lo[b]), end = max(end, hi[b]);
+    m[b] = -INFINITY, l[b] = 0.f;
 #pragma unroll
-    for (int c = 0; c < kMaxDim / 32; ++c)
-      if (lane + 32 * c < a.d) dot = fmaf(q[c], prompt_element(a.k, k0 + j * a.ks[2] + lane + 32 * c, a.dtype), dot);
-    for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, off);
-    float x = a.cap_log2 > 0.f ? a.cap_log2 * tanhf(dot * a.inv_cap) : dot * a.scale_log2;
-    x -= slope * (float)abs(i - j);
-    const float mx = fmaxf(m, x), mn = mx == -INFINITY ? 0.f : mx, corr = exp2f(m - mn), p = exp2f(x - mn);
-    l = l * corr + p;
-    m = mx;
+    for (int w = 0; w < SLOTS; ++w)
 #pragma unroll
-    for (int c = 0; c < kMaxDim / 32; ++c)
-      if (lane + 32 * c < a.d) o[c] = o[c] * corr + p * prompt_element(a.v, k0 + j * a.ks[2] + lane + 32 * c, a.dtype);
+      for (int e = 0; e < EPC; ++e) o[b][w][e] = 0.f;
   }
-  const long long o0 = s * a.os[0] + head * a.os[1] + i * a.os[2];
+  for (int j0 = begin; j0 < end; j0 += 32) {
+    if (beat != nullptr && ((j0 - begin) & 1023) == 0 && lane == 0) *beat = *beat + 1;
+    const int j = min(j0 + lane, end - 1), count = min(end - j0, 32);
+    float dot[RB] = {};
+#pragma unroll 4
+    for (int at = 0; at < cpr; ++at) {
+      float kf[EPC];
+      prompt_unpack<ES>(chunk(a.k, k0 + j * a.ks[2], at), kf);
 #pragma unroll
-  for (int c = 0; c < kMaxDim / 32; ++c)
-    if (lane + 32 * c < a.d) prompt_store(a.out, o0 + lane + 32 * c, a.dtype, l != 0.f ? o[c] / l : 0.f);
+      for (int b = 0; b < RB; ++b) {
+        float qf[EPC];
+        prompt_unpack<ES>(chunk(a.q, q0 + row[b] * a.qs[2], at), qf);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) dot[b] = fmaf(qf[e], kf[e], dot[b]);
+      }
+    }
+    float p[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      float x = a.cap_log2 > 0.f ? a.cap_log2 * tanhf(dot[b] * a.inv_cap) : dot[b] * a.scale_log2;
+      x -= slope * (float)abs(row[b] - j);
+      x = j0 + lane >= lo[b] && j0 + lane < hi[b] ? x : -INFINITY;
+      float mx = fmaxf(m[b], x);
+      for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(all_lanes, mx, off));
+      const float mn = mx == -INFINITY ? 0.f : mx, corr = exp2f(m[b] - mn);
+      p[b] = exp2f(x - mn);
+      l[b] = l[b] * corr + p[b];
+      m[b] = mx;
+#pragma unroll
+      for (int w = 0; w < SLOTS; ++w)
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) o[b][w][e] *= corr;
+    }
+#pragma unroll 4
+    for (int t = 0; t < count; t += per) {
+      const int key = j0 + t + sub;
+      float pj[RB];
+#pragma unroll
+      for (int b = 0; b < RB; ++b) pj[b] = __shfl_sync(all_lanes, p[b], (t + sub) & 31);
+      if (sub < per && t + sub < count)
+#pragma unroll
+        for (int w = 0; w < SLOTS; ++w)
+          if (c + 32 * w < cpr) {
+            float vf[EPC];
+            prompt_unpack<ES>(chunk(a.v, k0 + key * a.ks[2], c + 32 * w), vf);
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+              for (int e = 0; e < EPC; ++e) o[b][w][e] = fmaf(pj[b], key >= lo[b] && key < hi[b] ? vf[e] : 0.f, o[b][w][e]);
+          }
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    for (int off = 16; off > 0; off >>= 1) l[b] += __shfl_xor_sync(all_lanes, l[b], off);
+    const long long o0 = s * a.os[0] + head * a.os[1] + row[b] * a.os[2];
+#pragma unroll
+    for (int w = 0; w < SLOTS; ++w)
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        float sum = o[b][w][e];
+        for (int k = 1; k < per; ++k) sum += __shfl_sync(all_lanes, o[b][w][e], (c + k * cpr) & 31);  // (per > 1: cpr < 32)
+        if (sub == 0 && c + 32 * w < cpr) prompt_store(a.out, o0 + EPC * (c + 32 * w) + e, a.dtype, l[b] != 0.f ? sum / l[b] : 0.f);
+      }
+  }
+}
+
+// A bit for each element of 16 bytes that is a NaN or, without `nan_only`, an infinity.
+__device__ __forceinline__ uint32_t prompt_odd_bits(const uint4& chunk, int dtype, bool nan_only) {
+  const uint32_t w[4] = {chunk.x, chunk.y, chunk.z, chunk.w}, least = nan_only ? 1u : 0u;
+  uint32_t bits = 0u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (dtype == HE_DTYPE_BF16)
+      bits |= (uint32_t)((w[e] & 0x7FFFu) >= 0x7F80u + least) << (2 * e) | (uint32_t)((w[e] >> 16 & 0x7FFFu) >= 0x7F80u + least) << (2 * e + 1);
+    else
+      bits |= (uint32_t)((w[e] & 0x7FFFFFFFu) >= 0x7F800000u + least) << e;
+  return bits;
+}
+
+// The rows i0 + b of one head, b a bit of `again`, whose outputs are stored, hold a NaN and have a number for the sum of their weights; their tile has
+// multiplied the V rows [from, to). Computes those anew whose NaNs may come from rows that they hide. By a whole warp.
+static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s, int head, int i0, uint32_t again, int n, int from, int to, volatile int* beat = nullptr) {
+  constexpr int STEPS = 4;  // loads in flight
+  const uint32_t all_lanes = 0xFFFFFFFFu;
+  const int lane = threadIdx.x & 31, kv = head / a.group, es = esize_of(a.dtype), cpr = a.d * es / 16;  // (16-byte chunks of a row: up to 64)
+  const int per = cpr < 32 ? 32 / cpr : 1, sub = cpr < 32 ? lane / cpr : 0, c = cpr < 32 ? lane % cpr : lane;  // rows at a time; this lane's row of them and chunk
+  const char* v = static_cast<const char*>(a.v) + (s * a.ks[0] + kv * a.ks[1]) * es;
+  const char* out = static_cast<const char*>(a.out) + (s * a.os[0] + head * a.os[1]) * es;
+  auto odd = [&](const char* p, long long stride, int row, int chunk, bool nan_only) -> uint32_t {
+    return chunk < cpr ? prompt_odd_bits(*reinterpret_cast<const uint4*>(p + row * stride * es + 16 * chunk), a.dtype, nan_only) : 0u;
+  };
+  auto hides_odd = [&](int row) { return (odd(v, a.ks[2], row, c, false) | odd(v, a.ks[2], row, c + 32, false)) != 0u; };
+  auto alive = [&](int step) {
+    if (beat != nullptr && (step & 63) == 0 && lane == 0) *beat = *beat + 1;
+  };
+  int lo, hi;
+  prompt_interval(a, s, i0 + lane, n, lo, hi);
+  bool mine = (again >> lane) & 1u;
+  // The last row behind what they see, and the first before it, that is not all numbers.
+  const int begin = __reduce_min_sync(all_lanes, mine ? hi : to), end = __reduce_max_sync(all_lanes, mine ? lo : from);
+  int last = -1, first = 0x7FFFFFFF, step = 0;
+  for (int j = to; j > begin && last < 0; j -= STEPS * per) {
+    int found = -1;
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) {
+      const int row = j - 1 - u * per - sub;
+      if (sub < per && row >= begin && hides_odd(row)) found = max(found, row);
+    }
+    last = __reduce_max_sync(all_lanes, found);
+    alive(++step);
+  }
+  for (int j = from; j < end && first == 0x7FFFFFFF; j += STEPS * per) {
+    int found = 0x7FFFFFFF;
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) {
+      const int row = j + u * per + sub;
+      if (sub < per && row < end && hides_odd(row)) found = min(found, row);
+    }
+    first = __reduce_min_sync(all_lanes, found);
+    alive(++step);
+  }
+  mine = mine && (last >= hi || first < lo);
+  again = __ballot_sync(all_lanes, mine);
+  if (again == 0u) return;
+  // Channels that are NaN in rows that all the others see too, from the last on until they explain every output.
+  const int seen_begin = __reduce_max_sync(all_lanes, mine ? lo : 0), seen_end = __reduce_min_sync(all_lanes, mine ? hi : 0x7FFFFFFF);
+  uint32_t want[2] = {0u, 0u}, have[2] = {0u, 0u}, known[2] = {0u, 0u};
+  for (uint32_t rest = again; rest != 0u; rest &= rest - 1u)
+#pragma unroll
+    for (int w = 0; w < 2; ++w) want[w] |= odd(out, a.os[2], i0 + __ffs(rest) - 1, c + 32 * w, true);
+  for (int j = seen_end; j > seen_begin; j -= STEPS * per) {
+#pragma unroll
+    for (int u = 0; u < STEPS; ++u) {
+      const int row = j - 1 - u * per - sub;
+      if (sub < per && row >= seen_begin)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) have[w] |= odd(v, a.ks[2], row, c + 32 * w, true);
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      known[w] = have[w];
+      for (int k = 0; k < per && cpr < 32; ++k) known[w] |= __shfl_sync(all_lanes, have[w], c + k * cpr);
+    }
+    if (__all_sync(all_lanes, ((want[0] & ~known[0]) | (want[1] & ~known[1])) == 0u)) break;
+    alive(++step);
+  }
+  int row[kPromptAgain], rows = 0;
+  for (uint32_t rest = again; rest != 0u;) {
+    const int i = i0 + __ffs(rest) - 1;
+    rest &= rest - 1u;
+    const uint32_t open = (odd(out, a.os[2], i, c, true) & ~known[0]) | (odd(out, a.os[2], i, c + 32, true) & ~known[1]);
+    if (__any_sync(all_lanes, open != 0u)) {
+#pragma unroll
+      for (int b = 0; b < kPromptAgain; ++b)
+        if (b >= rows) row[b] = i;  // (places that stay empty repeat the last row)
+      ++rows;
+    }
+    if (rows == kPromptAgain || (rest == 0u && rows > 0)) {
+      if (es == 2) prompt_compute_again<2>(a, s, head, row, n, beat);
+      else prompt_compute_again<4>(a, s, head, row, n, beat);
+      rows = 0;
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ CUDA cores
@@ -264,6 +429,7 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
     }
     __syncthreads();  // the tile has been read
   }
+  uint32_t again = 0u;  // rows of this warp with a NaN that a score does not explain
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int i = i0 + R * ty + r;
@@ -277,12 +443,13 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
         const float f = l[r] != 0.f ? o[r][4 * q + e] / l[r] : 0.f;
         if (i < n && c < d) prompt_store(a.out, o0 + c, a.dtype, f), bad |= f != f;
       }
-    const uint32_t again = __ballot_sync(0xFFFFFFFFu, bad);
-    __syncwarp();
+    const uint32_t odd = __ballot_sync(0xFFFFFFFFu, bad && l[r] == l[r]);
 #pragma unroll
     for (int w = 0; w < 2; ++w)  // the rows of this warp's two ty
-      if ((again >> (16 * w)) & 0xFFFFu) prompt_row_again(a, s, head, i0 + R * ((tid - lane) / 16 + w) + r, n);
+      if ((odd >> (16 * w)) & 0xFFFFu) again |= 1u << (R * w + r);
   }
+  __syncwarp();
+  if (again != 0u) prompt_rows_again(a, s, head, i0 + R * (tid - lane) / 16, again, n, j_begin, min((j_end + 63) / 64 * 64, n));
 }
 
 // ------------------------------------------------------------------------------------------------ tensor cores
@@ -857,10 +1024,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         for (int e = 0; e < 4; ++e)
           if (i < w.n && c + 8 * e < a.d) *reinterpret_cast<uint4*>(out + c + 8 * e) = make_uint4(word[4 * e], word[4 * e + 1], word[4 * e + 2], word[4 * e + 3]);
       }
-      const bool bad = !none && pt_max(nan[0], nan[1]) != pt_max(nan[0], nan[1]);
-      uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
+      const bool bad = !none && l == l && pt_max(nan[0], nan[1]) != pt_max(nan[0], nan[1]);
+      const uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
       __syncwarp();
-      for (; again != 0u; again &= again - 1u) prompt_row_again(a, w.s, head, i - lane + __ffs(again) - 1, w.n, beat);
+      if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, w.jb[t] * kPtTile, min(w.je[t] * kPtTile, w.n), beat);
       tc_fence_before();
       give_item(k);
     }
