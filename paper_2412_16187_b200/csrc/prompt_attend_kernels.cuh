@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
     for (int c = 0; c < 4 * NQ; ++c) o[r][c] = 0.f;
   }
   __syncthreads();
-  const int j_begin = run[0] / 64 * 64, j_end = run[1];
+  const int j_begin = run[0], j_end = run[1];  // (nothing ahead of the first key that a row sees is read)
   const int r_first = tid / cpr, c_first = tid % cpr, r_step = kPromptThreads / cpr, c_step = kPromptThreads % cpr;
   const bool async = a.dtype == HE_DTYPE_F32;
   auto fetch = [&](int j0, int stage) {
@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
       if ((odd >> (16 * w)) & 0xFFFFu) again |= 1u << (R * w + r);
   }
   __syncwarp();
-  if (again != 0u) prompt_rows_again(a, s, head, i0 + R * (tid - lane) / 16, again, n, j_begin, min((j_end + 63) / 64 * 64, n));
+  if (again != 0u) prompt_rows_again(a, s, head, i0 + R * (tid - lane) / 16, again, n, j_begin, min(j_begin + (j_end - j_begin + 63) / 64 * 64, n));
 }
 
 // ------------------------------------------------------------------------------------------------ tensor cores
@@ -492,9 +492,10 @@ struct PromptMaps {
   alignas(64) CUtensorMap q, k, v;
 };
 
-// An item: its rows, and per tile the blocks of keys [jb, je) that it needs and the keys [all_lo, all_hi) that all of its rows see.
+// An item: its rows, the first key that any of them sees (block j holds the keys base + 128 j on: what lies before, say the padding ahead of a prompt, is
+// never multiplied), and per tile the blocks of keys [jb, je) that it needs and the keys [all_lo, all_hi) that all of its rows see.
 struct PtItem {
-  int some, s, n, p, tok0;
+  int some, s, n, p, tok0, base;
   int jb[2], je[2], all_lo[2], all_hi[2];
 };
 
@@ -846,7 +847,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       const PtItem& w = item_s[k & 1];  // (read where it is used: registers are short here)
       const int i = tok_of(w, t) + row, head = head_of(w, t), steps = w.je[t] - w.jb[t];
       // blocks of keys from the last to the first; all rows see all keys in those from inner_begin to before inner_end
-      const int inner_begin = w.je[t] - w.all_hi[t] / kPtTile, inner_end = w.je[t] - (int)(((unsigned)w.all_lo[t] + kPtTile - 1) / kPtTile);
+      const int inner_begin = w.je[t] - max(w.all_hi[t] - w.base, 0) / kPtTile, inner_end = w.je[t] - (int)(((unsigned)(w.all_lo[t] - w.base) + kPtTile - 1) / kPtTile);
       int lo, hi;
       prompt_interval(a, w.s, i, w.n, lo, hi);
       const float slope = BIAS ? a.slopes[head] * kPromptLog2e : 0.f;
@@ -865,7 +866,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
           for (int c = 0; c < 128; ++c) x[c] = __uint_as_float(raw[c >> 5][c & 31]);
         }
         const bool edge = it < inner_begin || it >= inner_end;
-        const int j0 = (w.je[t] - 1 - it) * kPtTile;
+        const int j0 = w.base + (w.je[t] - 1 - it) * kPtTile;
         float scale = a.scale_log2;  // from x to log2 units
         if (CAP) {  // x <- tanh(inv x) / inv
           const float inv = a.inv_cap;
@@ -1027,7 +1028,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       const bool bad = !none && l == l && pt_max(nan[0], nan[1]) != pt_max(nan[0], nan[1]);
       const uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
       __syncwarp();
-      if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, w.jb[t] * kPtTile, min(w.je[t] * kPtTile, w.n), beat);
+      if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, w.base + w.jb[t] * kPtTile, min(w.base + w.je[t] * kPtTile, w.n), beat);
       tc_fence_before();
       give_item(k);
     }
@@ -1066,8 +1067,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             mbar_arrive_expect_tx(bar, (step > 0 && step < blocks ? 2u : 1u) * T::kTileBytes);
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
-              if (step > 0) tma_load_4d(at + T::kTileBytes + h * BOX, &maps.v, 64 * h, (j_end - step) * kPtTile, kv, w.s, bar);
-              if (step < blocks) tma_load_4d(at + h * BOX, &maps.k, 64 * h, (j_end - 1 - step) * kPtTile, kv, w.s, bar);
+              if (step > 0) tma_load_4d(at + T::kTileBytes + h * BOX, &maps.v, 64 * h, w.base + (j_end - step) * kPtTile, kv, w.s, bar);
+              if (step < blocks) tma_load_4d(at + h * BOX, &maps.k, 64 * h, w.base + (j_end - 1 - step) * kPtTile, kv, w.s, bar);
             }
           }
           ++used;
@@ -1098,7 +1099,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
           // O += P V of block j, S of block j - 1, tile by tile
           ok = pt_wait_small(smem_u32(&full_s[slot]), lap, abort_flag, beat);
           if (!ok) break;
-          const int rows = w.n - j * kPtTile;
+          const int rows = w.n - w.base - j * kPtTile;
           if (__builtin_expect(j < j_end && rows < kPtTile, 0)) {  // V rows behind the prompt's end hold anything: zeros
             const int chunks = (kPtTile - rows) * 8;
             for (int c = lane; c < chunks * NH; c += 32)
@@ -1169,6 +1170,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         w.tok0 = by_heads ? tile * kPtTile : tile * 2 * kPtTile;
         w.n = min(max(a.lens[w.s], 0), a.tokens);
         if (w.tok0 < w.n) {
+          w.base = 0x7FFFFFFF;
           for (int t = 0; t < 2; ++t) {
             int first = 0x7FFFFFFF, end = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
 #pragma unroll 1
@@ -1181,7 +1183,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             }
             first = __reduce_min_sync(0xFFFFFFFFu, first), end = __reduce_max_sync(0xFFFFFFFFu, end);
             w.all_lo[t] = __reduce_max_sync(0xFFFFFFFFu, all_lo), w.all_hi[t] = __reduce_min_sync(0xFFFFFFFFu, all_hi);
-            w.jb[t] = end > 0 ? first / kPtTile : 0, w.je[t] = end > 0 ? (end + kPtTile - 1) / kPtTile : 0;
+            w.jb[t] = first, w.je[t] = end, w.base = min(w.base, first);
+          }
+          for (int t = 0; t < 2; ++t) {
+            const bool any = w.je[t] > 0;
+            w.jb[t] = any ? (w.jb[t] - w.base) / kPtTile : 0, w.je[t] = any ? (w.je[t] - w.base + kPtTile - 1) / kPtTile : 0;
           }
           hand_over(w);
           // not before this item is nearly done: a CTA that took the next one at once would be bound to it however long this one lasts

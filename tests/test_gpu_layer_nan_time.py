@@ -112,3 +112,30 @@ def test_seen_and_hidden_values_that_are_not_finite_together(dtype, d, n):
         # elsewhere: both within the tolerance of exact arithmetic, which rows computed again meet with fp32 weights
         near = (got - out["without"][0].double()).abs()[:, ~touched]
         assert float(near.max()) <= 2 * (2.0 ** -8 + 2.0 ** -8 + 2e-5) * float(v.abs().max())
+
+
+@pytest.mark.parametrize("dtype, d, n", SHAPES)
+@pytest.mark.parametrize("mask", ["plain", "cap", "slopes", "window"])
+@pytest.mark.parametrize("group", [4, 1])
+def test_padding_ahead_of_a_prompt_may_hold_anything(dtype, d, n, mask, group):
+    """Padded on the left: padding sees nothing and nobody sees it. Nothing of it is ever multiplied, so the call costs what it always does."""
+    cache, q, k, v, _ = prompt(dtype, d, n, heads=8 if group > 1 else 3, group=group)
+    cache2 = make_cache(2, k.shape[1], group, d, dtype)
+    q, k, v = (x.expand(2, -1, -1, -1).clone() for x in (q, k, v))
+    pads = [37, n // 3 + 1]
+    at = torch.arange(n, device="cuda")
+    doc = torch.stack([torch.where(at < p, 2 ** 30, p) for p in pads]).to(torch.int32)
+    plen = torch.tensor([n, n], dtype=torch.int32, device="cuda")
+    heads = q.shape[1]
+    mod = {"plain": None, "cap": ScoreMod(softcap=20.0), "slopes": ScoreMod(slopes=torch.full((heads,), 0.1, device="cuda")), "window": ScoreMod(window=101)}[mask]
+    out = torch.empty_like(q)
+    call = lambda: cache2.attend_prompt(q, k, v, plen, mod=mod, doc_start=doc, out=out)  # noqa: E731
+    usual = least_time(call)
+    clean = out.clone()
+    assert bool(torch.isfinite(clean).all()) and not clean[0, :, :37].any()
+    for s, p in enumerate(pads):
+        q[s, :, :p], k[s, :, :p], v[s, :, :p] = math.inf, math.nan, math.nan
+    out.fill_(7.0)
+    took = least_time(call)
+    assert torch.equal(out, clean)
+    assert took <= 10 * usual, (took, usual)
