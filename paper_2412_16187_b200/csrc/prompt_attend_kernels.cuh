@@ -1198,6 +1198,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         ++asked;
         if (!pt_wait_small(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
         const bool more = pt_read_work(answer, cta);
+        __syncwarp();  // every lane has read the answer before the next one may be written
         if (!more) {
           w.some = 0;
           hand_over(w);
