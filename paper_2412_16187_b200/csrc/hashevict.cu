@@ -22,6 +22,7 @@
 #include <mutex>
 #include <utility>
 
+#include "attend_generic_kernels.cuh"
 #include "attend_kernels.cuh"
 #include "common.cuh"
 #include "decode_kernels.cuh"
