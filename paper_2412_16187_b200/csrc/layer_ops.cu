@@ -364,6 +364,7 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
   if (max_prompt_len > kMaxTokens) return fail(HE_ERR_UNSUPPORTED, "max_prompt_len %d > 2^24", max_prompt_len);
   PromptArgs a{};
   if (int rc = check_mod(mod, cfg->head_dim, &a.scale_log2, &a.cap_log2, &a.inv_cap, &a.window, &a.slopes)) return rc;
+  a.near_end = a.inv_cap >= kPtNearInv && a.inv_cap <= kPtNearMost ? kPtNearEnd : -1.f;
   if (max_prompt_len == 0) return HE_OK;
   if (!q || !k || !v || !out || !prompt_len) return fail(HE_ERR_INVALID_ARG, "q, k, v, out or prompt_len is null");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");

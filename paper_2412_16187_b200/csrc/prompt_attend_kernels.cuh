@@ -29,6 +29,7 @@ struct PromptArgs {
   const int32_t* prefix;     // [B] or null
   const float* slopes;       // [Hkv*G] or null
   float scale_log2, cap_log2, inv_cap;  // scores in log2 units: scale_log2 * q.k, or cap_log2 * tanh(inv_cap * q.k)
+  float near_end;  // kPtNearEnd where the near form of the tanh can be written for inv_cap, else -1
   int window;
 };
 
@@ -479,7 +480,7 @@ constexpr int kPtReaders = 10;       // warps that read an item: softmax, produc
 constexpr float kPtSlack = 8.f;      // log2 of how far weights may exceed 1 before the output is rescaled
 constexpr float kPtTanhEnd = 7.f;    // see pt_tanh
 constexpr float kPtNearEnd = 0.7f;   // see pt_tanh_near
-constexpr float kPtNearInv = 1e-5f, kPtNearMost = 1e5f;  // the powers of a smaller or larger factor leave fp32
+constexpr float kPtNearInv = 1e-5f, kPtNearMost = 1e5f;  // the powers of a smaller or larger factor leave fp32: PromptArgs::near_end is -1 there
 
 template <int D>
 struct PromptTc {
@@ -493,10 +494,11 @@ struct PromptMaps {
 };
 
 // An item: its rows, the first key that any of them sees (block j holds the keys base + 128 j on: what lies before, say the padding ahead of a prompt, is
-// never multiplied), and per tile the blocks of keys [jb, je) that it needs and the keys [all_lo, all_hi) that all of its rows see.
+// never multiplied), how many keys of the last block lie within the prompt, and per tile the blocks of keys [jb, je) that it needs and at
+// which steps from the last of them on, [all_from, all_to), its rows see every key of the block.
 struct PtItem {
-  int some, s, n, p, tok0, base;
-  int jb[2], je[2], all_lo[2], all_hi[2];
+  int some, s, n, p, tok0, base, last_rows;
+  int jb[2], je[2], all_from[2], all_to[2];
 };
 
 // One product or commit, issued by the lane of a converged warp that has `leader` set: a predicate on the instruction, so that descriptors stay in
@@ -734,13 +736,15 @@ __device__ __forceinline__ bool pt_wait(uint32_t bar, uint32_t parity, volatile 
   return pt_wait_on(bar, parity, abort_flag, beat);
 }
 
-// The same for the roles beside the softmax, what follows the first poll in one place.
+// The same for the roles beside the softmax, what follows the first poll in one place (for each kernel, next to its code: one place for all costs up to 2 %).
+template <int D, bool CAP, bool BIAS>
 static __device__ __noinline__ bool pt_wait_far(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   return pt_wait_on(bar, parity, abort_flag, beat);
 }
+template <int D, bool CAP, bool BIAS>
 __device__ __forceinline__ bool pt_wait_small(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)), 1)) return true;
-  return pt_wait_far(bar, parity, abort_flag, beat);
+  return pt_wait_far<D, CAP, BIAS>(bar, parity, abort_flag, beat);
 }
 
 // The grid's next waiting CTA, cancelled and taken over: asked for by one lane, answered in 16 bytes of shared memory.
@@ -828,7 +832,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
     if (lane == 0) mbar_arrive(smem_u32(&iempty_s[k & 1]));
   };
   auto read_item = [&](int k, PtItem& w) -> bool {
-    if (!pt_wait_small(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat)) return false;
+    if (!pt_wait_small<D, CAP, BIAS>(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat)) return false;
     w = item_s[k & 1];
     if (w.some == 0) return false;
     give_item(k);
@@ -846,9 +850,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
     for (int k = 0; ok && take_item(k); ++k) {
       const PtItem& w = item_s[k & 1];  // (read where it is used: registers are short here)
       const int i = tok_of(w, t) + row, head = head_of(w, t), steps = w.je[t] - w.jb[t];
-      // blocks of keys from the last to the first; all rows see all keys in those from inner_begin to before inner_end
-      const int inner_begin = w.je[t] - max(w.all_hi[t] - w.base, 0) / kPtTile, inner_end = w.je[t] - (int)(((unsigned)(w.all_lo[t] - w.base) + kPtTile - 1) / kPtTile);
-      int lo, hi;
+      const int all_from = w.all_from[t], all_to = w.all_to[t];
+      int lo, hi, j0 = w.base + w.je[t] * kPtTile;  // the block's first key
       prompt_interval(a, w.s, i, w.n, lo, hi);
       const float slope = BIAS ? a.slopes[head] * kPromptLog2e : 0.f;
       float m = -INFINITY, l = 0.f;
@@ -865,12 +868,11 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll
           for (int c = 0; c < 128; ++c) x[c] = __uint_as_float(raw[c >> 5][c & 31]);
         }
-        const bool edge = it < inner_begin || it >= inner_end;
-        const int j0 = w.base + (w.je[t] - 1 - it) * kPtTile;
+        const bool edge = it < all_from || it >= all_to;
+        j0 -= kPtTile;
         float scale = a.scale_log2;  // from x to log2 units
         if (CAP) {  // x <- tanh(inv x) / inv
           const float inv = a.inv_cap;
-          const bool near_holds = inv >= kPtNearInv && inv <= kPtNearMost;
           float far[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int c = 0; c < 128; c += 8)
@@ -878,7 +880,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             for (int e = 0; e < 4; ++e) far[e] = pt_max3_abs(far[e], x[c + e], x[c + e + 4]);
           const float most = i < w.n ? pt_max(pt_max(far[0], far[1]), pt_max(far[2], far[3])) * inv : 0.f;  // (rows behind the end hold anything)
           const PtNear near = pt_near(inv);
-          if (__builtin_expect(near_holds && __all_sync(0xFFFFFFFFu, most <= kPtNearEnd), 1)) {
+          if (__builtin_expect(__all_sync(0xFFFFFFFFu, most <= a.near_end), 1)) {
 #pragma unroll
             for (int c = 0; c < 128; c += 16) {
               pt2 z[8];
@@ -903,7 +905,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
               for (int e = 0; e < 4; ++e) {
                 float z0, z1, y0, y1;
                 pt_mul(z[e], pt2(back, back)).get(z0, z1), y[e].get(y0, y1);
-                const bool n0 = near_holds && fabsf(x[c + 2 * e] * inv) <= kPtNearEnd, n1 = near_holds && fabsf(x[c + 2 * e + 1] * inv) <= kPtNearEnd;
+                const bool n0 = fabsf(x[c + 2 * e] * inv) <= a.near_end, n1 = fabsf(x[c + 2 * e + 1] * inv) <= a.near_end;
                 x[c + 2 * e] = n0 ? y0 : z0, x[c + 2 * e + 1] = n1 ? y1 : z1;
               }
             }
@@ -912,7 +914,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         if (BIAS) {
           const float away = (float)(j0 - i);
           const pt2 sc(scale, scale);
-          if (j0 + kPtTile - 1 <= i - row) {  // no key behind any of the tile's rows
+          if (a.prefix == nullptr || j0 + kPtTile - 1 <= i - row) {  // no row sees a key behind it
             const pt2 up(8.f * slope, 8.f * slope);
 #pragma unroll
             for (int q = 0; q < 128; q += 32) {
@@ -1043,7 +1045,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           if (ok && w.je[t] > w.jb[t]) {
-            if (queries[t] > 0) ok = pt_wait_small(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
+            if (queries[t] > 0) ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
             if (!ok) break;
             if (lane == 0) {
               const uint32_t bar = smem_u32(&qfull_s[t]);
@@ -1056,22 +1058,23 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         const int j_begin = w.jb[0] == w.je[0] ? w.jb[1] : w.jb[1] == w.je[1] ? w.jb[0] : min(w.jb[0], w.jb[1]), j_end = max(w.je[0], w.je[1]);
         const int kv = head_of(w, 0) / a.group;
         const int blocks = j_end - j_begin, ask = max(blocks + 1 - kPtAsk, 0);
+        int at_key = w.base + j_end * kPtTile;  // of the V block
         if (ok && lane == 0 && blocks == 0) mbar_arrive(smem_u32(&ask_s));
         for (int step = 0; ok && blocks > 0 && step <= blocks; ++step) {
           if (lane == 0 && step == ask) mbar_arrive(smem_u32(&ask_s));
           const uint32_t slot = used % NS;
-          if (used >= NS) ok = pt_wait_small(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
+          if (used >= NS) ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
           if (!ok) break;
           if (lane == 0) {
             const uint32_t bar = smem_u32(&full_s[slot]), at = ring + slot * 2 * T::kTileBytes;
             mbar_arrive_expect_tx(bar, (step > 0 && step < blocks ? 2u : 1u) * T::kTileBytes);
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
-              if (step > 0) tma_load_4d(at + T::kTileBytes + h * BOX, &maps.v, 64 * h, w.base + (j_end - step) * kPtTile, kv, w.s, bar);
-              if (step < blocks) tma_load_4d(at + h * BOX, &maps.k, 64 * h, w.base + (j_end - 1 - step) * kPtTile, kv, w.s, bar);
+              if (step > 0) tma_load_4d(at + T::kTileBytes + h * BOX, &maps.v, 64 * h, at_key, kv, w.s, bar);
+              if (step < blocks) tma_load_4d(at + h * BOX, &maps.k, 64 * h, at_key - kPtTile, kv, w.s, bar);
             }
           }
-          ++used;
+          ++used, at_key -= kPtTile;
         }
       }
       __syncwarp();
@@ -1097,10 +1100,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll 1
         for (int j = j_end; j >= j_begin; --j) {
           // O += P V of block j, S of block j - 1, tile by tile
-          ok = pt_wait_small(smem_u32(&full_s[slot]), lap, abort_flag, beat);
+          ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&full_s[slot]), lap, abort_flag, beat);
           if (!ok) break;
-          const int rows = w.n - w.base - j * kPtTile;
-          if (__builtin_expect(j < j_end && rows < kPtTile, 0)) {  // V rows behind the prompt's end hold anything: zeros
+          const int rows = w.last_rows;  // (of block j_end - 1; all others are full)
+          if (__builtin_expect(j + 1 == j_end && rows < kPtTile, 0)) {  // V rows behind the prompt's end hold anything: zeros
             const int chunks = (kPtTile - rows) * 8;
             for (int c = lane; c < chunks * NH; c += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + (2 * slot + 1) * T::kTileBytes + (c / chunks) * BOX + rows * 128 + (c % chunks) * 16), "r"(0) : "memory");
@@ -1113,7 +1116,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             const int t_begin = t ? w.jb[1] : w.jb[0], t_end = t ? w.je[1] : w.je[0];
             const uint32_t s_at = tmem + t * kPtTile;
             if (j >= t_begin && j < t_end) {
-              ok = pt_wait_small(smem_u32(&pfull_s[t]), (taken >> t) & 1, abort_flag, beat);
+              ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&pfull_s[t]), (taken >> t) & 1, abort_flag, beat);
               if (!ok) break;
               taken ^= 1u << t;
               tc_fence_after();
@@ -1124,7 +1127,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             }
             if (j > t_begin && j <= t_end) {
               if (j == t_end) {
-                ok = pt_wait_small(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
+                ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
                 if (!ok) break;
                 queries ^= 1u << t;
               }
@@ -1154,7 +1157,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       uint32_t asked = 0;
       bool ok = true;
       auto hand_over = [&](const PtItem& w) {
-        if (k >= 2) ok = ok && pt_wait_small(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
+        if (k >= 2) ok = ok && pt_wait_small<D, CAP, BIAS>(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
         if (!ok) return;
         if (lane == 0) {
           item_s[k & 1] = w;
@@ -1172,7 +1175,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         if (w.tok0 < w.n) {
           w.base = 0x7FFFFFFF;
           for (int t = 0; t < 2; ++t) {
-            int first = 0x7FFFFFFF, end = 0, all_lo = 0, all_hi = 0x7FFFFFFF;
+            int first = 0x7FFFFFFF, end = 0, all_lo = 0, all_hi = 0x7FFFFFFF;  // what its rows see, any and all of them
 #pragma unroll 1
             for (int r = 0; r < kPtTile / 32; ++r) {
               const int i = tok_of(w, t) + 32 * r + lane;
@@ -1182,21 +1185,24 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
               if (i < w.n) all_lo = max(all_lo, lo < hi ? lo : 0x7FFFFFFF), all_hi = min(all_hi, hi);
             }
             first = __reduce_min_sync(0xFFFFFFFFu, first), end = __reduce_max_sync(0xFFFFFFFFu, end);
-            w.all_lo[t] = __reduce_max_sync(0xFFFFFFFFu, all_lo), w.all_hi[t] = __reduce_min_sync(0xFFFFFFFFu, all_hi);
+            w.all_from[t] = __reduce_min_sync(0xFFFFFFFFu, all_hi), w.all_to[t] = __reduce_max_sync(0xFFFFFFFFu, all_lo);
             w.jb[t] = first, w.je[t] = end, w.base = min(w.base, first);
           }
+          w.last_rows = w.n - w.base - (max(w.je[0], w.je[1]) - w.base + kPtTile - 1) / kPtTile * kPtTile + kPtTile;
           for (int t = 0; t < 2; ++t) {
             const bool any = w.je[t] > 0;
             w.jb[t] = any ? (w.jb[t] - w.base) / kPtTile : 0, w.je[t] = any ? (w.je[t] - w.base + kPtTile - 1) / kPtTile : 0;
+            w.all_from[t] = w.je[t] - max(w.all_from[t] - w.base, 0) / kPtTile;
+            w.all_to[t] = w.je[t] - (int)(((unsigned)(w.all_to[t] - w.base) + kPtTile - 1) / kPtTile);
           }
           hand_over(w);
           // not before this item is nearly done: a CTA that took the next one at once would be bound to it however long this one lasts
-          ok = ok && pt_wait_small(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
+          ok = ok && pt_wait_small<D, CAP, BIAS>(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
         }
         if (!ok) break;
         if (lane == 0) pt_ask_work(answer, smem_u32(&work_s));
         ++asked;
-        if (!pt_wait_small(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
+        if (!pt_wait_small<D, CAP, BIAS>(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
         const bool more = pt_read_work(answer, cta);
         __syncwarp();  // every lane has read the answer before the next one may be written
         if (!more) {
