@@ -29,19 +29,28 @@ DEBUG_LIB_PATH = os.path.join(_PKG, "libhashevict_debug.so")
 _OBJ_DIR = os.path.join(_PKG, "build")
 
 
+def _fresh(obj: str, deps: str, source: str) -> bool:
+    """Whether an object was made from this source file (not from that of a tree that it was copied with) and nothing that it read is newer."""
+    if not (os.path.exists(obj) and os.path.exists(deps)):
+        return False
+    with open(deps) as f:
+        read = f.read().replace("\\\n", " ").partition(":")[2].split()
+    return os.path.abspath(source) in map(os.path.abspath, read) and \
+        all(os.path.exists(p) and os.path.getmtime(p) <= os.path.getmtime(obj) for p in read + [os.path.abspath(__file__)])
+
+
 def _object(source: str, debug: bool, force: bool, verbose: bool) -> str:
     """One translation unit; compiled again when it or a header that it read the last time is newer than its object."""
     obj = os.path.join(_OBJ_DIR, os.path.basename(source)[:-3] + ("_debug.o" if debug else ".o"))
     deps = obj[:-2] + ".d"
-    if not force and os.path.exists(obj) and os.path.exists(deps):
-        read = open(deps).read().replace("\\\n", " ").split(":", 1)[1].split()
-        if all(os.path.exists(p) and os.path.getmtime(p) <= os.path.getmtime(obj) for p in read + [os.path.abspath(__file__)]):
-            return obj
+    if not force and _fresh(obj, deps, source):
+        return obj
     os.makedirs(_OBJ_DIR, exist_ok=True)
-    tmp, began = obj + f".tmp{os.getpid()}", time.time()
+    tmp, began = f"{obj}.tmp{os.getpid()}", time.time()
     subprocess.run([nvcc_path()] + NVCC_FLAGS + (["-DHE_BOUNDS_CHECK"] if debug else []) + (["-Xptxas", "-v"] if verbose else []) +
-                   ["-I", os.path.join(_ROOT, "include"), "-MD", "-MF", deps, "-MT", "object", "-c", "-o", tmp, source], check=True)
+                   ["-I", os.path.join(_ROOT, "include"), "-MD", "-MF", tmp + ".d", "-MT", "object", "-c", "-o", tmp, source], check=True)
     os.utime(tmp, (began, began))  # a source edited meanwhile is newer
+    os.replace(tmp + ".d", deps)   # (both whole at any time: another process may be building too)
     os.replace(tmp, obj)
     return obj
 
