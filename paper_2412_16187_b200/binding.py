@@ -208,7 +208,7 @@ class Rotary:
     `frequencies` (radians per position, channels/2 of them) and `amplitude` replace base and scaling altogether."""
 
     def __init__(self, head_dim, channels=None, base=10000.0, interleaved=False, scaling=None, frequencies=None, amplitude=1.0):
-        self.head_dim, self.channels, self.interleaved = int(head_dim), int(head_dim if channels is None else channels), bool(interleaved)
+        self.head_dim, self.channels, self.interleaved = int(head_dim), _int32("channels", head_dim if channels is None else channels), bool(interleaved)
         if self.channels > self.head_dim:
             raise HashEvictError(f"rotary channels {self.channels} > head_dim {self.head_dim}")
         self.raw = he_rotary()
@@ -235,6 +235,21 @@ class Rotary:
                                     float(s.get("high", 4.0 if kind == "bands" else 32.0))))
 
 
+def _fp32(name, x):
+    """x as the library takes it: what is not zero may not become it."""
+    x = float(x)
+    if x != 0.0 and ctypes.c_float(x).value == 0.0:
+        raise HashEvictError(f"{name} {x!r} is nothing in fp32")
+    return x
+
+
+def _int32(name, x):
+    """x as the library takes it (ctypes would drop the upper bits)."""
+    if not -2 ** 31 <= int(x) < 2 ** 31 or int(x) != x:
+        raise HashEvictError(f"{name} {x!r} is not an int32")
+    return int(x)
+
+
 class ScoreMod:
     """he_score_mod: what scores go through before the softmax. scale (0: 1/sqrt(d)), softcap c (x -> c tanh(x / c), 0: none), window w
     (the newest w positions are seen, 0: all), slopes (device fp32 [H*G]: x - slope * distance). slopes is kept alive here."""
@@ -243,7 +258,7 @@ class ScoreMod:
         if slopes is not None and not (slopes.is_cuda and slopes.dtype == torch.float32 and slopes.is_contiguous()):
             raise HashEvictError("slopes must be a contiguous fp32 tensor on the device")
         self.slopes = slopes
-        self.raw = he_score_mod(float(scale), float(softcap), int(window), 0, _ptr(slopes))
+        self.raw = he_score_mod(_fp32("scale", scale), _fp32("softcap", softcap), _int32("window", window), 0, _ptr(slopes))
         self.pointer = ctypes.pointer(self.raw)
 
 

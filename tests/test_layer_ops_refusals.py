@@ -1,7 +1,9 @@
 """Calls around the cache that the library and its binding turn down before anything is launched."""
 import ctypes
 
-from paper_2412_16187_b200 import HE_FLAG_EARLY_INPUTS, Rotary, binding
+import pytest
+
+from paper_2412_16187_b200 import HE_FLAG_EARLY_INPUTS, HashEvictError, Rotary, ScoreMod, binding
 
 FAKE, FAR = 0x10000, 0x40000000  # never followed: every check below comes before the launch
 
@@ -29,3 +31,18 @@ def test_a_cap_whose_ratio_to_the_scale_is_no_normal_number_is_refused():
         assert b"leaves fp32" in L.he_last_error()
         assert L.he_attend_scored(ctypes.byref(cfg), ctypes.byref(cache), ctypes.byref(bad), FAKE, None, FAR, None) == 1
         assert b"leaves fp32" in L.he_last_error()
+
+
+@pytest.mark.parametrize("kw, name", [(dict(window=2 ** 32 + 5), "window"), (dict(window=-(2 ** 32)), "window"), (dict(window=2 ** 31), "window"),
+                                      (dict(window=2.5), "window"), (dict(softcap=1e-50), "softcap"), (dict(scale=1e-46), "scale"), (dict(scale=-1e-60), "scale")])
+def test_numbers_that_the_library_has_no_type_for(kw, name):
+    """None of them may turn into another number, or into none, on the way."""
+    with pytest.raises(HashEvictError, match=name):
+        ScoreMod(**kw)
+    with pytest.raises(HashEvictError, match="channels"):
+        Rotary(2 ** 33, 2 ** 32 + 64)
+
+
+def test_numbers_at_the_ends_of_their_types_are_taken():
+    raw = ScoreMod(window=2 ** 31 - 1, softcap=1e-40, scale=1e38).raw
+    assert raw.window == 2 ** 31 - 1 and raw.cap > 0.0 and ScoreMod(window=16.0, scale=0, softcap=0).raw.window == 16
