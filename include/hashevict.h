@@ -216,8 +216,9 @@ int he_rotary_init_frequencies(he_rotary* out, int32_t channels, int32_t interle
  * like those of he_prefill_compress, into q_out and k_out of the same shapes with strides of their own. Row n of sequence s
  * is rotated by positions[s * max_prompt_len + n] (device int32 [B, max_prompt_len], any value), or by n where positions is NULL.
  * Rows n >= prompt_len[s] are neither read nor written (prompt_len NULL: every row is taken). An output may be its input
- * (same address, same strides), not overlap it otherwise, and its rows do not overlap each other: sorted by stride, each axis steps over
- * all that the ones before it cover. q and q_out may both be NULL, and so may k and k_out.
+ * (same address, same strides), not overlap it otherwise, nor the other input or output; its rows do not overlap each other: sorted by
+ * stride, each axis steps over all that the ones before it cover. (Refused where addresses or strides show it; parts of one buffer that
+ * lie between each other are taken, and not looked at further.) q and q_out may both be NULL, and so may k and k_out.
  */
 int he_rotate_prompt(const he_config* cfg, const he_rotary* rotary, const void* q, const void* k, const int64_t q_strides[3],
                      const int64_t k_strides[3], const int32_t* positions, const int32_t* prompt_len, int32_t max_prompt_len, void* q_out,

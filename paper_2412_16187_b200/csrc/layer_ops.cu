@@ -117,6 +117,8 @@ int rotate_sides(RotateArgs& a, const he_config* cfg, const void* q, const void*
       for (int i = 0; i < n; ++i)
         if (a.in[w][i] != a.out[w][i]) return fail(HE_ERR_INVALID_ARG, "%s is rotated in place with other strides", what);
   }
+  if (a.heads[0] > 0 && a.heads[1] > 0 && (q_out == k_out || q_out == k || k_out == q))
+    return fail(HE_ERR_INVALID_ARG, "q_out and k_out overlap each other or the other's input");
   return HE_OK;
 }
 
@@ -374,6 +376,7 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
   if (int rc = check_strides("out", out_strides, 3, es)) return rc;
   const long long sizes[3] = {cfg->batch, (long long)cfg->n_kv_heads * cfg->group_size, max_prompt_len};
   if (int rc = check_apart("out", out_strides, sizes, 3, cfg->head_dim)) return rc;
+  if (out == q || out == k || out == v) return fail(HE_ERR_INVALID_ARG, "out overlaps q, k or v");
   a.q = q, a.k = k, a.v = v, a.out = out;
   for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i], a.ks[i] = kv_strides[i], a.os[i] = out_strides[i];
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_prompt_len;

@@ -46,3 +46,15 @@ def test_numbers_that_the_library_has_no_type_for(kw, name):
 def test_numbers_at_the_ends_of_their_types_are_taken():
     raw = ScoreMod(window=2 ** 31 - 1, softcap=1e-40, scale=1e38).raw
     assert raw.window == 2 ** 31 - 1 and raw.cap > 0.0 and ScoreMod(window=16.0, scale=0, softcap=0).raw.window == 16
+
+
+def test_outputs_that_are_other_arguments_are_refused():
+    L, cache = binding.lib(), binding.he_cache(*([FAKE] * 9), None, None)
+    cfg, rot, two, three = config(), Rotary(64), ctypes.c_int64 * 2, ctypes.c_int64 * 3
+    q3, k3, q2, k2 = three(8 * 64 * 16, 64 * 16, 64), three(2 * 64 * 16, 64 * 16, 64), two(8 * 64, 64), two(2 * 64, 64)
+    a, b, c, d = FAKE, FAR, 2 * FAR, 3 * FAR
+    for q, k, qo, ko in ((a, b, c, c), (a, b, b, c), (a, b, c, a), (a, b, b, a)):
+        assert L.he_rotate_prompt(ctypes.byref(cfg), rot.pointer, q, k, q3, k3, None, None, 16, qo, ko, q3, k3, None) == 1 and b"overlap" in L.he_last_error()
+        assert L.he_rotate_step(ctypes.byref(cfg), rot.pointer, ctypes.byref(cache), q, k, q2, k2, qo, ko, q2, k2, None) == 1 and b"overlap" in L.he_last_error()
+    for out in (a, b, c):
+        assert L.he_attend_prompt(ctypes.byref(cfg), None, a, b, c, q3, k3, d, 16, None, None, out, q3, None) == 1 and b"out overlaps" in L.he_last_error()
