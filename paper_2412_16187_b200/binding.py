@@ -164,6 +164,17 @@ def _current_device() -> int:
         return torch.cuda.current_device()
 
 
+def _empty(shape, dtype, device, stream=None):
+    """An output that a call makes for itself, of the stream that writes it: memory of the current stream may still be read by what is
+    pending there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):  # anything with a handle is taken for a stream
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -178,7 +189,7 @@ def hash_keys(x: torch.Tensor, W: torch.Tensor, hash_bits: int | None = None, st
     assert x.is_cuda and W.is_cuda and x.dim() == 2 and x.stride(1) == 1 and W.dtype == torch.float32 and W.is_contiguous()
     b = W.shape[1] if hash_bits is None else hash_bits
     cfg = he_config(1, 1, 1, x.shape[1], b, 4, 0, 0, _DTYPES[x.dtype], 0)
-    out = torch.empty((x.shape[0], (b + 31) // 32), dtype=torch.int32, device=x.device)
+    out = _empty((x.shape[0], (b + 31) // 32), torch.int32, x.device, stream)
     _check(lib().he_hash_keys(ctypes.byref(cfg), _ptr(x), x.shape[0], x.stride(0), _ptr(W), _ptr(out), _stream(stream)))
     return out
 
@@ -324,7 +335,7 @@ class HashEvictCache:
     def decode_step(self, q, k, v, victim_out=None, evicted_pos_out=None, qcodes_out=None, stream=None):
         """he_decode_step. q [B, H*G, d], k / v [B, H, d], contiguous. Returns victim_out [B, H] (int32)."""
         if victim_out is None:
-            victim_out = torch.empty((self.B, self.H), dtype=torch.int32, device=self.k_cache.device)
+            victim_out = _empty((self.B, self.H), torch.int32, self.k_cache.device, stream)
         _check(lib().he_decode_step(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(k), _ptr(v),
                                     _ptr(victim_out), _ptr(evicted_pos_out), _ptr(qcodes_out), _stream(stream)))
         return victim_out
@@ -332,7 +343,7 @@ class HashEvictCache:
     def attend(self, q, out=None, stream=None):
         """he_attend: softmax(q K^T / sqrt(d)) V over the valid slots (Eq. 1). q [B, H*G, d] -> fp32 [B, H*G, d]."""
         if out is None:
-            out = torch.empty((self.B, self.H * self.G, self.d), dtype=torch.float32, device=self.k_cache.device)
+            out = _empty((self.B, self.H * self.G, self.d), torch.float32, self.k_cache.device, stream)
         _check(lib().he_attend(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(out), _stream(stream)))
         return out
 
@@ -380,23 +391,23 @@ class HashEvictCache:
             found += (None, None) if x is None else (self._rows(name, x, shape, self.dtype), self._rows(name + "_out", out, shape, self.dtype))
         return found
 
-    def _outputs(self, q, k, q_out, k_out):
+    def _outputs(self, q, k, q_out, k_out, stream):
         """Outputs of a rotation, made where they are missing."""
         if q is None and k is None:
             raise HashEvictError("neither q nor k is given")
         if q is None and q_out is not None or k is None and k_out is not None:
             raise HashEvictError("an output without its input")
         if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _empty(q.shape, q.dtype, q.device, stream)
         if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            k_out = _empty(k.shape, k.dtype, k.device, stream)
         return q_out, k_out
 
     def rotate_prompt(self, rotary, q, k, prompt_len=None, positions=None, q_out=None, k_out=None, stream=None):
         """he_rotate_prompt. q [B, H*G, N, d], k [B, H, N, d] (any strides on the first three axes; either may be None), positions
         int32 [B, N] (None: 0, 1, ...), prompt_len int32 [B] (None: every row). Returns (q_out, k_out); q_out = q works in place.
         Rows behind a prompt's end are left as they were."""
-        q_out, k_out = self._outputs(q, k, q_out, k_out)
+        q_out, k_out = self._outputs(q, k, q_out, k_out, stream)
         n = (k if q is None else q).shape[-2]
         qs, qos, ks, kos = self._known(("rotate", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
                                        lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, (n,)))
@@ -411,7 +422,7 @@ class HashEvictCache:
     def rotate_step(self, rotary, q, k, q_out=None, k_out=None, stream=None):
         """he_rotate_step: q [B, H*G, d] and k [B, H, d] of the next decode_step, rotated by the cache's next_pos. Returns (q_out, k_out).
         Refused by a cache with early_inputs, whose decode_step would read the rows before they are written."""
-        q_out, k_out = self._outputs(q, k, q_out, k_out)
+        q_out, k_out = self._outputs(q, k, q_out, k_out, stream)
         qs, qos, ks, kos = self._known(("step", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
                                        lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, ()))
         self._call(lib().he_rotate_step, stream, self._cfg_p, rotary.pointer, self._ca_p, _ptr(q), _ptr(k), qs, ks, _ptr(q_out), _ptr(k_out), qos, kos)
@@ -443,7 +454,7 @@ class HashEvictCache:
         prefix_len int32 [B] (tokens that all of a prompt's tokens see). Returns out [B, H*G, N, d] in the dtype of q; rows behind a
         prompt's end are left as they were (undefined in an `out` that this call makes)."""
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = _empty(q.shape, q.dtype, q.device, stream)
         qs, ks, os_ = self._known(("prompt", _layout(q), _layout(k), _layout(v), _layout(out), _layout(prompt_len), _layout(doc_start), _layout(prefix_len)),
                                   lambda: self._prompt(q, k, v, out, prompt_len, doc_start, prefix_len))
         self._call(lib().he_attend_prompt, stream, self._cfg_p, self._mod(mod), _ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(prompt_len), q.shape[-2],
@@ -461,7 +472,7 @@ class HashEvictCache:
         """he_attend_scored: attend with a ScoreMod. q [B, H*G, d] -> fp32 [B, H*G, d]; the query is the token that the last decode_step
         inserted, first_pos int32 [B] the first position that it sees (the start of its document)."""
         if out is None:
-            out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+            out = _empty(q.shape, torch.float32, q.device, stream)
         self._known(("scored", _layout(q), _layout(out), _layout(first_pos)), lambda: self._scored(q, first_pos, out))
         self._call(lib().he_attend_scored, stream, self._cfg_p, self._ca_p, self._mod(mod), _ptr(q), _ptr(first_pos), _ptr(out))
         return out
@@ -510,7 +521,7 @@ class HashEvictCache:
     def decode_step_l2(self, k, v, victim_out=None, evicted_pos_out=None, stream=None):
         """he_decode_step_l2: one step of the L2-norm comparison policy. k / v [B, H, d]. Returns victim_out [B, H]."""
         if victim_out is None:
-            victim_out = torch.empty((self.B, self.H), dtype=torch.int32, device=self.k_cache.device)
+            victim_out = _empty((self.B, self.H), torch.int32, self.k_cache.device, stream)
         _check(lib().he_decode_step_l2(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(k), _ptr(v), _ptr(victim_out),
                                        _ptr(evicted_pos_out), _stream(stream)))
         return victim_out
@@ -518,7 +529,7 @@ class HashEvictCache:
     def attention_loss(self, q, k_full, out=None, stream=None):
         """he_attention_loss: attention mass of the tokens that are no longer cached. q [B, H*G, d], k_full [B, H, n, d] -> fp32 [B, H*G]."""
         if out is None:
-            out = torch.empty((self.B, self.H * self.G), dtype=torch.float32, device=self.k_cache.device)
+            out = _empty((self.B, self.H * self.G), torch.float32, self.k_cache.device, stream)
         assert k_full.stride(3) == 1
         i64x3 = ctypes.c_int64 * 3
         _check(lib().he_attention_loss(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(k_full), i64x3(*k_full.stride()[:3]),
