@@ -212,7 +212,8 @@ struct AttendRing {
 // 6e-7. Groups of up to 4 heads (FOLD) hold the third terms in the rows that they leave empty (rows 4..7 repeat the heads of rows 0..3), larger
 // ones take products of their own.
 // Measured, d = 128 and G = 4: 512 units of 512 to 4096 slots 85.6 us without modification (6.6 TB/s), 86.2 with a cap, a window or slopes: bound by
-// HBM (94.5 and 97 with the units in their own order; he_attend 91). 8 units of 9830 slots 11.0 us (he_attend 10.1), 11.9 with a cap: bound by what the 16 CTAs of a cluster pull. Groups of 8 without room
+// HBM (94.5 and 97 with the units in their own order; he_attend 91). 8 units of 9830 slots 11.0 us (he_attend 10.1), 11.9 with a cap: HBM needs 6.3, and a call with clusters pays 4 us
+// whatever it reads. Rows that a mask hides are copied like the others (with a window of 1024 over 9830 slots a call from Python takes 12.7 us, without 12.0). Groups of 8 without room
 // for the third terms: 128 units of 2048 slots at d = 64 13.6 us (he_attend 10.8), bound by the issue of MMAs and their operands.
 template <int D, int NW, bool MOD, bool CAP = false, bool FOLD = false, bool BELOW = false>
 __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const AttendArgsOf<MOD> a, const int S, const __grid_constant__ CUtensorMap kmap,
@@ -534,8 +535,9 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
 // 64 slots at a time in shared memory as fp32, K rows padded so that lanes that read neighbouring rows meet every bank once. Scores: a warp
 // works for one query head (8 / GP warps share a head's slots, GP the group rounded up to a power of two), a lane for one or more slots.
 // Output: warp w adds up slots 8 w .. 8 w + 7 of the tile for all heads, a lane for four channels of every 128. A cluster of S CTAs shares a
-// unit as in attend_bf16_kernel. Bound by HBM where the grid fills the SMs (three CTAs of 70 KB each at d = 128), else by what an SM pulls.
-// Measured, fp32 at d = 128: 8 units of 4096 slots 28 us (188 us with one CTA a unit), 128 units of 1024 slots 45 us, 3.0 TB/s (55 us with one CTA a unit);
+// unit as in attend_bf16_kernel. Bound by the bytes in flight: a tile of 64 KB a CTA at most, with the scores and the output of the tile before in between.
+// Measured, fp32 at d = 128: 8 units of 4096 slots 29 us (188 us with one CTA a unit; HBM needs 5.2), 128 units of 1024 slots 47 us, 2.9 TB/s (55 us with one
+// CTA a unit; HBM needs 21); bf16 at d = 256, whose rows go through registers: 52 and 105 us;
 // 4 units of 64 slots at d = 64 4.3 us, the latency of a launch and of two dependent reads.
 // Hidden slots are not read at all: their rows are zeros. fp32 rows are copied asynchronously, with `stages` = 2 a tile ahead (calls that leave an SM
 // to one CTA); which slots of a tile are hidden is found out one tile earlier still, so that no copy waits for a position (28 us, 31 with one stage).

@@ -255,11 +255,13 @@ static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s
 // 16 R rows of one query head per CTA, 64 keys at a time. Thread (ty, tx) of 16 x 16 holds the scores of rows R ty .. + R - 1 and keys
 // tx, tx + 16, tx + 32, tx + 48, and of the output the same rows and channels 4 tx .. + 3 of every 64. Q and K lie in shared memory row by row, four
 // floats longer than the row, so that the 16 threads that read neighbouring keys meet every bank once; the weights go through shared memory key by key, in the place of K.
-// Bound by the FMA pipe and the loads that feed it (R = 4: 8 loads of 16 bytes for 64 products). 4 x 32 heads of 2048 tokens at d = 128 take
-// 4.4 ms: 31 TFLOP/s, of about 70 that the FMA pipe has. With one CTA an SM instead of two it is
-// 6.0 ms there, and 32 heads of 2048 tokens at d = 64 take 1.03 ms beside 0.75.
-// R = 1 for calls that would leave SMs idle: 5 x 311 tokens of one head at d = 128 take 38 us beside 76 with R = 4 (44 without a tile ahead);
-// 32 heads of 1024 tokens, which fill the SMs, 313 us with R = 4 beside 772.
+// What bounds it: issue slots (69 % used), which the products share with the loads that feed them (R = 4: 8 of 16 bytes for 64 products; shared memory is 61 %
+// busy) and with the softmax; the FMA pipe is 50 % busy, waiting for copies or at barriers 5 % of the stalls. 4 x 32 heads of 2048 tokens at d = 128 take
+// 4.5 ms: 31 TFLOP/s, of about 70 that the FMA pipe has. With one CTA an SM instead of two it was
+// 6.0 ms there, and 32 heads of 2048 tokens at d = 64 took 1.03 ms beside 0.70. bf16 heads of 136 to 256, which come here too: 23 TFLOP/s (16 heads of 2048
+// tokens at d = 256 1.5 ms).
+// R = 1 for calls that would leave SMs idle: 5 x 311 tokens of one head at d = 128 take 35 us beside 76 with R = 4 (44 without a tile ahead);
+// 32 heads of 1024 tokens, which fill the SMs, 319 us with R = 4 beside 772.
 constexpr int kPromptThreads = 256;
 template <int R>
 constexpr int kPromptPitch = 16 * R + 4;  // of the weights
@@ -471,7 +473,8 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
 // The items come with the prompts' last tokens first, as those see the most keys. The roles run on from item to item: the next one's Q, K
 // and first S are under way while the rows of this one are written.
 //
-// Registers: 384 threads are launched with 168 each, 64,512 in all; warps 0-7 take 224, warps 8-11 keep 56: 256 * 224 + 128 * 56 = 64,512.
+// Registers: 384 threads are launched with 168 each, 64,512 in all; warps 0-7 take 224, warps 8-11 keep 56: 256 * 224 + 128 * 56 = 64,512. The compiler
+// allocates for 168 and spills in every instance (12 to 56 bytes of stores a thread without a cap, 100 to 156 with one).
 // Channels from d up to D are filled with zeros by the tensor maps.
 constexpr int kPtThreads = 384, kPtTile = 128, kPtMmaWarp = 8, kPtLoadWarp = 9, kPtWorkWarp = 10;
 constexpr int kPtSoftRegs = 224, kPtOtherRegs = 56;
@@ -771,16 +774,17 @@ __device__ __forceinline__ bool pt_read_work(uint32_t answer, int& cta) {
 
 // EMU of a row's 64 pairs of weights are computed on the FMA pipe: the special-function pipe (16 a cycle and SM) takes 2048 cycles for a block's
 // 2 x 128 x 128 weights, as long as the block's products at D = 128 and twice as long at D = 64. With hardly any there (EMU = 1), 16 heads of 8192 tokens
-// take 324 us instead of 316 with a cap, 128 heads of 512 tokens 33 instead of 31; with cap and slopes together the FMA pipe is the
+// took 324 us instead of 316 with a cap, 128 heads of 512 tokens 33 instead of 31; with cap and slopes together the FMA pipe is the
 // busier one (d = 64: 322 us with EMU = 2, 347 with 8).
 //
-// What bounds it (16 heads of 8192 tokens, d = 128: 232 us = 1.19 PFLOP/s plain, 316 with a cap, 264 with slopes, 358 with both; d = 64: 200, 300, 232): a
-// tile's way around, some 3500 cycles for a block. Its softmax takes about 2000 of them, as one thread walks over a row of 128 in the registers it
+// What bounds it (16 heads of 8192 tokens, d = 128: 231 us = 1.19 PFLOP/s plain, 311 with a cap, 267 with slopes, 358 with both; d = 64: 190, 285, 220, 321; with
+// scores beyond 0.7 of the cap, whose blocks go through both forms of the tanh, 688 and 645): a tile's way around, some 3500 cycles for a block. Its softmax takes about 2000 of them, as one thread walks over a row of 128 in the registers it
 // has; then the products P V and the next S take 1024 of their own and 400 of hand-overs, while the other tile's softmax runs. The
 // issue slots are 36 to 40 % used, the special-function pipe 40 %, the tensor pipe 50 %. An item adds about 9000 cycles (first S, last product, output).
-// Short prompts have few blocks an item and are bound by that (32 heads of 1024 tokens: 30 us).
+// Short prompts have few blocks an item and are bound by that (32 heads of 1024 tokens: 24 us).
+// At D = 64 a quarter of tensor memory (columns 384 to 511) is not used: P lies where S was, and the next S of a tile waits for it.
 // Tried and slower: blocks of 64 keys with two places for S (0.90 PFLOP/s), one warp that polls both tiles for whichever is ready (0.81), weights handed over
-// in two or four parts, 208 / 80 registers (spills in the softmax).
+// in two or four parts, 208 / 80 registers (more spills in the softmax).
 template <int D, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_constant__ PromptArgs a, const int tiles, const int by_heads,
                                                                    const __grid_constant__ PromptMaps maps) {
