@@ -56,8 +56,8 @@ static __global__ void __launch_bounds__(kAttendThreads) attend_generic_kernel(c
         }
         for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, off);
         const float sc = dot * scale;
-        const float mn = fmaxf(m[g], sc);
-        const float corr = exp2f(m[g] - mn), p = exp2f(sc - mn);  // exp2f(-inf) = 0 on the first slot
+        const float mn = fmaxf(m[g], sc), ref = mn == -INFINITY ? 0.f : mn;    // (scores of -inf alone so far: no weight)
+        const float corr = exp2f(m[g] - ref), p = exp2f(sc - ref);  // exp2f(-inf) = 0 on the first slot
         l[g] = l[g] * corr + p;
 #pragma unroll
         for (int i = 0; i < kMaxDim / 32; ++i) o[g][i] = o[g][i] * corr + p * vv[i];

@@ -390,9 +390,9 @@ __global__ void __launch_bounds__(32 * NW, 8 / NW) attend_bf16_kernel(const Atte
       if (t + 2 < items) fetch_pos(g0 + stride);
     }
     gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 1));
-    gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 2));  // without MOD finite: slot g0 is valid
+    gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 2));
     const float mx = fmaxf(m, gm);
-    const float mn = MOD && mx == -INFINITY ? 0.f : mx;  // (nothing seen so far: all weights are exp2(-inf))
+    const float mn = mx == -INFINITY ? 0.f : mx;  // (nothing seen so far, or scores of -inf alone: all weights are exp2(-inf))
     const float corr = exp2f(m - mn);
     float p[8], ps = 0.f;
 #pragma unroll

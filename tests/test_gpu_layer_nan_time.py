@@ -80,7 +80,7 @@ def test_what_is_not_finite_costs_little(dtype, d, n, what):
     else:
         assert torch.equal(torch.isnan(out[0, :g]), bad.expand(g, n, d))
     # (a window lets one tile of rows a head out of sight of the NaN: those rows are computed anew)
-    assert took <= (200 if what == "late value" else 10) * usual, (took, usual)
+    assert took <= (400 if what == "late value" else 10) * usual, (took, usual)
 
 
 @pytest.mark.parametrize("dtype, d, n", [(BF16, 128, 700), (BF16, 64, 500), (BF16, 136, 400), (F32, 64, 300)])

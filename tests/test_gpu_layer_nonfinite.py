@@ -61,3 +61,28 @@ def test_a_visible_key_that_is_not_finite_reaches_its_unit(shape, slots, bad, ca
     others = torch.ones(got.shape[:2], dtype=torch.bool, device="cuda")
     others[0, u * g:] = False
     assert torch.equal(got[others], clean[others]) and bool(torch.isfinite(clean).all())
+
+
+@pytest.mark.parametrize("shape, slots", CACHES, ids=NAMES)
+@pytest.mark.parametrize("call", ["scored", "attend"])
+def test_scores_of_minus_infinity_have_no_weight(shape, slots, call):
+    """The first 33 slots (fewer than all) of a unit: whoever walks over them first sees nothing else for a while."""
+    cache, q = filled(shape, slots)
+    g, u, first = shape[2], shape[1] - 1, min(33, slots - 3)
+    q[0, u * g:, 3] = 1.0
+    run = cache.attend if call == "attend" else cache.attend_scored
+    cache.k_cache[0, u, :first, 3] = -math.inf
+    got = run(q)[0, u * g:].double()
+    k, v = cache.k_cache[0, u, first:slots].double(), cache.v_cache[0, u, first:slots].double()
+    want = torch.softmax(q[0, u * g:].double() @ k.T / math.sqrt(shape[3]), -1) @ v
+    # scores, weights and sums in fp32: a few 1e-6 of the largest |V|
+    assert bool(((got - want).abs() <= 2e-5 * float(cache.v_cache[0, u, :slots].double().abs().max())).all())
+
+
+def test_a_unit_whose_scores_are_all_minus_infinity_gives_zeros():
+    for shape, slots in CACHES:
+        cache, q = filled(shape, slots)
+        g, u = shape[2], shape[1] - 1
+        q[0, u * g:, 3] = 1.0
+        cache.k_cache[0, u, :slots, 3] = -math.inf
+        assert not cache.attend(q)[0, u * g:].any() and not cache.attend_scored(q)[0, u * g:].any()
