@@ -1008,7 +1008,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       if (ok && steps > 0) ok = pt_wait(smem_u32(&odone_s[t]), outputs++ & 1, abort_flag, beat);
       if (!ok) break;
       tc_fence_after();
-      const float inv = l != 0.f ? 1.f / l : 0.f;
+      const float inv = m != -INFINITY ? 1.f / l : 0.f;  // (scores of -inf alone: pt_ex2_fma leaves 2^-125 of their weights)
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (w.s * a.os[0] + head * a.os[1] + i * a.os[2]);
       const bool none = inv == 0.f;  // (a row that sees nothing: zeros)
       float nan[2] = {0.f, 0.f};     // NaN once an output is

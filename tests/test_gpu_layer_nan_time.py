@@ -139,3 +139,22 @@ def test_padding_ahead_of_a_prompt_may_hold_anything(dtype, d, n, mask, group):
     took = least_time(call)
     assert torch.equal(out, clean)
     assert took <= 10 * usual, (took, usual)
+
+
+@pytest.mark.parametrize("dtype, d, n", SHAPES)
+@pytest.mark.parametrize("mod", [None, ScoreMod(window=200)])
+def test_prompt_scores_of_minus_infinity_have_no_weight(dtype, d, n, mod):
+    """Keys of the first half at -inf: rows that see them alone give zeros, the others what they would give without them."""
+    cache, q, k, v, plen = prompt(dtype, d, n)
+    g, half = q.shape[1] // k.shape[1], n // 2 + 3
+    q[0, :g, :, 3] = 1.0
+    out = cache.attend_prompt(q, k, v, plen, mod=mod)
+    doc = torch.full((1, n), half, dtype=torch.int32, device="cuda")
+    want = cache.attend_prompt(q, k, v, plen, mod=mod, doc_start=doc)
+    k[0, 0, :half, 3] = -math.inf
+    got = cache.attend_prompt(q, k, v, plen, mod=mod)
+    assert torch.equal(got[0, g:], out[0, g:])
+    assert not got[0, :g, :half].any()
+    # both within the tolerance of exact arithmetic: weights and outputs rounded to bf16 where they are
+    limit = (2 * 2e-5 + (2.0 ** -7 if dtype == BF16 and d <= 128 else 0.0) + (2.0 ** -7 if dtype == BF16 else 0.0)) * float(v[0, 0].abs().max())
+    assert float((got[0, :g, half:].double() - want[0, :g, half:].double()).abs().max()) <= limit
