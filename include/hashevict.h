@@ -265,7 +265,7 @@ typedef struct he_score_mod {
  * weight so moves by as much, relatively: 0.3 % where a cap of 1000 leaves scores of 500). All else runs in fp32 on the CUDA cores.
  * Speed: the tensor cores read q, k and v by tensor maps, which take no stride of zero on an axis of more than one entry. KV heads or sequences
  * that are one tensor seen several times run on the CUDA cores, 33 times as long (32 heads of 4096 tokens 4.4 ms instead of 0.13):
- * copy them. So do head_dim 136 to 256 and fp32.
+ * copy them. head_dim 136 to 256 and fp32 run there too.
  */
 int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
                      const int64_t kv_strides[3], const int32_t* prompt_len, int32_t max_prompt_len, const int32_t* doc_start,
@@ -277,7 +277,7 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
  * pos[j] < first_pos[s] (device int32 [B], or NULL; the start of the token's document) are hidden, and so are those that the window
  * leaves behind. mod NULL: as he_attend. Layouts are those of he_attend. Results agree with exact arithmetic to about 1e-6 of the largest |V|
  * entry where scores are small; a score is the result of fp32 arithmetic, and what that leaves of it (some 2^-22 of scale * sum |q_c k_c|, of the cap and of
- * the bias) moves its weight, relatively, by as much. Rows of hidden slots may hold anything, and are read all the same.
+ * the bias) moves its weight, relatively, by as much. Rows of hidden slots may hold anything (bf16 ones are read all the same).
  */
 int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out,
                      void* stream);
