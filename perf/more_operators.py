@@ -240,7 +240,7 @@ def run(st):
 def _power(top):
     """The least power of two s >= 2^-100 with top <= 448 s; 2^-100 where there is nothing."""
     part, e = torch.frexp(top)  # top = part 2^e, part in [1/2, 1); 448 = 0.875 2^9
-    return torch.ldexp(torch.ones_like(top), torch.where(part > 0.875, e - 8, e - 9).clamp(min=-100))
+    return torch.ldexp(torch.ones_like(top), torch.where(top > 0, torch.where(part > 0.875, e - 8, e - 9).clamp(min=-100), -100))
 
 
 def _rotated(st, x, pos):
