@@ -282,6 +282,86 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
 int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out,
                      void* stream);
 
+/*
+ * he_attend_cross - he_attend_prompt for rows over keys of another length: q, out [B, Hkv*G, Nq, d] with q_len [B] rows (each <= max_q_len), k, v [B, Hkv, Nk, d] with
+ * kv_len [B] keys (each <= max_kv_len); all lengths are device int32, larger ones count as the maximum, negative ones as 0.
+ *   q_pos given (device int32 [B]): the rows are tokens of the keys' sequence, row i the one at position q_pos[s] + i, key j the one at position j. Row i sees what a
+ *     token of he_attend_prompt sees there: max(first_key[s * max_q_len + i], q_pos[s] + i - w + 1, 0) <= j < min(kv_len[s], max(q_pos[s] + i + 1, prefix_len[s])).
+ *     So a prompt may come in chunks: the rows of a chunk (q_pos = tokens before it) over all keys up to its end (kv_len = q_pos + q_len).
+ *     A q_pos outside [-2^24, 2^24] counts as the nearer end.
+ *   q_pos NULL: every row sees every key from first_key on, as a decoder's rows see an encoder's states; a window, slopes or a prefix is refused.
+ * first_key (device int32 [B, max_q_len]), prefix_len and mod may be NULL. Rows i >= q_len of out are left as they were; a row that sees no key gives zeros. All else
+ * (layouts, strides, accuracy, what runs where) as for he_attend_prompt.
+ * workspace (16-byte aligned; he_attend_cross_workspace_bytes(cfg, max_q_len, max_kv_len) bytes, 0 where none is of use) lets few rows over many keys fill the GPU: the
+ * keys are then shared out and the shares' results joined in a fixed order. It holds nothing from one call to the next; calls that may run at the same time need one
+ * each. NULL: a tile of rows walks over all its keys.
+ */
+size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, int32_t max_kv_len);
+int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
+                    const int64_t kv_strides[3], const int32_t* q_len, int32_t max_q_len, const int32_t* kv_len, int32_t max_kv_len, const int32_t* q_pos,
+                    const int32_t* first_key, const int32_t* prefix_len, void* out, const int64_t out_strides[3], void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * A cache of the full history, in pages: what is kept beside the compressed cache, or before the compression. Each sequence's tokens lie in pages of page_size tokens
+ * that page_table names in order; a page holds all KV heads. batch, n_kv_heads, group_size, head_dim and dtype of cfg are used. All arrays are the caller's, on the device:
+ *   k_pages, v_pages  [n_pages, Hkv, page_size, d], 16-byte aligned, in the dtype of cfg or, with eight_bit, e4m3 codes of one byte (d a multiple of 16)
+ *   k_scale, v_scale  [n_pages, Hkv] fp32, with eight_bit only: a row is its codes times the scale of its page and head. he_page_append makes them powers of
+ *                     two, which leaves every value exact in bf16 and fp32; the calls that read take any finite scale (and round to the dtype).
+ *   page_table        [B, max_pages] int32. An entry outside [0, n_pages) is never followed: rows for such a page are dropped, and it reads as zeros. Entries
+ *                     behind a sequence's end, or behind which its window has passed, may hold anything.
+ *   len               [B] int32, tokens that each sequence holds, those of the append under way included. The calls only read it (several layers may share one, and
+ *                     one page_table); what exceeds max_pages * page_size counts as that, a negative one as 0.
+ * Sequences may share pages that are complete; a page that a sequence still appends to belongs to it alone. A sequence may be cut back by lowering len.
+ */
+typedef struct he_pages {
+  void* k_pages;
+  void* v_pages;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* page_table;
+  const int32_t* len;
+  int32_t n_pages;
+  int32_t page_size; /* 16, 32, 64 or 128 */
+  int32_t max_pages; /* per sequence; max_pages * page_size <= 2^24 */
+  int32_t eight_bit; /* 0 or 1 */
+} he_pages;
+
+/*
+ * he_page_append - the keys and values of a sequence's newest tokens into its pages: k, v [B, Hkv, N, d] in the dtype of cfg with element strides (batch, head,
+ * token), channels contiguous, rows 16-byte aligned. With n = new_len[s] (device int32 [B], at most max_new; NULL: max_new) row i is the token at position
+ * len[s] - n + i; rows ahead of position 0 or behind the last page are dropped, rows i >= n not read. Keys are rotated by their positions on the way (rotary NULL: they
+ * are taken as they are), computed in fp32 and rounded once to the dtype: a page holds what he_rotate_prompt gives.
+ * 8-bit pages: the scale of a page and head, of K and of V, is the least power of two s >= 2^-100 with |x| <= 448 s for every finite entry of the page's tokens so far; the
+ * codes are e4m3 of x / s, rounded to nearest even, entries that are not finite NaN. A page begun by an earlier call keeps its scale or, where the new tokens
+ * need a larger one, has its codes moved to that: exact but for values below 2^-6 s, which are rounded once more (off by 2^-10 s at most each time). Appending a prompt at
+ * once or token by token gives the same pages but for these. A page that begins with the call's rows starts its scale anew.
+ * The same call may be made again (its rows are written once more), not two at the same time on one page.
+ */
+int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary* rotary, const void* k, const void* v, const int64_t kv_strides[3],
+                   const int32_t* new_len, int32_t max_new, void* stream);
+
+/*
+ * he_page_attend - he_attend_scored over the pages: one token per sequence, at position len[s] - 1 (appended before the call), over the tokens
+ * max(first_pos[s], len[s] - w, 0) <= j < len[s]. q: [B, Hkv*G, d] in the dtype of cfg (contiguous), out: [B, Hkv*G, d] fp32; mod and first_pos may be NULL, as there. Without
+ * either it is also the single-token form of he_attend_cross over encoder states that were appended without a rotation. A sequence that holds nothing, or whose every token is
+ * hidden, gives zeros; a token whose score is a NaN or +inf gives NaN; what hidden tokens hold reaches nobody. Pages that the query does not see are not read.
+ * Accuracy as for he_attend_scored, over the values that the pages stand for.
+ * workspace: 16-byte aligned, he_page_attend_workspace_bytes(cfg, pages) bytes (0: may be NULL; it depends on the shapes alone); it holds nothing from one call to the next;
+ * calls that may run at the same time need one each.
+ */
+size_t he_page_attend_workspace_bytes(const he_config* cfg, const he_pages* pages);
+int he_page_attend(const he_config* cfg, const he_pages* pages, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/*
+ * he_page_read - rows back out of the pages, in the dtype of cfg, as he_prefill_compress, he_attention_loss and he_attend_cross take them: row i of k_out, v_out
+ * [B, Hkv, N, d] (element strides as above; one of the two may be NULL) is the token at position first[s] + i (device int32 [B], negative counts as 0; NULL: 0) for
+ * i < max_rows and positions below len[s]. Rows beyond are left as they were.
+ */
+int he_page_read(const he_config* cfg, const he_pages* pages, const int32_t* first, int32_t max_rows, void* k_out, void* v_out, const int64_t kv_strides[3],
+                 void* stream);
+
 /* he_reset - empty every unit: fill = 0, next_pos = 0, pos = -1, codes = 0, scores = 0. K/V are left as they are. */
 int he_reset(const he_config* cfg, const he_cache* cache, void* stream);
 
@@ -408,7 +488,7 @@ int he_prefill_compress_noalloc(const he_config* cfg, const he_cache* cache, con
  * block that hits one releases what it holds and returns), plus, in the bounds-checking debug build, how many
  * indices were found out of range. A call during which the counter rose has returned HE_OK all the same (calls
  * only enqueue work), but its outputs are undefined: he_hash_keys, he_prefill_compress and its variants,
- * he_attend, he_attend_scored, he_attend_prompt (bf16) and he_decode_step with a step scratch are the calls whose kernels contain such waits. This is the one call of the
+ * he_attend, he_attend_scored, he_page_attend, he_attend_prompt and he_attend_cross (bf16) and he_decode_step with a step scratch are the calls whose kernels contain such waits. This is the one call of the
  * library, besides the *_host variants, that synchronises the device. Returns -1 if the counter cannot be read.
  * Diagnostic only: the paper has no counterpart.
  */

@@ -49,11 +49,17 @@ class he_score_mod(ctypes.Structure):
                 ("slopes", ctypes.c_void_p)]
 
 
+class he_pages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale", "page_table", "len")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "max_pages", "eight_bit")]
+
+
 EXPORTS = (
     "he_hash_keys", "he_decode_step", "he_prefill_compress", "he_workspace_bytes", "he_reset",
     "he_decode_staging_bytes", "he_decode_step_host", "he_decode_step_host_enqueue", "he_decode_step_host_block_enqueue", "he_decode_host_block_bytes", "he_prefill_staging_bytes", "he_prefill_compress_host",
     "he_prefill_compress_noalloc", "he_attend", "he_prefill_oneshot", "he_oneshot_workspace_bytes", "he_prefill_oneshot_l2", "he_attention_loss", "he_decode_step_l2", "he_step_scratch_bytes", "he_device_error_count", "he_prefill_phase_events", "he_last_error",
     "he_rotary_init", "he_rotary_init_frequencies", "he_rotate_prompt", "he_rotate_step", "he_attend_prompt", "he_attend_scored",
+    "he_attend_cross", "he_attend_cross_workspace_bytes", "he_page_append", "he_page_attend", "he_page_attend_workspace_bytes", "he_page_read",
 )
 
 _lib = None
@@ -116,7 +122,17 @@ def lib():
     L.he_rotate_step.argtypes = [cfgp, rotp, cap, vp, vp, i64p, i64p, vp, vp, i64p, i64p, vp]
     L.he_attend_prompt.argtypes = [cfgp, modp, vp, vp, vp, i64p, i64p, vp, i32, vp, vp, vp, i64p, vp]
     L.he_attend_scored.argtypes = [cfgp, cap, modp, vp, vp, vp, vp]
-    for name in ("he_rotary_init", "he_rotary_init_frequencies", "he_rotate_prompt", "he_rotate_step", "he_attend_prompt", "he_attend_scored"):
+    pagep = ctypes.POINTER(he_pages)
+    L.he_attend_cross_workspace_bytes.argtypes = [cfgp, i32, i32]
+    L.he_attend_cross_workspace_bytes.restype = sz
+    L.he_attend_cross.argtypes = [cfgp, modp, vp, vp, vp, i64p, i64p, vp, i32, vp, i32, vp, vp, vp, vp, i64p, vp, sz, vp]
+    L.he_page_append.argtypes = [cfgp, pagep, rotp, vp, vp, i64p, vp, i32, vp]
+    L.he_page_attend_workspace_bytes.argtypes = [cfgp, pagep]
+    L.he_page_attend_workspace_bytes.restype = sz
+    L.he_page_attend.argtypes = [cfgp, pagep, modp, vp, vp, vp, vp, sz, vp]
+    L.he_page_read.argtypes = [cfgp, pagep, vp, i32, vp, vp, i64p, vp]
+    for name in ("he_rotary_init", "he_rotary_init_frequencies", "he_rotate_prompt", "he_rotate_step", "he_attend_prompt", "he_attend_scored",
+                 "he_attend_cross", "he_page_append", "he_page_attend", "he_page_read"):
         getattr(L, name).restype = ctypes.c_int
     for name in ("he_hash_keys", "he_decode_step", "he_prefill_compress", "he_reset", "he_decode_step_host", "he_decode_step_host_enqueue",
                  "he_prefill_compress_host", "he_prefill_compress_noalloc"):
@@ -177,6 +193,11 @@ def _empty(shape, dtype, device, stream=None):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _scratch(t):
+    """A workspace as the library takes it: address and bytes."""
+    return (None, 0) if t is None or t.numel() == 0 else (t.data_ptr(), t.numel())
 
 
 def _layout(t):
@@ -273,81 +294,14 @@ class ScoreMod:
         self.pointer = ctypes.pointer(self.raw)
 
 
-class HashEvictCache:
-    """Device-side cache state (the arrays of he_cache, allocated with torch) plus the calls that act on it."""
+class _Layer:
+    """A layer's shape (B sequences, H KV heads, G query heads each, rows of d channels) and the calls that need no cache: rotary positions of prompts,
+    attention of prompts over themselves and of rows over keys of another length."""
 
-    def __init__(self, batch, n_kv_heads, group_size, head_dim, hash_bits, budgets, W, dtype=torch.bfloat16,
-                 max_budget=None, n_sink=0, n_recent=0, write_scores=True, device="cuda", host_budget_mirror=True,
-                 packed_codes=False, early_inputs=False):
-        lib()
-        dev = torch.device(device)
-        budgets = torch.as_tensor(budgets, dtype=torch.int32).reshape(-1)
-        assert budgets.numel() == batch
-        cmax = int(budgets.max()) if max_budget is None else int(max_budget)
-        cmax = (cmax + 3) // 4 * 4  # the slot stride must keep 16-byte alignment
-        if packed_codes:
-            cmax = (cmax + 15) // 16 * 16  # ... also with one byte per slot
-        self.B, self.H, self.G, self.d, self.b, self.Cmax = batch, n_kv_heads, group_size, head_dim, hash_bits, cmax
-        self.Wd = (hash_bits + 31) // 32
-        self.dtype = dtype
-        self.k_cache = torch.zeros((batch, n_kv_heads, cmax, head_dim), dtype=dtype, device=dev)
-        self.v_cache = torch.zeros_like(self.k_cache)
-        # code table: Wd 32-bit words per slot, or ceil(b/8) bytes per slot with HE_FLAG_PACKED_CODES
-        self.packed_codes = bool(packed_codes)
-        if self.packed_codes:
-            self.codes_storage = torch.zeros((batch, n_kv_heads, cmax, (hash_bits + 7) // 8), dtype=torch.uint8, device=dev)
-        else:
-            self.codes_storage = torch.zeros((batch, n_kv_heads, cmax, self.Wd), dtype=torch.int32, device=dev)
-        self.scores = torch.zeros((batch, n_kv_heads, cmax), dtype=torch.float32, device=dev)
-        self.pos = torch.full((batch, n_kv_heads, cmax), -1, dtype=torch.int32, device=dev)
-        self.budget = budgets.to(dev)
-        self.fill = torch.zeros((batch, n_kv_heads), dtype=torch.int32, device=dev)
-        self.next_pos = torch.zeros((batch, n_kv_heads), dtype=torch.int32, device=dev)
-        self.W = W.to(device=dev, dtype=torch.float32).contiguous()
-        assert self.W.shape == (head_dim, hash_bits)
-        self.cfg = _config(batch, n_kv_heads, group_size, head_dim, hash_bits, cmax, n_sink, n_recent, dtype,
-                           (HE_FLAG_WRITE_SCORES if write_scores else 0) | (HE_FLAG_PACKED_CODES if packed_codes else 0) |
-                           (HE_FLAG_EARLY_INPUTS if early_inputs else 0))
-        self._budget_host = (ctypes.c_int32 * batch)(*[int(x) for x in budgets.tolist()])  # host mirror of `budget`
-        self.ca = he_cache(*[_ptr(t) for t in (self.k_cache, self.v_cache, self.codes_storage, self.scores, self.pos,
-                                               self.budget, self.fill, self.next_pos, self.W)],
-                           ctypes.cast(self._budget_host, ctypes.c_void_p) if host_budget_mirror else None, None)
-        # scratch for the bulk-hashed decode step that large batches use (codes of the step's new rows)
-        self.step_scratch = torch.empty(lib().he_step_scratch_bytes(ctypes.byref(self.cfg)), dtype=torch.uint8, device=dev)
-        self.ca.step_scratch = _ptr(self.step_scratch)
-        self._ws = None
-        self._cfg_p, self._ca_p, self._layouts = ctypes.pointer(self.cfg), ctypes.pointer(self.ca), {}
+    def _shape(self, cfg, device):
+        self.cfg, self.device = cfg, device
+        self._cfg_p, self._layouts = ctypes.pointer(cfg), {}
 
-    @property
-    def codes(self):
-        """The code table as int32 words [B, Hkv, Cmax, Wd]: the storage itself, or (packed layout) a copy widened to words."""
-        if not self.packed_codes:
-            return self.codes_storage
-        raw = self.codes_storage
-        wide = torch.zeros(raw.shape[:-1] + (4 * self.Wd,), dtype=torch.uint8, device=raw.device)
-        wide[..., :raw.shape[-1]] = raw
-        return wide.view(torch.int32)
-
-    # --- the four calls of the boundary -------------------------------------------------------------
-    def reset(self, stream=None):
-        _check(lib().he_reset(ctypes.byref(self.cfg), ctypes.byref(self.ca), _stream(stream)))
-
-    def decode_step(self, q, k, v, victim_out=None, evicted_pos_out=None, qcodes_out=None, stream=None):
-        """he_decode_step. q [B, H*G, d], k / v [B, H, d], contiguous. Returns victim_out [B, H] (int32)."""
-        if victim_out is None:
-            victim_out = _empty((self.B, self.H), torch.int32, self.k_cache.device, stream)
-        _check(lib().he_decode_step(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(k), _ptr(v),
-                                    _ptr(victim_out), _ptr(evicted_pos_out), _ptr(qcodes_out), _stream(stream)))
-        return victim_out
-
-    def attend(self, q, out=None, stream=None):
-        """he_attend: softmax(q K^T / sqrt(d)) V over the valid slots (Eq. 1). q [B, H*G, d] -> fp32 [B, H*G, d]."""
-        if out is None:
-            out = _empty((self.B, self.H * self.G, self.d), torch.float32, self.k_cache.device, stream)
-        _check(lib().he_attend(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(out), _stream(stream)))
-        return out
-
-    # --- the layer around the cache: rotary positions, attention with modified scores ------------------
     # A decode loop makes these calls with tensors of the same layout at every token. What the checks of a call find - that every tensor has
     # its device, type, shape and contiguous channels - and the strides that the library takes are kept by layout (never by address).
     def _rows(self, name, t, shape, dtype):
@@ -360,8 +314,8 @@ class HashEvictCache:
 
     def _tensor(self, name, t, shape, dtype, rows=False):
         """A tensor of a call: its device, type and shape; `rows`: any strides but for the channels, else contiguous."""
-        if t.device != self.k_cache.device or t.dtype != dtype or t.shape != shape:
-            raise HashEvictError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, not {tuple(shape)} {dtype} on {self.k_cache.device}")
+        if t.device != self.device or t.dtype != dtype or t.shape != shape:
+            raise HashEvictError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}, not {tuple(shape)} {dtype} on {self.device}")
         if not (t.stride(-1) == 1 if rows else t.is_contiguous()):
             raise HashEvictError(f"{name}: " + ("channels must be contiguous" if rows else "must be contiguous"))
 
@@ -375,7 +329,7 @@ class HashEvictCache:
         return found
 
     def _call(self, fn, stream, *args):
-        dev = self.k_cache.device
+        dev = self.device
         if dev.index == _current_device():
             _check(fn(*args, _stream(stream)))
         else:  # the library launches on the current device
@@ -419,20 +373,11 @@ class HashEvictCache:
                    _ptr(q_out), _ptr(k_out), qos, kos)
         return q_out, k_out
 
-    def rotate_step(self, rotary, q, k, q_out=None, k_out=None, stream=None):
-        """he_rotate_step: q [B, H*G, d] and k [B, H, d] of the next decode_step, rotated by the cache's next_pos. Returns (q_out, k_out).
-        Refused by a cache with early_inputs, whose decode_step would read the rows before they are written."""
-        q_out, k_out = self._outputs(q, k, q_out, k_out, stream)
-        qs, qos, ks, kos = self._known(("step", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
-                                       lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, ()))
-        self._call(lib().he_rotate_step, stream, self._cfg_p, rotary.pointer, self._ca_p, _ptr(q), _ptr(k), qs, ks, _ptr(q_out), _ptr(k_out), qos, kos)
-        return q_out, k_out
-
     def _mod(self, mod):
         if mod is None:
             return None
-        if mod.slopes is not None and (mod.slopes.shape[0] != self.H * self.G or mod.slopes.dim() != 1 or mod.slopes.device != self.k_cache.device):
-            raise HashEvictError(f"slopes: {tuple(mod.slopes.shape)} on {mod.slopes.device}, not {(self.H * self.G,)} on {self.k_cache.device}")
+        if mod.slopes is not None and (mod.slopes.shape[0] != self.H * self.G or mod.slopes.dim() != 1 or mod.slopes.device != self.device):
+            raise HashEvictError(f"slopes: {tuple(mod.slopes.shape)} on {mod.slopes.device}, not {(self.H * self.G,)} on {self.device}")
         return mod.pointer
 
     def _prompt(self, q, k, v, out, prompt_len, doc_start, prefix_len):
@@ -460,6 +405,135 @@ class HashEvictCache:
         self._call(lib().he_attend_prompt, stream, self._cfg_p, self._mod(mod), _ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(prompt_len), q.shape[-2],
                    _ptr(doc_start), _ptr(prefix_len), _ptr(out), os_)
         return out
+
+    def _cross(self, q, k, v, out, lengths, q_pos, first_key, prefix_len):
+        n, m = q.shape[-2], k.shape[-2]
+        ks, vs = self._rows("k", k, (self.B, self.H, m, self.d), self.dtype), self._rows("v", v, (self.B, self.H, m, self.d), self.dtype)
+        if ks[:3] != vs[:3]:
+            raise HashEvictError("k and v must have the same strides")
+        for name, t in (("q_len", lengths[0]), ("kv_len", lengths[1]), ("q_pos", q_pos), ("prefix_len", prefix_len)):
+            if t is not None:
+                self._tensor(name, t, (self.B,), torch.int32)
+        if first_key is not None:
+            self._tensor("first_key", first_key, (self.B, n), torch.int32)
+        qs = self._rows("q", q, (self.B, self.H * self.G, n, self.d), self.dtype)
+        return qs, ks, self._rows("out", out, q.shape, self.dtype)
+
+    def cross_workspace(self, max_q_len, max_kv_len):
+        """A workspace of he_attend_cross for calls of up to these lengths (uint8, perhaps empty). Calls that may run at the same time need one each."""
+        with torch.cuda.device(self.device):
+            need = lib().he_attend_cross_workspace_bytes(self._cfg_p, max_q_len, max_kv_len)
+        return torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def attend_cross(self, q, k, v, q_len, kv_len, q_pos=None, mod=None, first_key=None, prefix_len=None, out=None, workspace=None, stream=None):
+        """he_attend_cross: attention of rows q [B, H*G, N, d] over keys of another length, k / v [B, H, M, d] (any strides on the first three axes), q_len and kv_len
+        int32 [B]. With q_pos int32 [B] row i is the token at position q_pos + i of the keys' sequence (a chunk of a prompt over all before it); without, every
+        row sees every key (encoder states). mod a ScoreMod, first_key int32 [B, N] the first key of each row, prefix_len int32 [B]. workspace: as
+        cross_workspace gives it; None: one for this call. Returns out [B, H*G, N, d] in the dtype of q; rows behind q_len are left as they were
+        (undefined in an `out` that this call makes)."""
+        if out is None:
+            out = _empty(q.shape, q.dtype, q.device, stream)
+        qs, ks, os_ = self._known(("cross", _layout(q), _layout(k), _layout(v), _layout(out), _layout(q_len), _layout(kv_len), _layout(q_pos), _layout(first_key),
+                                   _layout(prefix_len)), lambda: self._cross(q, k, v, out, (q_len, kv_len), q_pos, first_key, prefix_len))
+        n, m = q.shape[-2], k.shape[-2]
+        if workspace is None:
+            need = self._known(("cross workspace", n, m), lambda: self.cross_workspace(n, m).numel())
+            workspace = _empty((need,), torch.uint8, self.device, stream) if need else None
+        else:
+            self._workspace(workspace)
+        self._call(lib().he_attend_cross, stream, self._cfg_p, self._mod(mod), _ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(q_len), n, _ptr(kv_len), m, _ptr(q_pos),
+                   _ptr(first_key), _ptr(prefix_len), _ptr(out), os_, *_scratch(workspace))
+        return out
+
+    def _workspace(self, t):
+        if t.device != self.device or t.dtype != torch.uint8 or t.dim() != 1 or not t.is_contiguous():
+            raise HashEvictError(f"workspace: {tuple(t.shape)} {t.dtype} on {t.device}, not contiguous bytes on {self.device}")
+
+
+class HashEvictCache(_Layer):
+    """Device-side cache state (the arrays of he_cache, allocated with torch) plus the calls that act on it."""
+
+    def __init__(self, batch, n_kv_heads, group_size, head_dim, hash_bits, budgets, W, dtype=torch.bfloat16,
+                 max_budget=None, n_sink=0, n_recent=0, write_scores=True, device="cuda", host_budget_mirror=True,
+                 packed_codes=False, early_inputs=False):
+        lib()
+        dev = torch.device(device)
+        budgets = torch.as_tensor(budgets, dtype=torch.int32).reshape(-1)
+        assert budgets.numel() == batch
+        cmax = int(budgets.max()) if max_budget is None else int(max_budget)
+        cmax = (cmax + 3) // 4 * 4  # the slot stride must keep 16-byte alignment
+        if packed_codes:
+            cmax = (cmax + 15) // 16 * 16  # ... also with one byte per slot
+        self.B, self.H, self.G, self.d, self.b, self.Cmax = batch, n_kv_heads, group_size, head_dim, hash_bits, cmax
+        self.Wd = (hash_bits + 31) // 32
+        self.dtype = dtype
+        self.k_cache = torch.zeros((batch, n_kv_heads, cmax, head_dim), dtype=dtype, device=dev)
+        self.v_cache = torch.zeros_like(self.k_cache)
+        # code table: Wd 32-bit words per slot, or ceil(b/8) bytes per slot with HE_FLAG_PACKED_CODES
+        self.packed_codes = bool(packed_codes)
+        if self.packed_codes:
+            self.codes_storage = torch.zeros((batch, n_kv_heads, cmax, (hash_bits + 7) // 8), dtype=torch.uint8, device=dev)
+        else:
+            self.codes_storage = torch.zeros((batch, n_kv_heads, cmax, self.Wd), dtype=torch.int32, device=dev)
+        self.scores = torch.zeros((batch, n_kv_heads, cmax), dtype=torch.float32, device=dev)
+        self.pos = torch.full((batch, n_kv_heads, cmax), -1, dtype=torch.int32, device=dev)
+        self.budget = budgets.to(dev)
+        self.fill = torch.zeros((batch, n_kv_heads), dtype=torch.int32, device=dev)
+        self.next_pos = torch.zeros((batch, n_kv_heads), dtype=torch.int32, device=dev)
+        self.W = W.to(device=dev, dtype=torch.float32).contiguous()
+        assert self.W.shape == (head_dim, hash_bits)
+        self.cfg = _config(batch, n_kv_heads, group_size, head_dim, hash_bits, cmax, n_sink, n_recent, dtype,
+                           (HE_FLAG_WRITE_SCORES if write_scores else 0) | (HE_FLAG_PACKED_CODES if packed_codes else 0) |
+                           (HE_FLAG_EARLY_INPUTS if early_inputs else 0))
+        self._budget_host = (ctypes.c_int32 * batch)(*[int(x) for x in budgets.tolist()])  # host mirror of `budget`
+        self.ca = he_cache(*[_ptr(t) for t in (self.k_cache, self.v_cache, self.codes_storage, self.scores, self.pos,
+                                               self.budget, self.fill, self.next_pos, self.W)],
+                           ctypes.cast(self._budget_host, ctypes.c_void_p) if host_budget_mirror else None, None)
+        # scratch for the bulk-hashed decode step that large batches use (codes of the step's new rows)
+        self.step_scratch = torch.empty(lib().he_step_scratch_bytes(ctypes.byref(self.cfg)), dtype=torch.uint8, device=dev)
+        self.ca.step_scratch = _ptr(self.step_scratch)
+        self._ws = None
+        self._shape(self.cfg, self.k_cache.device)
+        self._ca_p = ctypes.pointer(self.ca)
+
+    @property
+    def codes(self):
+        """The code table as int32 words [B, Hkv, Cmax, Wd]: the storage itself, or (packed layout) a copy widened to words."""
+        if not self.packed_codes:
+            return self.codes_storage
+        raw = self.codes_storage
+        wide = torch.zeros(raw.shape[:-1] + (4 * self.Wd,), dtype=torch.uint8, device=raw.device)
+        wide[..., :raw.shape[-1]] = raw
+        return wide.view(torch.int32)
+
+    # --- the four calls of the boundary -------------------------------------------------------------
+    def reset(self, stream=None):
+        _check(lib().he_reset(ctypes.byref(self.cfg), ctypes.byref(self.ca), _stream(stream)))
+
+    def decode_step(self, q, k, v, victim_out=None, evicted_pos_out=None, qcodes_out=None, stream=None):
+        """he_decode_step. q [B, H*G, d], k / v [B, H, d], contiguous. Returns victim_out [B, H] (int32)."""
+        if victim_out is None:
+            victim_out = _empty((self.B, self.H), torch.int32, self.k_cache.device, stream)
+        _check(lib().he_decode_step(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(k), _ptr(v),
+                                    _ptr(victim_out), _ptr(evicted_pos_out), _ptr(qcodes_out), _stream(stream)))
+        return victim_out
+
+    def attend(self, q, out=None, stream=None):
+        """he_attend: softmax(q K^T / sqrt(d)) V over the valid slots (Eq. 1). q [B, H*G, d] -> fp32 [B, H*G, d]."""
+        if out is None:
+            out = _empty((self.B, self.H * self.G, self.d), torch.float32, self.k_cache.device, stream)
+        _check(lib().he_attend(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q), _ptr(out), _stream(stream)))
+        return out
+
+    # --- the layer around the cache: a new token's rotary positions and attention with modified scores ----
+    def rotate_step(self, rotary, q, k, q_out=None, k_out=None, stream=None):
+        """he_rotate_step: q [B, H*G, d] and k [B, H, d] of the next decode_step, rotated by the cache's next_pos. Returns (q_out, k_out).
+        Refused by a cache with early_inputs, whose decode_step would read the rows before they are written."""
+        q_out, k_out = self._outputs(q, k, q_out, k_out, stream)
+        qs, qos, ks, kos = self._known(("step", rotary.head_dim, _layout(q), _layout(k), _layout(q_out), _layout(k_out)),
+                                       lambda: self._rotation(rotary.head_dim, q, k, q_out, k_out, ()))
+        self._call(lib().he_rotate_step, stream, self._cfg_p, rotary.pointer, self._ca_p, _ptr(q), _ptr(k), qs, ks, _ptr(q_out), _ptr(k_out), qos, kos)
+        return q_out, k_out
 
     def _scored(self, q, first_pos, out):
         self._tensor("q", q, (self.B, self.H * self.G, self.d), self.dtype)
@@ -582,3 +656,89 @@ class HashEvictCache:
         _check(lib().he_prefill_compress_host(ctypes.byref(self.cfg), ctypes.byref(self.ca), _ptr(q_host), _ptr(k_host),
                                               _ptr(v_host), _ptr(prompt_len_host), max_prompt_len, _ptr(fill_host),
                                               _ptr(staging), staging.numel(), _stream(stream)))
+
+
+class PagedCache(_Layer):
+    """The full history of a layer in pages (he_pages, allocated with torch; he_page_append, he_page_attend, he_page_read).
+
+    page_table int32 [B, max_pages] on the device names each sequence's pages in order, `length` int32 [B] the tokens that each holds, those of an append under way
+    included; both stay the caller's, are only read, and may be shared by the caches of several layers. The pages themselves are k_pages, v_pages
+    [n_pages, H, page_size, d] in `dtype` or, with eight_bit, as torch.float8_e4m3fn codes with k_scale, v_scale fp32 [n_pages, H]."""
+
+    def __init__(self, batch, n_kv_heads, group_size, head_dim, page_table, n_pages, page_size=64, dtype=torch.bfloat16, eight_bit=False, length=None):
+        lib()
+        self.B, self.H, self.G, self.d, self.dtype = batch, n_kv_heads, group_size, head_dim, dtype
+        self._shape(_config(batch, n_kv_heads, group_size, head_dim, 1, 4, 0, 0, dtype, 0), page_table.device)
+        self.n_pages, self.page_size, self.eight_bit = _int32("n_pages", n_pages), _int32("page_size", page_size), bool(eight_bit)
+        self.page_table = page_table
+        self.length = torch.zeros((batch,), dtype=torch.int32, device=self.device) if length is None else length
+        if not page_table.is_cuda or page_table.dim() != 2:
+            raise HashEvictError(f"page_table: {tuple(page_table.shape)} on {page_table.device}, not [batch, pages of a sequence] on a CUDA device")
+        self._tensor("page_table", page_table, (batch, page_table.shape[1]), torch.int32)
+        self._tensor("length", self.length, (batch,), torch.int32)
+        shape = (self.n_pages, n_kv_heads, self.page_size, head_dim)
+        self.k_pages = torch.zeros(shape, dtype=torch.uint8 if eight_bit else dtype, device=self.device)
+        self.v_pages = torch.zeros_like(self.k_pages)
+        self.k_scale = self.v_scale = None
+        if eight_bit:
+            self.k_pages, self.v_pages = self.k_pages.view(torch.float8_e4m3fn), self.v_pages.view(torch.float8_e4m3fn)
+            self.k_scale = torch.ones((self.n_pages, n_kv_heads), dtype=torch.float32, device=self.device)
+            self.v_scale = torch.ones_like(self.k_scale)
+        self.raw = he_pages(*[_ptr(t) for t in (self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table, self.length)], self.n_pages, self.page_size,
+                            page_table.shape[1], int(self.eight_bit))
+        self._pages_p = ctypes.pointer(self.raw)
+
+    def _pair(self, k, v, names, n):
+        ks, vs = (self._rows(name, t, (self.B, self.H, n, self.d), self.dtype) for name, t in zip(names, (k, v)))
+        if ks[:3] != vs[:3]:
+            raise HashEvictError(f"{names[0]} and {names[1]} must have the same strides")
+        return ks
+
+    def append(self, k, v, new_len=None, rotary=None, stream=None):
+        """he_page_append: k, v [B, H, N, d] (any strides on the first three axes) of the newest tokens, the last new_len (int32 [B]; None: N) of the `length` that each
+        sequence holds. Keys are rotated by their positions with `rotary` (a Rotary), or taken as they are."""
+        n = k.shape[-2]
+        strides = self._known(("append", _layout(k), _layout(v)), lambda: self._pair(k, v, ("k", "v"), n))
+        if new_len is not None:
+            self._tensor("new_len", new_len, (self.B,), torch.int32)
+        if rotary is not None and rotary.head_dim != self.d:
+            raise HashEvictError(f"rotary of head_dim {rotary.head_dim} for rows of {self.d}")
+        self._call(lib().he_page_append, stream, self._cfg_p, self._pages_p, None if rotary is None else rotary.pointer, _ptr(k), _ptr(v), strides, _ptr(new_len), n)
+
+    def workspace(self):
+        """A workspace of he_page_attend (uint8, perhaps empty). Calls that may run at the same time need one each."""
+        with torch.cuda.device(self.device):
+            need = lib().he_page_attend_workspace_bytes(self._cfg_p, self._pages_p)
+        return torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def _attended(self, q, first_pos, out):
+        self._tensor("q", q, (self.B, self.H * self.G, self.d), self.dtype)
+        self._tensor("out", out, q.shape, torch.float32)
+        if first_pos is not None:
+            self._tensor("first_pos", first_pos, (self.B,), torch.int32)
+        return self.workspace().numel()
+
+    def attend(self, q, mod=None, first_pos=None, out=None, workspace=None, stream=None):
+        """he_page_attend: q [B, H*G, d], the newest token of each sequence, over its pages -> fp32 [B, H*G, d]. mod a ScoreMod, first_pos int32 [B] the first position that
+        it sees. workspace: as workspace() gives it; None: one for this call."""
+        if out is None:
+            out = _empty(q.shape, torch.float32, q.device, stream)
+        need = self._known(("attend", _layout(q), _layout(out), _layout(first_pos)), lambda: self._attended(q, first_pos, out))
+        if workspace is None:
+            workspace = _empty((need,), torch.uint8, self.device, stream) if need else None
+        else:
+            self._workspace(workspace)
+        self._call(lib().he_page_attend, stream, self._cfg_p, self._pages_p, self._mod(mod), _ptr(q), _ptr(first_pos), _ptr(out), *_scratch(workspace))
+        return out
+
+    def read(self, rows, first=None, k_out=None, v_out=None, stream=None):
+        """he_page_read: the rows from position `first` (int32 [B]; None: 0) on, up to `rows` of a sequence, in the dtype of the cache. Returns (k_out, v_out) [B, H, rows, d]; with
+        one of the two given, only that. Rows behind a sequence's end are left as they were (undefined in outputs that this call makes)."""
+        if k_out is None and v_out is None:
+            k_out, v_out = (_empty((self.B, self.H, _int32("rows", rows), self.d), self.dtype, self.device, stream) for _ in "kv")
+        a, b = (v_out if k_out is None else k_out), (k_out if v_out is None else v_out)
+        strides = self._known(("read", rows, _layout(a), _layout(b)), lambda: self._pair(a, b, ("k_out", "v_out"), rows))
+        if first is not None:
+            self._tensor("first", first, (self.B,), torch.int32)
+        self._call(lib().he_page_read, stream, self._cfg_p, self._pages_p, _ptr(first), rows, _ptr(k_out), _ptr(v_out), strides)
+        return k_out, v_out

@@ -8,9 +8,10 @@
 //                          m16n8k16 MMAs (bf16 products are exact, fp32 accumulation, P as hi + lo bf16); a cluster of up
 //                          to 16 CTAs shares a unit when there are few units.
 //   attend_generic_kernel  any supported dtype / d, and where no tensor map can be encoded (attend_generic_kernels.cuh).
-//   attend_scored_kernel   the same for he_attend_scored.
+//   attend_scored_kernel   the same for he_attend_scored, and for he_page_attend.
 #pragma once
 #include <cuda.h>  // CUtensorMap (types only; the encoder is fetched through the runtime)
+#include <cuda_fp16.h>
 
 #include <type_traits>
 
@@ -37,6 +38,21 @@ struct ScoredArgs : AttendArgs {
   int n_order;  // > 0: the sequences in the order in which their CTAs start, largest budgets first
   uint8_t order[256];
 };
+// he_page_attend: the slots of a unit are the tokens of a sequence, which lie in pages.
+struct PagedAttendArgs {
+  he_config cfg;
+  he_pages pages;
+  const void* q;  // [B, Hkv*G, d]
+  float* out;     // [B, Hkv*G, d] fp32
+  AttendMod mod;
+};
+__host__ __device__ inline long long page_capacity(const he_pages& p) { return (long long)p.max_pages * p.page_size; }
+__device__ __forceinline__ int page_length(const he_pages& p, int s) { return (int)min((long long)max(p.len[s], 0), page_capacity(p)); }
+// The page that holds token j of sequence s, or -1: none that could be followed.
+__device__ __forceinline__ int page_of(const he_pages& p, int s, int j) {
+  const int page = __ldg(p.page_table + (long long)s * p.max_pages + j / p.page_size);
+  return (unsigned)page < (unsigned)p.n_pages ? page : -1;
+}
 template <bool MOD>
 using AttendArgsOf = std::conditional_t<MOD, ScoredArgs, AttendArgs>;
 
@@ -168,6 +184,23 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t& hi, uint3
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n" : "=r"(hi) : "f"(y), "f"(x));
   const float xr = x - __uint_as_float(hi << 16), yr = y - __uint_as_float(hi & 0xFFFF0000u);
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n" : "=r"(lo) : "f"(yr), "f"(xr));
+}
+
+// Two e4m3 codes (the lower byte first) as half precision, which holds all of their values.
+__device__ __forceinline__ uint32_t e4m3_halves(uint32_t two) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+  return r;
+}
+// Sixteen e4m3 codes times their scale.
+__device__ __forceinline__ void page_unpack(const uint4& codes, float scale, float (&f)[16]) {
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t h = e4m3_halves((i & 1) ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu);
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    f[2 * i] = v.x * scale, f[2 * i + 1] = v.y * scale;
+  }
 }
 
 __device__ __forceinline__ uint4 ldg_stream16(const uint4* p) {
@@ -552,13 +585,16 @@ __device__ __forceinline__ void cp_async16_or_zero(void* smem_dst, const void* g
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(gmem_src), "r"(some ? 16u : 0u) : "memory");
 }
 
-template <int E, int GP>
-__global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const ScoredArgs a, const int S, const int stages) {
+// With PAGED (he_page_attend) slot j is token j, from the tile that holds the first visible one on, and its rows lie in a page (E = 1: codes of 8 bits, times the
+// page's scale); rows of a page that is not there are zeros.
+template <int E, int GP, bool PAGED = false>
+__global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const std::conditional_t<PAGED, PagedAttendArgs, ScoredArgs> a, const int S, const int stages) {
   extern __shared__ __align__(16) float asm_[];
   __shared__ __align__(8) unsigned long long merge_bar;
   const he_config& cfg = a.cfg;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int seq = a.n_order > 0 ? a.order[blockIdx.y] : blockIdx.y;
+  int seq = blockIdx.y;
+  if constexpr (!PAGED) seq = a.n_order > 0 ? a.order[blockIdx.y] : seq;
   const int rank = blockIdx.x % S, head = blockIdx.x / S, unit = seq * cfg.n_kv_heads + head;
   const int d = cfg.head_dim, G = cfg.group_size, pitch = d + 4;
   float* qs = asm_;                                  // [G][d]
@@ -580,14 +616,25 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Sco
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // waited for before the first remote store
   }
   griddep_wait();
-  const int fill = __ldcg(a.ca.fill + unit), now = __ldcg(a.ca.next_pos + unit) - 1;
+  int fill, now;
+  if constexpr (PAGED) fill = page_length(a.pages, seq), now = fill - 1;
+  else fill = __ldcg(a.ca.fill + unit), now = __ldcg(a.ca.next_pos + unit) - 1;
   int low = a.mod.first_pos != nullptr ? max(0, a.mod.first_pos[seq]) : 0;
   if (a.mod.window > 0) low = max(low, now - a.mod.window + 1);
+  if (PAGED) low = min(low, fill);  // (where the walk starts)
   const int cpr = d * E / 16;
-  for (int i = tid; i < G * cpr; i += kAttendThreads) stage_chunk(qs + (i / cpr) * d, static_cast<const char*>(a.q) + ((size_t)unit * G + i / cpr) * d * E, i % cpr, cfg.dtype);
-  const char* Kb = static_cast<const char*>(a.ca.k_cache) + (size_t)unit * cfg.max_budget * d * E;
-  const char* Vb = static_cast<const char*>(a.ca.v_cache) + (size_t)unit * cfg.max_budget * d * E;
-  const int32_t* pos = a.ca.pos + (size_t)unit * cfg.max_budget;
+  const int eq = PAGED ? esize_of(cfg.dtype) : E, cpq = d * eq / 16;
+  for (int i = tid; i < G * cpq; i += kAttendThreads) stage_chunk(qs + (i / cpq) * d, static_cast<const char*>(a.q) + ((size_t)unit * G + i / cpq) * d * eq, i % cpq, cfg.dtype);
+  const char *Kb, *Vb;
+  const int32_t* pos = nullptr;
+  if constexpr (PAGED) {
+    Kb = static_cast<const char*>(a.pages.k_pages), Vb = static_cast<const char*>(a.pages.v_pages);
+  } else {
+    Kb = static_cast<const char*>(a.ca.k_cache) + (size_t)unit * cfg.max_budget * d * E;
+    Vb = static_cast<const char*>(a.ca.v_cache) + (size_t)unit * cfg.max_budget * d * E;
+    pos = a.ca.pos + (size_t)unit * cfg.max_budget;
+  }
+  auto pos_of = [&](int j) { return PAGED ? j : __ldcg(pos + j); };
   constexpr int WPH = 8 / GP, MINE = kScoredSlots / (32 * WPH) > 0 ? kScoredSlots / (32 * WPH) : 1;  // warps of a head, slots of a lane
   constexpr int LANES = kScoredSlots / (WPH * MINE);                                                   // lanes of a warp with slots
   const int g = warp / WPH, part = warp % WPH;
@@ -598,11 +645,11 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Sco
   for (int h = 0; h < 8; ++h)
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[h][e] = 0.f;
-  const int step = kScoredSlots * S, j_first = kScoredSlots * rank;
+  const int step = kScoredSlots * S, j_first = kScoredSlots * rank + (PAGED ? low / kScoredSlots * kScoredSlots : 0);
   auto look = [&](int tile) {  // which slots of a tile are visible (warps 0 and 1)
     if (warp < 2) {
       const int j = j_first + tile * step + 32 * warp + lane;
-      const uint32_t bits = __ballot_sync(0xFFFFFFFFu, j < fill && __ldcg(pos + j) >= low);
+      const uint32_t bits = __ballot_sync(0xFFFFFFFFu, j < fill && pos_of(j) >= low);
       if (lane == 0) seen_s[2 * (tile % 3) + warp] = bits;
     }
   };
@@ -618,10 +665,35 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Sco
       if (c >= cpr) c -= cpr, ++r;
     };
     auto visible = [&](int row) { return ((row < 32 ? seen[0] : seen[1]) >> (row & 31)) & 1u; };
-    if (E == 4) {
+    // the row of K and V that holds a visible slot, -1 where its page is not there
+    auto row_of = [&](int j) -> long long {
+      if constexpr (PAGED) {
+        const int page = page_of(a.pages, seq, j);
+        return page < 0 ? -1 : ((long long)page * cfg.n_kv_heads + head) * a.pages.page_size + j % a.pages.page_size;
+      } else {
+        return j;
+      }
+    };
+    if constexpr (E == 1) {
       for (; r < kScoredSlots; next()) {
-        const bool some = visible(r) != 0u;
-        const size_t at = ((size_t)(some ? j0 + r : 0) * d) * E + 16 * c;
+        const long long row = visible(r) ? row_of(j0 + r) : -1;
+        float kf[16] = {}, vf[16] = {};
+        if (row >= 0) {
+          const long long at = row / a.pages.page_size;
+          page_unpack(ldg_stream16(reinterpret_cast<const uint4*>(Kb + row * d + 16 * c)), __ldcg(a.pages.k_scale + at), kf);
+          page_unpack(ldg_stream16(reinterpret_cast<const uint4*>(Vb + row * d + 16 * c)), __ldcg(a.pages.v_scale + at), vf);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          *reinterpret_cast<float4*>(kt + r * pitch + 16 * c + e) = make_float4(kf[e], kf[e + 1], kf[e + 2], kf[e + 3]);
+          *reinterpret_cast<float4*>(vt + r * d + 16 * c + e) = make_float4(vf[e], vf[e + 1], vf[e + 2], vf[e + 3]);
+        }
+      }
+    } else if (E == 4) {
+      for (; r < kScoredSlots; next()) {
+        const long long row = visible(r) ? row_of(j0 + r) : -1;
+        const bool some = row >= 0;
+        const size_t at = ((size_t)(some ? row : 0) * d) * E + 16 * c;
         cp_async16_or_zero(kt + r * pitch + 4 * c, Kb + at, some);
         cp_async16_or_zero(vt + r * d + 4 * c, Vb + at, some);
       }
@@ -633,8 +705,9 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Sco
         for (int u = 0; u < 4; ++u, next()) {
           rr[u] = r, cc[u] = c;
           k4[u] = v4[u] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < kScoredSlots && visible(r)) {
-            const size_t at = ((size_t)(j0 + r) * d) * E + 16 * c;
+          const long long row = r < kScoredSlots && visible(r) ? row_of(j0 + r) : -1;
+          if (row >= 0) {
+            const size_t at = ((size_t)row * d) * E + 16 * c;
             k4[u] = ldg_stream16(reinterpret_cast<const uint4*>(Kb + at)), v4[u] = ldg_stream16(reinterpret_cast<const uint4*>(Vb + at));
           }
         }
@@ -664,7 +737,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const Sco
 #pragma unroll
     for (int u = 0; u < MINE; ++u) {
       const int r = part * LANES * MINE + u * LANES + lane % LANES;
-      p[u] = j0 + r < fill ? __ldcg(pos + j0 + r) : -1;
+      p[u] = j0 + r < fill ? pos_of(j0 + r) : -1;
     }
     __syncthreads();
     // scores of head g

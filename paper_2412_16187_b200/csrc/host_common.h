@@ -3,6 +3,9 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
@@ -22,6 +25,9 @@ namespace he {
 
 // The trouble counter (g_tc_error) of layer_ops.cu's kernels, -1 if it cannot be read.
 int layer_error_count();
+// The same of pages.cu's and cross_ops.cu's.
+int page_error_count();
+int cross_error_count();
 
 inline thread_local char g_err[512] = "";
 
@@ -68,6 +74,57 @@ inline int check_cache(const he_cache* ca) {
     return fail(HE_ERR_INVALID_ARG, "cache has a null pointer");
   if (!aligned16(ca->k_cache) || !aligned16(ca->v_cache) || !aligned16(ca->codes) || !aligned16(ca->scores) || !aligned16(ca->pos))
     return fail(HE_ERR_INVALID_ARG, "cache arrays must be 16-byte aligned");
+  return HE_OK;
+}
+
+constexpr int kMaxTokens = 1 << 24;  // positions and distances are exact in fp32
+
+inline int check_rotary(const he_rotary* r, int d) {
+  if (r == nullptr) return fail(HE_ERR_INVALID_ARG, "rotary is null");
+  if (r->channels < 2 || r->channels % 2 != 0 || r->channels > 2 * HE_ROTARY_MAX_PAIRS)
+    return fail(HE_ERR_INVALID_ARG, "rotary channels %d are not even and in [2, %d]", r->channels, 2 * HE_ROTARY_MAX_PAIRS);
+  if (d > 0 && r->channels > d) return fail(HE_ERR_INVALID_ARG, "rotary channels %d > head_dim %d", r->channels, d);
+  return HE_OK;
+}
+
+// Element strides of 16-byte aligned rows.
+inline int check_strides(const char* what, const int64_t* strides, int n, int esize) {
+  if (strides == nullptr) return fail(HE_ERR_INVALID_ARG, "%s strides are null", what);
+  for (int i = 0; i < n; ++i)
+    if (strides[i] < 0 || (strides[i] * esize) % 16 != 0)
+      return fail(HE_ERR_INVALID_ARG, "%s stride %lld does not keep rows 16-byte aligned", what, (long long)strides[i]);
+  return HE_OK;
+}
+
+// The rows of an output do not overlap: each axis of more than one entry steps over all that the axes of smaller strides cover. (n <= 3)
+inline int check_apart(const char* what, const int64_t* strides, const long long* sizes, int n, int d) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + n, [&](int x, int y) { return strides[x] < strides[y]; });
+  double covered = d;  // (exact as far as addresses go)
+  for (int i = 0; i < n; ++i) {
+    const int x = order[i];
+    if (sizes[x] <= 1) continue;
+    if ((double)strides[x] < covered) return fail(HE_ERR_INVALID_ARG, "%s stride %lld lets rows overlap", what, (long long)strides[x]);
+    covered += (double)strides[x] * (double)(sizes[x] - 1);
+  }
+  return HE_OK;
+}
+
+// he_score_mod with its defaults filled in: the factor of q.k in log2 units and, with a cap, its two factors.
+inline int check_mod(const he_score_mod* mod, int d, float* scale_log2, float* cap_log2, float* inv_cap, int* window, const float** slopes) {
+  float scale = 1.0f / std::sqrt((float)d), cap = 0.f;
+  *window = 0, *slopes = nullptr;
+  if (mod != nullptr) {
+    if (!(mod->scale >= 0.f) || std::isinf(mod->scale)) return fail(HE_ERR_INVALID_ARG, "scale %g is not finite and >= 0", (double)mod->scale);
+    if (!(mod->cap >= 0.f) || std::isinf(mod->cap)) return fail(HE_ERR_INVALID_ARG, "cap %g is not finite and >= 0", (double)mod->cap);
+    if (mod->window < 0) return fail(HE_ERR_INVALID_ARG, "window %d < 0", mod->window);
+    if (mod->scale > 0.f) scale = mod->scale;
+    cap = mod->cap, *window = mod->window, *slopes = mod->slopes;
+  }
+  *scale_log2 = scale * kLog2e, *cap_log2 = cap * kLog2e, *inv_cap = cap > 0.f ? scale / cap : 0.f;
+  // (a ratio below the normal numbers would be lost, or its inverse: such a cap is none)
+  if (!std::isfinite(*scale_log2) || !std::isfinite(*cap_log2) || !std::isfinite(*inv_cap) || (cap > 0.f && *inv_cap < FLT_MIN))
+    return fail(HE_ERR_INVALID_ARG, "scale %g with cap %g leaves fp32", (double)scale, (double)cap);
   return HE_OK;
 }
 

@@ -3,7 +3,6 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <cfloat>
 #include <cmath>
 #include <cstring>
 
@@ -12,6 +11,7 @@
 #include "hashevict.h"
 #include "host_common.h"
 #include "prompt_attend_kernels.cuh"
+#include "prompt_launch.h"
 #include "rotary_kernels.cuh"
 
 using namespace he;
@@ -22,39 +22,6 @@ int he::layer_error_count() {
 }
 
 namespace {
-
-constexpr int kMaxTokens = 1 << 24;  // positions and distances are exact in fp32
-
-int check_rotary(const he_rotary* r, int d) {
-  if (r == nullptr) return fail(HE_ERR_INVALID_ARG, "rotary is null");
-  if (r->channels < 2 || r->channels % 2 != 0 || r->channels > 2 * HE_ROTARY_MAX_PAIRS)
-    return fail(HE_ERR_INVALID_ARG, "rotary channels %d are not even and in [2, %d]", r->channels, 2 * HE_ROTARY_MAX_PAIRS);
-  if (d > 0 && r->channels > d) return fail(HE_ERR_INVALID_ARG, "rotary channels %d > head_dim %d", r->channels, d);
-  return HE_OK;
-}
-
-// Element strides of 16-byte aligned rows.
-int check_strides(const char* what, const int64_t* strides, int n, int esize) {
-  if (strides == nullptr) return fail(HE_ERR_INVALID_ARG, "%s strides are null", what);
-  for (int i = 0; i < n; ++i)
-    if (strides[i] < 0 || (strides[i] * esize) % 16 != 0)
-      return fail(HE_ERR_INVALID_ARG, "%s stride %lld does not keep rows 16-byte aligned", what, (long long)strides[i]);
-  return HE_OK;
-}
-
-// The rows of an output do not overlap: each axis of more than one entry steps over all that the axes of smaller strides cover. (n <= 3)
-int check_apart(const char* what, const int64_t* strides, const long long* sizes, int n, int d) {
-  int order[3] = {0, 1, 2};
-  std::sort(order, order + n, [&](int x, int y) { return strides[x] < strides[y]; });
-  double covered = d;  // (exact as far as addresses go)
-  for (int i = 0; i < n; ++i) {
-    const int x = order[i];
-    if (sizes[x] <= 1) continue;
-    if ((double)strides[x] < covered) return fail(HE_ERR_INVALID_ARG, "%s stride %lld lets rows overlap", what, (long long)strides[x]);
-    covered += (double)strides[x] * (double)(sizes[x] - 1);
-  }
-  return HE_OK;
-}
 
 template <int E, int V, bool INTER>
 int launch_rotate_as(const RotateArgs& a, const he_rotary& r, dim3 grid, cudaStream_t st) {
@@ -122,28 +89,10 @@ int rotate_sides(RotateArgs& a, const he_config* cfg, const void* q, const void*
   return HE_OK;
 }
 
-// he_score_mod with its defaults filled in: the factor of q.k in log2 units and, with a cap, its two factors.
-int check_mod(const he_score_mod* mod, int d, float* scale_log2, float* cap_log2, float* inv_cap, int* window, const float** slopes) {
-  float scale = 1.0f / std::sqrt((float)d), cap = 0.f;
-  *window = 0, *slopes = nullptr;
-  if (mod != nullptr) {
-    if (!(mod->scale >= 0.f) || std::isinf(mod->scale)) return fail(HE_ERR_INVALID_ARG, "scale %g is not finite and >= 0", (double)mod->scale);
-    if (!(mod->cap >= 0.f) || std::isinf(mod->cap)) return fail(HE_ERR_INVALID_ARG, "cap %g is not finite and >= 0", (double)mod->cap);
-    if (mod->window < 0) return fail(HE_ERR_INVALID_ARG, "window %d < 0", mod->window);
-    if (mod->scale > 0.f) scale = mod->scale;
-    cap = mod->cap, *window = mod->window, *slopes = mod->slopes;
-  }
-  *scale_log2 = scale * kLog2e, *cap_log2 = cap * kLog2e, *inv_cap = cap > 0.f ? scale / cap : 0.f;
-  // (a ratio below the normal numbers would be lost, or its inverse: such a cap is none)
-  if (!std::isfinite(*scale_log2) || !std::isfinite(*cap_log2) || !std::isfinite(*inv_cap) || (cap > 0.f && *inv_cap < FLT_MIN))
-    return fail(HE_ERR_INVALID_ARG, "scale %g with cap %g leaves fp32", (double)scale, (double)cap);
-  return HE_OK;
-}
-
 template <int NQ, int R>
 int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
   const int tiles = (a.tokens + 16 * R - 1) / (16 * R);
-  const long long ctas = (long long)tiles * a.batch * a.n_kv_heads * a.group;
+  const long long ctas = (long long)tiles * a.batch * a.n_kv_heads * a.group * a.splits;
   if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld tiles in one call", ctas);
   // a tile of keys ahead where an SM has one CTA and its 227 KB
   const int stages = R == 1 && a.dtype == HE_DTYPE_F32 && prompt_fp32_smem<R>(a.d, 2) <= kAttendMaxSmem ? 2 : 1;
@@ -157,55 +106,84 @@ template <int NQ>
 int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
-  const long long large = (long long)((a.tokens + 63) / 64) * a.batch * a.n_kv_heads * a.group;
-  return large >= sms ? launch_prompt_fp32<NQ, 4>(a, st) : launch_prompt_fp32<NQ, 1>(a, st);
+  return prompt_fp32_tiles(a, 64) >= sms ? launch_prompt_fp32<NQ, 4>(a, st) : launch_prompt_fp32<NQ, 1>(a, st);
 }
 
-// Tensor map of q, k or v: {channel, token, head, sequence} in boxes of 64 channels x 128 tokens, 128-byte swizzle. An axis of one
-// entry may come with any stride, and gets one that the encoder takes.
-bool prompt_tmap(const void* base, const PromptArgs& a, const long long strides[3], int heads, CUtensorMap* out) {
-  const EncodeTiledFn encode = tmap_encoder();
-  if (encode == nullptr || env_flag_set<4>("HE_DISABLE_TMA")) return false;
-  const cuuint64_t dims[4] = {(cuuint64_t)a.d, (cuuint64_t)a.tokens, (cuuint64_t)heads, (cuuint64_t)a.batch};
-  cuuint64_t st[3] = {(cuuint64_t)strides[2] * 2, (cuuint64_t)strides[1] * 2, (cuuint64_t)strides[0] * 2};
-  for (int i = 0; i < 3; ++i) {
-    if (dims[i + 1] == 1) st[i] = (cuuint64_t)a.d * 2;
-    if (st[i] == 0 || st[i] % 16 != 0 || st[i] >= (1ull << 40)) return false;
+bool on_tensor_cores(const PromptArgs& a) { return a.dtype == HE_DTYPE_BF16 && a.d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr; }
+
+// Into how many shares the keys are cut where there are fewer tiles of rows than SMs. Tiles run side by side on the SMs, in rounds; a block of 128 keys costs
+// a tile 3500 cycles on the tensor cores and the tile's own start and end 9000 (prompt_tc_kernel), so the best count is the one with the shortest rounds, each share
+// counted with its start and end, all for the longest rows and keys of the call. On the CUDA cores a block of 64 keys by 16 or 64 rows takes the place.
+int prompt_splits(const PromptArgs& a, bool tc, int* out) {
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  long long items = tc ? prompt_tc_tiles(a).items : prompt_fp32_tiles(a, 64);
+  if (!tc && items < sms) items = prompt_fp32_tiles(a, 16);
+  *out = 1;
+  const long long blocks = ((long long)a.keys + (tc ? 127 : 63)) / (tc ? 128 : 64);
+  double best = 0.0;
+  for (int z = 1; z <= 64 && 2 * z <= blocks && (z == 1 || items * z <= 8LL * sms); ++z) {
+    const double rounds = (double)((items * z + sms - 1) / sms), cost = rounds * ((double)((blocks + z - 1) / z) * 3500.0 + 9000.0) + (z > 1 ? 6000.0 : 0.0);
+    if (z == 1 || cost < 0.95 * best) best = cost, *out = z;
   }
-  const cuuint32_t box[4] = {64, (cuuint32_t)kPtTile, 1, 1}, estr[4] = {1, 1, 1, 1};
-  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, st, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Whether the kernel was built with as many registers a thread as its warps share out among themselves.
-template <typename K>
-int registers_suffice(K kernel, int* out) {
-  cudaFuncAttributes at;
-  HE_CUDA_CHECK(cudaFuncGetAttributes(&at, kernel));
-  *out = at.numRegs * kPtThreads >= 256 * kPtSoftRegs + 128 * kPtOtherRegs ? 1 : 2;
   return HE_OK;
 }
-
-// HE_OK, an error, or -1: the caller's other kernel serves.
-template <int D, bool CAP, bool BIAS>
-int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
-  auto kernel = prompt_tc_kernel<D, CAP, BIAS>;
-  static DeviceTable<1> table;
-  int dev = 0, enough = 0;
-  HE_CUDA_CHECK(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= kMaxDevices) return fail(HE_ERR_UNSUPPORTED, "device index %d", dev);
-  if (int rc = table.get(dev, 0, &enough, [&](int* got) { return registers_suffice(kernel, got); })) return rc;
-  if (enough != 1) return -1;
-  const int by_heads = a.group % 2 == 0, rows = by_heads ? kPtTile : 2 * kPtTile, tiles = (a.tokens + rows - 1) / rows;
-  const long long ctas = (long long)tiles * a.batch * a.n_kv_heads * a.group / (by_heads ? 2 : 1);
-  if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld tiles in one call", ctas);
-  if (int rc = set_smem(kernel, PromptTc<D>::kSmem)) return rc;
-  return launch_pdl(kernel, dim3((unsigned)ctas), kPtThreads, PromptTc<D>::kSmem, true, st, a, tiles, by_heads, maps);
+size_t prompt_part_bytes(const PromptArgs& a, int splits) {
+  return splits > 1 ? (size_t)splits * a.batch * a.n_kv_heads * a.group * a.tokens * (a.d + 2) * sizeof(float) : 0;
 }
-template <int D>
-int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
-  if (a.cap_log2 > 0.f) return a.slopes != nullptr ? launch_prompt_tc<D, true, true>(a, maps, st) : launch_prompt_tc<D, true, false>(a, maps, st);
-  return a.slopes != nullptr ? launch_prompt_tc<D, false, true>(a, maps, st) : launch_prompt_tc<D, false, false>(a, maps, st);
+
+int launch_rows(const PromptArgs& a, bool tc, cudaStream_t st) {
+  if (tc) {
+    PromptMaps maps;
+    if (prompt_tmap(a.q, a, a.qs, a.n_kv_heads * a.group, a.tokens, &maps.q) && prompt_tmap(a.k, a, a.ks, a.n_kv_heads, a.keys, &maps.k) &&
+        prompt_tmap(a.v, a, a.ks, a.n_kv_heads, a.keys, &maps.v)) {
+      const int rc = a.splits > 1 ? launch_prompt_shares(a, maps, st) : a.d <= 64 ? launch_prompt_tc<64, false>(a, maps, st) : launch_prompt_tc<128, false>(a, maps, st);
+      if (rc >= 0) return rc;
+    }
+  }
+  switch ((a.d + 63) / 64) {
+    case 1: return launch_prompt_fp32<1>(a, st);
+    case 2: return launch_prompt_fp32<2>(a, st);
+    case 3: return launch_prompt_fp32<3>(a, st);
+    default: return launch_prompt_fp32<4>(a, st);
+  }
+}
+
+// he_attend_prompt and he_attend_cross. `a` comes with lengths, positions and masks.
+int attend_rows(PromptArgs& a, const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t* q_strides,
+                const int64_t* kv_strides, void* out, const int64_t* out_strides, const char* tokens_name, void* workspace, size_t workspace_bytes, cudaStream_t st) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (a.tokens < 0) return fail(HE_ERR_INVALID_ARG, "%s %d < 0", tokens_name, a.tokens);
+  if (a.keys < 0) return fail(HE_ERR_INVALID_ARG, "max_kv_len %d < 0", a.keys);
+  if (a.tokens > kMaxTokens) return fail(HE_ERR_UNSUPPORTED, "%s %d > 2^24", tokens_name, a.tokens);
+  if (a.keys > kMaxTokens) return fail(HE_ERR_UNSUPPORTED, "max_kv_len %d > 2^24", a.keys);
+  if (int rc = check_mod(mod, cfg->head_dim, &a.scale_log2, &a.cap_log2, &a.inv_cap, &a.window, &a.slopes)) return rc;
+  a.near_end = a.inv_cap >= kPtNearInv && a.inv_cap <= kPtNearMost ? kPtNearEnd : -1.f;
+  if (a.tokens == 0) return HE_OK;
+  if (!q || !out || !a.lens || !a.kv_lens || (a.keys > 0 && (!k || !v))) return fail(HE_ERR_INVALID_ARG, "q, k, v, out or a length is null");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+  const int es = esize_of(cfg->dtype);
+  if (int rc = check_strides("q", q_strides, 3, es)) return rc;
+  if (int rc = check_strides("k / v", kv_strides, 3, es)) return rc;
+  if (int rc = check_strides("out", out_strides, 3, es)) return rc;
+  const long long sizes[3] = {cfg->batch, (long long)cfg->n_kv_heads * cfg->group_size, a.tokens};
+  if (int rc = check_apart("out", out_strides, sizes, 3, cfg->head_dim)) return rc;
+  if (out == q || (a.keys > 0 && (out == k || out == v))) return fail(HE_ERR_INVALID_ARG, "out overlaps q, k or v");
+  a.q = q, a.k = k, a.v = v, a.out = out;
+  for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i], a.ks[i] = kv_strides[i], a.os[i] = out_strides[i];
+  a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype;
+  const bool tc = on_tensor_cores(a);
+  if (workspace != nullptr) {
+    if (int rc = prompt_splits(a, tc, &a.splits)) return rc;
+    if (prompt_part_bytes(a, a.splits) > workspace_bytes)
+      return fail(HE_ERR_WORKSPACE, "workspace of %zu bytes, %zu are needed", workspace_bytes, prompt_part_bytes(a, a.splits));
+    a.part = static_cast<float*>(workspace);
+  }
+  if (a.keys == 0) a.splits = 1;
+  if (int rc = launch_rows(a, tc && a.keys > 0, st)) return rc;
+  if (a.splits == 1) return HE_OK;
+  const long long ctas = ((long long)a.batch * a.n_kv_heads * a.group * a.tokens + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
+  return launch_pdl(prompt_join_kernel, dim3((unsigned)ctas), kJoinThreads, 0, true, st, a);
 }
 
 // Units that do not all run at once (two CTAs an SM) end evenly when the longest start first: 512 of 512 to 4096 slots 94 -> 85 us back to back. Known from the caller's mirror of the budgets; sorted again only when its contents
@@ -361,41 +339,31 @@ int he_rotate_step(const he_config* cfg, const he_rotary* rotary, const he_cache
 int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
                      const int64_t kv_strides[3], const int32_t* prompt_len, int32_t max_prompt_len, const int32_t* doc_start,
                      const int32_t* prefix_len, void* out, const int64_t out_strides[3], void* stream) {
-  if (int rc = check_config(cfg, true)) return rc;
-  if (max_prompt_len < 0) return fail(HE_ERR_INVALID_ARG, "max_prompt_len %d < 0", max_prompt_len);
-  if (max_prompt_len > kMaxTokens) return fail(HE_ERR_UNSUPPORTED, "max_prompt_len %d > 2^24", max_prompt_len);
   PromptArgs a{};
-  if (int rc = check_mod(mod, cfg->head_dim, &a.scale_log2, &a.cap_log2, &a.inv_cap, &a.window, &a.slopes)) return rc;
-  a.near_end = a.inv_cap >= kPtNearInv && a.inv_cap <= kPtNearMost ? kPtNearEnd : -1.f;
-  if (max_prompt_len == 0) return HE_OK;
-  if (!q || !k || !v || !out || !prompt_len) return fail(HE_ERR_INVALID_ARG, "q, k, v, out or prompt_len is null");
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
-  const int es = esize_of(cfg->dtype);
-  if (int rc = check_strides("q", q_strides, 3, es)) return rc;
-  if (int rc = check_strides("k / v", kv_strides, 3, es)) return rc;
-  if (int rc = check_strides("out", out_strides, 3, es)) return rc;
-  const long long sizes[3] = {cfg->batch, (long long)cfg->n_kv_heads * cfg->group_size, max_prompt_len};
-  if (int rc = check_apart("out", out_strides, sizes, 3, cfg->head_dim)) return rc;
-  if (out == q || out == k || out == v) return fail(HE_ERR_INVALID_ARG, "out overlaps q, k or v");
-  a.q = q, a.k = k, a.v = v, a.out = out;
-  for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i], a.ks[i] = kv_strides[i], a.os[i] = out_strides[i];
-  a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_prompt_len;
-  a.lens = prompt_len, a.doc_start = doc_start, a.prefix = prefix_len;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (a.dtype == HE_DTYPE_BF16 && a.d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr) {
-    PromptMaps maps;
-    if (prompt_tmap(q, a, a.qs, a.n_kv_heads * a.group, &maps.q) && prompt_tmap(k, a, a.ks, a.n_kv_heads, &maps.k) &&
-        prompt_tmap(v, a, a.ks, a.n_kv_heads, &maps.v)) {
-      const int rc = a.d <= 64 ? launch_prompt_tc<64>(a, maps, st) : launch_prompt_tc<128>(a, maps, st);
-      if (rc >= 0) return rc;
-    }
-  }
-  switch ((a.d + 63) / 64) {
-    case 1: return launch_prompt_fp32<1>(a, st);
-    case 2: return launch_prompt_fp32<2>(a, st);
-    case 3: return launch_prompt_fp32<3>(a, st);
-    default: return launch_prompt_fp32<4>(a, st);
-  }
+  a.tokens = a.keys = max_prompt_len, a.lens = a.kv_lens = prompt_len, a.doc_start = doc_start, a.prefix = prefix_len, a.splits = 1;
+  return attend_rows(a, cfg, mod, q, k, v, q_strides, kv_strides, out, out_strides, "max_prompt_len", nullptr, 0, static_cast<cudaStream_t>(stream));
+}
+
+size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, int32_t max_kv_len) {
+  if (check_config(cfg, true) || max_q_len < 1 || max_kv_len < 1 || max_q_len > kMaxTokens || max_kv_len > kMaxTokens) return 0;
+  PromptArgs a{};
+  a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_q_len, a.keys = max_kv_len;
+  int splits = 1;
+  if (prompt_splits(a, on_tensor_cores(a), &splits)) return 0;
+  return prompt_part_bytes(a, splits);
+}
+
+int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
+                    const int64_t kv_strides[3], const int32_t* q_len, int32_t max_q_len, const int32_t* kv_len, int32_t max_kv_len, const int32_t* q_pos,
+                    const int32_t* first_key, const int32_t* prefix_len, void* out, const int64_t out_strides[3], void* workspace, size_t workspace_bytes,
+                    void* stream) {
+  PromptArgs a{};
+  a.tokens = max_q_len, a.keys = max_kv_len, a.lens = q_len, a.kv_lens = kv_len, a.q_pos = q_pos, a.doc_start = first_key, a.prefix = prefix_len, a.splits = 1;
+  a.all = q_pos == nullptr;
+  if (q_pos == nullptr && (prefix_len != nullptr || (mod != nullptr && (mod->window != 0 || mod->slopes != nullptr))))
+    return fail(HE_ERR_INVALID_ARG, "a window, slopes or a prefix without q_pos: rows without positions see every key");
+  if (workspace != nullptr && !aligned16(workspace)) return fail(HE_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+  return attend_rows(a, cfg, mod, q, k, v, q_strides, kv_strides, out, out_strides, "max_q_len", workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out,

@@ -1,0 +1,174 @@
+// The cache of the full history, in pages: rows into it and back out (page_kernels.cuh), and a new token's attention over it (page_attend_kernels.cuh, and
+// attend_kernels.cuh for what that does not take). Host side of these calls.
+#include <cuda_runtime.h>
+
+#include <cmath>
+
+#include "attend_kernels.cuh"
+#include "common.cuh"
+#include "hashevict.h"
+#include "host_common.h"
+#include "page_kernels.cuh"
+
+using namespace he;
+
+int he::page_error_count() {
+  int n = 0;
+  return cudaMemcpyFromSymbol(&n, he::g_tc_error, sizeof(int)) == cudaSuccess ? n : -1;
+}
+
+namespace {
+
+int check_pages(const he_config* cfg, const he_pages* p) {
+  if (p == nullptr) return fail(HE_ERR_INVALID_ARG, "pages is null");
+  if (!p->k_pages || !p->v_pages || !p->page_table || !p->len) return fail(HE_ERR_INVALID_ARG, "pages has a null pointer");
+  if (!aligned16(p->k_pages) || !aligned16(p->v_pages)) return fail(HE_ERR_INVALID_ARG, "pages must be 16-byte aligned");
+  if (p->page_size < 16 || p->page_size > 128 || (p->page_size & (p->page_size - 1)) != 0)
+    return fail(HE_ERR_INVALID_ARG, "page_size %d is not 16, 32, 64 or 128", p->page_size);
+  if (p->n_pages < 0 || p->max_pages < 0) return fail(HE_ERR_INVALID_ARG, "n_pages %d / max_pages %d < 0", p->n_pages, p->max_pages);
+  if ((long long)p->max_pages * p->page_size > kMaxTokens) return fail(HE_ERR_UNSUPPORTED, "%d pages of %d tokens in a sequence: more than 2^24 tokens", p->max_pages, p->page_size);
+  if (p->eight_bit != 0 && p->eight_bit != 1) return fail(HE_ERR_INVALID_ARG, "eight_bit %d is not 0 or 1", p->eight_bit);
+  if (p->eight_bit) {
+    if (!p->k_scale || !p->v_scale) return fail(HE_ERR_INVALID_ARG, "8-bit pages without scales");
+    if (cfg->head_dim % 16 != 0) return fail(HE_ERR_UNSUPPORTED, "8-bit pages: head_dim %d is not a multiple of 16", cfg->head_dim);
+  }
+  return HE_OK;
+}
+
+template <int E, bool Q8>
+int launch_append(const AppendArgs& a, const he_rotary& r, int v, dim3 grid, int threads, bool hold, cudaStream_t st) {
+  constexpr int W = 16 / E;
+  auto as = [&](auto kernel) { return launch_pdl(kernel, grid, threads, 0, true, st, a, r); };
+  if (r.interleaved) return hold ? as(page_append_kernel<E, W, true, Q8, true>) : as(page_append_kernel<E, W, true, Q8, false>);
+  if (v == W) return hold ? as(page_append_kernel<E, W, false, Q8, true>) : as(page_append_kernel<E, W, false, Q8, false>);
+  return v == 4 ? as(page_append_kernel<E, 4, false, Q8, false>) : v == 2 ? as(page_append_kernel<E, 2, false, Q8, false>) : as(page_append_kernel<E, 1, false, Q8, false>);
+}
+
+// As many CTAs per unit as keep the grid within two per SM, at most 8 and no fewer than two tiles of tokens for each.
+template <int E, int GP>
+int launch_paged(const PagedAttendArgs& a, cudaStream_t st) {
+  const long long units = (long long)a.cfg.batch * a.cfg.n_kv_heads;
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  int S = 1;
+  while (S < 8 && 2 * S * units <= 2 * sms && 2 * S * 2 * kScoredSlots <= page_capacity(a.pages)) S *= 2;
+  const int stages = E == 4 && S * units <= sms && scored_smem(S, 2, a.cfg.group_size, a.cfg.head_dim) <= kAttendMaxSmem ? 2 : 1;
+  const size_t smem = scored_smem(S, stages, a.cfg.group_size, a.cfg.head_dim);
+  auto kernel = attend_scored_kernel<E, GP, true>;
+  if (int rc = set_smem(kernel, smem)) return rc;
+  cudaLaunchConfig_t lc{};
+  lc.gridDim = dim3((unsigned)(a.cfg.n_kv_heads * S), (unsigned)a.cfg.batch);
+  lc.blockDim = dim3(kAttendThreads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)S;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = S > 1 ? 2 : 1;
+  HE_CUDA_CHECK(cudaLaunchKernelEx(&lc, kernel, a, S, stages));
+  return HE_OK;
+}
+template <int E>
+int launch_paged(const PagedAttendArgs& a, cudaStream_t st) {
+  const int G = a.cfg.group_size;
+  return G == 1 ? launch_paged<E, 1>(a, st) : G == 2 ? launch_paged<E, 2>(a, st) : G <= 4 ? launch_paged<E, 4>(a, st) : launch_paged<E, 8>(a, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary* rotary, const void* k, const void* v, const int64_t kv_strides[3],
+                   const int32_t* new_len, int32_t max_new, void* stream) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (int rc = check_pages(cfg, pages)) return rc;
+  he_rotary none{};
+  if (rotary != nullptr)
+    if (int rc = check_rotary(rotary, cfg->head_dim)) return rc;
+  if (max_new < 0) return fail(HE_ERR_INVALID_ARG, "max_new %d < 0", max_new);
+  if (max_new == 0 || pages->max_pages == 0) return HE_OK;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(HE_ERR_INVALID_ARG, "k or v is null or not 16-byte aligned");
+  const int es = esize_of(cfg->dtype);
+  if (int rc = check_strides("k / v", kv_strides, 3, es)) return rc;
+  const he_rotary& r = rotary != nullptr ? *rotary : none;
+  AppendArgs a{};
+  a.pages = *pages, a.x[0] = k, a.x[1] = v, a.new_len = new_len, a.max_new = max_new, a.n_kv_heads = cfg->n_kv_heads, a.d = cfg->head_dim;
+  for (int i = 0; i < 3; ++i) a.strides[i] = kv_strides[i];
+  const int P = pages->page_size, V = rotary_piece(r, es);
+  a.units = rotary_units(r, cfg->head_dim, V);
+  const long long most = ((long long)max_new + P - 2) / P + 1;  // (they may begin on a page's last row)
+  a.tiles = (int)(most < pages->max_pages ? most : pages->max_pages);
+  const long long ctas = (long long)cfg->batch * a.tiles;
+  if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld pages in one call", ctas);
+  const int items = (max_new < P ? max_new : P) * a.units;  // of a page's new rows
+  const int each = (es == 2 ? kAppendPairs<2> : kAppendPairs<4>) / V;
+  const bool hold = V == 16 / es && items <= each * kAppendThreads;
+  const int wanted = hold ? (items + each - 1) / each : items, threads = wanted < kAppendThreads ? (wanted + 31) / 32 * 32 : kAppendThreads;
+  // Heads are shared out until there are enough CTAs for every SM, but a thread that has worked out its sines keeps at least four heads of a whole page.
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  const long long shares = (4LL * sms + ctas - 1) / ctas;
+  a.heads_per_cta = (int)((cfg->n_kv_heads + shares - 1) / shares);
+  const int least = max_new < P ? 1 : 4;
+  if (a.heads_per_cta < least) a.heads_per_cta = least;
+  if (a.heads_per_cta > cfg->n_kv_heads) a.heads_per_cta = cfg->n_kv_heads;
+  const dim3 grid((unsigned)ctas, (unsigned)((cfg->n_kv_heads + a.heads_per_cta - 1) / a.heads_per_cta));
+  if (grid.y > 65535) return fail(HE_ERR_UNSUPPORTED, "%d KV heads in one call", cfg->n_kv_heads);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (es == 2) return pages->eight_bit ? launch_append<2, true>(a, r, V, grid, threads, hold, st) : launch_append<2, false>(a, r, V, grid, threads, hold, st);
+  return pages->eight_bit ? launch_append<4, true>(a, r, V, grid, threads, hold, st) : launch_append<4, false>(a, r, V, grid, threads, hold, st);
+}
+
+int he_page_read(const he_config* cfg, const he_pages* pages, const int32_t* first, int32_t max_rows, void* k_out, void* v_out, const int64_t kv_strides[3],
+                 void* stream) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (int rc = check_pages(cfg, pages)) return rc;
+  if (max_rows < 0) return fail(HE_ERR_INVALID_ARG, "max_rows %d < 0", max_rows);
+  if (max_rows == 0 || pages->max_pages == 0) return HE_OK;
+  if (!k_out && !v_out) return fail(HE_ERR_INVALID_ARG, "neither k_out nor v_out is given");
+  if (!aligned16(k_out) || !aligned16(v_out)) return fail(HE_ERR_INVALID_ARG, "k_out or v_out is not 16-byte aligned");
+  if (k_out == v_out) return fail(HE_ERR_INVALID_ARG, "k_out and v_out overlap");
+  const int es = esize_of(cfg->dtype);
+  if (int rc = check_strides("k_out / v_out", kv_strides, 3, es)) return rc;
+  const long long sizes[3] = {cfg->batch, cfg->n_kv_heads, max_rows};
+  if (int rc = check_apart("k_out / v_out", kv_strides, sizes, 3, cfg->head_dim)) return rc;
+  if (cfg->batch > 65535) return fail(HE_ERR_UNSUPPORTED, "batch %d > 65535 in one call", cfg->batch);
+  ReadArgs a{};
+  a.pages = *pages, a.out[0] = k_out, a.out[1] = v_out, a.first = first, a.max_rows = max_rows, a.n_kv_heads = cfg->n_kv_heads, a.d = cfg->head_dim;
+  for (int i = 0; i < 3; ++i) a.strides[i] = kv_strides[i];
+  a.sides = k_out && v_out ? 2 : 1, a.side = k_out ? 0 : 1;
+  const long long chunks = (long long)max_rows * (cfg->head_dim * es / 16), ctas = (chunks + kReadThreads * kReadUnroll - 1) / (kReadThreads * kReadUnroll);
+  if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%d rows in one call", max_rows);
+  const long long heads = (long long)a.sides * cfg->n_kv_heads;
+  if (heads > 65535) return fail(HE_ERR_UNSUPPORTED, "%d KV heads in one call", cfg->n_kv_heads);
+  const dim3 grid((unsigned)ctas, (unsigned)heads, (unsigned)cfg->batch);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (es == 2)
+    return pages->eight_bit ? launch_pdl(page_read_kernel<2, true>, grid, kReadThreads, 0, true, st, a) : launch_pdl(page_read_kernel<2, false>, grid, kReadThreads, 0, true, st, a);
+  return pages->eight_bit ? launch_pdl(page_read_kernel<4, true>, grid, kReadThreads, 0, true, st, a) : launch_pdl(page_read_kernel<4, false>, grid, kReadThreads, 0, true, st, a);
+}
+
+size_t he_page_attend_workspace_bytes(const he_config* cfg, const he_pages* pages) {
+  if (check_config(cfg, true) || check_pages(cfg, pages)) return 0;
+  return 0;
+}
+
+int he_page_attend(const he_config* cfg, const he_pages* pages, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out, void* workspace,
+                   size_t workspace_bytes, void* stream) {
+  if (int rc = check_config(cfg, true)) return rc;
+  if (int rc = check_pages(cfg, pages)) return rc;
+  if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q or out is null or not 16-byte aligned");
+  if (cfg->batch > 65535) return fail(HE_ERR_UNSUPPORTED, "batch %d > 65535 in one call", cfg->batch);
+  PagedAttendArgs a{};
+  a.cfg = *cfg, a.pages = *pages, a.q = q, a.out = out;
+  if (int rc = check_mod(mod, cfg->head_dim, &a.mod.scale_log2, &a.mod.cap_log2, &a.mod.inv_cap, &a.mod.window, &a.mod.slopes)) return rc;
+  a.mod.first_pos = first_pos;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return pages->eight_bit ? launch_paged<1>(a, st) : cfg->dtype == HE_DTYPE_BF16 ? launch_paged<2>(a, st) : launch_paged<4>(a, st);
+}
+
+}  // extern "C"

@@ -1,5 +1,7 @@
 // he_attend_prompt: attention of prompts over themselves, out_i = sum_j softmax_j(x_ij) V_j with
 //   x_ij = cap(scale q_i . k_j) - slope |i - j|   for the j of one interval [lo_i, hi_i) per token (document, window, past, prefix).
+// he_attend_cross: the same for rows over keys of another length. Keys are numbered as the rows see them: key j is the one at position j + shift of its sequence,
+// where shift is the position of row 0, so it may be negative and nothing but addresses and the two ends of the keys depends on the shift.
 // One interval per row means that a tile of rows walks over one run of key tiles and compares column numbers only in those at the run's ends.
 // All kernels keep the running maximum, the sum of the weights and the unnormalised output of a row in fp32, in log2 units.
 //
@@ -19,6 +21,8 @@
 
 namespace he {
 
+constexpr int kPromptMaxKeys = 1 << 24;  // positions and distances are exact in fp32
+
 struct PromptArgs {
   const void *q, *k, *v;
   void* out;
@@ -31,19 +35,45 @@ struct PromptArgs {
   float scale_log2, cap_log2, inv_cap;  // scores in log2 units: scale_log2 * q.k, or cap_log2 * tanh(inv_cap * q.k)
   float near_end;  // kPtNearEnd where the near form of the tanh can be written for inv_cap, else -1
   int window;
+  // he_attend_cross (he_attend_prompt: keys = tokens, kv_lens = lens, no q_pos, all = 0, splits = 1)
+  int keys;                // max_kv
+  const int32_t* kv_lens;  // [B]
+  const int32_t* q_pos;    // [B] or null: position of row 0
+  int all;                 // rows see every key, not only those up to their own position
+  int splits;              // > 1: the keys of a tile are shared out, and `part` takes what each share gives
+  float* part;             // [splits][B][heads][tokens][d], then [splits][B][heads][tokens][2]: unnormalised outputs; maximum in log2 units and sum of the weights
 };
+
+// The keys of a sequence, numbered as its rows see them, are [-shift, end).
+struct PromptKeys {
+  int shift, end;
+};
+__device__ __forceinline__ PromptKeys prompt_keys(const PromptArgs& a, int s) {
+  PromptKeys k;
+  k.shift = a.q_pos != nullptr ? min(max(a.q_pos[s], -kPromptMaxKeys), kPromptMaxKeys) : 0;
+  k.end = min(max(a.kv_lens[s], 0), a.keys) - k.shift;
+  return k;
+}
+// Where share z of a row's partial result lies.
+__device__ __forceinline__ long long prompt_part_row(const PromptArgs& a, int z, int s, int head, int i) {
+  return (((long long)z * a.batch + s) * (a.n_kv_heads * a.group) + head) * a.tokens + i;
+}
+__device__ __forceinline__ float* prompt_part_ml(const PromptArgs& a, long long row) {
+  return a.part + (long long)a.splits * a.batch * (a.n_kv_heads * a.group) * a.tokens * a.d + 2 * row;
+}
 
 constexpr float kPromptLog2e = 1.4426950408889634f;
 
-// The keys that token i sees; empty for i >= n.
-__device__ __forceinline__ void prompt_interval(const PromptArgs& a, int s, int i, int n, int& lo, int& hi) {
+// The keys that row i sees; empty for i >= n.
+__device__ __forceinline__ void prompt_interval(const PromptArgs& a, int s, int i, int n, const PromptKeys& keys, int& lo, int& hi) {
   lo = 0, hi = 0;
   if (i >= n) return;
+  lo = -keys.shift;
   if (a.window > 0) lo = max(lo, i - a.window + 1);
-  if (a.doc_start != nullptr) lo = max(lo, a.doc_start[(long long)s * a.tokens + i]);
-  hi = i + 1;
-  if (a.prefix != nullptr) hi = max(hi, a.prefix[s]);
-  hi = min(hi, n);
+  if (a.doc_start != nullptr) lo = max(lo, min(max(a.doc_start[(long long)s * a.tokens + i], 0), kPromptMaxKeys) - keys.shift);
+  hi = a.all ? keys.end : i + 1;
+  if (a.prefix != nullptr) hi = max(hi, min(max(a.prefix[s], 0), kPromptMaxKeys) - keys.shift);
+  hi = min(hi, keys.end);
 }
 
 __device__ __forceinline__ void prompt_store(void* p, long long at, int dtype, float f) {
@@ -64,19 +94,19 @@ __device__ __forceinline__ void prompt_unpack(const uint4& chunk, float (&f)[16 
 // who wait meanwhile. Four rows over 2048 keys at d = 128 take 0.6 ms.
 constexpr int kPromptAgain = 4;
 template <int ES>
-static __device__ __noinline__ void prompt_compute_again(const PromptArgs& a, int s, int head, const int (&row)[kPromptAgain], int n, volatile int* beat) {
+static __device__ __noinline__ void prompt_compute_again(const PromptArgs& a, int s, int head, const int (&row)[kPromptAgain], int n, const PromptKeys& keys, volatile int* beat) {
   constexpr int EPC = 16 / ES, SLOTS = ES == 4 ? 2 : 1, RB = kPromptAgain;  // elements of a chunk; chunks of a lane (rows have up to 64)
   const uint32_t all_lanes = 0xFFFFFFFFu;
   const int lane = threadIdx.x & 31, kv = head / a.group, cpr = a.d / EPC;
   const int per = cpr < 32 ? 32 / cpr : 1, sub = cpr < 32 ? lane / cpr : 0, c = cpr < 32 ? lane % cpr : lane;
   auto chunk = [&](const void* p, long long at_row, int at) { return *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + at_row * ES + 16 * at); };
-  const long long q0 = s * a.qs[0] + head * a.qs[1], k0 = s * a.ks[0] + kv * a.ks[1];
+  const long long q0 = s * a.qs[0] + head * a.qs[1], k0 = s * a.ks[0] + kv * a.ks[1] + keys.shift * a.ks[2];
   const float slope = a.slopes != nullptr ? a.slopes[head] * kPromptLog2e : 0.f;
-  int lo[RB], hi[RB], begin = 0x7FFFFFFF, end = 0;
+  int lo[RB], hi[RB], begin = 0x7FFFFFFF, end = -0x7FFFFFFF;
   float m[RB], l[RB], o[RB][SLOTS][EPC];  // l: of this lane's keys; o: of this lane's chunks and keys
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
-    prompt_interval(a, s, row[b], n, lo[b], hi[b]);
+    prompt_interval(a, s, row[b], n, keys, lo[b], hi[b]);
     begin = min(begin, lo[b]), end = max(end, hi[b]);
     m[b] = -INFINITY, l[b] = 0.f;
 #pragma unroll
@@ -166,12 +196,12 @@ __device__ __forceinline__ uint32_t prompt_odd_bits(const uint4& chunk, int dtyp
 
 // The rows i0 + b of one head, b a bit of `again`, whose outputs are stored, hold a NaN and have a number for the sum of their weights; their tile has
 // multiplied the V rows [from, to). Computes those anew whose NaNs may come from rows that they hide. By a whole warp.
-static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s, int head, int i0, uint32_t again, int n, int from, int to, volatile int* beat = nullptr) {
+static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s, int head, int i0, uint32_t again, int n, const PromptKeys keys, int from, int to, volatile int* beat = nullptr) {
   constexpr int STEPS = 4;  // loads in flight
   const uint32_t all_lanes = 0xFFFFFFFFu;
   const int lane = threadIdx.x & 31, kv = head / a.group, es = esize_of(a.dtype), cpr = a.d * es / 16;  // (16-byte chunks of a row: up to 64)
   const int per = cpr < 32 ? 32 / cpr : 1, sub = cpr < 32 ? lane / cpr : 0, c = cpr < 32 ? lane % cpr : lane;  // rows at a time; this lane's row of them and chunk
-  const char* v = static_cast<const char*>(a.v) + (s * a.ks[0] + kv * a.ks[1]) * es;
+  const char* v = static_cast<const char*>(a.v) + (s * a.ks[0] + kv * a.ks[1] + keys.shift * a.ks[2]) * es;
   const char* out = static_cast<const char*>(a.out) + (s * a.os[0] + head * a.os[1]) * es;
   auto odd = [&](const char* p, long long stride, int row, int chunk, bool nan_only) -> uint32_t {
     return chunk < cpr ? prompt_odd_bits(*reinterpret_cast<const uint4*>(p + row * stride * es + 16 * chunk), a.dtype, nan_only) : 0u;
@@ -181,13 +211,14 @@ static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s
     if (beat != nullptr && (step & 63) == 0 && lane == 0) *beat = *beat + 1;
   };
   int lo, hi;
-  prompt_interval(a, s, i0 + lane, n, lo, hi);
+  prompt_interval(a, s, i0 + lane, n, keys, lo, hi);
   bool mine = (again >> lane) & 1u;
   // The last row behind what they see, and the first before it, that is not all numbers.
   const int begin = __reduce_min_sync(all_lanes, mine ? hi : to), end = __reduce_max_sync(all_lanes, mine ? lo : from);
-  int last = -1, first = 0x7FFFFFFF, step = 0;
-  for (int j = to; j > begin && last < 0; j -= STEPS * per) {
-    int found = -1;
+  constexpr int kNone = -0x7FFFFFFF;
+  int last = kNone, first = 0x7FFFFFFF, step = 0;
+  for (int j = to; j > begin && last == kNone; j -= STEPS * per) {
+    int found = kNone;
 #pragma unroll
     for (int u = 0; u < STEPS; ++u) {
       const int row = j - 1 - u * per - sub;
@@ -210,7 +241,7 @@ static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s
   again = __ballot_sync(all_lanes, mine);
   if (again == 0u) return;
   // Channels that are NaN in rows that all the others see too, from the last on until they explain every output.
-  const int seen_begin = __reduce_max_sync(all_lanes, mine ? lo : 0), seen_end = __reduce_min_sync(all_lanes, mine ? hi : 0x7FFFFFFF);
+  const int seen_begin = __reduce_max_sync(all_lanes, mine ? lo : -0x7FFFFFFF), seen_end = __reduce_min_sync(all_lanes, mine ? hi : 0x7FFFFFFF);
   uint32_t want[2] = {0u, 0u}, have[2] = {0u, 0u}, known[2] = {0u, 0u};
   for (uint32_t rest = again; rest != 0u; rest &= rest - 1u)
 #pragma unroll
@@ -243,8 +274,8 @@ static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s
       ++rows;
     }
     if (rows == kPromptAgain || (rest == 0u && rows > 0)) {
-      if (es == 2) prompt_compute_again<2>(a, s, head, row, n, beat);
-      else prompt_compute_again<4>(a, s, head, row, n, beat);
+      if (es == 2) prompt_compute_again<2>(a, s, head, row, n, keys, beat);
+      else prompt_compute_again<4>(a, s, head, row, n, keys, beat);
       rows = 0;
     }
   }
@@ -284,7 +315,8 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
   constexpr int UNROLL = R == 1 ? 8 : 2;  // one row has few loads in flight otherwise
   const int d = a.d, pitch = d + 4, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
   const int heads = a.n_kv_heads * a.group;
-  const int head = blockIdx.x % heads, s = (blockIdx.x / heads) % a.batch, tile = tiles - 1 - blockIdx.x / heads / a.batch;
+  const int share = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
+  const int head = item % heads, s = (item / heads) % a.batch, tile = tiles - 1 - item / heads / a.batch;
   const int kv = head / a.group, i0 = tile * 16 * R;
   float* qs = psm_;                // [16 R][d + 4]
   float* ks = qs + 16 * R * pitch; // [64][d + 4]
@@ -294,16 +326,17 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
   griddep_wait();
   const int n = min(max(a.lens[s], 0), a.tokens);
   if (i0 >= n) return;
-  if (tid == 0) run[0] = 0x7FFFFFFF, run[1] = 0;
+  const PromptKeys keys = prompt_keys(a, s);
+  if (tid == 0) run[0] = 0x7FFFFFFF, run[1] = -0x7FFFFFFF;
   int lo[R], hi[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) prompt_interval(a, s, i0 + R * ty + r, n, lo[r], hi[r]);
+  for (int r = 0; r < R; ++r) prompt_interval(a, s, i0 + R * ty + r, n, keys, lo[r], hi[r]);
   __syncthreads();
   if (tx == 0)
 #pragma unroll
     for (int r = 0; r < R; ++r)
       if (lo[r] < hi[r]) atomicMin(&run[0], lo[r]), atomicMax(&run[1], hi[r]);
-  const long long q0 = s * a.qs[0] + head * a.qs[1], k0 = s * a.ks[0] + kv * a.ks[1];
+  const long long q0 = s * a.qs[0] + head * a.qs[1], k0 = s * a.ks[0] + kv * a.ks[1] + keys.shift * a.ks[2];
   const int es = esize_of(a.dtype), cpr = d * es / 16;  // 16-byte chunks of a row
   auto chunk = [&](const void* p, long long row_at, int c) {
     return __ldg(reinterpret_cast<const uint4*>(static_cast<const char*>(p) + row_at * es) + c);
@@ -321,7 +354,11 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
     for (int c = 0; c < 4 * NQ; ++c) o[r][c] = 0.f;
   }
   __syncthreads();
-  const int j_begin = run[0], j_end = run[1];  // (nothing ahead of the first key that a row sees is read)
+  int j_begin = run[0], j_end = run[1];  // (nothing ahead of the first key that a row sees is read)
+  if (a.splits > 1 && j_begin < j_end) {  // this share's blocks
+    const int blocks = (j_end - j_begin + 63) / 64, from = (int)((long long)blocks * share / a.splits), to = (int)((long long)blocks * (share + 1) / a.splits);
+    j_end = min(j_begin + 64 * to, j_end), j_begin += 64 * from;
+  }
   const int r_first = tid / cpr, c_first = tid % cpr, r_step = kPromptThreads / cpr, c_step = kPromptThreads % cpr;
   const bool async = a.dtype == HE_DTYPE_F32;
   auto fetch = [&](int j0, int stage) {
@@ -330,13 +367,13 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
 #pragma unroll 4
     for (int r = r_first, c = c_first; r < 64;) {
       const int j = j0 + r;
-      const long long at = k0 + (j < n ? j : 0) * a.ks[2];
+      const long long at = k0 + (j < keys.end ? j : -keys.shift) * a.ks[2];
       if (async) {
-        prompt_copy16(kt + r * pitch + 4 * c, static_cast<const float*>(a.k) + at + 4 * c, j < n);
-        prompt_copy16(vt + r * d + 4 * c, static_cast<const float*>(a.v) + at + 4 * c, j < n);
+        prompt_copy16(kt + r * pitch + 4 * c, static_cast<const float*>(a.k) + at + 4 * c, j < keys.end);
+        prompt_copy16(vt + r * d + 4 * c, static_cast<const float*>(a.v) + at + 4 * c, j < keys.end);
       } else {
         uint4 k4 = make_uint4(0u, 0u, 0u, 0u), v4 = k4;
-        if (j < n) k4 = chunk(a.k, at, c), v4 = chunk(a.v, at, c);
+        if (j < keys.end) k4 = chunk(a.k, at, c), v4 = chunk(a.v, at, c);
         store_chunk(kt + r * pitch, k4, c, HE_DTYPE_BF16);
         store_chunk(vt + r * d, v4, c, HE_DTYPE_BF16);
       }
@@ -432,6 +469,19 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
     }
     __syncthreads();  // the tile has been read
   }
+  if (a.splits > 1) {  // (hidden values: prompt_join_kernel)
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int i = i0 + R * ty + r;
+      if (i >= n) continue;
+      const long long at = prompt_part_row(a, share, s, head, i);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+        if (64 * q + 4 * tx < d) *reinterpret_cast<float4*>(a.part + at * d + 64 * q + 4 * tx) = make_float4(o[r][4 * q], o[r][4 * q + 1], o[r][4 * q + 2], o[r][4 * q + 3]);
+      if (tx == 0) *reinterpret_cast<float2*>(prompt_part_ml(a, at)) = make_float2(m[r], l[r]);
+    }
+    return;
+  }
   uint32_t again = 0u;  // rows of this warp with a NaN that a score does not explain
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -452,7 +502,7 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
       if ((odd >> (16 * w)) & 0xFFFFu) again |= 1u << (R * w + r);
   }
   __syncwarp();
-  if (again != 0u) prompt_rows_again(a, s, head, i0 + R * (tid - lane) / 16, again, n, j_begin, min(j_begin + (j_end - j_begin + 63) / 64 * 64, n));
+  if (again != 0u) prompt_rows_again(a, s, head, i0 + R * (tid - lane) / 16, again, n, keys, j_begin, min(j_begin + (j_end - j_begin + 63) / 64 * 64, keys.end));
 }
 
 // ------------------------------------------------------------------------------------------------ tensor cores
@@ -500,7 +550,8 @@ struct PromptMaps {
 // never multiplied), how many keys of the last block lie within the prompt, and per tile the blocks of keys [jb, je) that it needs and at
 // which steps from the last of them on, [all_from, all_to), its rows see every key of the block.
 struct PtItem {
-  int some, s, n, p, tok0, base, last_rows;
+  int some, s, n, p, tok0, base, last_rows, share;
+  PromptKeys keys;
   int jb[2], je[2], all_from[2], all_to[2];
 };
 
@@ -740,14 +791,14 @@ __device__ __forceinline__ bool pt_wait(uint32_t bar, uint32_t parity, volatile 
 }
 
 // The same for the roles beside the softmax, what follows the first poll in one place (for each kernel, next to its code: one place for all costs up to 2 %).
-template <int D, bool CAP, bool BIAS>
+template <int D, bool CAP, bool BIAS, bool SPLIT>
 static __device__ __noinline__ bool pt_wait_far(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   return pt_wait_on(bar, parity, abort_flag, beat);
 }
-template <int D, bool CAP, bool BIAS>
+template <int D, bool CAP, bool BIAS, bool SPLIT>
 __device__ __forceinline__ bool pt_wait_small(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)), 1)) return true;
-  return pt_wait_far<D, CAP, BIAS>(bar, parity, abort_flag, beat);
+  return pt_wait_far<D, CAP, BIAS, SPLIT>(bar, parity, abort_flag, beat);
 }
 
 // The grid's next waiting CTA, cancelled and taken over: asked for by one lane, answered in 16 bytes of shared memory.
@@ -785,7 +836,7 @@ __device__ __forceinline__ bool pt_read_work(uint32_t answer, int& cta) {
 // At D = 64 a quarter of tensor memory (columns 384 to 511) is not used: P lies where S was, and the next S of a tile waits for it.
 // Tried and slower: blocks of 64 keys with two places for S (0.90 PFLOP/s), one warp that polls both tiles for whichever is ready (0.81), weights handed over
 // in two or four parts, 208 / 80 registers (more spills in the softmax).
-template <int D, bool CAP, bool BIAS>
+template <int D, bool CAP, bool BIAS, bool SPLIT>
 __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_constant__ PromptArgs a, const int tiles, const int by_heads,
                                                                    const __grid_constant__ PromptMaps maps) {
   using T = PromptTc<D>;
@@ -836,7 +887,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
     if (lane == 0) mbar_arrive(smem_u32(&iempty_s[k & 1]));
   };
   auto read_item = [&](int k, PtItem& w) -> bool {
-    if (!pt_wait_small<D, CAP, BIAS>(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat)) return false;
+    if (!pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat)) return false;
     w = item_s[k & 1];
     if (w.some == 0) return false;
     give_item(k);
@@ -856,7 +907,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       const int i = tok_of(w, t) + row, head = head_of(w, t), steps = w.je[t] - w.jb[t];
       const int all_from = w.all_from[t], all_to = w.all_to[t];
       int lo, hi, j0 = w.base + w.je[t] * kPtTile;  // the block's first key
-      prompt_interval(a, w.s, i, w.n, lo, hi);
+      prompt_interval(a, w.s, i, w.n, w.keys, lo, hi);
       const float slope = BIAS ? a.slopes[head] * kPromptLog2e : 0.f;
       float m = -INFINITY, l = 0.f;
       for (int it = 0; it < steps; ++it, ++blocks) {
@@ -1008,6 +1059,25 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       if (ok && steps > 0) ok = pt_wait(smem_u32(&odone_s[t]), outputs++ & 1, abort_flag, beat);
       if (!ok) break;
       tc_fence_after();
+      if (SPLIT) {  // what this share gives, relative to its own maximum
+        const long long at = prompt_part_row(a, w.share, w.s, head, i);
+        float* part = a.part + at * a.d;
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32] = {};
+          if (steps > 0) {
+            tc_ld32(o_t + c, o);
+            tc_wait_ld();
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            if (i < w.n && c + e < a.d) *reinterpret_cast<uint4*>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+        if (i < w.n) *reinterpret_cast<float2*>(prompt_part_ml(a, at)) = make_float2(m, m != -INFINITY ? l : 0.f);
+        tc_fence_before();
+        give_item(k);
+        continue;
+      }
       const float inv = m != -INFINITY ? 1.f / l : 0.f;  // (scores of -inf alone: pt_ex2_fma leaves 2^-125 of their weights)
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (w.s * a.os[0] + head * a.os[1] + i * a.os[2]);
       const bool none = inv == 0.f;  // (a row that sees nothing: zeros)
@@ -1034,7 +1104,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       const bool bad = !none && l == l && pt_max(nan[0], nan[1]) != pt_max(nan[0], nan[1]);
       const uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
       __syncwarp();
-      if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, w.base + w.jb[t] * kPtTile, min(w.base + w.je[t] * kPtTile, w.n), beat);
+      if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, w.keys, w.base + w.jb[t] * kPtTile, min(w.base + w.je[t] * kPtTile, w.keys.end), beat);
       tc_fence_before();
       give_item(k);
     }
@@ -1049,7 +1119,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           if (ok && w.je[t] > w.jb[t]) {
-            if (queries[t] > 0) ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
+            if (queries[t] > 0) ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
             if (!ok) break;
             if (lane == 0) {
               const uint32_t bar = smem_u32(&qfull_s[t]);
@@ -1062,12 +1132,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         const int j_begin = w.jb[0] == w.je[0] ? w.jb[1] : w.jb[1] == w.je[1] ? w.jb[0] : min(w.jb[0], w.jb[1]), j_end = max(w.je[0], w.je[1]);
         const int kv = head_of(w, 0) / a.group;
         const int blocks = j_end - j_begin, ask = max(blocks + 1 - kPtAsk, 0);
-        int at_key = w.base + j_end * kPtTile;  // of the V block
+        int at_key = w.base + w.keys.shift + j_end * kPtTile;  // of the V block: its position
         if (ok && lane == 0 && blocks == 0) mbar_arrive(smem_u32(&ask_s));
         for (int step = 0; ok && blocks > 0 && step <= blocks; ++step) {
           if (lane == 0 && step == ask) mbar_arrive(smem_u32(&ask_s));
           const uint32_t slot = used % NS;
-          if (used >= NS) ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
+          if (used >= NS) ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
           if (!ok) break;
           if (lane == 0) {
             const uint32_t bar = smem_u32(&full_s[slot]), at = ring + slot * 2 * T::kTileBytes;
@@ -1104,7 +1174,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll 1
         for (int j = j_end; j >= j_begin; --j) {
           // O += P V of block j, S of block j - 1, tile by tile
-          ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&full_s[slot]), lap, abort_flag, beat);
+          ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&full_s[slot]), lap, abort_flag, beat);
           if (!ok) break;
           const int rows = w.last_rows;  // (of block j_end - 1; all others are full)
           if (__builtin_expect(j + 1 == j_end && rows < kPtTile, 0)) {  // V rows behind the prompt's end hold anything: zeros
@@ -1120,7 +1190,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             const int t_begin = t ? w.jb[1] : w.jb[0], t_end = t ? w.je[1] : w.je[0];
             const uint32_t s_at = tmem + t * kPtTile;
             if (j >= t_begin && j < t_end) {
-              ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&pfull_s[t]), (taken >> t) & 1, abort_flag, beat);
+              ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&pfull_s[t]), (taken >> t) & 1, abort_flag, beat);
               if (!ok) break;
               taken ^= 1u << t;
               tc_fence_after();
@@ -1131,7 +1201,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             }
             if (j > t_begin && j <= t_end) {
               if (j == t_end) {
-                ok = pt_wait_small<D, CAP, BIAS>(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
+                ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
                 if (!ok) break;
                 queries ^= 1u << t;
               }
@@ -1161,7 +1231,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       uint32_t asked = 0;
       bool ok = true;
       auto hand_over = [&](const PtItem& w) {
-        if (k >= 2) ok = ok && pt_wait_small<D, CAP, BIAS>(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
+        if (k >= 2) ok = ok && pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
         if (!ok) return;
         if (lane == 0) {
           item_s[k & 1] = w;
@@ -1172,19 +1242,23 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       };
       PtItem w;
       while (ok) {
-        w.some = 1, w.p = cta % per, w.s = (cta / per) % a.batch;
-        const int tile = tiles - 1 - cta / per / a.batch;
+        int item = cta;
+        w.some = 1, w.share = 0;
+        if (SPLIT) w.share = cta % a.splits, item = cta / a.splits;
+        w.p = item % per, w.s = (item / per) % a.batch;
+        const int tile = tiles - 1 - item / per / a.batch;
         w.tok0 = by_heads ? tile * kPtTile : tile * 2 * kPtTile;
         w.n = min(max(a.lens[w.s], 0), a.tokens);
         if (w.tok0 < w.n) {
+          w.keys = prompt_keys(a, w.s);
           w.base = 0x7FFFFFFF;
           for (int t = 0; t < 2; ++t) {
-            int first = 0x7FFFFFFF, end = 0, all_lo = 0, all_hi = 0x7FFFFFFF;  // what its rows see, any and all of them
+            int first = 0x7FFFFFFF, end = -0x7FFFFFFF, all_lo = -0x7FFFFFFF, all_hi = 0x7FFFFFFF;  // what its rows see, any and all of them
 #pragma unroll 1
             for (int r = 0; r < kPtTile / 32; ++r) {
               const int i = tok_of(w, t) + 32 * r + lane;
               int lo, hi;
-              prompt_interval(a, w.s, i, w.n, lo, hi);
+              prompt_interval(a, w.s, i, w.n, w.keys, lo, hi);
               if (lo < hi) first = min(first, lo), end = max(end, hi);
               if (i < w.n) all_lo = max(all_lo, lo < hi ? lo : 0x7FFFFFFF), all_hi = min(all_hi, hi);
             }
@@ -1192,21 +1266,32 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             w.all_from[t] = __reduce_min_sync(0xFFFFFFFFu, all_hi), w.all_to[t] = __reduce_max_sync(0xFFFFFFFFu, all_lo);
             w.jb[t] = first, w.je[t] = end, w.base = min(w.base, first);
           }
-          w.last_rows = w.n - w.base - (max(w.je[0], w.je[1]) - w.base + kPtTile - 1) / kPtTile * kPtTile + kPtTile;
           for (int t = 0; t < 2; ++t) {
-            const bool any = w.je[t] > 0;
+            const bool any = w.jb[t] < w.je[t];
             w.jb[t] = any ? (w.jb[t] - w.base) / kPtTile : 0, w.je[t] = any ? (w.je[t] - w.base + kPtTile - 1) / kPtTile : 0;
             w.all_from[t] = w.je[t] - max(w.all_from[t] - w.base, 0) / kPtTile;
-            w.all_to[t] = w.je[t] - (int)(((unsigned)(w.all_to[t] - w.base) + kPtTile - 1) / kPtTile);
+            w.all_to[t] = w.je[t] - (int)(((unsigned)w.all_to[t] - (unsigned)w.base + kPtTile - 1) / kPtTile);
           }
+          if (SPLIT) {  // this share's blocks, of those that either tile needs
+            const bool one = w.jb[0] < w.je[0], two = w.jb[1] < w.je[1];
+            const int begin = one && two ? min(w.jb[0], w.jb[1]) : one ? w.jb[0] : w.jb[1], blocks = max(w.je[0], w.je[1]) - begin;
+            const int from = begin + (int)((long long)blocks * w.share / a.splits), to = begin + (int)((long long)blocks * (w.share + 1) / a.splits);
+            for (int t = 0; t < 2; ++t) {
+              const int end = min(w.je[t], to), less = w.je[t] - end;
+              w.jb[t] = max(w.jb[t], from), w.je[t] = end;
+              w.all_from[t] -= less, w.all_to[t] -= less;
+              if (w.jb[t] >= w.je[t]) w.jb[t] = w.je[t] = 0;
+            }
+          }
+          w.last_rows = w.keys.end - w.base - (max(w.je[0], w.je[1]) - 1) * kPtTile;
           hand_over(w);
           // not before this item is nearly done: a CTA that took the next one at once would be bound to it however long this one lasts
-          ok = ok && pt_wait_small<D, CAP, BIAS>(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
+          ok = ok && pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
         }
         if (!ok) break;
         if (lane == 0) pt_ask_work(answer, smem_u32(&work_s));
         ++asked;
-        if (!pt_wait_small<D, CAP, BIAS>(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
+        if (!pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
         const bool more = pt_read_work(answer, cta);
         __syncwarp();  // every lane has read the answer before the next one may be written
         if (!more) {
@@ -1224,6 +1309,63 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
   if (warp == kPtMmaWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ shares of the keys, joined
+//
+// A warp per row: the shares' outputs, weighted by 2^(m - M), over the weighted sum of their sums. A row whose output is a NaN that its sum does not explain
+// is computed once more, as the kernels above do.
+constexpr int kJoinThreads = 128;
+static __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const __grid_constant__ PromptArgs a) {
+  const int lane = threadIdx.x & 31, heads = a.n_kv_heads * a.group;
+  const long long item = (long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+  griddep_wait();
+  griddep_launch_dependents();
+  const int i = (int)(item % a.tokens), head = (int)(item / a.tokens % heads);
+  const long long sequence = item / a.tokens / heads;
+  if (sequence >= a.batch) return;
+  const int s = (int)sequence, n = min(max(a.lens[s], 0), a.tokens);
+  if (i >= n) return;
+  float m = -INFINITY, M = -INFINITY, l = 0.f, L = 0.f;
+  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // channels 4 lane + e, 128 + 4 lane + e
+  for (int z0 = 0; z0 < a.splits; z0 += 32) {
+    if (z0 + lane < a.splits) m = fmaxf(m, prompt_part_ml(a, prompt_part_row(a, z0 + lane, s, head, i))[0]);
+  }
+  M = m;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
+#pragma unroll 4
+  for (int z = 0; z < a.splits; ++z) {
+    const long long at = prompt_part_row(a, z, s, head, i);
+    const float2 ml = *reinterpret_cast<const float2*>(prompt_part_ml(a, at));
+    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+    L = fmaf(ml.y, f, L);
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      if (128 * w + 4 * lane < a.d) {
+        const float4 v = *reinterpret_cast<const float4*>(a.part + at * a.d + 128 * w + 4 * lane);
+        if (ml.x != -INFINITY) {  // (a share that saw nothing holds anything)
+          o[4 * w] = fmaf(v.x, f, o[4 * w]), o[4 * w + 1] = fmaf(v.y, f, o[4 * w + 1]);
+          o[4 * w + 2] = fmaf(v.z, f, o[4 * w + 2]), o[4 * w + 3] = fmaf(v.w, f, o[4 * w + 3]);
+        }
+      }
+  }
+  l = L != 0.f ? 1.f / L : 0.f;
+  const long long o0 = s * a.os[0] + head * a.os[1] + i * a.os[2];
+  bool bad = false;
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = 128 * w + 4 * lane + e;
+      const float f = L != 0.f ? o[4 * w + e] * l : 0.f;
+      if (c < a.d) prompt_store(a.out, o0 + c, a.dtype, f), bad |= f != f;
+    }
+  if (__any_sync(0xFFFFFFFFu, bad) && L == L) {
+    const PromptKeys keys = prompt_keys(a, s);
+    __syncwarp();
+    prompt_rows_again(a, s, head, i, 1u, n, keys, -keys.shift, keys.end);
   }
 }
 

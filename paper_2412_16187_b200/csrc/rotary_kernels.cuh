@@ -93,6 +93,30 @@ inline int rotary_units(const he_rotary& r, int d, int v) {
   return r.channels / 2 / v + (d - r.channels + 2 * v - 1) / (2 * v);
 }
 
+// The pairs of a thread's two pieces, turned. u: which pieces of the row; half: pairs of a row; turns: whether they hold any (half layout).
+template <int E, int V, bool INTER>
+__device__ __forceinline__ void rotary_turn(RotaryPiece<E, V>& p0, RotaryPiece<E, V>& p1, const float (&sn)[V], const float (&cs)[V], int u, int half, bool turns) {
+  if (!turns) return;
+  float x[V], y[V];
+  if (INTER) {  // pairs are neighbours: the first piece's, then the second's; those beyond r stay
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const int j = i / 2, k = (V + i) / 2;
+      const float a0 = p0.get(i), b0 = p0.get(i + 1), a1 = p1.get(i), b1 = p1.get(i + 1);
+      const bool in0 = V * u + j < half, in1 = V * u + k < half;
+      x[i] = in0 ? a0 * cs[j] - b0 * sn[j] : a0, x[i + 1] = in0 ? b0 * cs[j] + a0 * sn[j] : b0;
+      y[i] = in1 ? a1 * cs[k] - b1 * sn[k] : a1, y[i + 1] = in1 ? b1 * cs[k] + a1 * sn[k] : b1;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float a0 = p0.get(i), b0 = p1.get(i);
+      x[i] = a0 * cs[i] - b0 * sn[i], y[i] = b0 * cs[i] + a0 * sn[i];
+    }
+  }
+  p0.put(x), p1.put(y);
+}
+
 // grid.x: threads of (sequence, token, unit), grid.y: shares of the heads (q's first, then k's).
 template <int E, int V, bool INTER>
 __global__ void __launch_bounds__(kRotateThreads) rotate_kernel(const RotateArgs a, const __grid_constant__ he_rotary rot) {
@@ -121,27 +145,6 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_kernel(const RotateArgs
     sn[i] = 0.f, cs[i] = 1.f;
     if (V * u + i < half) rotary_sincos(rot, V * u + i, pos, sn[i], cs[i]);
   }
-  auto rotate = [&](Piece& p0, Piece& p1) {
-    if (!turns) return;
-    float x[V], y[V];
-    if (INTER) {  // pairs are neighbours: the first piece's, then the second's; those beyond r stay
-#pragma unroll
-      for (int i = 0; i < V; i += 2) {
-        const int j = i / 2, k = (V + i) / 2;
-        const float a0 = p0.get(i), b0 = p0.get(i + 1), a1 = p1.get(i), b1 = p1.get(i + 1);
-        const bool in0 = V * u + j < half, in1 = V * u + k < half;
-        x[i] = in0 ? a0 * cs[j] - b0 * sn[j] : a0, x[i + 1] = in0 ? b0 * cs[j] + a0 * sn[j] : b0;
-        y[i] = in1 ? a1 * cs[k] - b1 * sn[k] : a1, y[i + 1] = in1 ? b1 * cs[k] + a1 * sn[k] : b1;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float a0 = p0.get(i), b0 = p1.get(i);
-        x[i] = a0 * cs[i] - b0 * sn[i], y[i] = b0 * cs[i] + a0 * sn[i];
-      }
-    }
-    p0.put(x), p1.put(y);
-  };
   constexpr int UNROLL = 4;  // heads whose pieces are asked for before the first is used
   for (int h = h_begin; h < h_end; h += UNROLL) {
     Piece p0[UNROLL], p1[UNROLL];
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(kRotateThreads) rotate_kernel(const RotateArgs
     for (int i = 0; i < UNROLL; ++i)
       if (h + i < h_end) {
         const int w = h + i >= a.heads[0] ? 1 : 0, hh = w ? h + i - a.heads[0] : h + i;
-        rotate(p0[i], p1[i]);
+        rotary_turn<E, V, INTER>(p0[i], p1[i], sn, cs, u, half, turns);
         char* dst = static_cast<char*>(a.y[w]) + (s * a.out[w][0] + hh * a.out[w][1] + n * a.out[w][2]) * E;
         p0[i].store(dst + c0 * E);
         if (second) p1[i].store(dst + c1 * E);
