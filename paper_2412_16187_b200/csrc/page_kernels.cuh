@@ -180,10 +180,10 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
       if (!Q8) {
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) write(mine[k], x[0][k], dst[0], 1.f), write(mine[k], x[1][k], dst[1], 1.f);
-        continue;
-      }
+      } else {
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k) look(mine[k], 0, x[0][k]), look(mine[k], 1, x[1][k]);
+        for (int k = 0; k < ITEMS; ++k) look(mine[k], 0, x[0][k]), look(mine[k], 1, x[1][k]);
+      }
     } else {
       for (int item = tid; item < items; item += threads) {
         const AppendPlace p = place(item);
@@ -191,8 +191,8 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
         if (Q8) look(p, 0, x[0][0]), look(p, 1, x[1][0]);
         else write(p, x[0][0], dst[0], 1.f), write(p, x[1][0], dst[1], 1.f);
       }
-      if (!Q8) continue;
     }
+    if constexpr (!Q8) continue;
     top[0] = __reduce_max_sync(0xFFFFFFFFu, top[0]), top[1] = __reduce_max_sync(0xFFFFFFFFu, top[1]);
     if (threads > 32) {  // (by turns: one barrier a head)
       const int lane = tid & 31;

@@ -8,6 +8,7 @@
 #include "common.cuh"
 #include "hashevict.h"
 #include "host_common.h"
+#include "page_attend_kernels.cuh"
 #include "page_kernels.cuh"
 
 using namespace he;
@@ -76,6 +77,64 @@ template <int E>
 int launch_paged(const PagedAttendArgs& a, cudaStream_t st) {
   const int G = a.cfg.group_size;
   return G == 1 ? launch_paged<E, 1>(a, st) : G == 2 ? launch_paged<E, 2>(a, st) : G <= 4 ? launch_paged<E, 4>(a, st) : launch_paged<E, 8>(a, st);
+}
+
+// Tensor map of the rows of all pages of K or V: boxes of 64 bf16 channels, or of 64 or 128 codes, by a page's rows, at most 32. A map depends on the address and the
+// shape alone, so the last few are kept per thread (a decode loop asks for the same ones at every token).
+bool page_rows_tmap(const void* base, long long rows, int d, int box_rows, bool codes, CUtensorMap* out) {
+  struct Entry {
+    const void* base;
+    long long rows;
+    int d, box_rows, codes;
+    CUtensorMap map;
+  };
+  constexpr int kEntries = 128;
+  thread_local Entry known[kEntries] = {};
+  Entry& e = known[(reinterpret_cast<uintptr_t>(base) >> 9) * 0x9E3779B97F4A7C15ull >> 57];
+  if (e.base != base || e.rows != rows || e.d != d || e.box_rows != box_rows || e.codes != (int)codes) {
+    const EncodeTiledFn encode = tmap_encoder();
+    if (encode == nullptr || env_flag_set<5>("HE_DISABLE_TMA")) return false;
+    const int wide = codes && d > 64;
+    const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)d * (codes ? 1 : 2)};
+    const cuuint32_t box[2] = {wide ? 128u : 64u, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    if (encode(&e.map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, codes && !wide ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+      e.base = nullptr;
+      return false;
+    }
+    e.base = base, e.rows = rows, e.d = d, e.box_rows = box_rows, e.codes = codes;
+  }
+  *out = e.map;
+  return true;
+}
+
+template <int D, bool Q8, int NBOX, bool LO, bool FOLD>
+int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  auto kernel = page_attend_kernel<D, Q8, NBOX, LO, FOLD>;
+  static_assert(1024 + kPageWarps * (kPageRing + kMaxGroup * (D + 2) * sizeof(float)) <= 227 * 1024 - 1536, "rings and pieces beside what the kernel holds itself");
+  const size_t smem = page_attend_smem(a.cfg.group_size, a.cfg.head_dim);
+  if (int rc = set_smem(kernel, smem)) return rc;
+  if (int rc = launch_pdl(kernel, dim3((unsigned)sms), kPageThreads, smem, true, st, a, part, maps)) return rc;
+  return sms > 1 ? launch_pdl(page_join_kernel, dim3((unsigned)sms - 1), kPageThreads, 0, true, st, a, static_cast<const float*>(part), sms) : HE_OK;
+}
+template <int D>
+int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
+  const bool two = a.pages.page_size < kPageGroup;
+  if (a.pages.eight_bit) {
+    if (a.cfg.dtype == HE_DTYPE_F32) return two ? launch_page_attend<D, true, 2, true, false>(a, part, maps, st) : launch_page_attend<D, true, 1, true, false>(a, part, maps, st);
+    return two ? launch_page_attend<D, true, 2, false, false>(a, part, maps, st) : launch_page_attend<D, true, 1, false, false>(a, part, maps, st);
+  }
+  if (a.cfg.group_size <= 4) return two ? launch_page_attend<D, false, 2, false, true>(a, part, maps, st) : launch_page_attend<D, false, 1, false, true>(a, part, maps, st);
+  return two ? launch_page_attend<D, false, 2, false, false>(a, part, maps, st) : launch_page_attend<D, false, 1, false, false>(a, part, maps, st);
+}
+
+// Whether the tensor cores serve a call (where the driver makes tensor maps): rows of bf16 or of codes up to 128 channels, few enough for a map's coordinates.
+bool page_tensor_cores(const he_config* cfg, const he_pages* p) {
+  return (p->eight_bit || cfg->dtype == HE_DTYPE_BF16) && cfg->head_dim <= 128 && (long long)p->n_pages * cfg->n_kv_heads * p->page_size < 0x7FFFFF00LL &&
+         getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
 }
 
 }  // namespace
@@ -153,8 +212,9 @@ int he_page_read(const he_config* cfg, const he_pages* pages, const int32_t* fir
 }
 
 size_t he_page_attend_workspace_bytes(const he_config* cfg, const he_pages* pages) {
-  if (check_config(cfg, true) || check_pages(cfg, pages)) return 0;
-  return 0;
+  int sms = 0;
+  if (check_config(cfg, true) || check_pages(cfg, pages) || !page_tensor_cores(cfg, pages) || sm_count(&sms)) return 0;
+  return 2 * (size_t)sms * page_part_floats(cfg->group_size, cfg->head_dim) * sizeof(float);
 }
 
 int he_page_attend(const he_config* cfg, const he_pages* pages, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out, void* workspace,
@@ -163,11 +223,22 @@ int he_page_attend(const he_config* cfg, const he_pages* pages, const he_score_m
   if (int rc = check_pages(cfg, pages)) return rc;
   if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q or out is null or not 16-byte aligned");
   if (cfg->batch > 65535) return fail(HE_ERR_UNSUPPORTED, "batch %d > 65535 in one call", cfg->batch);
+  if (pages->n_pages == 0 || pages->max_pages == 0) return fail(HE_ERR_INVALID_ARG, "no pages");
   PagedAttendArgs a{};
   a.cfg = *cfg, a.pages = *pages, a.q = q, a.out = out;
   if (int rc = check_mod(mod, cfg->head_dim, &a.mod.scale_log2, &a.mod.cap_log2, &a.mod.inv_cap, &a.mod.window, &a.mod.slopes)) return rc;
   a.mod.first_pos = first_pos;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (workspace != nullptr && !aligned16(workspace)) return fail(HE_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+  if (page_tensor_cores(cfg, pages)) {
+    const size_t need = he_page_attend_workspace_bytes(cfg, pages);
+    if (workspace_bytes < need || (need > 0 && workspace == nullptr)) return fail(HE_ERR_WORKSPACE, "workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+    const long long rows = (long long)pages->n_pages * cfg->n_kv_heads * pages->page_size;
+    const int box = pages->page_size < kPageGroup ? pages->page_size : kPageGroup;
+    PageMaps maps;
+    if (page_rows_tmap(pages->k_pages, rows, cfg->head_dim, box, pages->eight_bit, &maps.k) && page_rows_tmap(pages->v_pages, rows, cfg->head_dim, box, pages->eight_bit, &maps.v))
+      return cfg->head_dim <= 64 ? launch_page_attend<64>(a, static_cast<float*>(workspace), maps, st) : launch_page_attend<128>(a, static_cast<float*>(workspace), maps, st);
+  }
   return pages->eight_bit ? launch_paged<1>(a, st) : cfg->dtype == HE_DTYPE_BF16 ? launch_paged<2>(a, st) : launch_paged<4>(a, st);
 }
 
