@@ -114,11 +114,12 @@ int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& ma
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
   auto kernel = page_attend_kernel<D, Q8, NBOX, LO, FOLD>;
-  static_assert(1024 + kPageWarps * (kPageRing + kMaxGroup * (D + 2) * sizeof(float)) <= 227 * 1024 - 1536, "rings and pieces beside what the kernel holds itself");
-  const size_t smem = page_attend_smem(a.cfg.group_size, a.cfg.head_dim);
+  static_assert(1024 + kPageRings<Q8> + kPageWarps<Q8> * (kMaxGroup * (D + 2)) * sizeof(float) <= 227 * 1024 - (Q8 ? 2048 : 1024), "rings and pieces beside what the kernel holds itself");
+  const size_t smem = page_attend_smem<Q8>(a.cfg.group_size, a.cfg.head_dim);
   if (int rc = set_smem(kernel, smem)) return rc;
-  if (int rc = launch_pdl(kernel, dim3((unsigned)sms), kPageThreads, smem, true, st, a, part, maps)) return rc;
-  return sms > 1 ? launch_pdl(page_join_kernel, dim3((unsigned)sms - 1), kPageThreads, 0, true, st, a, static_cast<const float*>(part), sms) : HE_OK;
+  if (int rc = launch_pdl(kernel, dim3((unsigned)sms), 32 * kPageWarps<Q8>, smem, true, st, a, part, maps)) return rc;
+  if (sms == 1) return HE_OK;
+  return launch_pdl(page_join_kernel, dim3((unsigned)sms - 1), kPageJoinThreads, 0, true, st, part, a.out, sms, a.cfg.group_size, a.cfg.head_dim);
 }
 template <int D>
 int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
@@ -134,6 +135,7 @@ int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& ma
 // Whether the tensor cores serve a call (where the driver makes tensor maps): rows of bf16 or of codes up to 128 channels, few enough for a map's coordinates.
 bool page_tensor_cores(const he_config* cfg, const he_pages* p) {
   return (p->eight_bit || cfg->dtype == HE_DTYPE_BF16) && cfg->head_dim <= 128 && (long long)p->n_pages * cfg->n_kv_heads * p->page_size < 0x7FFFFF00LL &&
+         (long long)cfg->n_kv_heads * (page_capacity(*p) / kPageGroup + 1) <= 0x7FFFFFFFLL &&
          getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
 }
 
@@ -214,7 +216,7 @@ int he_page_read(const he_config* cfg, const he_pages* pages, const int32_t* fir
 size_t he_page_attend_workspace_bytes(const he_config* cfg, const he_pages* pages) {
   int sms = 0;
   if (check_config(cfg, true) || check_pages(cfg, pages) || !page_tensor_cores(cfg, pages) || sm_count(&sms)) return 0;
-  return 2 * (size_t)sms * page_part_floats(cfg->group_size, cfg->head_dim) * sizeof(float);
+  return page_workspace(sms, cfg->group_size, cfg->head_dim);
 }
 
 int he_page_attend(const he_config* cfg, const he_pages* pages, const he_score_mod* mod, const void* q, const int32_t* first_pos, float* out, void* workspace,
