@@ -50,7 +50,7 @@ __host__ __device__ inline long long page_capacity(const he_pages& p) { return (
 __device__ __forceinline__ int page_length(const he_pages& p, int s) { return (int)min((long long)max(p.len[s], 0), page_capacity(p)); }
 // The page that holds token j of sequence s, or -1: none that could be followed.
 __device__ __forceinline__ int page_of(const he_pages& p, int s, int j) {
-  const int page = __ldg(p.page_table + (long long)s * p.max_pages + j / p.page_size);
+  const int page = __ldg(p.page_table + (long long)s * p.max_pages + (j >> (31 - __clz(p.page_size))));  // (a power of two)
   return (unsigned)page < (unsigned)p.n_pages ? page : -1;
 }
 template <bool MOD>
@@ -669,7 +669,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const std
     auto row_of = [&](int j) -> long long {
       if constexpr (PAGED) {
         const int page = page_of(a.pages, seq, j);
-        return page < 0 ? -1 : ((long long)page * cfg.n_kv_heads + head) * a.pages.page_size + j % a.pages.page_size;
+        return page < 0 ? -1 : ((long long)page * cfg.n_kv_heads + head) * a.pages.page_size + (j & (a.pages.page_size - 1));
       } else {
         return j;
       }

@@ -18,14 +18,17 @@
 #pragma once
 #include "attend_kernels.cuh"
 #include "common.cuh"
+#include "tc_common.cuh"
 
 namespace he {
 
 constexpr int kPageGroup = 32;            // tokens of a group
-template <bool Q8>
-constexpr int kPageWarps = Q8 ? 12 : 8;
-template <bool Q8>
-constexpr int kPageRings = kPageWarps<Q8> * (Q8 ? 12 : 24) * 1024;  // bytes of a CTA's rings
+// Warps of a CTA: as many as hold their state in registers (168 each with 12 of them, 128 with 16). The loop waits for its own instructions, so more warps are faster: codes of
+// 128 channels took 82 us with 10 warps and 69 with 12 at 512 units of 2304 tokens, and 65 with 16, which spill, where 12 took 60; codes of 64 channels 73 with 12 and 65 with 16.
+template <int D, bool Q8>
+constexpr int kPageWarps = Q8 ? (D == 128 ? 12 : 16) : 8;
+template <int D, bool Q8>
+constexpr int kPageRings = kPageWarps<D, Q8> * (Q8 ? (D == 128 ? 12 : 8) : 24) * 1024;  // bytes of a CTA's rings
 
 struct PageMaps {
   alignas(64) CUtensorMap k, v;
@@ -33,12 +36,12 @@ struct PageMaps {
 
 template <int D, bool Q8>
 struct PageRing {
-  static constexpr int kRowBytes = Q8 ? D : 2 * D, kItemBytes = kPageGroup * kRowBytes, kBytes = kPageRings<Q8> / kPageWarps<Q8>, kBufs = kBytes / kItemBytes;
+  static constexpr int kRowBytes = Q8 ? D : 2 * D, kItemBytes = kPageGroup * kRowBytes, kBytes = kPageRings<D, Q8> / kPageWarps<D, Q8>, kBufs = kBytes / kItemBytes < 3 ? kBytes / kItemBytes : 3;
 };
 // Floats of a unit's piece: [G][d] outputs, [G] maxima in log2 units, [G] sums.
 __host__ __device__ inline int page_piece(int G, int d) { return G * d + (2 * G + 3) / 4 * 4; }
-template <bool Q8>
-inline size_t page_attend_smem(int G, int d) { return 1024 + kPageRings<Q8> + kPageWarps<Q8> * page_piece(G, d) * sizeof(float); }
+template <int D, bool Q8>
+inline size_t page_attend_smem(int G, int d) { return 1024 + kPageRings<D, Q8> + kPageWarps<D, Q8> * page_piece(G, d) * sizeof(float); }
 // What a CTA leaves for page_join_kernel: the unit whose first groups other CTAs have (-1: none), the unit whose last groups others have, then their pieces.
 struct PageRest {
   int unit[2];
@@ -65,6 +68,26 @@ static __device__ __noinline__ PageSpan page_span(const PagedAttendArgs& a, int 
 struct PageCursor {
   int s, h, g;
   PageSpan span;
+};
+
+__device__ __forceinline__ float page_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Pieces of a unit put together: maximum in log2 units, sum of the weights, four channels of the output.
+struct PageSum {
+  float M = -INFINITY, L = 0.f;
+  float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void add(float m, float l, const float4& o) {
+    const float top = fmaxf(M, m), ref = top == -INFINITY ? 0.f : top, f = page_ex2(M - ref), g = page_ex2(m - ref);
+    L = fmaf(l, g, L * f), M = top;
+    O.x = fmaf(o.x, g, O.x * f), O.y = fmaf(o.y, g, O.y * f), O.z = fmaf(o.z, g, O.z * f), O.w = fmaf(o.w, g, O.w * f);
+  }
+  __device__ __forceinline__ float4 result() const {
+    const float inv = L != 0.f ? 1.f / L : 0.f;
+    return make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
+  }
 };
 
 // How the line of groups is cut: into `parts` of `each` groups, the first `more` parts one more, no fewer than a group per warp in each.
@@ -140,11 +163,6 @@ __device__ __forceinline__ void page_find(const PagedAttendArgs& a, int each, co
   c.h = in / n, c.g = c.span.g0 + in % n;
 }
 
-__device__ __forceinline__ float page_ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void mma_f16_m16n8k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
@@ -162,6 +180,12 @@ __device__ __forceinline__ void mma_bf16_from_zero(float (&c)[4], uint32_t a0, u
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// Rows of 8 x 8 values of 16 bits become columns (lane 4 r + c holds values 2 c, 2 c + 1 of row r).
+__device__ __forceinline__ uint32_t half_turned(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 // Pairs of fp32 values, two to an instruction.
 __device__ __forceinline__ unsigned long long pair_of(float x, float y) {
@@ -196,15 +220,20 @@ __device__ __forceinline__ void half_split(float x, float y, uint32_t& hi, uint3
   lo = half_pair(x - h.x, y - h.y);
 }
 
+// A group under way: its unit, how far the query's token lies behind the group's first, which of its tokens are seen, whether it is the unit's first (1), last (2).
+struct PageNow {
+  int unit, away;
+  uint32_t seen;
+  int flags;
+};
+
 // NBOX: pages of a group (2 for pages of 16 tokens). LO: the queries come in fp32 (8-bit pages). FOLD: G <= 4 (bf16 pages).
 template <int D, bool Q8, int NBOX, bool LO, bool FOLD>
-__global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(const __grid_constant__ PagedAttendArgs a, float* part, const __grid_constant__ PageMaps maps) {
+__global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(const __grid_constant__ PagedAttendArgs a, float* part, const __grid_constant__ PageMaps maps) {
   using Ring = PageRing<D, Q8>;
-  constexpr int WARPS = kPageWarps<Q8>, THREADS = 32 * WARPS, NBUF = Ring::kBufs, ITEM = Ring::kItemBytes, GRP = kPageGroup, NH = Q8 ? 1 : D / 64, SLOTS = (NBUF + 1) / 2;
-  constexpr int NT = D / 8;  // output tiles of 8 channels
+  constexpr int WARPS = kPageWarps<D, Q8>, THREADS = 32 * WARPS, NBUF = Ring::kBufs, ITEM = Ring::kItemBytes, GRP = kPageGroup, NH = Q8 ? 1 : D / 64;
   extern __shared__ __align__(16) unsigned char page_smem_raw[];
   __shared__ __align__(8) unsigned long long ring_bar[WARPS][NBUF];
-  __shared__ float scale_s[WARPS][SLOTS][4];  // of the groups under way: K's of each box, V's of each
   __shared__ int ent_unit[2 * WARPS], ent_flag[2 * WARPS];
   __shared__ long long scan_s[WARPS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
@@ -214,7 +243,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
   unsigned char* ring = smem + warp * Ring::kBytes;
   const int per = page_piece(G, d);
   // pieces of units that began before a warp's first group, and of those that go on behind its last one: in the place of its ring
-  auto piece_of = [&](int e) { return reinterpret_cast<float*>((e & 1) ? smem + (e >> 1) * Ring::kBytes : smem + kPageRings<Q8> + (e >> 1) * per * sizeof(float)); };
+  auto piece_of = [&](int e) { return reinterpret_cast<float*>((e & 1) ? smem + (e >> 1) * Ring::kBytes : smem + kPageRings<D, Q8> + (e >> 1) * per * sizeof(float)); };
   auto full = [&](int b) { return (uint32_t)__cvta_generic_to_shared(&ring_bar[warp][b]); };
   if (lane == 0) {
 #pragma unroll
@@ -226,7 +255,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
   griddep_launch_dependents();
   // ---- the work: this CTA's part of the line, and where its warps begin
   PageTable<THREADS>& table = *reinterpret_cast<PageTable<THREADS>*>(smem);  // (the rings are not in use yet)
-  static_assert(sizeof(PageTable<THREADS>) <= kPageRings<Q8>, "the rings hold the table");
+  static_assert(sizeof(PageTable<THREADS>) <= kPageRings<D, Q8>, "the rings hold the table");
   const int each = (a.cfg.batch + THREADS - 1) / THREADS;
   const PageLine line = page_line<WARPS>(a, gridDim.x, each, scan_s, table, [&](int s) {
     if (s % (int)gridDim.x == (int)blockIdx.x)
@@ -239,9 +268,8 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
   const int some = (int)(line.begin(blockIdx.x + 1) - begin);  // groups of this CTA
   auto warp_begin = [&](int w) { return w * (some / WARPS) + min(w, some % WARPS); };
   const int groups = warp_begin(warp + 1) - warp_begin(warp), items = 2 * groups;
-  PageCursor cur{}, ask{};  // the group that is worked on, the one that is asked for next
-  if (groups > 0) page_find<WARPS>(a, each, table, begin + warp_begin(warp), cur);
-  ask = cur;
+  PageCursor ask{};  // the group that is asked for next
+  if (groups > 0) page_find<WARPS>(a, each, table, begin + warp_begin(warp), ask);
   __syncthreads();  // the table has been read
   auto advance = [&](PageCursor& c) {
     if (++c.g < c.span.g1) return;
@@ -253,6 +281,68 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
     }
     c.g = c.span.g0;
   };
+  // ---- the queries of a unit
+  const int my_head = FOLD ? gid & 3 : gid;
+  constexpr int NQ = Q8 ? D / 64 * 8 : D / 32 * 4;
+  uint32_t qf[NQ], ql[LO ? NQ : 1];
+  float slope[2] = {0.f, 0.f}, by[2] = {1.f, 1.f};  // of this lane's heads; by (8 bits): what makes a score of a product, or what its cap's tanh takes
+  uint4 raw[Q8 && LO ? D / 16 : D / 32];  // as they lie in memory
+  auto ask_q = [&](int unit) {
+    const long long at = ((long long)unit * G + my_head) * d;
+    if (a.mod.slopes != nullptr) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int g = !Q8 ? my_head : FOLD ? (2 * tig + k) & 3 : 2 * tig + k;
+        slope[k] = g < G ? a.mod.slopes[unit % H * G + g] * kLog2e : 0.f;
+      }
+    }
+    constexpr int PER = LO ? 4 : 8, EACH = Q8 ? 16 / PER : 1;  // channels of 16 bytes, such pieces in a lane's 16 channels
+#pragma unroll
+    for (int c = 0; c < (int)(sizeof(raw) / sizeof(uint4)); ++c) {
+      // 8 bits: 16 channels a lane and 64 (d is a multiple of 16); bf16: 8
+      const int ch = Q8 ? 16 * (D == 128 ? 2 * tig + c / EACH : tig) + c % EACH * PER : 8 * (2 * tig + (c & 1) + 8 * (c >> 1));
+      raw[c] = make_uint4(0u, 0u, 0u, 0u);
+      if (my_head < G && ch < d) raw[c] = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + (at + ch) * (LO ? 4 : 2));
+    }
+  };
+  auto take_q = [&]() {
+    if constexpr (!Q8) {
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) qf[4 * c] = raw[c].x, qf[4 * c + 1] = raw[c].y, qf[4 * c + 2] = raw[c].z, qf[4 * c + 3] = raw[c].w;
+    } else {
+      float f[NQ * 2];
+      uint32_t top = 0u;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+#pragma unroll
+        for (int e = 0; e < 16; e += LO ? 4 : 8) {
+          const uint4 t = raw[(16 * c + e) / (LO ? 4 : 8)];
+          const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+          for (int i = 0; i < (LO ? 4 : 8); ++i)
+            f[16 * c + e + i] = LO ? __uint_as_float(w[i % 4]) : __uint_as_float((i & 1) ? w[(i / 2) % 4] & 0xFFFF0000u : w[(i / 2) % 4] << 16);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NQ * 2; ++i) {
+        const uint32_t bits = __float_as_uint(f[i]) & 0x7FFFFFFFu;
+        top = max(top, bits < 0x7F800000u ? bits : 0u);
+      }
+      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+      const int k = top == 0u ? 0 : min(13 - ((int)(top >> 23) - 127), 126);  // the row times 2^k is below 2^14
+      const float up = __int_as_float((k + 127) << 23), down = __int_as_float((127 - k) << 23);
+      const float mine = (a.mod.cap_log2 > 0.f ? a.mod.inv_cap : a.mod.scale_log2) * down;  // of head gid
+#pragma unroll
+      for (int k = 0; k < 2; ++k) by[k] = __shfl_sync(0xFFFFFFFFu, mine, 4 * (2 * tig + k));
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        if constexpr (LO) half_split(f[2 * i] * up, f[2 * i + 1] * up, qf[i], ql[i]);
+        else qf[i] = half_pair(f[2 * i] * up, f[2 * i + 1] * up);
+      }
+    }
+  };
+  if (groups > 0) ask_q(ask.s * H + ask.h);
   // ---- copies. Lane i holds the page of box i & 1 of the group to be asked for, -1 where there is none, and fetches one of its scales.
   int page = -1;
   float scale = 0.f;
@@ -261,15 +351,12 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
     page = j < ask.span.hi ? page_of(pg, ask.s, j) : -1;
   };
   if (groups > 0) look_up();
+  PageNow now{}, next{};  // the group that is worked on, the last one whose V has been asked for
   const int none = pg.n_pages * H * P;  // a row behind all: zeros
-  int row[NBOX], ask_slot = 0;
+  int row[NBOX];
   // K (even t) or V of the next group into buffer b
   auto issue = [&](int t, int b) {
     const bool v = t & 1;
-    if (Q8 && !v && t > 0 && t <= items) {  // the scales of the group before have come
-      if (lane < 4) scale_s[warp][ask_slot][lane] = scale;
-      if (++ask_slot == SLOTS) ask_slot = 0;
-    }
     if (t >= items) return;
     if (!v) {
 #pragma unroll
@@ -293,76 +380,33 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
               "l"(map), "r"(h * 64), "r"(row[i]), "r"(full(b))
               : "memory");
     }
-    if (v && t + 1 < items) {
-      advance(ask);
-      look_up();
+    if (v) {
+      const int j0 = ask.g * GRP, lo = ask.span.lo - j0, hi = ask.span.hi - j0;
+      next.unit = ask.s * H + ask.h, next.away = hi - 1;
+      next.seen = (lo > 0 ? 0xFFFFFFFFu << lo : 0xFFFFFFFFu) & (hi < GRP ? (1u << hi) - 1u : 0xFFFFFFFFu);
+      next.flags = (ask.g == ask.span.g0 ? 1 : 0) | (ask.g + 1 == ask.span.g1 ? 2 : 0);
+      if (t + 1 < items) {
+        advance(ask);
+        look_up();
+      }
     }
   };
 #pragma unroll 1
   for (int t = 0; t < NBUF - 1; ++t) issue(t, t);
 
-  // ---- the queries of a unit
-  const int my_head = !Q8 && FOLD ? gid & 3 : gid;
-  constexpr int NQ = Q8 ? D / 64 * 8 : D / 32 * 4;
-  uint32_t qf[NQ], ql[LO ? NQ : 1];
-  float factor = a.mod.scale_log2, inv_cap = a.mod.inv_cap, slope = 0.f;
-  auto load_q = [&]() {
-    const long long at = (((long long)cur.s * H + cur.h) * G + my_head) * d;
-    slope = a.mod.slopes != nullptr && my_head < G ? a.mod.slopes[cur.h * G + my_head] * kLog2e : 0.f;
-    if constexpr (!Q8) {
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        uint4 t = make_uint4(0u, 0u, 0u, 0u);
-        const int chunk = 2 * tig + (c & 1) + 8 * (c >> 1);
-        if (my_head < G && chunk < d / 8) t = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + 2 * (at + 8 * chunk));
-        qf[4 * c] = t.x, qf[4 * c + 1] = t.y, qf[4 * c + 2] = t.z, qf[4 * c + 3] = t.w;
-      }
-    } else {
-      float f[NQ * 2];
-      uint32_t top = 0u;
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        const int c0 = 16 * (D == 128 ? 2 * tig + c : tig);  // (d is a multiple of 16)
-#pragma unroll
-        for (int e = 0; e < 16; e += LO ? 4 : 8) {
-          uint4 t = make_uint4(0u, 0u, 0u, 0u);
-          if (my_head < G && c0 < d) t = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + (at + c0 + e) * (LO ? 4 : 2));
-          const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-          for (int i = 0; i < (LO ? 4 : 8); ++i)
-            f[16 * c + e + i] = LO ? __uint_as_float(w[i % 4]) : __uint_as_float((i & 1) ? w[(i / 2) % 4] & 0xFFFF0000u : w[(i / 2) % 4] << 16);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < NQ * 2; ++i) {
-        const uint32_t bits = __float_as_uint(f[i]) & 0x7FFFFFFFu;
-        top = max(top, bits < 0x7F800000u ? bits : 0u);
-      }
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-      const int k = top == 0u ? 0 : min(13 - ((int)(top >> 23) - 127), 126);  // the row times 2^k is below 2^14
-      const float up = __int_as_float((k + 127) << 23), down = __int_as_float((127 - k) << 23);
-      factor = a.mod.scale_log2 * down, inv_cap = a.mod.inv_cap * down;
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        if constexpr (LO) half_split(f[2 * i] * up, f[2 * i + 1] * up, qf[i], ql[i]);
-        else qf[i] = half_pair(f[2 * i] * up, f[2 * i + 1] * up);
-      }
-    }
-  };
-  // Outputs of columns 2 tig, 2 tig + 1 of each tile as pairs; bf16: of rows gid, then of rows gid + 8.
-  constexpr int OW = Q8 ? 1 : 2;
-  float m = -INFINITY, l = 0.f;
-  unsigned long long o[NT][OW];
+  // bf16: outputs of columns 2 tig, 2 tig + 1 of each tile of 8 channels as pairs, of rows (heads) gid, then of rows gid + 8. 8 bits: of heads 2 tig, 2 tig + 1 as pairs, of rows
+  // (channels) gid, then gid + 8 of each tile of 16.
+  constexpr int NO = Q8 ? D / 16 : D / 8, HEADS = Q8 ? 2 : 1;  // heads of a lane
+  float m[HEADS], l[HEADS];
+  unsigned long long o[NO][2];
   auto clear = [&]() {
-    m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int k = 0; k < HEADS; ++k) m[k] = -INFINITY, l[k] = 0.f;
 #pragma unroll
-      for (int e = 0; e < OW; ++e) o[t][e] = 0ull;
+    for (int t = 0; t < NO; ++t) o[t][0] = o[t][1] = 0ull;
   };
   clear();
-  int buf = 0, slot = 0;
+  int buf = 0;
   uint32_t phase = 0;
   bool ok = true, fresh = true, begins = false;
   // the next item has landed; its predecessor's buffer, read by the whole warp, takes the item NBUF - 1 ahead
@@ -387,34 +431,148 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
   };
   // where chunk c of row r of an 8-bit tile lies
   auto code_at = [&](const unsigned char* tile, int r, int c) { return tile + r * D + 16 * (D == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)); };
+  // Rows of V that are hidden (weighted by zero) hold anything: zeros.
+  auto hide = [&](const unsigned char* tile) {
+    for (int i = lane; i < GRP * Ring::kRowBytes / 16; i += 32) {
+      const int r = Q8 ? i / (D / 16) : (i >> 3) % GRP;
+      if (((now.seen >> r) & 1u) == 0u) *reinterpret_cast<uint4*>(const_cast<unsigned char*>(tile) + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    fence_proxy_async();  // (the next copy into these rows comes after them)
+    __syncwarp();
+  };
 #pragma unroll 1
   for (int t = 0; t < items && ok; t += 2) {
-    if (fresh) load_q(), begins = cur.g == cur.span.g0, fresh = false;
-    const int j0 = cur.g * GRP, lo = cur.span.lo, hi = cur.span.hi;
-    float sa[4][4], sb[4][4];
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
-    {
-      const unsigned char* tile = step(t);
-      if constexpr (Q8) {
-        __syncwarp();
+    if constexpr (Q8) {  // (up to three items in a ring: the next group's have not been asked for yet)
+      static_assert(NBUF <= 3, "scales of one group at a time");
 #pragma unroll
-        for (int b = 0; b < NBOX; ++b) ks[b] = scale_s[warp][slot][b], vs[b] = scale_s[warp][slot][2 + b];
-        if (++slot == SLOTS) slot = 0;
+      for (int b = 0; b < NBOX; ++b) ks[b] = __shfl_sync(0xFFFFFFFFu, scale, b), vs[b] = __shfl_sync(0xFFFFFFFFu, scale, 2 + b);
+    }
+    const unsigned char* tile = step(t);  // (V of this group has been asked for by now, that of the next one not: that is another step)
+    now = next;
+    if (fresh) take_q(), begins = now.flags & 1, fresh = false;
+    const bool edge = now.seen != 0xFFFFFFFFu;
+    if constexpr (Q8) {
+      // S = K q^T: tokens 16 u + gid (+ 8), heads 2 tig, + 1
+      float x[2][2][2];
+      {
+        float c[2][4];
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c)
+        for (int w = 0; w < D / 64; ++w)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint4 kv = *reinterpret_cast<const uint4*>(code_at(tile, 8 * i + gid, D == 128 ? 2 * tig + c : tig));
-            const uint32_t w[4] = {kv.x, kv.y, kv.z, kv.w};
+          for (int u = 0; u < 2; ++u) {
+            const int ch = D == 128 ? 2 * tig + w : tig;
+            const uint4 k0 = *reinterpret_cast<const uint4*>(code_at(tile, 16 * u + gid, ch)), k1 = *reinterpret_cast<const uint4*>(code_at(tile, 16 * u + 8 + gid, ch));
+            const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const uint32_t a0 = qf[8 * c + 2 * u], a1 = LO ? ql[LO ? 8 * c + 2 * u : 0] : 0u, a2 = qf[8 * c + 2 * u + 1], a3 = LO ? ql[LO ? 8 * c + 2 * u + 1 : 0] : 0u;
-              const uint32_t b0 = e4m3_halves(w[u] & 0xFFFFu), b1 = e4m3_halves(w[u] >> 16);
-              if (c == 0 && u == 0) mma_f16_from_zero(sa[i], a0, a1, a2, a3, b0, b1);
-              else mma_f16_m16n8k16(sa[i], a0, a1, a2, a3, b0, b1);
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t a0 = e4m3_halves(w0[i] & 0xFFFFu), a1 = e4m3_halves(w1[i] & 0xFFFFu), a2 = e4m3_halves(w0[i] >> 16), a3 = e4m3_halves(w1[i] >> 16);
+              if (w == 0 && i == 0) mma_f16_from_zero(c[u], a0, a1, a2, a3, qf[0], qf[1]);
+              else mma_f16_m16n8k16(c[u], a0, a1, a2, a3, qf[8 * w + 2 * i], qf[8 * w + 2 * i + 1]);
+              if constexpr (LO) mma_f16_m16n8k16(c[u], a0, a1, a2, a3, ql[8 * w + 2 * i], ql[8 * w + 2 * i + 1]);
             }
           }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) x[u][r][k] = c[u][2 * r + k];
+      }
+      if (a.mod.cap_log2 > 0.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] = a.mod.cap_log2 * tanhf(x[i >> 2][(i >> 1) & 1][i & 1] * (by[i & 1] * ks[NBOX == 2 ? i >> 2 : 0]));
       } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] *= by[i & 1] * ks[NBOX == 2 ? i >> 2 : 0];
+      }
+      if (a.mod.slopes != nullptr) {
+        const float away = (float)(now.away - gid);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] = fmaf(-slope[i & 1], away - (float)(8 * (i >> 1)), x[i >> 2][(i >> 1) & 1][i & 1]);
+      }
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] = (now.seen >> (8 * (i >> 1) + gid)) & 1u ? x[i >> 2][(i >> 1) & 1][i & 1] : -INFINITY;
+      }
+      float corr[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float gm = fmaxf(fmaxf(x[0][0][k], x[0][1][k]), fmaxf(x[1][0][k], x[1][1][k]));
+        gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 4));
+        gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 8));
+        gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 16));
+        const float mx = fmaxf(m[k], gm), mn = mx == -INFINITY ? 0.f : mx;
+        const float up = mn - 14.f;  // weights times 2^14: sums and outputs alike
+        corr[k] = page_ex2(m[k] - mn);
+        m[k] = mx;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i >> 1][i & 1][k] = page_ex2(x[i >> 1][i & 1][k] - up);
+        l[k] = fmaf(l[k], corr[k], (x[0][0][k] + x[0][1][k]) + (x[1][0][k] + x[1][1][k]));
+      }
+      // the weights of 8 tokens by 8 heads at a time, turned round: rows of tokens become the products' columns of heads
+      uint32_t p[2][2], rest_p[FOLD ? 1 : 2][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          uint32_t hi, lo;
+          half_split(x[u][r][0], x[u][r][1], hi, lo);
+          p[u][r] = half_turned(FOLD && tig >= 2 ? lo : hi);
+          if constexpr (!FOLD) rest_p[u][r] = half_turned(lo);
+        }
+      if (__any_sync(0xFFFFFFFFu, corr[0] != 1.f || corr[1] != 1.f)) {
+        const unsigned long long both = pair_of(corr[0], corr[1]);
+#pragma unroll
+        for (int i = 0; i < NO; ++i) o[i][0] = pair_mul(o[i][0], both), o[i][1] = pair_mul(o[i][1], both);
+      }
+      tile = step(t + 1);
+      if (edge) {
+        hide(tile);
+#pragma unroll
+        for (int b = 0; b < NBOX; ++b)
+          if (NBOX == 2 && ((now.seen >> (16 * b)) & 0xFFFFu) == 0u) vs[b] = 0.f;  // (a page that is not seen has any scale)
+      }
+      unsigned long long scales[NBOX];
+#pragma unroll
+      for (int b = 0; b < NBOX; ++b) scales[b] = pair_of(vs[b], vs[b]);
+      // O^T += V^T P^T: rows gid, gid + 8 of tile i are channels gid * D / 8 + 2 i, + 1
+#pragma unroll
+      for (int q = 0; q < D / 64; ++q) {  // eight of the lane's channels
+        uint2 v[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            const int r = 16 * u + 2 * tig + (s & 1) + 8 * (s >> 1);
+            v[u][s] = *reinterpret_cast<const uint2*>(D == 128 ? code_at(tile, r, gid) + 8 * q : code_at(tile, r, gid >> 1) + 8 * (gid & 1));
+          }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float c[NBOX][4];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            auto word = [&](int s) { return i < 2 ? v[u][s].x : v[u][s].y; };
+            // codes of two tokens, of two channels
+            const uint32_t first = __byte_perm(word(0), word(1), i & 1 ? 0x7362u : 0x5140u), second = __byte_perm(word(2), word(3), i & 1 ? 0x7362u : 0x5140u);
+            const uint32_t a0 = e4m3_halves(first & 0xFFFFu), a1 = e4m3_halves(first >> 16), a2 = e4m3_halves(second & 0xFFFFu), a3 = e4m3_halves(second >> 16);
+            const int set = NBOX == 2 ? u : 0;
+            if (NBOX == 2 || u == 0) mma_f16_from_zero(c[set], a0, a1, a2, a3, p[u][0], p[u][1]);
+            else mma_f16_m16n8k16(c[set], a0, a1, a2, a3, p[u][0], p[u][1]);
+            if constexpr (!FOLD) mma_f16_m16n8k16(c[set], a0, a1, a2, a3, rest_p[u][0], rest_p[u][1]);
+          }
+#pragma unroll
+          for (int b = 0; b < NBOX; ++b) {
+            o[4 * q + i][0] = pair_fma(pair_of(c[b][0], c[b][1]), scales[b], o[4 * q + i][0]);
+            o[4 * q + i][1] = pair_fma(pair_of(c[b][2], c[b][3]), scales[b], o[4 * q + i][1]);
+          }
+        }
+      }
+    } else {
+      // S = q K^T: head gid, tokens 8 i + 2 tig, + 1
+      float x[8];
+      {
+        float sa[4][4], sb[4][4];
         const uint4* kr = reinterpret_cast<const uint4*>(tile) + gid * 8;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
@@ -424,49 +582,38 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
             if (c == 0) mma_bf16_from_zero(sa[i], qf[0], 0u, qf[1], 0u, kv.x, kv.y), mma_bf16_from_zero(sb[i], qf[2], 0u, qf[3], 0u, kv.z, kv.w);
             else mma_bf16_m16n8k16(sa[i], qf[4 * c], 0u, qf[4 * c + 1], 0u, kv.x, kv.y), mma_bf16_m16n8k16(sb[i], qf[4 * c + 2], 0u, qf[4 * c + 3], 0u, kv.z, kv.w);
           }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = sa[k >> 1][k & 1] + sb[k >> 1][k & 1];
       }
-    }
-    // This lane: head gid, tokens j0 + 8 i + 2 tig, + 1.
-    const bool edge = lo > j0 || hi < j0 + GRP;
-    const uint32_t seen = (lo > j0 ? 0xFFFFFFFFu << (lo - j0) : 0xFFFFFFFFu) & (hi < j0 + GRP ? (1u << (hi - j0)) - 1u : 0xFFFFFFFFu);
-    float x[8];
+      if (a.mod.cap_log2 > 0.f) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) x[2 * i + e] = Q8 ? (LO ? sa[i][e] + sa[i][2 + e] : sa[i][e]) : sa[i][e] + sb[i][e];
-    if (a.mod.cap_log2 > 0.f) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = a.mod.cap_log2 * tanhf(x[k] * (inv_cap * ks[NBOX == 2 ? k >> 2 : 0]));
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] *= factor * ks[NBOX == 2 ? k >> 2 : 0];
-    }
-    if (a.mod.slopes != nullptr) {
-      const float away = (float)(hi - 1 - j0 - 2 * tig);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = fmaf(-slope, away - (float)(8 * (k >> 1) + (k & 1)), x[k]);
-    }
-    if (edge) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = (seen >> (8 * (k >> 1) + 2 * tig + (k & 1))) & 1u ? x[k] : -INFINITY;
-    }
-    float gm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 1));
-    gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 2));
-    constexpr float kUp = Q8 ? 14.f : 0.f;  // weights times 2^14: sums and outputs alike
-    const float mx = fmaxf(m, gm), mn = mx == -INFINITY ? 0.f : mx;
-    const float corr = page_ex2(m - mn);
-    float p[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) p[k] = page_ex2(x[k] - mn + kUp);
-    l = l * corr + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
-    m = mx;
-    uint32_t w[4][2], third[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (Q8) {
-        half_split(p[2 * i], p[2 * i + 1], w[i][0], w[i][1]);
+        for (int k = 0; k < 8; ++k) x[k] = a.mod.cap_log2 * tanhf(x[k] * a.mod.inv_cap);
       } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] *= a.mod.scale_log2;
+      }
+      if (a.mod.slopes != nullptr) {
+        const float away = (float)(now.away - 2 * tig);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = fmaf(-slope[0], away - (float)(8 * (k >> 1) + (k & 1)), x[k]);
+      }
+      if (edge) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = (now.seen >> (8 * (k >> 1) + 2 * tig + (k & 1))) & 1u ? x[k] : -INFINITY;
+      }
+      float gm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 1));
+      gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 2));
+      const float mx = fmaxf(m[0], gm), mn = mx == -INFINITY ? 0.f : mx;
+      const float corr = page_ex2(m[0] - mn);
+      float p[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) p[k] = page_ex2(x[k] - mn);
+      l[0] = l[0] * corr + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
+      m[0] = mx;
+      uint32_t w[4][2], third[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
         split_pair(p[2 * i], p[2 * i + 1], w[i][0], w[i][1]);
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n"
             : "=r"(third[i])
@@ -474,64 +621,13 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
               "f"(p[2 * i] - __uint_as_float(w[i][0] << 16) - __uint_as_float(w[i][1] << 16)));
         if (FOLD && gid >= 4) w[i][0] = third[i], w[i][1] = 0u;
       }
-    }
-    if (__any_sync(0xFFFFFFFFu, corr != 1.f)) {
-      const unsigned long long both = pair_of(corr, corr);
+      if (__any_sync(0xFFFFFFFFu, corr != 1.f)) {
+        const unsigned long long both = pair_of(corr, corr);
 #pragma unroll
-      for (int u = 0; u < NT; ++u)
-#pragma unroll
-        for (int e = 0; e < OW; ++e) o[u][e] = pair_mul(o[u][e], both);
-    }
-    const unsigned char* tile = step(t + 1);
-    if constexpr (Q8) {
-#pragma unroll
-      for (int b = 0; b < NBOX; ++b)
-        if (NBOX == 2 && ((seen >> (16 * b)) & 0xFFFFu) == 0u) vs[b] = 0.f;  // (a page that is not seen has any scale)
-      unsigned long long scales[NBOX];
-#pragma unroll
-      for (int b = 0; b < NBOX; ++b) scales[b] = pair_of(vs[b], vs[b]);
-#pragma unroll
-      for (int q = 0; q < D / 64; ++q) {  // eight channels of each lane column at a time: tiles 8 q .. 8 q + 7
-        uint2 v[2][4];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-          for (int s = 0; s < 4; ++s) {
-            const int r = 16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1);
-            v[hf][s] = *reinterpret_cast<const uint2*>(D == 128 ? code_at(tile, r, gid) + 8 * q : code_at(tile, r, gid >> 1) + 8 * (gid & 1));
-            if (edge) {  // hidden rows (weighted by zero) hold anything: zeros
-              const uint32_t keep = 0u - ((seen >> r) & 1u);
-              v[hf][s].x &= keep, v[hf][s].y &= keep;
-            }
-          }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float c[NBOX][4][4];
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            auto word = [&](int s) { return half ? v[hf][s].y : v[hf][s].x; };
-            // codes of two tokens by channel
-            const uint32_t a01 = __byte_perm(word(0), word(1), 0x5140u), a23 = __byte_perm(word(0), word(1), 0x7362u);
-            const uint32_t b01 = __byte_perm(word(2), word(3), 0x5140u), b23 = __byte_perm(word(2), word(3), 0x7362u);
-            const int set = NBOX == 2 ? hf : 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t first = e < 2 ? a01 : a23, second = e < 2 ? b01 : b23;
-              const uint32_t b0 = e4m3_halves((e & 1) ? first >> 16 : first & 0xFFFFu), b1 = e4m3_halves((e & 1) ? second >> 16 : second & 0xFFFFu);
-              if (NBOX == 2 || hf == 0) mma_f16_from_zero(c[set][e], w[2 * hf][0], w[2 * hf][1], w[2 * hf + 1][0], w[2 * hf + 1][1], b0, b1);
-              else mma_f16_m16n8k16(c[set][e], w[2 * hf][0], w[2 * hf][1], w[2 * hf + 1][0], w[2 * hf + 1][1], b0, b1);
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int b = 0; b < NBOX; ++b) {
-              unsigned long long& to = o[8 * q + 4 * half + e][0];
-              to = pair_fma(pair_add(pair_of(c[b][e][0], c[b][e][1]), pair_of(c[b][e][2], c[b][e][3])), scales[b], to);
-            }
-        }
+        for (int i = 0; i < NO; ++i) o[i][0] = pair_mul(o[i][0], both), o[i][1] = pair_mul(o[i][1], both);
       }
-    } else {
+      tile = step(t + 1);
+      if (edge) hide(tile);
       const uint4* vr = reinterpret_cast<const uint4*>(tile);
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
@@ -543,15 +639,6 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
             const int r = 16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1);
             vb[hf][s] = vr[h * GRP * 8 + r * 8 + (gid ^ (r & 7))];
           }
-        if (edge) {
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-              const uint32_t keep = 0u - ((seen >> (16 * hf + 2 * tig + (s & 1) + 8 * (s >> 1))) & 1u);
-              vb[hf][s].x &= keep, vb[hf][s].y &= keep, vb[hf][s].z &= keep, vb[hf][s].w &= keep;
-            }
-        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float c[4];
@@ -565,48 +652,72 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
             if (!FOLD) mma_bf16_m16n8k16(c, third[2 * hf], 0u, third[2 * hf + 1], 0u, b0, b1);
           }
           o[8 * h + e][0] = pair_add(o[8 * h + e][0], pair_of(c[0], c[1]));
-          o[8 * h + e][OW - 1] = pair_add(o[8 * h + e][OW - 1], pair_of(c[2], c[3]));
+          o[8 * h + e][1] = pair_add(o[8 * h + e][1], pair_of(c[2], c[3]));
         }
       }
     }
-    const bool ends = cur.g + 1 == cur.span.g1;
+    const bool ends = now.flags & 2;
     if (ends || t + 2 == items) {  // the unit's result, or this warp's piece of it
-      l += __shfl_xor_sync(0xFFFFFFFFu, l, 1);
-      l += __shfl_xor_sync(0xFFFFFFFFu, l, 2);
+#pragma unroll
+      for (int k = 0; k < HEADS; ++k) {
+        l[k] += __shfl_xor_sync(0xFFFFFFFFu, l[k], Q8 ? 4 : 1);
+        l[k] += __shfl_xor_sync(0xFFFFFFFFu, l[k], Q8 ? 8 : 2);
+        if (Q8) l[k] += __shfl_xor_sync(0xFFFFFFFFu, l[k], 16);
+      }
       const bool whole = begins && ends;
       const int e = 2 * warp + (ends ? 0 : 1);
-      float* dst = whole ? a.out + ((long long)cur.s * H + cur.h) * G * d : piece_of(e);
-      const float inv = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
+      float* dst = whole ? a.out + (long long)now.unit * G * d : piece_of(e);
+      float inv[HEADS];
+#pragma unroll
+      for (int k = 0; k < HEADS; ++k) inv[k] = whole ? (l[k] != 0.f ? 1.f / l[k] : 0.f) : 1.f;
       __syncwarp();  // (the ring has been read: its first bytes take the last piece)
+      if constexpr (Q8) {
+        const int first = FOLD ? 2 * (tig & 1) : 2 * tig;
 #pragma unroll
-      for (int u = 0; u < NT; u += 4) {
-        float f[2][4];
+        for (int i = 0; i < NO; i += 2) {
+          float f[2][4];  // four channels of each head
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          unsigned long long r = o[u + i][0];
-          asm("mov.b64 {%0, %1}, %2;" : "=f"(f[0][i]), "=f"(f[1][i]) : "l"(r));
-          if constexpr (!Q8) {
-            if (FOLD) f[0][i] += __shfl_down_sync(0xFFFFFFFFu, f[0][i], 16), f[1][i] += __shfl_down_sync(0xFFFFFFFFu, f[1][i], 16);  // the third terms' share
+          for (int c = 0; c < 4; ++c) {
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(f[0][c]), "=f"(f[1][c]) : "l"(o[i + (c >> 1)][c & 1]));
+            if (FOLD) f[0][c] += __shfl_xor_sync(0xFFFFFFFFu, f[0][c], 2), f[1][c] += __shfl_xor_sync(0xFFFFFFFFu, f[1][c], 2);  // the second terms' share
+          }
+          const int ch = gid * (D / 8) + 2 * i;
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            if ((!FOLD || tig < 2) && first + k < G && ch < d)
+              *reinterpret_cast<float4*>(dst + (first + k) * d + ch) = make_float4(f[k][0] * inv[k], f[k][1] * inv[k], f[k][2] * inv[k], f[k][3] * inv[k]);
+        }
+        if (!whole && gid == 0 && (!FOLD || tig < 2)) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+            if (first + k < G) dst[G * d + first + k] = m[k], dst[G * d + G + first + k] = l[k];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NO; i += 4) {
+          float f[2][4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
             float f0, f1;
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(f0), "=f"(f1) : "l"(o[u + i][OW - 1]));
-            f[0][i] += f0, f[1][i] += f1;
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(f[0][c]), "=f"(f[1][c]) : "l"(o[i + c][0]));
+            if (FOLD) f[0][c] += __shfl_down_sync(0xFFFFFFFFu, f[0][c], 16), f[1][c] += __shfl_down_sync(0xFFFFFFFFu, f[1][c], 16);  // the third terms' share
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(f0), "=f"(f1) : "l"(o[i + c][1]));
+            f[0][c] += f0, f[1][c] += f1;
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int ch = (2 * tig + k + 8 * (i >> 3)) * 8 + (i & 7);  // tile 8 h + e of lane column n is channel (n + 8 h) * 8 + e
+            if (gid < G && ch < d) *reinterpret_cast<float4*>(dst + gid * d + ch) = make_float4(f[k][0] * inv[0], f[k][1] * inv[0], f[k][2] * inv[0], f[k][3] * inv[0]);
           }
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int n = 2 * tig + k;  // lane column: 8 bits: channels n * D / 8 + u; bf16: channels (n + 8 h) * 8 + e of tile 8 h + e
-          const int ch = Q8 ? n * NT + u : (n + 8 * (u >> 3)) * 8 + (u & 7);
-          if (gid < G && ch < d) *reinterpret_cast<float4*>(dst + gid * d + ch) = make_float4(f[k][0] * inv, f[k][1] * inv, f[k][2] * inv, f[k][3] * inv);
-        }
+        if (!whole && gid < G && tig == 0) dst[G * d + gid] = m[0], dst[G * d + G + gid] = l[0];
       }
-      if (!whole) {
-        if (gid < G && tig == 0) dst[G * d + gid] = m, dst[G * d + G + gid] = l;
-        if (lane == 0) ent_unit[e] = cur.s * H + cur.h, ent_flag[e] = (begins ? 1 : 0) | (ends ? 2 : 0);
-      }
+      if (!whole && lane == 0) ent_unit[e] = now.unit, ent_flag[e] = (begins ? 1 : 0) | (ends ? 2 : 0);
       clear();
       fresh = true;
+      // (with two items in a ring the next group's V has not been asked for: it is the one that `ask` stands at)
+      if (t + 2 < items) ask_q(NBUF == 2 ? ask.s * H + ask.h : next.unit);
     }
-    if (t + 2 < items) advance(cur);
   }
   if (!ok) {  // gave up on a copy: count it, and let what is in flight land (bounded) before the rings are reused
     if (lane == 0) {
@@ -629,91 +740,72 @@ __global__ void __launch_bounds__(32 * kPageWarps<Q8>, 1) page_attend_kernel(con
   __syncthreads();
   // ---- units that several warps share. Lane e has piece e; units are dealt out to the warps, several warps to one where there are few.
   const int mine = lane < 2 * WARPS ? ent_unit[lane] : -1;
-  const uint32_t valid = __ballot_sync(0xFFFFFFFFu, mine >= 0), alike = __match_any_sync(0xFFFFFFFFu, mine);
+  const uint32_t alike = __match_any_sync(0xFFFFFFFFu, mine);
   uint32_t leaders = __ballot_sync(0xFFFFFFFFu, mine >= 0 && lane == __ffs(alike) - 1);
+  static_assert(2 * WARPS <= 32, "a lane for each piece");
   const int units = __popc(leaders);
-  float* fold_s = reinterpret_cast<float*>(smem + warp * Ring::kBytes + 8192);  // [2 WARPS][8] weights of the pieces, behind this warp's own piece
-  static_assert(kMaxGroup * (D + 2) * sizeof(float) <= 8192 && 8192 + 2 * WARPS * kMaxGroup * sizeof(float) <= Ring::kBytes && 2 * WARPS <= 32, "a ring holds its piece and the weights");
 #pragma unroll 1
   for (int k = 0; leaders != 0u; ++k, leaders &= leaders - 1u) {
     if (units >= WARPS ? k % WARPS != warp : warp % units != k) continue;
     const int helpers = units >= WARPS ? 1 : (WARPS - 1 - k) / units + 1, helper = units >= WARPS ? 0 : warp / units;
-    const int first = __ffs(leaders) - 1, unit = ent_unit[first];
-    const uint32_t pieces = __ballot_sync(0xFFFFFFFFu, mine == unit) & valid;
-    const int last = 31 - __clz(pieces);
-    const bool from_start = ent_flag[first] & 1, whole = from_start && (ent_flag[last] & 2);
-    const bool in = (pieces >> lane) & 1u;
-    float* dst = whole ? a.out + (long long)unit * G * d : page_rest_piece(part, gridDim.x, blockIdx.x, from_start ? 1 : 0, per);
-    float inv = 0.f;  // of head `lane`
+    const int first = __ffs(leaders) - 1;
+    const uint32_t pieces = __shfl_sync(0xFFFFFFFFu, alike, first);
+    const int unit = ent_unit[first], which = ent_flag[first] & 1;
+    const bool whole = which && (ent_flag[31 - __clz(pieces)] & 2);
+    float* dst = whole ? a.out + (long long)unit * G * d : page_rest_piece(part, gridDim.x, blockIdx.x, which, per);
 #pragma unroll 1
-    for (int g = 0; g < G; ++g) {
-      const float mz = in ? piece_of(lane)[G * d + g] : -INFINITY;
-      float M = mz;
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
-      const float f = mz == -INFINITY ? 0.f : exp2f(mz - M);
-      float L = in ? f * piece_of(lane)[G * d + G + g] : 0.f;
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) L += __shfl_xor_sync(0xFFFFFFFFu, L, off);
-      if (in) fold_s[lane * kMaxGroup + g] = f;
-      if (lane == g) inv = whole ? (L != 0.f ? 1.f / L : 0.f) : 1.f;
-      if (!whole && helper == 0 && lane == 0) dst[G * d + g] = M, dst[G * d + G + g] = L;
-    }
-    __syncwarp();
+    for (int i = 4 * (helper * 32 + lane); i < G * d; i += 128 * helpers) {
+      PageSum sum;
+      const int g = i / d;
 #pragma unroll 1
-    for (int at = helper * 32 + lane; at < (G * d / 4 + 31) / 32 * 32; at += 32 * helpers) {
-      const int i = min(4 * at, G * d - 4), g = i / d;
-      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-      for (uint32_t rest_of = pieces; rest_of != 0u; rest_of &= rest_of - 1u) {
-        const int z = __ffs(rest_of) - 1;
-        const float4 v = *reinterpret_cast<const float4*>(piece_of(z) + i);
-        const float f = fold_s[z * kMaxGroup + g];
-        O.x = fmaf(v.x, f, O.x), O.y = fmaf(v.y, f, O.y), O.z = fmaf(v.z, f, O.z), O.w = fmaf(v.w, f, O.w);
+      for (uint32_t left = pieces; left != 0u; left &= left - 1u) {
+        const float* p = piece_of(__ffs(left) - 1);
+        sum.add(p[G * d + g], p[G * d + G + g], *reinterpret_cast<const float4*>(p + i));
       }
-      const float by = __shfl_sync(0xFFFFFFFFu, inv, g);
-      if (4 * at < G * d) *reinterpret_cast<float4*>(dst + i) = make_float4(O.x * by, O.y * by, O.z * by, O.w * by);
+      *reinterpret_cast<float4*>(dst + i) = whole ? sum.result() : sum.O;
+      if (!whole && i % d == 0) dst[G * d + g] = sum.M, dst[G * d + G + g] = sum.L;
     }
-    __syncwarp();
-    if (!whole && helper == 0 && lane == 0) rest->unit[from_start ? 1 : 0] = unit;
+    if (!whole && helper == 0 && lane == 0) rest->unit[which] = unit;
   }
 }
 
-// Units that several CTAs share: the CTA that has a unit's second part puts all of its pieces together, a thread for four channels, in one pass over the pieces with a
-// running maximum. (Few registers and threads, so that it waits beside the kernel before it, and few loads that wait for others: what it takes is latency.)
-constexpr int kPageJoinThreads = 128;
+// Units that several CTAs share: the CTA that has a unit's second part puts all of its pieces together, a thread for four channels, the pieces dealt out to as many shares of
+// the threads as there are. What it takes is latency: of two loads that wait for others, and of the pieces' own, eight in flight.
+constexpr int kPageJoinThreads = 512;
 static __global__ void __launch_bounds__(kPageJoinThreads) page_join_kernel(float* part, float* out, int ctas, int G, int d) {
   __shared__ int last_s;
-  const int c = blockIdx.x + 1, tid = threadIdx.x, per = page_piece(G, d);
+  __shared__ PageSum share_s[kPageJoinThreads];
+  const int c = blockIdx.x + 1, tid = threadIdx.x, per = page_piece(G, d), columns = G * d / 4, shares = kPageJoinThreads / columns;  // (columns <= 256: d <= 128)
   if (tid == 0) last_s = ctas;
   __syncthreads();
   griddep_wait();
   griddep_launch_dependents();
   const int unit = __ldcg(&page_rest(part, c)->unit[0]), before = __ldcg(&page_rest(part, c - 1)->unit[1]);
-  for (int z = c + 1 + tid; z < ctas; z += kPageJoinThreads)
-    if (__ldcg(&page_rest(part, z)->unit[0]) != unit) {
-      atomicMin(&last_s, z);
-      break;
-    }
+  if (tid + c + 1 < ctas && __ldcg(&page_rest(part, tid + c + 1)->unit[0]) != unit) atomicMin(&last_s, tid + c + 1);  // (fewer CTAs than threads)
   if (unit < 0 || before != unit) return;
   __syncthreads();
-  const int last = last_s;
-  for (int i = 4 * tid; i < G * d; i += 4 * kPageJoinThreads) {
-    const int g = i / d;
-    float M = -INFINITY, L = 0.f;
-    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 5
-    for (int z = c - 1; z < last; ++z) {
-      const float* p = page_rest_piece(part, ctas, z, z < c ? 1 : 0, per);
-      const float mz = __ldcg(p + G * d + g), lz = __ldcg(p + G * d + G + g);
-      const float4 oz = __ldcg(reinterpret_cast<const float4*>(p + i));
-      const float top = fmaxf(M, mz), ref = top == -INFINITY ? 0.f : top, f = exp2f(M - ref), fz = exp2f(mz - ref);
-      L = L * f + lz * fz;
-      O.x = O.x * f + oz.x * fz, O.y = O.y * f + oz.y * fz, O.z = O.z * f + oz.z * fz, O.w = O.w * f + oz.w * fz;
-      M = top;
+  const int last = last_s, share = tid / columns, i = 4 * (tid % columns), g = i / d;
+  PageSum sum;
+  if (share < shares)
+#pragma unroll 1
+    for (int z0 = c - 1 + share; z0 < last; z0 += 8 * shares) {
+      float m[8], l[8];
+      float4 o[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int z = min(z0 + k * shares, last - 1);
+        const float* p = page_rest_piece(part, ctas, z, z < c ? 1 : 0, per);
+        m[k] = __ldcg(p + G * d + g), l[k] = __ldcg(p + G * d + G + g), o[k] = __ldcg(reinterpret_cast<const float4*>(p + i));
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (z0 + k * shares < last) sum.add(m[k], l[k], o[k]);
     }
-    const float inv = L != 0.f ? 1.f / L : 0.f;
-    *reinterpret_cast<float4*>(out + (long long)unit * G * d + i) = make_float4(O.x * inv, O.y * inv, O.z * inv, O.w * inv);
+  share_s[tid] = sum;
+  __syncthreads();
+  if (share == 0) {
+    for (int k = 1; k < shares; ++k) sum.add(share_s[columns * k + tid].M, share_s[columns * k + tid].L, share_s[columns * k + tid].O);
+    *reinterpret_cast<float4*>(out + (long long)unit * G * d + i) = sum.result();
   }
 }
 

@@ -114,22 +114,25 @@ int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& ma
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
   auto kernel = page_attend_kernel<D, Q8, NBOX, LO, FOLD>;
-  static_assert(1024 + kPageRings<Q8> + kPageWarps<Q8> * (kMaxGroup * (D + 2)) * sizeof(float) <= 227 * 1024 - (Q8 ? 2048 : 1024), "rings and pieces beside what the kernel holds itself");
-  const size_t smem = page_attend_smem<Q8>(a.cfg.group_size, a.cfg.head_dim);
+  static_assert(1024 + kPageRings<D, Q8> + kPageWarps<D, Q8> * (kMaxGroup * (D + 2)) * sizeof(float) <= 227 * 1024 - (Q8 ? 2048 : 1024), "rings and pieces beside what the kernel holds itself");
+  const size_t smem = page_attend_smem<D, Q8>(a.cfg.group_size, a.cfg.head_dim);
   if (int rc = set_smem(kernel, smem)) return rc;
-  if (int rc = launch_pdl(kernel, dim3((unsigned)sms), 32 * kPageWarps<Q8>, smem, true, st, a, part, maps)) return rc;
+  if (int rc = launch_pdl(kernel, dim3((unsigned)sms), 32 * kPageWarps<D, Q8>, smem, true, st, a, part, maps)) return rc;
   if (sms == 1) return HE_OK;
+  if (sms > kPageJoinThreads) return fail(HE_ERR_UNSUPPORTED, "%d multiprocessors", sms);
   return launch_pdl(page_join_kernel, dim3((unsigned)sms - 1), kPageJoinThreads, 0, true, st, part, a.out, sms, a.cfg.group_size, a.cfg.head_dim);
 }
 template <int D>
 int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
-  const bool two = a.pages.page_size < kPageGroup;
-  if (a.pages.eight_bit) {
-    if (a.cfg.dtype == HE_DTYPE_F32) return two ? launch_page_attend<D, true, 2, true, false>(a, part, maps, st) : launch_page_attend<D, true, 1, true, false>(a, part, maps, st);
-    return two ? launch_page_attend<D, true, 2, false, false>(a, part, maps, st) : launch_page_attend<D, true, 1, false, false>(a, part, maps, st);
-  }
-  if (a.cfg.group_size <= 4) return two ? launch_page_attend<D, false, 2, false, true>(a, part, maps, st) : launch_page_attend<D, false, 1, false, true>(a, part, maps, st);
-  return two ? launch_page_attend<D, false, 2, false, false>(a, part, maps, st) : launch_page_attend<D, false, 1, false, false>(a, part, maps, st);
+  const bool two = a.pages.page_size < kPageGroup, fold = a.cfg.group_size <= 4;
+  if (!a.pages.eight_bit)
+    return two ? (fold ? launch_page_attend<D, false, 2, false, true>(a, part, maps, st) : launch_page_attend<D, false, 2, false, false>(a, part, maps, st))
+               : (fold ? launch_page_attend<D, false, 1, false, true>(a, part, maps, st) : launch_page_attend<D, false, 1, false, false>(a, part, maps, st));
+  if (a.cfg.dtype == HE_DTYPE_F32)
+    return two ? (fold ? launch_page_attend<D, true, 2, true, true>(a, part, maps, st) : launch_page_attend<D, true, 2, true, false>(a, part, maps, st))
+               : (fold ? launch_page_attend<D, true, 1, true, true>(a, part, maps, st) : launch_page_attend<D, true, 1, true, false>(a, part, maps, st));
+  return two ? (fold ? launch_page_attend<D, true, 2, false, true>(a, part, maps, st) : launch_page_attend<D, true, 2, false, false>(a, part, maps, st))
+             : (fold ? launch_page_attend<D, true, 1, false, true>(a, part, maps, st) : launch_page_attend<D, true, 1, false, false>(a, part, maps, st));
 }
 
 // Whether the tensor cores serve a call (where the driver makes tensor maps): rows of bf16 or of codes up to 128 channels, few enough for a map's coordinates.
