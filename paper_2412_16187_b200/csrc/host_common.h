@@ -167,10 +167,10 @@ bool env_flag_set(const char* name) {
 // Launch with the programmatic-serialization attribute: the kernel may start while the stream's previous kernel still runs and
 // calls griddepcontrol.wait before it touches anything that kernel or an earlier one may have written.
 template <typename... P, typename... A>
-int launch_pdl(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, bool pdl, cudaStream_t stream, A... args) {
+int launch_pdl(void (*kernel)(P...), dim3 grid, dim3 threads, size_t smem, bool pdl, cudaStream_t stream, A... args) {
   cudaLaunchConfig_t lc{};
   lc.gridDim = grid;
-  lc.blockDim = dim3(threads);
+  lc.blockDim = threads;
   lc.dynamicSmemBytes = smem;
   lc.stream = stream;
   cudaLaunchAttribute attr[1];

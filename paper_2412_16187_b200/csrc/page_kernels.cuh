@@ -25,9 +25,8 @@ struct AppendArgs {
   int units, heads_per_cta;
 };
 
-constexpr int kAppendThreads = 512;  // at most
-template <int E>
-constexpr int kAppendPairs = E == 2 ? 16 : 8;  // of a thread that holds them: what 128 registers take
+constexpr int kAppendThreads = 1024;  // at most
+inline size_t append_smem(int threads) { return (size_t)threads * 2 * 4 * 16; }
 
 // The exponent of the least power of two s >= 2^-100 with top <= 448 s (448 = 1.75 * 2^8), top >= 0 finite and given by its bits.
 __host__ __device__ inline int page_scale_exponent(uint32_t top) {
@@ -35,15 +34,15 @@ __host__ __device__ inline int page_scale_exponent(uint32_t top) {
   return e > -100 ? e : -100;
 }
 
-// V values over a scale as e4m3 codes; what is not finite becomes NaN.
+// V values over a scale as e4m3 codes; what is not finite becomes NaN (`odd`: there may be infinities, which the conversion would saturate).
 template <int V>
-__device__ __forceinline__ void e4m3_store(uint8_t* dst, const float (&f)[V], float inv) {
+__device__ __forceinline__ void e4m3_store(uint8_t* dst, const float (&f)[V], float inv, bool odd) {
   uint16_t two[(V + 1) / 2];
 #pragma unroll
   for (int i = 0; i < V; i += 2) {
-    const float x = f[i], y = i + 1 < V ? f[(i + 1) % V] : 0.f;
-    const float cx = fabsf(x) < INFINITY ? x * inv : __int_as_float(0x7FC00000), cy = fabsf(y) < INFINITY ? y * inv : __int_as_float(0x7FC00000);
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two[i / 2]) : "f"(cy), "f"(cx));
+    float x = f[i], y = i + 1 < V ? f[(i + 1) % V] : 0.f;
+    if (odd) x = fabsf(x) < INFINITY ? x : __int_as_float(0x7FC00000), y = fabsf(y) < INFINITY ? y : __int_as_float(0x7FC00000);
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two[i / 2]) : "f"(y * inv), "f"(x * inv));
   }
   if constexpr (V == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(two[0] | (uint32_t)two[1] << 16, two[2] | (uint32_t)two[3] << 16);
   else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(dst) = two[0] | (uint32_t)two[1] << 16;
@@ -69,15 +68,23 @@ __device__ __forceinline__ void e4m3_rescale(uint8_t* codes, int bytes, float ra
   }
 }
 
-// The largest of the bits of finite magnitudes, of V values.
+// The largest magnitudes seen so far: a pair of bf16 values, or an fp32 one; NaNs are passed over, infinities count.
 template <int E, int V>
-__device__ __forceinline__ uint32_t page_top(uint32_t top, const RotaryPiece<E, V>& p) {
+__device__ __forceinline__ void page_top(uint32_t& top, const RotaryPiece<E, V>& p) {
+#pragma unroll
+  for (int i = 0; i < RotaryPiece<E, V>::kWords; ++i) {
+    if constexpr (E == 2) asm("max.bf16x2 %0, %0, %1;" : "+r"(top) : "r"(p.w[i] & 0x7FFF7FFFu));
+    else top = __float_as_uint(fmaxf(__uint_as_float(top), fabsf(__uint_as_float(p.w[i]))));
+  }
+}
+// The same of the finite ones alone, as the bits of an fp32 number.
+template <int E, int V>
+__device__ __forceinline__ void page_top_finite(uint32_t& top, const RotaryPiece<E, V>& p) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const uint32_t bits = __float_as_uint(p.get(i)) & 0x7FFFFFFFu;
     top = max(top, bits < 0x7F800000u ? bits : 0u);
   }
-  return top;
 }
 
 // A row of a page and the two pieces of it that one thread owns.
@@ -86,13 +93,14 @@ struct AppendPlace {
   bool some, second, turns;  // whether there is such a row, a second piece, pairs in them
 };
 
-// grid.x: pages of sequences, grid.y: shares of the KV heads. With HOLD a thread owns pieces of kAppendPairs pairs at most and holds what it has read; without (pieces of fewer
-// than 16 bytes, pages too large for 512 threads) it walks over as many as there are, twice where the maximum has to be known first.
+// grid.x: pages of sequences, grid.y: shares of the KV heads. With HOLD a thread owns one place of the page, whose pieces of 16 bytes it asks for a head ahead (into
+// shared memory that it alone reads) and holds until they are written; without (smaller pieces, pages of more than 1024 places) it walks over as many places as there are,
+// twice where the maximum has to be known first.
 template <int E, int V, bool INTER, bool Q8, bool HOLD>
 __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const AppendArgs a, const __grid_constant__ he_rotary rot) {
   using Piece = RotaryPiece<E, V>;
-  constexpr int ITEMS = HOLD ? kAppendPairs<E> / V : 1;
-  __shared__ uint32_t top_s[2][2][kAppendThreads / 32];
+  __shared__ uint32_t top_s[3][2][kAppendThreads / 32];
+  extern __shared__ __align__(16) uint4 append_s[];  // HOLD: [2][4][threads]
   const he_pages& pg = a.pages;
   const int tid = threadIdx.x, threads = blockDim.x, P = pg.page_size, H = a.n_kv_heads;
   const int s = blockIdx.x / a.tiles;
@@ -127,7 +135,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
     if (p.some) x[0].load(src + p.c0 * E);
     if (p.second) x[1].load(src + p.c1 * E);
   };
-  auto write = [&](const AppendPlace& p, const Piece (&x)[2], char* dst, float inv) {  // dst: the page's rows of this head
+  auto write = [&](const AppendPlace& p, const Piece (&x)[2], char* dst, float inv, bool odd) {  // dst: the page's rows of this head
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       if (e ? p.second : p.some) {
@@ -136,20 +144,30 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
           float f[V];
 #pragma unroll
           for (int i = 0; i < V; ++i) f[i] = x[e].get(i);
-          e4m3_store<V>(reinterpret_cast<uint8_t*>(dst) + to, f, inv);
+          e4m3_store<V>(reinterpret_cast<uint8_t*>(dst) + to, f, inv, odd);
         } else {
           x[e].store(dst + to * E);
         }
       }
   };
-  AppendPlace mine[ITEMS];
-  float sn[ITEMS][V], cs[ITEMS][V];
-#pragma unroll
-  for (int k = 0; k < ITEMS; ++k) {
-    mine[k] = place(tid + k * threads);
-    if (HOLD) sines(mine[k], sn[k], cs[k]);
-  }
+  const AppendPlace mine = place(tid);
+  float sn[V], cs[V];
+  if (HOLD) sines(mine, sn, cs);
   const int h_begin = blockIdx.y * a.heads_per_cta, h_end = min(h_begin + a.heads_per_cta, H);
+  auto ask = [&](int h) {  // (HOLD)
+    if (h < h_end) {
+      const long long from = s * a.strides[0] + h * a.strides[1] + (long long)(at * P + mine.row - first) * a.strides[2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const char* src = static_cast<const char*>(a.x[w]) + from * E;
+        uint4* to = append_s + (size_t)(((h & 1) * 4 + 2 * w) * threads + tid);
+        if (mine.some) cp_async16(to, src + mine.c0 * E);
+        if (mine.second) cp_async16(to + threads, src + mine.c1 * E);
+      }
+    }
+    cp_async_commit();
+  };
+  if (HOLD) ask(h_begin);
   for (int h = h_begin; h < h_end; ++h) {
     const long long block = (long long)page * H + h;  // of the pages' heads
     char* dst[2];
@@ -157,49 +175,66 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
     for (int w = 0; w < 2; ++w) dst[w] = static_cast<char*>(w ? pg.v_pages : pg.k_pages) + block * P * a.d * (Q8 ? 1 : E);
     float old[2] = {0.f, 0.f};
     if (Q8 && r0 > 0) old[0] = __ldcg(pg.k_scale + block), old[1] = __ldcg(pg.v_scale + block);
-    Piece x[2][ITEMS][2];
+    Piece x[2][2];
     uint32_t top[2] = {0u, 0u};
-    auto look = [&](const AppendPlace& p, int w, const Piece (&y)[2]) {
-      if (p.some) top[w] = page_top(top[w], y[0]);
-      if (p.second) top[w] = page_top(top[w], y[1]);
+    auto look = [&](const AppendPlace& p, int w, const Piece (&y)[2], bool odd) {
+      if (p.some) odd ? page_top_finite(top[w], y[0]) : page_top(top[w], y[0]);
+      if (p.second) odd ? page_top_finite(top[w], y[1]) : page_top(top[w], y[1]);
     };
-    // the rows of an item as they go into the page
-    auto fetch = [&](const AppendPlace& p, Piece (&k)[2], Piece (&v)[2]) {
-      read(p, 0, h, k), read(p, 1, h, v);
+    // the rows of a place as they go into the page
+    auto fetch = [&](const AppendPlace& p) {
+      read(p, 0, h, x[0]), read(p, 1, h, x[1]);
       if (p.some) {
-        sines(p, sn[0], cs[0]);
-        rotary_turn<E, V, INTER>(k[0], k[1], sn[0], cs[0], p.u, half, p.turns);
+        sines(p, sn, cs);
+        rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, p.u, half, p.turns);
       }
     };
     if constexpr (HOLD) {
+      ask(h + 1);
+      cp_async_wait_pending(1);
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k) read(mine[k], 0, h, x[0][k]), read(mine[k], 1, h, x[1][k]);
+      for (int w = 0; w < 2; ++w)
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k)
-        if (mine[k].some) rotary_turn<E, V, INTER>(x[0][k][0], x[0][k][1], sn[k], cs[k], mine[k].u, half, mine[k].turns);
-      if (!Q8) {
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) write(mine[k], x[0][k], dst[0], 1.f), write(mine[k], x[1][k], dst[1], 1.f);
-      } else {
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) look(mine[k], 0, x[0][k]), look(mine[k], 1, x[1][k]);
-      }
+        for (int e = 0; e < 2; ++e) x[w][e].load(reinterpret_cast<const char*>(append_s + (size_t)(((h & 1) * 4 + 2 * w + e) * threads + tid)));
+      if (mine.some) rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, mine.u, half, mine.turns);
+      if (Q8) look(mine, 0, x[0], false), look(mine, 1, x[1], false);
+      else write(mine, x[0], dst[0], 1.f, false), write(mine, x[1], dst[1], 1.f, false);
     } else {
       for (int item = tid; item < items; item += threads) {
         const AppendPlace p = place(item);
-        fetch(p, x[0][0], x[1][0]);
-        if (Q8) look(p, 0, x[0][0]), look(p, 1, x[1][0]);
-        else write(p, x[0][0], dst[0], 1.f), write(p, x[1][0], dst[1], 1.f);
+        fetch(p);
+        if (Q8) look(p, 0, x[0], false), look(p, 1, x[1], false);
+        else write(p, x[0], dst[0], 1.f, false), write(p, x[1], dst[1], 1.f, false);
       }
     }
     if constexpr (!Q8) continue;
-    top[0] = __reduce_max_sync(0xFFFFFFFFu, top[0]), top[1] = __reduce_max_sync(0xFFFFFFFFu, top[1]);
-    if (threads > 32) {  // (by turns: one barrier a head)
-      const int lane = tid & 31;
-      if (lane == 0) top_s[h & 1][0][tid >> 5] = top[0], top_s[h & 1][1][tid >> 5] = top[1];
-      __syncthreads();
+    // over the CTA, as the bits of fp32 numbers
+    auto gather = [&](int turn) {
+      top[0] = __reduce_max_sync(0xFFFFFFFFu, top[0]), top[1] = __reduce_max_sync(0xFFFFFFFFu, top[1]);
+      if (threads > 32) {  // (by turns: one barrier a head)
+        const int lane = tid & 31;
+        if (lane == 0) top_s[turn][0][tid >> 5] = top[0], top_s[turn][1][tid >> 5] = top[1];
+        __syncthreads();
 #pragma unroll
-      for (int w = 0; w < 2; ++w) top[w] = __reduce_max_sync(0xFFFFFFFFu, lane < threads / 32 ? top_s[h & 1][w][lane] : 0u);
+        for (int w = 0; w < 2; ++w) top[w] = __reduce_max_sync(0xFFFFFFFFu, lane < threads / 32 ? top_s[turn][w][lane] : 0u);
+      }
+    };
+    if (E == 2) top[0] = max(top[0] << 16, top[0] & 0xFFFF0000u), top[1] = max(top[1] << 16, top[1] & 0xFFFF0000u);
+    gather(h & 1);
+    const bool odd = max(top[0], top[1]) >= 0x7F800000u;  // an infinity (of the whole CTA): the largest of the others is to be found
+    if (__builtin_expect(odd, 0)) {
+      top[0] = top[1] = 0u;
+      if constexpr (HOLD) {
+        look(mine, 0, x[0], true), look(mine, 1, x[1], true);
+      } else {
+        for (int item = tid; item < items; item += threads) {
+          const AppendPlace p = place(item);
+          fetch(p);
+          look(p, 0, x[0], true), look(p, 1, x[1], true);
+        }
+      }
+      gather(2);
+      if (threads > 32) __syncthreads();  // (the third place is used by any head)
     }
     float inv[2];
 #pragma unroll
@@ -210,13 +245,12 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
       if (tid == 0 && (r0 == 0 || old[w] != scale)) (w ? pg.v_scale : pg.k_scale)[block] = scale;
     }
     if constexpr (HOLD) {
-#pragma unroll
-      for (int k = 0; k < ITEMS; ++k) write(mine[k], x[0][k], dst[0], inv[0]), write(mine[k], x[1][k], dst[1], inv[1]);
+      write(mine, x[0], dst[0], inv[0], odd), write(mine, x[1], dst[1], inv[1], odd);
     } else {
       for (int item = tid; item < items; item += threads) {
         const AppendPlace p = place(item);
-        fetch(p, x[0][0], x[1][0]);
-        write(p, x[0][0], dst[0], inv[0]), write(p, x[1][0], dst[1], inv[1]);
+        fetch(p);
+        write(p, x[0], dst[0], inv[0], odd), write(p, x[1], dst[1], inv[1], odd);
       }
     }
   }
@@ -230,63 +264,64 @@ struct ReadArgs {
   int max_rows, n_kv_heads, d, sides, side;
 };
 
-constexpr int kReadThreads = 256, kReadUnroll = 4;
+constexpr int kReadThreads = 256, kReadUnroll = 4, kReadRows = 64;
 
-// 16 bytes of a row at a time. grid.x: rows, grid.y: KV heads of K and of V, grid.z: sequences.
+// 64 positions of a sequence a CTA, one KV head of K or of V, threads (chunk of 16 bytes, row). grid.x: blocks of positions from the first row's on, grid.y: KV heads of K
+// and of V, grid.z: sequences.
 template <int E, bool Q8>
 __global__ void __launch_bounds__(kReadThreads) page_read_kernel(const ReadArgs a) {
   constexpr int N = 16 / E;  // elements
   const he_pages& pg = a.pages;
-  const int s = blockIdx.z, h = blockIdx.y % a.n_kv_heads, w = a.sides == 2 ? blockIdx.y / a.n_kv_heads : a.side;
+  const int s = blockIdx.z, h = blockIdx.y % a.n_kv_heads, w = a.sides == 2 ? blockIdx.y / a.n_kv_heads : a.side, c = threadIdx.x * N, P = pg.page_size;
   griddep_wait();
   griddep_launch_dependents();  // (in this order: a kernel behind this one finds no L1 line of one before it)
-  const int first = a.first != nullptr ? max(a.first[s], 0) : 0, rows = min(page_length(pg, s) - first, a.max_rows), cpr = a.d / N;
+  const int first = a.first != nullptr ? max(a.first[s], 0) : 0, end = (int)min((long long)page_length(pg, s), (long long)first + a.max_rows);
+  const int block = (first / kReadRows + blockIdx.x) * kReadRows;  // (first < end < 2^24 wherever it is used)
+  if (first >= end || block >= end) return;
   const char* pages = static_cast<const char*>(w ? pg.v_pages : pg.k_pages);
   const float* scales = w ? pg.v_scale : pg.k_scale;
-  char* out = static_cast<char*>(a.out[w]) + (s * a.strides[0] + h * a.strides[1]) * E;
-  const long long item0 = (long long)blockIdx.x * kReadThreads * kReadUnroll + threadIdx.x;
-  if (item0 - threadIdx.x >= (long long)rows * cpr) return;
-  int row[kReadUnroll], c[kReadUnroll], page[kReadUnroll];
+  char* out = static_cast<char*>(a.out[w]) + (s * a.strides[0] + h * a.strides[1] + c) * E;
+  for (int j0 = block + threadIdx.y; j0 < min(block + kReadRows, end); j0 += kReadUnroll * blockDim.y) {
+    int page[kReadUnroll];
+    uint4 v[kReadUnroll];
+    float scale[kReadUnroll];
+    auto at = [&](int k) { return j0 + k * (int)blockDim.y; };
+    auto some = [&](int k) { return at(k) >= first && at(k) < min(block + kReadRows, end); };
 #pragma unroll
-  for (int k = 0; k < kReadUnroll; ++k) {
-    const long long item = item0 + k * kReadThreads;
-    row[k] = (int)(item / cpr), c[k] = (int)(item % cpr);
-    page[k] = row[k] < rows ? page_of(pg, s, first + row[k]) : -1;
-  }
-  uint4 v[kReadUnroll];
-  float scale[kReadUnroll];
+    for (int k = 0; k < kReadUnroll; ++k) page[k] = some(k) ? page_of(pg, s, at(k)) : -1;
 #pragma unroll
-  for (int k = 0; k < kReadUnroll; ++k) {
-    v[k] = make_uint4(0u, 0u, 0u, 0u), scale[k] = 0.f;
-    if (page[k] < 0) continue;
-    const long long block = (long long)page[k] * a.n_kv_heads + h, at = (block * pg.page_size + (first + row[k]) % pg.page_size) * a.d + c[k] * N;
-    if constexpr (!Q8) {
-      v[k] = ldg_stream16(reinterpret_cast<const uint4*>(pages + at * E));
-    } else {
-      scale[k] = __ldcg(scales + block);
-      if constexpr (N == 8) {
-        const uint2 r = __ldcs(reinterpret_cast<const uint2*>(pages + at));
-        v[k].x = r.x, v[k].y = r.y;
+    for (int k = 0; k < kReadUnroll; ++k) {
+      v[k] = make_uint4(0u, 0u, 0u, 0u), scale[k] = 0.f;
+      if (page[k] < 0) continue;
+      const long long rows = (long long)page[k] * a.n_kv_heads + h, from = (rows * P + (at(k) & (P - 1))) * a.d + c;
+      if constexpr (!Q8) {
+        v[k] = ldg_stream16(reinterpret_cast<const uint4*>(pages + from * E));
       } else {
-        v[k].x = __ldcs(reinterpret_cast<const uint32_t*>(pages + at));
+        scale[k] = __ldcg(scales + rows);
+        if constexpr (N == 8) {
+          const uint2 r = __ldcs(reinterpret_cast<const uint2*>(pages + from));
+          v[k].x = r.x, v[k].y = r.y;
+        } else {
+          v[k].x = __ldcs(reinterpret_cast<const uint32_t*>(pages + from));
+        }
       }
     }
-  }
 #pragma unroll
-  for (int k = 0; k < kReadUnroll; ++k) {
-    if (row[k] >= rows) continue;
-    uint4 r = v[k];
-    if constexpr (Q8) {
-      float f[16];
-      page_unpack(v[k], scale[k], f);
-      RotaryPiece<E, N> p;
-      float g[N];
+    for (int k = 0; k < kReadUnroll; ++k) {
+      if (!some(k)) continue;
+      uint4 r = v[k];
+      if constexpr (Q8) {
+        float f[16];
+        page_unpack(v[k], scale[k], f);  // (zeros times zero where the page is not there)
+        RotaryPiece<E, N> p;
+        float g[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) g[i] = page[k] < 0 ? 0.f : f[i];
-      p.put(g);
-      r = make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]);
+        for (int i = 0; i < N; ++i) g[i] = f[i];
+        p.put(g);
+        r = make_uint4(p.w[0], p.w[1], p.w[2], p.w[3]);
+      }
+      __stcs(reinterpret_cast<uint4*>(out + (long long)(at(k) - first) * a.strides[2] * E), r);
     }
-    *reinterpret_cast<uint4*>(out + ((long long)row[k] * a.strides[2] + c[k] * N) * E) = r;
   }
 }
 

@@ -39,7 +39,11 @@ int check_pages(const he_config* cfg, const he_pages* p) {
 template <int E, bool Q8>
 int launch_append(const AppendArgs& a, const he_rotary& r, int v, dim3 grid, int threads, bool hold, cudaStream_t st) {
   constexpr int W = 16 / E;
-  auto as = [&](auto kernel) { return launch_pdl(kernel, grid, threads, 0, true, st, a, r); };
+  const size_t smem = hold ? append_smem(threads) : 0;
+  auto as = [&](auto kernel) {
+    if (int rc = set_smem(kernel, smem)) return rc;
+    return launch_pdl(kernel, grid, threads, smem, true, st, a, r);
+  };
   if (r.interleaved) return hold ? as(page_append_kernel<E, W, true, Q8, true>) : as(page_append_kernel<E, W, true, Q8, false>);
   if (v == W) return hold ? as(page_append_kernel<E, W, false, Q8, true>) : as(page_append_kernel<E, W, false, Q8, false>);
   return v == 4 ? as(page_append_kernel<E, 4, false, Q8, false>) : v == 2 ? as(page_append_kernel<E, 2, false, Q8, false>) : as(page_append_kernel<E, 1, false, Q8, false>);
@@ -169,13 +173,12 @@ int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary*
   const long long ctas = (long long)cfg->batch * a.tiles;
   if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld pages in one call", ctas);
   const int items = (max_new < P ? max_new : P) * a.units;  // of a page's new rows
-  const int each = (es == 2 ? kAppendPairs<2> : kAppendPairs<4>) / V;
-  const bool hold = V == 16 / es && items <= each * kAppendThreads;
-  const int wanted = hold ? (items + each - 1) / each : items, threads = wanted < kAppendThreads ? (wanted + 31) / 32 * 32 : kAppendThreads;
+  const bool hold = V == 16 / es && items <= kAppendThreads;
+  const int threads = items < kAppendThreads ? (items + 31) / 32 * 32 : kAppendThreads;
   // Heads are shared out until there are enough CTAs for every SM, but a thread that has worked out its sines keeps at least four heads of a whole page.
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
-  const long long shares = (4LL * sms + ctas - 1) / ctas;
+  const long long shares = (8LL * sms + ctas - 1) / ctas;
   a.heads_per_cta = (int)((cfg->n_kv_heads + shares - 1) / shares);
   const int least = max_new < P ? 1 : 4;
   if (a.heads_per_cta < least) a.heads_per_cta = least;
@@ -205,15 +208,15 @@ int he_page_read(const he_config* cfg, const he_pages* pages, const int32_t* fir
   a.pages = *pages, a.out[0] = k_out, a.out[1] = v_out, a.first = first, a.max_rows = max_rows, a.n_kv_heads = cfg->n_kv_heads, a.d = cfg->head_dim;
   for (int i = 0; i < 3; ++i) a.strides[i] = kv_strides[i];
   a.sides = k_out && v_out ? 2 : 1, a.side = k_out ? 0 : 1;
-  const long long chunks = (long long)max_rows * (cfg->head_dim * es / 16), ctas = (chunks + kReadThreads * kReadUnroll - 1) / (kReadThreads * kReadUnroll);
-  if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%d rows in one call", max_rows);
+  const long long most = (long long)max_rows < page_capacity(*pages) ? max_rows : page_capacity(*pages), ctas = (most + kReadRows - 2) / kReadRows + 1;
+  const int chunks = cfg->head_dim * es / 16;  // of a row
   const long long heads = (long long)a.sides * cfg->n_kv_heads;
   if (heads > 65535) return fail(HE_ERR_UNSUPPORTED, "%d KV heads in one call", cfg->n_kv_heads);
-  const dim3 grid((unsigned)ctas, (unsigned)heads, (unsigned)cfg->batch);
+  const dim3 grid((unsigned)ctas, (unsigned)heads, (unsigned)cfg->batch), block((unsigned)chunks, (unsigned)(kReadThreads / chunks));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (es == 2)
-    return pages->eight_bit ? launch_pdl(page_read_kernel<2, true>, grid, kReadThreads, 0, true, st, a) : launch_pdl(page_read_kernel<2, false>, grid, kReadThreads, 0, true, st, a);
-  return pages->eight_bit ? launch_pdl(page_read_kernel<4, true>, grid, kReadThreads, 0, true, st, a) : launch_pdl(page_read_kernel<4, false>, grid, kReadThreads, 0, true, st, a);
+  auto as = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, true, st, a); };
+  if (es == 2) return pages->eight_bit ? as(page_read_kernel<2, true>) : as(page_read_kernel<2, false>);
+  return pages->eight_bit ? as(page_read_kernel<4, true>) : as(page_read_kernel<4, false>);
 }
 
 size_t he_page_attend_workspace_bytes(const he_config* cfg, const he_pages* pages) {
