@@ -34,14 +34,14 @@ __host__ __device__ inline int page_scale_exponent(uint32_t top) {
   return e > -100 ? e : -100;
 }
 
-// V values over a scale as e4m3 codes; what is not finite becomes NaN (`odd`: there may be infinities, which the conversion would saturate).
-template <int V>
-__device__ __forceinline__ void e4m3_store(uint8_t* dst, const float (&f)[V], float inv, bool odd) {
+// V values over a scale as e4m3 codes; what is not finite becomes NaN (ODD: there may be infinities, which the conversion would saturate).
+template <int V, bool ODD>
+__device__ __forceinline__ void e4m3_store(uint8_t* dst, const float (&f)[V], float inv) {
   uint16_t two[(V + 1) / 2];
 #pragma unroll
   for (int i = 0; i < V; i += 2) {
     float x = f[i], y = i + 1 < V ? f[(i + 1) % V] : 0.f;
-    if (odd) x = fabsf(x) < INFINITY ? x : __int_as_float(0x7FC00000), y = fabsf(y) < INFINITY ? y : __int_as_float(0x7FC00000);
+    if (ODD) x = fabsf(x) < INFINITY ? x : __int_as_float(0x7FC00000), y = fabsf(y) < INFINITY ? y : __int_as_float(0x7FC00000);
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two[i / 2]) : "f"(y * inv), "f"(x * inv));
   }
   if constexpr (V == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(two[0] | (uint32_t)two[1] << 16, two[2] | (uint32_t)two[3] << 16);
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
     if (p.some) x[0].load(src + p.c0 * E);
     if (p.second) x[1].load(src + p.c1 * E);
   };
-  auto write = [&](const AppendPlace& p, const Piece (&x)[2], char* dst, float inv, bool odd) {  // dst: the page's rows of this head
+  auto write = [&](const AppendPlace& p, const Piece (&x)[2], char* dst, float inv, auto odd) {  // dst: the page's rows of this head
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       if (e ? p.second : p.some) {
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
           float f[V];
 #pragma unroll
           for (int i = 0; i < V; ++i) f[i] = x[e].get(i);
-          e4m3_store<V>(reinterpret_cast<uint8_t*>(dst) + to, f, inv, odd);
+          e4m3_store<V, decltype(odd)::value>(reinterpret_cast<uint8_t*>(dst) + to, f, inv);
         } else {
           x[e].store(dst + to * E);
         }
@@ -198,13 +198,13 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
         for (int e = 0; e < 2; ++e) x[w][e].load(reinterpret_cast<const char*>(append_s + (size_t)(((h & 1) * 4 + 2 * w + e) * threads + tid)));
       if (mine.some) rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, mine.u, half, mine.turns);
       if (Q8) look(mine, 0, x[0], false), look(mine, 1, x[1], false);
-      else write(mine, x[0], dst[0], 1.f, false), write(mine, x[1], dst[1], 1.f, false);
+      else write(mine, x[0], dst[0], 1.f, std::false_type()), write(mine, x[1], dst[1], 1.f, std::false_type());
     } else {
       for (int item = tid; item < items; item += threads) {
         const AppendPlace p = place(item);
         fetch(p);
         if (Q8) look(p, 0, x[0], false), look(p, 1, x[1], false);
-        else write(p, x[0], dst[0], 1.f, false), write(p, x[1], dst[1], 1.f, false);
+        else write(p, x[0], dst[0], 1.f, std::false_type()), write(p, x[1], dst[1], 1.f, std::false_type());
       }
     }
     if constexpr (!Q8) continue;
@@ -244,15 +244,19 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
       if (r0 > 0 && old[w] != scale) e4m3_rescale(reinterpret_cast<uint8_t*>(dst[w]), r0 * a.d, old[w] / scale);
       if (tid == 0 && (r0 == 0 || old[w] != scale)) (w ? pg.v_scale : pg.k_scale)[block] = scale;
     }
-    if constexpr (HOLD) {
-      write(mine, x[0], dst[0], inv[0], odd), write(mine, x[1], dst[1], inv[1], odd);
-    } else {
-      for (int item = tid; item < items; item += threads) {
-        const AppendPlace p = place(item);
-        fetch(p);
-        write(p, x[0], dst[0], inv[0], odd), write(p, x[1], dst[1], inv[1], odd);
+    auto finish = [&](auto is_odd) {
+      if constexpr (HOLD) {
+        write(mine, x[0], dst[0], inv[0], is_odd), write(mine, x[1], dst[1], inv[1], is_odd);
+      } else {
+        for (int item = tid; item < items; item += threads) {
+          const AppendPlace p = place(item);
+          fetch(p);
+          write(p, x[0], dst[0], inv[0], is_odd), write(p, x[1], dst[1], inv[1], is_odd);
+        }
       }
-    }
+    };
+    if (__builtin_expect(odd, 0)) finish(std::true_type());
+    else finish(std::false_type());
   }
 }
 

@@ -178,7 +178,7 @@ int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary*
   // Heads are shared out until there are enough CTAs for every SM, but a thread that has worked out its sines keeps at least four heads of a whole page.
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
-  const long long shares = (8LL * sms + ctas - 1) / ctas;
+  const long long shares = (4LL * sms + ctas - 1) / ctas;
   a.heads_per_cta = (int)((cfg->n_kv_heads + shares - 1) / shares);
   const int least = max_new < P ? 1 : 4;
   if (a.heads_per_cta < least) a.heads_per_cta = least;
