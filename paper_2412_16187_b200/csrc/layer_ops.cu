@@ -8,6 +8,7 @@
 
 #include "attend_kernels.cuh"
 #include "common.cuh"
+#include "few_rows.h"
 #include "hashevict.h"
 #include "host_common.h"
 #include "prompt_attend_kernels.cuh"
@@ -111,9 +112,14 @@ int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
 
 bool on_tensor_cores(const PromptArgs& a) { return a.dtype == HE_DTYPE_BF16 && a.d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr; }
 
+size_t prompt_part_bytes(const PromptArgs& a, int splits) {
+  return splits > 1 ? (size_t)splits * a.batch * a.n_kv_heads * a.group * a.tokens * (a.d + 2) * sizeof(float) : 0;
+}
+
 // Into how many shares the keys are cut where there are fewer tiles of rows than SMs. Tiles run side by side on the SMs, in rounds; a block of 128 keys costs
-// a tile 3500 cycles on the tensor cores and the tile's own start and end 9000 (prompt_tc_kernel), so the best count is the one with the shortest rounds, each share
-// counted with its start and end, all for the longest rows and keys of the call. On the CUDA cores a block of 64 keys by 16 or 64 rows takes the place.
+// a tile 3500 cycles on the tensor cores and the tile's own start and end 9000 (prompt_tc_kernel), and each share of a row goes through HBM or L2 twice in fp32 (3400 bytes
+// a cycle). So the best count is the one with the least of rounds, starts and traffic, all for the longest rows and keys of the call: 32 heads of 512 rows over 32768 keys 271 us
+// with 9 shares, 250 with 2. On the CUDA cores a block of 64 keys by 16 or 64 rows takes the place.
 int prompt_splits(const PromptArgs& a, bool tc, int* out) {
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
@@ -123,15 +129,11 @@ int prompt_splits(const PromptArgs& a, bool tc, int* out) {
   const long long blocks = ((long long)a.keys + (tc ? 127 : 63)) / (tc ? 128 : 64);
   double best = 0.0;
   for (int z = 1; z <= 64 && 2 * z <= blocks && (z == 1 || items * z <= 8LL * sms); ++z) {
-    const double rounds = (double)((items * z + sms - 1) / sms), cost = rounds * ((double)((blocks + z - 1) / z) * 3500.0 + 9000.0) + (z > 1 ? 6000.0 : 0.0);
+    const double rounds = (double)((items * z + sms - 1) / sms), cost = rounds * ((double)((blocks + z - 1) / z) * 3500.0 + 9000.0) + (z > 1 ? 6000.0 + (double)prompt_part_bytes(a, z) * 2.0 / 3400.0 : 0.0);
     if (z == 1 || cost < 0.95 * best) best = cost, *out = z;
   }
   return HE_OK;
 }
-size_t prompt_part_bytes(const PromptArgs& a, int splits) {
-  return splits > 1 ? (size_t)splits * a.batch * a.n_kv_heads * a.group * a.tokens * (a.d + 2) * sizeof(float) : 0;
-}
-
 int launch_rows(const PromptArgs& a, bool tc, cudaStream_t st) {
   if (tc) {
     PromptMaps maps;
@@ -174,6 +176,15 @@ int attend_rows(PromptArgs& a, const he_config* cfg, const he_score_mod* mod, co
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype;
   const bool tc = on_tensor_cores(a);
   if (workspace != nullptr) {
+    // one row a sequence, or a few that see the same keys: K and V are read once for all of them
+    const size_t few = a.prefix == nullptr && (a.tokens == 1 || (a.all && a.doc_start == nullptr)) ? few_rows_workspace(cfg, a.tokens, a.keys) : 0;
+    if (few > 0) {
+      if (few > workspace_bytes) return fail(HE_ERR_WORKSPACE, "workspace of %zu bytes, %zu are needed", workspace_bytes, few);
+      const RowsOverCall call{q, k, v, out, q_strides, kv_strides, out_strides, a.lens, a.kv_lens, a.q_pos, a.doc_start, a.slopes, static_cast<float*>(workspace),
+                              a.scale_log2, a.cap_log2, a.inv_cap, a.window, a.tokens, a.keys};
+      const int rc = launch_few_rows(cfg, call, st);
+      if (rc >= 0) return rc;
+    }
     if (int rc = prompt_splits(a, tc, &a.splits)) return rc;
     if (prompt_part_bytes(a, a.splits) > workspace_bytes)
       return fail(HE_ERR_WORKSPACE, "workspace of %zu bytes, %zu are needed", workspace_bytes, prompt_part_bytes(a, a.splits));
@@ -182,7 +193,9 @@ int attend_rows(PromptArgs& a, const he_config* cfg, const he_score_mod* mod, co
   if (a.keys == 0) a.splits = 1;
   if (int rc = launch_rows(a, tc && a.keys > 0, st)) return rc;
   if (a.splits == 1) return HE_OK;
-  const long long ctas = ((long long)a.batch * a.n_kv_heads * a.group * a.tokens + kJoinThreads / 32 - 1) / (kJoinThreads / 32);
+  const int rows = kJoinThreads / prompt_join_lanes(a.d);  // of a CTA
+  const long long ctas = ((long long)a.batch * a.n_kv_heads * a.group * a.tokens + rows - 1) / rows;
+  if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%d rows in one call", a.tokens);
   return launch_pdl(prompt_join_kernel, dim3((unsigned)ctas), kJoinThreads, 0, true, st, a);
 }
 
@@ -350,7 +363,7 @@ size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, 
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_q_len, a.keys = max_kv_len;
   int splits = 1;
   if (prompt_splits(a, on_tensor_cores(a), &splits)) return 0;
-  return prompt_part_bytes(a, splits);
+  return std::max(prompt_part_bytes(a, splits), few_rows_workspace(cfg, max_q_len, max_kv_len));
 }
 
 int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],

@@ -50,25 +50,60 @@ inline size_t page_workspace(int ctas, int G, int d) { return (size_t)ctas * (16
 __device__ __forceinline__ PageRest* page_rest(float* part, int cta) { return reinterpret_cast<PageRest*>(part) + 2 * cta; }
 __device__ __forceinline__ float* page_rest_piece(float* part, int ctas, int cta, int which, int piece) { return part + 4 * ctas + (2LL * cta + which) * piece; }
 
-// The tokens [lo, hi) that the query of a sequence sees, and their groups [g0, g1).
-struct PageSpan {
-  int lo, hi, g0, g1;
+// The same kernel for few rows over plain keys and values (he_attend_cross: bf16, at most 8 rows for a KV head, all of which see the same keys): cfg.group_size counts the
+// rows of a unit, row g * rows + i being row i of query head g of the group.
+struct RowsOver {
+  const int32_t *q_len, *kv_len, *q_pos;  // [B]; q_pos or null: rows see all keys
+  long long qs[3], os[3];                 // element strides (sequence, head, row)
+  void* out;                              // bf16
+  int keys, rows;
 };
-static __device__ __noinline__ PageSpan page_span(const PagedAttendArgs& a, int s) {
+struct TokenArgs : PagedAttendArgs {
+  RowsOver over;  // read with ROWS only
+};
+
+// The tokens [lo, hi) that the query of a sequence sees, their groups [g0, g1), and where the query's own token is.
+struct PageSpan {
+  int lo, hi, g0, g1, at;
+};
+template <bool ROWS>
+static __device__ __noinline__ PageSpan page_span(const TokenArgs& a, int s) {
   PageSpan p;
-  p.hi = page_length(a.pages, s);
-  p.lo = a.mod.first_pos != nullptr ? max(a.mod.first_pos[s], 0) : 0;
-  if (a.mod.window > 0) p.lo = max(p.lo, p.hi - a.mod.window);
+  if constexpr (ROWS) {
+    p.hi = min(max(a.over.kv_len[s], 0), a.over.keys), p.at = p.hi - 1;
+    if (a.over.q_pos != nullptr) p.at = min(max(a.over.q_pos[s], -(1 << 24)), 1 << 24), p.hi = min(p.hi, max(p.at + 1, 0));
+    p.lo = a.mod.first_pos != nullptr ? max(a.mod.first_pos[s * a.over.rows], 0) : 0;
+    if (max(a.over.q_len[s], 0) == 0) p.lo = p.hi;
+  } else {
+    p.hi = page_length(a.pages, s), p.at = p.hi - 1;
+    p.lo = a.mod.first_pos != nullptr ? max(a.mod.first_pos[s], 0) : 0;
+  }
+  if (a.mod.window > 0) p.lo = max(p.lo, p.at - a.mod.window + 1);
   p.lo = min(p.lo, p.hi);
   p.g0 = p.lo / kPageGroup, p.g1 = p.lo < p.hi ? (p.hi + kPageGroup - 1) / kPageGroup : p.g0;
   return p;
 }
-
 // A place on the line: group g of unit (s, h).
 struct PageCursor {
   int s, h, g;
   PageSpan span;
 };
+// Four channels of a result.
+template <bool ROWS>
+__device__ __forceinline__ void page_emit(const TokenArgs& a, int unit, int row, int ch, const float4& v) {
+  const int H = a.cfg.n_kv_heads, G = a.cfg.group_size;
+  if constexpr (ROWS) {
+    const int s = unit / H, g = row / a.over.rows, i = row % a.over.rows;
+    if (i >= a.over.q_len[s]) return;
+    uint2 two;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.x) : "f"(v.y), "f"(v.x));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.y) : "f"(v.w), "f"(v.z));
+    const long long at = s * a.over.os[0] + ((long long)(unit % H) * (G / a.over.rows) + g) * a.over.os[1] + i * a.over.os[2] + ch;
+    *reinterpret_cast<uint2*>(static_cast<char*>(a.over.out) + 2 * at) = two;
+  } else {
+    *reinterpret_cast<float4*>(a.out + ((long long)unit * G + row) * a.cfg.head_dim + ch) = v;
+  }
+}
 
 __device__ __forceinline__ float page_ex2(float x) {
   float y;
@@ -103,13 +138,13 @@ struct PageTable {
   long long base[THREADS + 1];
   PageSpan span[THREADS];
 };
-template <int WARPS, typename F>
-__device__ __forceinline__ PageLine page_line(const PagedAttendArgs& a, int ctas, int each, long long* scan_s, PageTable<32 * WARPS>& table, F empty) {
+template <int WARPS, bool ROWS, typename F>
+__device__ __forceinline__ PageLine page_line(const TokenArgs& a, int ctas, int each, long long* scan_s, PageTable<32 * WARPS>& table, F empty) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   long long sum = 0;
 #pragma unroll 1
   for (int i = 0, s = tid * each; i < each && s < a.cfg.batch; ++i, ++s) {
-    const PageSpan p = page_span(a, s);
+    const PageSpan p = page_span<ROWS>(a, s);
     sum += (p.g1 - p.g0) * a.cfg.n_kv_heads;
     if (i == 0) table.span[tid] = p;
     if (p.g1 == p.g0) empty(s);
@@ -142,8 +177,8 @@ __device__ __forceinline__ PageLine page_line(const PagedAttendArgs& a, int ctas
   return line;
 }
 // Where group `at` of the line lies, by a whole warp: the last of the threads that begin no later, then that thread's sequences.
-template <int WARPS>
-__device__ __forceinline__ void page_find(const PagedAttendArgs& a, int each, const PageTable<32 * WARPS>& table, long long at, PageCursor& c) {
+template <int WARPS, bool ROWS>
+__device__ __forceinline__ void page_find(const TokenArgs& a, int each, const PageTable<32 * WARPS>& table, long long at, PageCursor& c) {
   const int lane = threadIdx.x & 31;
   const uint32_t coarse = __ballot_sync(0xFFFFFFFFu, lane < WARPS && table.base[32 * min(lane, WARPS - 1)] <= at);
   const int block = 31 - __clz(coarse);
@@ -156,7 +191,7 @@ __device__ __forceinline__ void page_find(const PagedAttendArgs& a, int each, co
     for (;;) {
       const int n = (c.span.g1 - c.span.g0) * a.cfg.n_kv_heads;
       if (in < n) break;
-      in -= n, c.span = page_span(a, ++c.s);
+      in -= n, c.span = page_span<ROWS>(a, ++c.s);
     }
   }
   const int n = c.span.g1 - c.span.g0;
@@ -228,8 +263,8 @@ struct PageNow {
 };
 
 // NBOX: pages of a group (2 for pages of 16 tokens). LO: the queries come in fp32 (8-bit pages). FOLD: G <= 4 (bf16 pages).
-template <int D, bool Q8, int NBOX, bool LO, bool FOLD>
-__global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(const __grid_constant__ PagedAttendArgs a, float* part, const __grid_constant__ PageMaps maps) {
+template <int D, bool Q8, int NBOX, bool LO, bool FOLD, bool ROWS>
+__global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(const __grid_constant__ TokenArgs a, float* part, const __grid_constant__ PageMaps maps) {
   using Ring = PageRing<D, Q8>;
   constexpr int WARPS = kPageWarps<D, Q8>, THREADS = 32 * WARPS, NBUF = Ring::kBufs, ITEM = Ring::kItemBytes, GRP = kPageGroup, NH = Q8 ? 1 : D / 64;
   extern __shared__ __align__(16) unsigned char page_smem_raw[];
@@ -257,9 +292,9 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
   PageTable<THREADS>& table = *reinterpret_cast<PageTable<THREADS>*>(smem);  // (the rings are not in use yet)
   static_assert(sizeof(PageTable<THREADS>) <= kPageRings<D, Q8>, "the rings hold the table");
   const int each = (a.cfg.batch + THREADS - 1) / THREADS;
-  const PageLine line = page_line<WARPS>(a, gridDim.x, each, scan_s, table, [&](int s) {
+  const PageLine line = page_line<WARPS, ROWS>(a, gridDim.x, each, scan_s, table, [&](int s) {
     if (s % (int)gridDim.x == (int)blockIdx.x)
-      for (int i = 0; i < H * G * d; i += 4) *reinterpret_cast<float4*>(a.out + (long long)s * H * G * d + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < H * G * d; i += 4) page_emit<ROWS>(a, s * H + i / (G * d), i / d % G, i % d, make_float4(0.f, 0.f, 0.f, 0.f));
   });
   PageRest* rest = page_rest(part, blockIdx.x);
   if (tid == 0) rest->unit[0] = rest->unit[1] = -1;
@@ -269,14 +304,14 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
   auto warp_begin = [&](int w) { return w * (some / WARPS) + min(w, some % WARPS); };
   const int groups = warp_begin(warp + 1) - warp_begin(warp), items = 2 * groups;
   PageCursor ask{};  // the group that is asked for next
-  if (groups > 0) page_find<WARPS>(a, each, table, begin + warp_begin(warp), ask);
+  if (groups > 0) page_find<WARPS, ROWS>(a, each, table, begin + warp_begin(warp), ask);
   __syncthreads();  // the table has been read
   auto advance = [&](PageCursor& c) {
     if (++c.g < c.span.g1) return;
     if (++c.h == H) {
       c.h = 0;
 #pragma unroll 1
-      do c.span = page_span(a, ++c.s);
+      do c.span = page_span<ROWS>(a, ++c.s);
       while (c.span.g0 == c.span.g1);  // (there is another group)
     }
     c.g = c.span.g0;
@@ -288,7 +323,8 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
   float slope[2] = {0.f, 0.f}, by[2] = {1.f, 1.f};  // of this lane's heads; by (8 bits): what makes a score of a product, or what its cap's tanh takes
   uint4 raw[Q8 && LO ? D / 16 : D / 32];  // as they lie in memory
   auto ask_q = [&](int unit) {
-    const long long at = ((long long)unit * G + my_head) * d;
+    long long at = ((long long)unit * G + my_head) * d;
+    if constexpr (ROWS) at = unit / H * a.over.qs[0] + ((long long)(unit % H) * (G / a.over.rows) + my_head / a.over.rows) * a.over.qs[1] + my_head % a.over.rows * a.over.qs[2];
     if (a.mod.slopes != nullptr) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -348,7 +384,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
   float scale = 0.f;
   auto look_up = [&]() {
     const int j = ask.g * GRP + (NBOX == 2 ? 16 * (lane & 1) : 0);
-    page = j < ask.span.hi ? page_of(pg, ask.s, j) : -1;
+    if constexpr (!ROWS) page = j < ask.span.hi ? page_of(pg, ask.s, j) : -1;
   };
   if (groups > 0) look_up();
   PageNow now{}, next{};  // the group that is worked on, the last one whose V has been asked for
@@ -358,7 +394,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
   auto issue = [&](int t, int b) {
     const bool v = t & 1;
     if (t >= items) return;
-    if (!v) {
+    if (!v && !ROWS) {
 #pragma unroll
       for (int i = 0; i < NBOX; ++i) {
         const int p = NBOX == 2 ? __shfl_sync(0xFFFFFFFFu, page, i) : page;
@@ -374,7 +410,8 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
       for (int i = 0; i < NBOX; ++i)
 #pragma unroll
         for (int h = 0; h < NH; ++h)
-          asm volatile(
+          if constexpr (ROWS) tma_load_4d(dst + h * GRP * 128, v ? &maps.v : &maps.k, 64 * h, ask.g * GRP, ask.h, ask.s, full(b));
+          else asm volatile(
               "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
                   dst + h * GRP * 128 + i * (GRP / NBOX) * (Ring::kRowBytes / NH)),
               "l"(map), "r"(h * 64), "r"(row[i]), "r"(full(b))
@@ -382,7 +419,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
     }
     if (v) {
       const int j0 = ask.g * GRP, lo = ask.span.lo - j0, hi = ask.span.hi - j0;
-      next.unit = ask.s * H + ask.h, next.away = hi - 1;
+      next.unit = ask.s * H + ask.h, next.away = ask.span.at - j0;
       next.seen = (lo > 0 ? 0xFFFFFFFFu << lo : 0xFFFFFFFFu) & (hi < GRP ? (1u << hi) - 1u : 0xFFFFFFFFu);
       next.flags = (ask.g == ask.span.g0 ? 1 : 0) | (ask.g + 1 == ask.span.g1 ? 2 : 0);
       if (t + 1 < items) {
@@ -666,7 +703,11 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
       }
       const bool whole = begins && ends;
       const int e = 2 * warp + (ends ? 0 : 1);
-      float* dst = whole ? a.out + (long long)now.unit * G * d : piece_of(e);
+      float* dst = piece_of(e);
+      auto put = [&](int row, int ch, const float4& v) {
+        if (whole) page_emit<ROWS>(a, now.unit, row, ch, v);
+        else *reinterpret_cast<float4*>(dst + row * d + ch) = v;
+      };
       float inv[HEADS];
 #pragma unroll
       for (int k = 0; k < HEADS; ++k) inv[k] = whole ? (l[k] != 0.f ? 1.f / l[k] : 0.f) : 1.f;
@@ -685,7 +726,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
 #pragma unroll
           for (int k = 0; k < 2; ++k)
             if ((!FOLD || tig < 2) && first + k < G && ch < d)
-              *reinterpret_cast<float4*>(dst + (first + k) * d + ch) = make_float4(f[k][0] * inv[k], f[k][1] * inv[k], f[k][2] * inv[k], f[k][3] * inv[k]);
+              put(first + k, ch, make_float4(f[k][0] * inv[k], f[k][1] * inv[k], f[k][2] * inv[k], f[k][3] * inv[k]));
         }
         if (!whole && gid == 0 && (!FOLD || tig < 2)) {
 #pragma unroll
@@ -707,7 +748,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int ch = (2 * tig + k + 8 * (i >> 3)) * 8 + (i & 7);  // tile 8 h + e of lane column n is channel (n + 8 h) * 8 + e
-            if (gid < G && ch < d) *reinterpret_cast<float4*>(dst + gid * d + ch) = make_float4(f[k][0] * inv[0], f[k][1] * inv[0], f[k][2] * inv[0], f[k][3] * inv[0]);
+            if (gid < G && ch < d) put(gid, ch, make_float4(f[k][0] * inv[0], f[k][1] * inv[0], f[k][2] * inv[0], f[k][3] * inv[0]));
           }
         }
         if (!whole && gid < G && tig == 0) dst[G * d + gid] = m[0], dst[G * d + G + gid] = l[0];
@@ -752,7 +793,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
     const uint32_t pieces = __shfl_sync(0xFFFFFFFFu, alike, first);
     const int unit = ent_unit[first], which = ent_flag[first] & 1;
     const bool whole = which && (ent_flag[31 - __clz(pieces)] & 2);
-    float* dst = whole ? a.out + (long long)unit * G * d : page_rest_piece(part, gridDim.x, blockIdx.x, which, per);
+    float* dst = page_rest_piece(part, gridDim.x, blockIdx.x, which, per);
 #pragma unroll 1
     for (int i = 4 * (helper * 32 + lane); i < G * d; i += 128 * helpers) {
       PageSum sum;
@@ -762,7 +803,8 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
         const float* p = piece_of(__ffs(left) - 1);
         sum.add(p[G * d + g], p[G * d + G + g], *reinterpret_cast<const float4*>(p + i));
       }
-      *reinterpret_cast<float4*>(dst + i) = whole ? sum.result() : sum.O;
+      if (whole) page_emit<ROWS>(a, unit, g, i % d, sum.result());
+      else *reinterpret_cast<float4*>(dst + i) = sum.O;
       if (!whole && i % d == 0) dst[G * d + g] = sum.M, dst[G * d + G + g] = sum.L;
     }
     if (!whole && helper == 0 && lane == 0) rest->unit[which] = unit;
@@ -772,10 +814,11 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
 // Units that several CTAs share: the CTA that has a unit's second part puts all of its pieces together, a thread for four channels, the pieces dealt out to as many shares of
 // the threads as there are. What it takes is latency: of two loads that wait for others, and of the pieces' own, eight in flight.
 constexpr int kPageJoinThreads = 512;
-static __global__ void __launch_bounds__(kPageJoinThreads) page_join_kernel(float* part, float* out, int ctas, int G, int d) {
+template <bool ROWS>
+static __global__ void __launch_bounds__(kPageJoinThreads) page_join_kernel(const __grid_constant__ TokenArgs a, float* part, int ctas) {
   __shared__ int last_s;
   __shared__ PageSum share_s[kPageJoinThreads];
-  const int c = blockIdx.x + 1, tid = threadIdx.x, per = page_piece(G, d), columns = G * d / 4, shares = kPageJoinThreads / columns;  // (columns <= 256: d <= 128)
+  const int G = a.cfg.group_size, d = a.cfg.head_dim, c = blockIdx.x + 1, tid = threadIdx.x, per = page_piece(G, d), columns = G * d / 4, shares = kPageJoinThreads / columns;  // (columns <= 256: d <= 128)
   if (tid == 0) last_s = ctas;
   __syncthreads();
   griddep_wait();
@@ -805,7 +848,7 @@ static __global__ void __launch_bounds__(kPageJoinThreads) page_join_kernel(floa
   __syncthreads();
   if (share == 0) {
     for (int k = 1; k < shares; ++k) sum.add(share_s[columns * k + tid].M, share_s[columns * k + tid].L, share_s[columns * k + tid].O);
-    *reinterpret_cast<float4*>(out + (long long)unit * G * d + i) = sum.result();
+    page_emit<ROWS>(a, unit, g, i % d, sum.result());
   }
 }
 

@@ -7,6 +7,7 @@
 #include "attend_kernels.cuh"
 #include "common.cuh"
 #include "hashevict.h"
+#include "few_rows.h"
 #include "host_common.h"
 #include "page_attend_kernels.cuh"
 #include "page_kernels.cuh"
@@ -113,21 +114,21 @@ bool page_rows_tmap(const void* base, long long rows, int d, int box_rows, bool 
   return true;
 }
 
-template <int D, bool Q8, int NBOX, bool LO, bool FOLD>
-int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
+template <int D, bool Q8, int NBOX, bool LO, bool FOLD, bool ROWS = false>
+int launch_page_attend(const TokenArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
-  auto kernel = page_attend_kernel<D, Q8, NBOX, LO, FOLD>;
+  auto kernel = page_attend_kernel<D, Q8, NBOX, LO, FOLD, ROWS>;
   static_assert(1024 + kPageRings<D, Q8> + kPageWarps<D, Q8> * (kMaxGroup * (D + 2)) * sizeof(float) <= 227 * 1024 - (Q8 ? 2048 : 1024), "rings and pieces beside what the kernel holds itself");
   const size_t smem = page_attend_smem<D, Q8>(a.cfg.group_size, a.cfg.head_dim);
   if (int rc = set_smem(kernel, smem)) return rc;
   if (int rc = launch_pdl(kernel, dim3((unsigned)sms), 32 * kPageWarps<D, Q8>, smem, true, st, a, part, maps)) return rc;
   if (sms == 1) return HE_OK;
   if (sms > kPageJoinThreads) return fail(HE_ERR_UNSUPPORTED, "%d multiprocessors", sms);
-  return launch_pdl(page_join_kernel, dim3((unsigned)sms - 1), kPageJoinThreads, 0, true, st, part, a.out, sms, a.cfg.group_size, a.cfg.head_dim);
+  return launch_pdl(page_join_kernel<ROWS>, dim3((unsigned)sms - 1), kPageJoinThreads, 0, true, st, a, part, sms);
 }
 template <int D>
-int launch_page_attend(const PagedAttendArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
+int launch_page_attend(const TokenArgs& a, float* part, const PageMaps& maps, cudaStream_t st) {
   const bool two = a.pages.page_size < kPageGroup, fold = a.cfg.group_size <= 4;
   if (!a.pages.eight_bit)
     return two ? (fold ? launch_page_attend<D, false, 2, false, true>(a, part, maps, st) : launch_page_attend<D, false, 2, false, false>(a, part, maps, st))
@@ -146,7 +147,43 @@ bool page_tensor_cores(const he_config* cfg, const he_pages* p) {
          getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
 }
 
+// Tensor map of keys or values: {channel, token, head, sequence} in boxes of 64 channels x 32 tokens. An axis of one entry may come with any stride.
+bool rows_over_tmap(const void* base, int d, int tokens, int heads, int batch, const int64_t* strides, CUtensorMap* out) {
+  const EncodeTiledFn encode = tmap_encoder();
+  if (encode == nullptr || env_flag_set<6>("HE_DISABLE_TMA")) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)batch};
+  cuuint64_t st[3] = {(cuuint64_t)strides[2] * 2, (cuuint64_t)strides[1] * 2, (cuuint64_t)strides[0] * 2};
+  for (int i = 0; i < 3; ++i) {
+    if (dims[i + 1] == 1) st[i] = (cuuint64_t)d * 2;
+    if (st[i] == 0 || st[i] % 16 != 0 || st[i] >= (1ull << 40)) return false;
+  }
+  const cuuint32_t box[4] = {64, (cuuint32_t)kPageGroup, 1, 1}, estr[4] = {1, 1, 1, 1};
+  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, st, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
+
+size_t he::few_rows_workspace(const he_config* cfg, int rows, int keys) {
+  int sms = 0;
+  if (!few_rows(cfg, rows, keys) || sm_count(&sms)) return 0;
+  return page_workspace(sms, rows * cfg->group_size, cfg->head_dim);
+}
+
+int he::launch_few_rows(const he_config* cfg, const RowsOverCall& c, cudaStream_t st) {
+  TokenArgs a{};
+  a.cfg = *cfg, a.cfg.group_size = cfg->group_size * c.rows, a.q = c.q;
+  a.mod.scale_log2 = c.scale_log2, a.mod.cap_log2 = c.cap_log2, a.mod.inv_cap = c.inv_cap, a.mod.window = c.window, a.mod.slopes = c.slopes, a.mod.first_pos = c.first_key;
+  a.pages.page_size = kPageGroup;
+  a.over = {c.q_len, c.kv_len, c.q_pos, {c.q_strides[0], c.q_strides[1], c.q_strides[2]}, {c.out_strides[0], c.out_strides[1], c.out_strides[2]}, c.out, c.keys, c.rows};
+  const int d = cfg->head_dim;
+  PageMaps maps;
+  if (!rows_over_tmap(c.k, d, c.keys, cfg->n_kv_heads, cfg->batch, c.kv_strides, &maps.k) || !rows_over_tmap(c.v, d, c.keys, cfg->n_kv_heads, cfg->batch, c.kv_strides, &maps.v))
+    return -1;
+  if (a.cfg.group_size <= 4)
+    return d <= 64 ? launch_page_attend<64, false, 1, false, true, true>(a, c.part, maps, st) : launch_page_attend<128, false, 1, false, true, true>(a, c.part, maps, st);
+  return d <= 64 ? launch_page_attend<64, false, 1, false, false, true>(a, c.part, maps, st) : launch_page_attend<128, false, 1, false, false, true>(a, c.part, maps, st);
+}
 
 extern "C" {
 
@@ -232,7 +269,7 @@ int he_page_attend(const he_config* cfg, const he_pages* pages, const he_score_m
   if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q or out is null or not 16-byte aligned");
   if (cfg->batch > 65535) return fail(HE_ERR_UNSUPPORTED, "batch %d > 65535 in one call", cfg->batch);
   if (pages->n_pages == 0 || pages->max_pages == 0) return fail(HE_ERR_INVALID_ARG, "no pages");
-  PagedAttendArgs a{};
+  TokenArgs a{};
   a.cfg = *cfg, a.pages = *pages, a.q = q, a.out = out;
   if (int rc = check_mod(mod, cfg->head_dim, &a.mod.scale_log2, &a.mod.cap_log2, &a.mod.inv_cap, &a.mod.window, &a.mod.slopes)) return rc;
   a.mod.first_pos = first_pos;

@@ -1314,58 +1314,73 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 
 // ------------------------------------------------------------------------------------------------ shares of the keys, joined
 //
-// A warp per row: the shares' outputs, weighted by 2^(m - M), over the weighted sum of their sums. A row whose output is a NaN that its sum does not explain
-// is computed once more, as the kernels above do.
+// A thread for four channels of a row (two times four from d = 136 on), the rows of a warp side by side: the shares' outputs, weighted by 2^(m - M) with a running maximum, over
+// the weighted sum of their sums. A row whose output is a NaN that its sum does not explain is computed once more, as the kernels above do.
 constexpr int kJoinThreads = 128;
+__host__ __device__ inline int prompt_join_lanes(int d) { return d <= 16 ? 4 : d <= 32 ? 8 : d <= 64 ? 16 : 32; }  // of a row
 static __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const __grid_constant__ PromptArgs a) {
-  const int lane = threadIdx.x & 31, heads = a.n_kv_heads * a.group;
-  const long long item = (long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, heads = a.n_kv_heads * a.group, lanes = prompt_join_lanes(a.d), at_lane = lane % lanes;
+  const long long item = ((long long)blockIdx.x * kJoinThreads + threadIdx.x) / lanes;
   griddep_wait();
   griddep_launch_dependents();
   const int i = (int)(item % a.tokens), head = (int)(item / a.tokens % heads);
   const long long sequence = item / a.tokens / heads;
-  if (sequence >= a.batch) return;
-  const int s = (int)sequence, n = min(max(a.lens[s], 0), a.tokens);
-  if (i >= n) return;
-  float m = -INFINITY, M = -INFINITY, l = 0.f, L = 0.f;
-  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // channels 4 lane + e, 128 + 4 lane + e
-  for (int z0 = 0; z0 < a.splits; z0 += 32) {
-    if (z0 + lane < a.splits) m = fmaxf(m, prompt_part_ml(a, prompt_part_row(a, z0 + lane, s, head, i))[0]);
-  }
-  M = m;
+  const int s = (int)min(sequence, (long long)a.batch - 1), n = min(max(a.lens[s], 0), a.tokens);
+  const bool some = sequence < a.batch && i < n;
+  if (!__any_sync(0xFFFFFFFFu, some)) return;
+  float M = -INFINITY, L = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // channels 4 at_lane + e, 128 + 4 at_lane + e
+  if (some)
+#pragma unroll 1
+    for (int z0 = 0; z0 < a.splits; z0 += 4) {
+      float2 ml[4];
+      float4 v[4][2];
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, off));
-#pragma unroll 4
-  for (int z = 0; z < a.splits; ++z) {
-    const long long at = prompt_part_row(a, z, s, head, i);
-    const float2 ml = *reinterpret_cast<const float2*>(prompt_part_ml(a, at));
-    const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-    L = fmaf(ml.y, f, L);
+      for (int k = 0; k < 4; ++k) {
+        const long long at = prompt_part_row(a, min(z0 + k, a.splits - 1), s, head, i);
+        ml[k] = __ldcg(reinterpret_cast<const float2*>(prompt_part_ml(a, at)));
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-      if (128 * w + 4 * lane < a.d) {
-        const float4 v = *reinterpret_cast<const float4*>(a.part + at * a.d + 128 * w + 4 * lane);
-        if (ml.x != -INFINITY) {  // (a share that saw nothing holds anything)
-          o[4 * w] = fmaf(v.x, f, o[4 * w]), o[4 * w + 1] = fmaf(v.y, f, o[4 * w + 1]);
-          o[4 * w + 2] = fmaf(v.z, f, o[4 * w + 2]), o[4 * w + 3] = fmaf(v.w, f, o[4 * w + 3]);
-        }
+        for (int w = 0; w < 2; ++w)
+          v[k][w] = 128 * w + 4 * at_lane < a.d ? __ldcg(reinterpret_cast<const float4*>(a.part + at * a.d + 128 * w + 4 * at_lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-  }
-  l = L != 0.f ? 1.f / L : 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (z0 + k < a.splits && ml[k].x != -INFINITY) {  // (a share that saw nothing holds anything)
+          const float top = fmaxf(M, ml[k].x), ref = top == -INFINITY ? 0.f : top, f = exp2f(M - ref), g = exp2f(ml[k].x - ref);
+          M = top, L = fmaf(ml[k].y, g, L * f);
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            o[4 * w] = fmaf(v[k][w].x, g, o[4 * w] * f), o[4 * w + 1] = fmaf(v[k][w].y, g, o[4 * w + 1] * f);
+            o[4 * w + 2] = fmaf(v[k][w].z, g, o[4 * w + 2] * f), o[4 * w + 3] = fmaf(v[k][w].w, g, o[4 * w + 3] * f);
+          }
+        }
+    }
+  const float inv = L != 0.f ? 1.f / L : 0.f;
   const long long o0 = s * a.os[0] + head * a.os[1] + i * a.os[2];
   bool bad = false;
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
+  for (int w = 0; w < 2; ++w) {
+    const int c = 128 * w + 4 * at_lane;
+    if (!some || c >= a.d) continue;
+    float f[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = 128 * w + 4 * lane + e;
-      const float f = L != 0.f ? o[4 * w + e] * l : 0.f;
-      if (c < a.d) prompt_store(a.out, o0 + c, a.dtype, f), bad |= f != f;
+    for (int e = 0; e < 4; ++e) f[e] = L != 0.f ? o[4 * w + e] * inv : 0.f, bad |= f[e] != f[e];
+    if (a.dtype == HE_DTYPE_BF16) {
+      uint2 two;
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.x) : "f"(f[1]), "f"(f[0]));
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two.y) : "f"(f[3]), "f"(f[2]));
+      *reinterpret_cast<uint2*>(static_cast<char*>(a.out) + 2 * (o0 + c)) = two;
+    } else {
+      *reinterpret_cast<float4*>(static_cast<char*>(a.out) + 4 * (o0 + c)) = make_float4(f[0], f[1], f[2], f[3]);
     }
-  if (__any_sync(0xFFFFFFFFu, bad) && L == L) {
-    const PromptKeys keys = prompt_keys(a, s);
-    __syncwarp();
-    prompt_rows_again(a, s, head, i, 1u, n, keys, -keys.shift, keys.end);
+  }
+  uint32_t odd = __ballot_sync(0xFFFFFFFFu, bad && L == L);
+  __syncwarp();
+  while (odd != 0u) {  // row by row, by the whole warp
+    const int from = (__ffs(odd) - 1) / lanes * lanes;
+    const int s1 = __shfl_sync(0xFFFFFFFFu, s, from), head1 = __shfl_sync(0xFFFFFFFFu, head, from), i1 = __shfl_sync(0xFFFFFFFFu, i, from), n1 = __shfl_sync(0xFFFFFFFFu, n, from);
+    const PromptKeys keys = prompt_keys(a, s1);
+    prompt_rows_again(a, s1, head1, i1, 1u, n1, keys, -keys.shift, keys.end);
+    odd &= ~((lanes == 32 ? 0xFFFFFFFFu : (1u << lanes) - 1u) << from);
   }
 }
 

@@ -232,3 +232,36 @@ def test_a_prompt_in_chunks_then_compressed_then_tokens(dtype, d, eight):
         every, _ = pages.read(n + t + 1)
         loss = cache.attention_loss(q_t, every)
         assert bool((loss.abs() <= 1e-5).all())
+
+
+# (B, H, G, d, rows of each sequence, rows of the tensor, keys): at most 8 rows for a KV head, through the kernel of a new token's attention
+FEW = [(3, 2, 4, 128, [1, 0, 1], 1, [1500, 40, 33]), (2, 1, 8, 64, [1, 1], 1, [2100, 700]), (2, 2, 1, 128, [8, 5], 8, [900, 31]), (1, 3, 2, 80, [3], 4, [1100]), (40, 2, 4, 64, [1] * 40, 1, [53 * i for i in range(40)]),
+       (2, 2, 7, 120, [1, 1], 1, [640, 0]), (1, 1, 1, 8, [7], 7, [300])]
+
+
+@pytest.mark.parametrize("opt", ["all keys", "all keys, cap", "all keys, first", "causal", "causal, cap + bias", "causal, window", "causal, ahead", "causal, behind"])
+@pytest.mark.parametrize("b, h, g, d, q_lens, n, kv_lens", FEW)
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+def test_few_rows(b, h, g, d, q_lens, n, kv_lens, opt, layout):
+    o = OPTIONS[opt]
+    gen = torch.Generator(device="cuda").manual_seed(n + d)
+    m = max(kv_lens) + 5
+    q, k, v = rows(gen, b, h * g, n, d, BF16, layout), rows(gen, b, h, m, d, BF16, layout) * 2, rows(gen, b, h, m, d, BF16, layout)
+    kw = {}
+    if o.get("causal"):
+        kw["q_pos"] = torch.tensor([y - x + o.get("shift", 0) for x, y in zip(q_lens, kv_lens)], dtype=torch.int32, device="cuda")
+    if "first" in o:
+        kw["first_key"] = torch.randint(0, max(kv_lens) // 2 + 1, (b, n), generator=gen, device="cuda").sort(1).values.to(torch.int32)
+    slopes = torch.exp2(-torch.arange(1, h * g + 1, device="cuda") * 8.0 / (h * g)) if o.get("slopes") else None
+    mod = ScoreMod(scale=o.get("scale", 0.0), softcap=o.get("cap", 0.0), window=o.get("window", 0), slopes=slopes)
+    for s in range(b):
+        k[s, :, kv_lens[s]:], v[s, :, kv_lens[s]:] = math.nan, math.nan
+    ql, kl = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (q_lens, kv_lens))
+    cache, out = make_cache(b, h, g, d, BF16), torch.full_like(q, 7.0)
+    ws = torch.full((cache.cross_workspace(n, m).numel(),), 255, dtype=torch.uint8, device="cuda")
+    assert ws.numel() > 0
+    cache.attend_cross(q, k, v, ql, kl, mod=mod, out=out, workspace=ws, **kw)
+    check(out, q, k, v, q_lens, kv_lens, o, kw, slopes, g, n == 1 or "first" not in o and not o.get("causal"))
+    again = torch.full_like(q, 7.0)
+    cache.attend_cross(q, k, v, ql, kl, mod=mod, out=again, workspace=ws, **kw)
+    assert torch.equal(out, again) and device_error_count() == 0
