@@ -779,40 +779,40 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
     __syncwarp();
   }
   __syncthreads();
-  // ---- units that several warps share. Lane e has piece e; units are dealt out to the warps, several warps to one where there are few.
+  // ---- units that several warps share. Lane e has piece e; a thread has four channels of each unit. (Little code: it comes from L2, past what other CTAs still read, and
+  // was waited for longer than executed when units were dealt out to warps: 2 to 8 us.)
   const int mine = lane < 2 * WARPS ? ent_unit[lane] : -1;
   const uint32_t alike = __match_any_sync(0xFFFFFFFFu, mine);
   uint32_t leaders = __ballot_sync(0xFFFFFFFFu, mine >= 0 && lane == __ffs(alike) - 1);
-  static_assert(2 * WARPS <= 32, "a lane for each piece");
-  const int units = __popc(leaders);
+  static_assert(2 * WARPS <= 32 && 4 * THREADS >= kMaxGroup * D, "a lane for each piece, a thread for four channels");
+  const int i = 4 * tid, g = i / d;
 #pragma unroll 1
-  for (int k = 0; leaders != 0u; ++k, leaders &= leaders - 1u) {
-    if (units >= WARPS ? k % WARPS != warp : warp % units != k) continue;
-    const int helpers = units >= WARPS ? 1 : (WARPS - 1 - k) / units + 1, helper = units >= WARPS ? 0 : warp / units;
+  for (; leaders != 0u; leaders &= leaders - 1u) {
     const int first = __ffs(leaders) - 1;
     const uint32_t pieces = __shfl_sync(0xFFFFFFFFu, alike, first);
     const int unit = ent_unit[first], which = ent_flag[first] & 1;
     const bool whole = which && (ent_flag[31 - __clz(pieces)] & 2);
-    float* dst = page_rest_piece(part, gridDim.x, blockIdx.x, which, per);
-#pragma unroll 1
-    for (int i = 4 * (helper * 32 + lane); i < G * d; i += 128 * helpers) {
+    if (i < G * d) {
       PageSum sum;
-      const int g = i / d;
 #pragma unroll 1
       for (uint32_t left = pieces; left != 0u; left &= left - 1u) {
         const float* p = piece_of(__ffs(left) - 1);
         sum.add(p[G * d + g], p[G * d + G + g], *reinterpret_cast<const float4*>(p + i));
       }
-      if (whole) page_emit<ROWS>(a, unit, g, i % d, sum.result());
-      else *reinterpret_cast<float4*>(dst + i) = sum.O;
-      if (!whole && i % d == 0) dst[G * d + g] = sum.M, dst[G * d + G + g] = sum.L;
+      float* dst = page_rest_piece(part, gridDim.x, blockIdx.x, which, per);
+      if (whole) {
+        page_emit<ROWS>(a, unit, g, i - g * d, sum.result());
+      } else {
+        *reinterpret_cast<float4*>(dst + i) = sum.O;
+        if (i == g * d) dst[G * d + g] = sum.M, dst[G * d + G + g] = sum.L;
+        rest->unit[which] = unit;
+      }
     }
-    if (!whole && helper == 0 && lane == 0) rest->unit[which] = unit;
   }
 }
 
 // Units that several CTAs share: the CTA that has a unit's second part puts all of its pieces together, a thread for four channels, the pieces dealt out to as many shares of
-// the threads as there are. What it takes is latency: of two loads that wait for others, and of the pieces' own, eight in flight.
+// the threads as there are. What it takes is latency: of two loads that wait for others, and of the pieces' own, four in flight.
 constexpr int kPageJoinThreads = 512;
 template <bool ROWS>
 static __global__ void __launch_bounds__(kPageJoinThreads) page_join_kernel(const __grid_constant__ TokenArgs a, float* part, int ctas) {
@@ -831,17 +831,17 @@ static __global__ void __launch_bounds__(kPageJoinThreads) page_join_kernel(cons
   PageSum sum;
   if (share < shares)
 #pragma unroll 1
-    for (int z0 = c - 1 + share; z0 < last; z0 += 8 * shares) {
-      float m[8], l[8];
-      float4 o[8];
+    for (int z0 = c - 1 + share; z0 < last; z0 += 4 * shares) {
+      float m[4], l[4];
+      float4 o[4];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < 4; ++k) {
         const int z = min(z0 + k * shares, last - 1);
         const float* p = page_rest_piece(part, ctas, z, z < c ? 1 : 0, per);
         m[k] = __ldcg(p + G * d + g), l[k] = __ldcg(p + G * d + G + g), o[k] = __ldcg(reinterpret_cast<const float4*>(p + i));
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
+      for (int k = 0; k < 4; ++k)
         if (z0 + k * shares < last) sum.add(m[k], l[k], o[k]);
     }
   share_s[tid] = sum;
