@@ -1,5 +1,4 @@
-// Attention of few rows over many keys on the tensor cores: the instances of prompt_tc_kernel that take a share of the keys each (he_attend_cross; their
-// results are joined in layer_ops.cu). A file of its own, as each instance compiles for a while.
+// Attention of rows over keys of another length on the tensor cores (he_attend_cross): its instances of prompt_tc_kernel. A file of its own, as each compiles for a while.
 #include "prompt_launch.h"
 
 using namespace he;
@@ -9,6 +8,6 @@ int he::cross_error_count() {
   return cudaMemcpyFromSymbol(&n, he::g_tc_error, sizeof(int)) == cudaSuccess ? n : -1;
 }
 
-int he::launch_prompt_shares(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
-  return a.d <= 64 ? launch_prompt_tc<64, true>(a, maps, st) : launch_prompt_tc<128, true>(a, maps, st);
+int he::launch_prompt_keys(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
+  return a.d <= 64 ? launch_prompt_tc<64, kOverKeys>(a, maps, st) : launch_prompt_tc<128, kOverKeys>(a, maps, st);
 }

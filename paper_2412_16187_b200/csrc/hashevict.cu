@@ -541,8 +541,11 @@ int he_prefill_phase_events(void* const* events) {
 int he_device_error_count(void) {
   int n = 0;
   if (cudaMemcpyFromSymbol(&n, he::g_tc_error, sizeof(int)) != cudaSuccess) return -1;
-  const int more = he::layer_error_count(), paged = he::page_error_count(), cross = he::cross_error_count();
-  return more < 0 || paged < 0 || cross < 0 ? -1 : n + more + paged + cross;
+  for (const int more : {he::layer_error_count(), he::page_error_count(), he::cross_error_count(), he::shares_error_count()}) {
+    if (more < 0) return -1;
+    n += more;
+  }
+  return n;
 }
 
 int he_hash_keys(const he_config* cfg, const void* x, int64_t rows, int64_t row_stride_elems, const float* W,

@@ -25,9 +25,10 @@ namespace he {
 
 // The trouble counter (g_tc_error) of layer_ops.cu's kernels, -1 if it cannot be read.
 int layer_error_count();
-// The same of pages.cu's and cross_ops.cu's.
+// The same of pages.cu's, cross_ops.cu's and cross_shares.cu's.
 int page_error_count();
 int cross_error_count();
+int shares_error_count();
 
 inline thread_local char g_err[512] = "";
 

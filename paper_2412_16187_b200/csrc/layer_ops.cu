@@ -139,7 +139,8 @@ int launch_rows(const PromptArgs& a, bool tc, cudaStream_t st) {
     PromptMaps maps;
     if (prompt_tmap(a.q, a, a.qs, a.n_kv_heads * a.group, a.tokens, &maps.q) && prompt_tmap(a.k, a, a.ks, a.n_kv_heads, a.keys, &maps.k) &&
         prompt_tmap(a.v, a, a.ks, a.n_kv_heads, a.keys, &maps.v)) {
-      const int rc = a.splits > 1 ? launch_prompt_shares(a, maps, st) : a.d <= 64 ? launch_prompt_tc<64, false>(a, maps, st) : launch_prompt_tc<128, false>(a, maps, st);
+      const int rc = a.splits > 1 ? launch_prompt_shares(a, maps, st) : !a.self ? launch_prompt_keys(a, maps, st)
+                     : a.d <= 64  ? launch_prompt_tc<64, kOverSelf>(a, maps, st) : launch_prompt_tc<128, kOverSelf>(a, maps, st);
       if (rc >= 0) return rc;
     }
   }
@@ -353,7 +354,7 @@ int he_attend_prompt(const he_config* cfg, const he_score_mod* mod, const void* 
                      const int64_t kv_strides[3], const int32_t* prompt_len, int32_t max_prompt_len, const int32_t* doc_start,
                      const int32_t* prefix_len, void* out, const int64_t out_strides[3], void* stream) {
   PromptArgs a{};
-  a.tokens = a.keys = max_prompt_len, a.lens = a.kv_lens = prompt_len, a.doc_start = doc_start, a.prefix = prefix_len, a.splits = 1;
+  a.tokens = a.keys = max_prompt_len, a.lens = a.kv_lens = prompt_len, a.doc_start = doc_start, a.prefix = prefix_len, a.splits = 1, a.self = 1;
   return attend_rows(a, cfg, mod, q, k, v, q_strides, kv_strides, out, out_strides, "max_prompt_len", nullptr, 0, static_cast<cudaStream_t>(stream));
 }
 

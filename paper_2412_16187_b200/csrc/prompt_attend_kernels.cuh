@@ -39,6 +39,7 @@ struct PromptArgs {
   int keys;                // max_kv
   const int32_t* kv_lens;  // [B]
   const int32_t* q_pos;    // [B] or null: position of row 0
+  int self;                // he_attend_prompt
   int all;                 // rows see every key, not only those up to their own position
   int splits;              // > 1: the keys of a tile are shared out, and `part` takes what each share gives
   float* part;             // [splits][B][heads][tokens][d], then [splits][B][heads][tokens][2]: unnormalised outputs; maximum in log2 units and sum of the weights
@@ -65,13 +66,14 @@ __device__ __forceinline__ float* prompt_part_ml(const PromptArgs& a, long long 
 constexpr float kPromptLog2e = 1.4426950408889634f;
 
 // The keys that row i sees; empty for i >= n.
+template <bool CROSS = true>
 __device__ __forceinline__ void prompt_interval(const PromptArgs& a, int s, int i, int n, const PromptKeys& keys, int& lo, int& hi) {
   lo = 0, hi = 0;
   if (i >= n) return;
   lo = -keys.shift;
   if (a.window > 0) lo = max(lo, i - a.window + 1);
   if (a.doc_start != nullptr) lo = max(lo, min(max(a.doc_start[(long long)s * a.tokens + i], 0), kPromptMaxKeys) - keys.shift);
-  hi = a.all ? keys.end : i + 1;
+  hi = CROSS && a.all ? keys.end : i + 1;
   if (a.prefix != nullptr) hi = max(hi, min(max(a.prefix[s], 0), kPromptMaxKeys) - keys.shift);
   hi = min(hi, keys.end);
 }
@@ -315,7 +317,8 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
   constexpr int UNROLL = R == 1 ? 8 : 2;  // one row has few loads in flight otherwise
   const int d = a.d, pitch = d + 4, tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, lane = tid & 31;
   const int heads = a.n_kv_heads * a.group;
-  const int share = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
+  int share = 0, item = blockIdx.x;
+  if (a.splits > 1) share = item % a.splits, item /= a.splits;
   const int head = item % heads, s = (item / heads) % a.batch, tile = tiles - 1 - item / heads / a.batch;
   const int kv = head / a.group, i0 = tile * 16 * R;
   float* qs = psm_;                // [16 R][d + 4]
@@ -326,7 +329,7 @@ __global__ void __launch_bounds__(kPromptThreads, NQ <= 2 ? 2 : 1) prompt_fp32_k
   griddep_wait();
   const int n = min(max(a.lens[s], 0), a.tokens);
   if (i0 >= n) return;
-  const PromptKeys keys = prompt_keys(a, s);
+  const PromptKeys keys = a.self ? PromptKeys{0, n} : prompt_keys(a, s);
   if (tid == 0) run[0] = 0x7FFFFFFF, run[1] = -0x7FFFFFFF;
   int lo[R], hi[R];
 #pragma unroll
@@ -550,10 +553,23 @@ struct PromptMaps {
 // never multiplied), how many keys of the last block lie within the prompt, and per tile the blocks of keys [jb, je) that it needs and at
 // which steps from the last of them on, [all_from, all_to), its rows see every key of the block.
 struct PtItem {
-  int some, s, n, p, tok0, base, last_rows, share;
-  PromptKeys keys;
+  int some, s, n, p, tok0, base, last_rows;
   int jb[2], je[2], all_from[2], all_to[2];
 };
+// What an item of the other kinds has besides. (Four more words in PtItem itself cost he_attend_prompt 5 %: roles copy it.)
+struct PtKeys {
+  PromptKeys keys;
+  int share;  // kOverShares
+};
+template <int KIND>
+struct PtMore {
+  PtKeys at[2];  // of items k & 1
+};
+template <>
+struct PtMore<0> {};
+
+// What the rows of a kernel look at: their own sequence (he_attend_prompt), keys of another length (he_attend_cross), or a share of those.
+constexpr int kOverSelf = 0, kOverKeys = 1, kOverShares = 2;
 
 // One product or commit, issued by the lane of a converged warp that has `leader` set: a predicate on the instruction, so that descriptors stay in
 // uniform registers.
@@ -791,14 +807,14 @@ __device__ __forceinline__ bool pt_wait(uint32_t bar, uint32_t parity, volatile 
 }
 
 // The same for the roles beside the softmax, what follows the first poll in one place (for each kernel, next to its code: one place for all costs up to 2 %).
-template <int D, bool CAP, bool BIAS, bool SPLIT>
+template <int D, bool CAP, bool BIAS, int KIND>
 static __device__ __noinline__ bool pt_wait_far(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   return pt_wait_on(bar, parity, abort_flag, beat);
 }
-template <int D, bool CAP, bool BIAS, bool SPLIT>
+template <int D, bool CAP, bool BIAS, int KIND>
 __device__ __forceinline__ bool pt_wait_small(uint32_t bar, uint32_t parity, volatile int* abort_flag, volatile int* beat) {
   if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity)), 1)) return true;
-  return pt_wait_far<D, CAP, BIAS, SPLIT>(bar, parity, abort_flag, beat);
+  return pt_wait_far<D, CAP, BIAS, KIND>(bar, parity, abort_flag, beat);
 }
 
 // The grid's next waiting CTA, cancelled and taken over: asked for by one lane, answered in 16 bytes of shared memory.
@@ -836,7 +852,7 @@ __device__ __forceinline__ bool pt_read_work(uint32_t answer, int& cta) {
 // At D = 64 a quarter of tensor memory (columns 384 to 511) is not used: P lies where S was, and the next S of a tile waits for it.
 // Tried and slower: blocks of 64 keys with two places for S (0.90 PFLOP/s), one warp that polls both tiles for whichever is ready (0.81), weights handed over
 // in two or four parts, 208 / 80 registers (more spills in the softmax).
-template <int D, bool CAP, bool BIAS, bool SPLIT>
+template <int D, bool CAP, bool BIAS, int KIND>
 __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_constant__ PromptArgs a, const int tiles, const int by_heads,
                                                                    const __grid_constant__ PromptMaps maps) {
   using T = PromptTc<D>;
@@ -845,6 +861,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
   __shared__ __align__(16) uint4 answer_s;
   __shared__ __align__(8) unsigned long long full_s[NS], empty_s[NS], qfull_s[2], qempty_s[2], sfull_s[2], pfull_s[2], odone_s[2], ifull_s[2], iempty_s[2], ask_s, work_s, drain_s;
   __shared__ PtItem item_s[2];
+  __shared__ PtMore<KIND> more_s;
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s, beat_s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -879,6 +896,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
   const uint32_t tmem = tmem_s;
   griddep_launch_dependents();
   auto head_of = [&](const PtItem& w, int t) { return by_heads ? 2 * w.p + t : w.p; };
+  auto keys_of = [&](const PtItem& w, int k) {
+    if constexpr (KIND == kOverSelf) return PromptKeys{0, w.n};
+    else return more_s.at[k & 1].keys;
+  };
   auto tok_of = [&](const PtItem& w, int t) { return by_heads ? w.tok0 : w.tok0 + t * kPtTile; };
   // Item k for a reader's warp (false: there is none, or the CTA has given up), and the end of the reading.
   auto take_item = [&](int k) -> bool { return pt_wait(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat) && item_s[k & 1].some != 0; };
@@ -886,10 +907,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&iempty_s[k & 1]));
   };
+  int key_shift = 0;  // of the item that was read last
   auto read_item = [&](int k, PtItem& w) -> bool {
-    if (!pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat)) return false;
+    if (!pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat)) return false;
     w = item_s[k & 1];
     if (w.some == 0) return false;
+    if constexpr (KIND != kOverSelf) key_shift = more_s.at[k & 1].keys.shift;
     give_item(k);
     return true;
   };
@@ -907,7 +930,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       const int i = tok_of(w, t) + row, head = head_of(w, t), steps = w.je[t] - w.jb[t];
       const int all_from = w.all_from[t], all_to = w.all_to[t];
       int lo, hi, j0 = w.base + w.je[t] * kPtTile;  // the block's first key
-      prompt_interval(a, w.s, i, w.n, w.keys, lo, hi);
+      prompt_interval<KIND != kOverSelf>(a, w.s, i, w.n, keys_of(w, k), lo, hi);
       const float slope = BIAS ? a.slopes[head] * kPromptLog2e : 0.f;
       float m = -INFINITY, l = 0.f;
       for (int it = 0; it < steps; ++it, ++blocks) {
@@ -1059,8 +1082,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       if (ok && steps > 0) ok = pt_wait(smem_u32(&odone_s[t]), outputs++ & 1, abort_flag, beat);
       if (!ok) break;
       tc_fence_after();
-      if (SPLIT) {  // what this share gives, relative to its own maximum
-        const long long at = prompt_part_row(a, w.share, w.s, head, i);
+      if constexpr (KIND == kOverShares) {  // what this share gives, relative to its own maximum
+        const long long at = prompt_part_row(a, more_s.at[k & 1].share, w.s, head, i);
         float* part = a.part + at * a.d;
 #pragma unroll
         for (int c = 0; c < D; c += 32) {
@@ -1104,7 +1127,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       const bool bad = !none && l == l && pt_max(nan[0], nan[1]) != pt_max(nan[0], nan[1]);
       const uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
       __syncwarp();
-      if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, w.keys, w.base + w.jb[t] * kPtTile, min(w.base + w.je[t] * kPtTile, w.keys.end), beat);
+      if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, keys_of(w, k), w.base + w.jb[t] * kPtTile, min(w.base + w.je[t] * kPtTile, keys_of(w, k).end), beat);
       tc_fence_before();
       give_item(k);
     }
@@ -1119,7 +1142,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll
         for (int t = 0; t < 2; ++t)
           if (ok && w.je[t] > w.jb[t]) {
-            if (queries[t] > 0) ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
+            if (queries[t] > 0) ok = pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&qempty_s[t]), (queries[t] - 1) & 1, abort_flag, beat);
             if (!ok) break;
             if (lane == 0) {
               const uint32_t bar = smem_u32(&qfull_s[t]);
@@ -1132,12 +1155,12 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         const int j_begin = w.jb[0] == w.je[0] ? w.jb[1] : w.jb[1] == w.je[1] ? w.jb[0] : min(w.jb[0], w.jb[1]), j_end = max(w.je[0], w.je[1]);
         const int kv = head_of(w, 0) / a.group;
         const int blocks = j_end - j_begin, ask = max(blocks + 1 - kPtAsk, 0);
-        int at_key = w.base + w.keys.shift + j_end * kPtTile;  // of the V block: its position
+        int at_key = w.base + key_shift + j_end * kPtTile;  // of the V block: its position
         if (ok && lane == 0 && blocks == 0) mbar_arrive(smem_u32(&ask_s));
         for (int step = 0; ok && blocks > 0 && step <= blocks; ++step) {
           if (lane == 0 && step == ask) mbar_arrive(smem_u32(&ask_s));
           const uint32_t slot = used % NS;
-          if (used >= NS) ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
+          if (used >= NS) ok = pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&empty_s[slot]), ((used / NS) - 1) & 1, abort_flag, beat);
           if (!ok) break;
           if (lane == 0) {
             const uint32_t bar = smem_u32(&full_s[slot]), at = ring + slot * 2 * T::kTileBytes;
@@ -1174,7 +1197,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 #pragma unroll 1
         for (int j = j_end; j >= j_begin; --j) {
           // O += P V of block j, S of block j - 1, tile by tile
-          ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&full_s[slot]), lap, abort_flag, beat);
+          ok = pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&full_s[slot]), lap, abort_flag, beat);
           if (!ok) break;
           const int rows = w.last_rows;  // (of block j_end - 1; all others are full)
           if (__builtin_expect(j + 1 == j_end && rows < kPtTile, 0)) {  // V rows behind the prompt's end hold anything: zeros
@@ -1190,7 +1213,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             const int t_begin = t ? w.jb[1] : w.jb[0], t_end = t ? w.je[1] : w.je[0];
             const uint32_t s_at = tmem + t * kPtTile;
             if (j >= t_begin && j < t_end) {
-              ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&pfull_s[t]), (taken >> t) & 1, abort_flag, beat);
+              ok = pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&pfull_s[t]), (taken >> t) & 1, abort_flag, beat);
               if (!ok) break;
               taken ^= 1u << t;
               tc_fence_after();
@@ -1201,7 +1224,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             }
             if (j > t_begin && j <= t_end) {
               if (j == t_end) {
-                ok = pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
+                ok = pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&qfull_s[t]), (queries >> t) & 1, abort_flag, beat);
                 if (!ok) break;
                 queries ^= 1u << t;
               }
@@ -1230,11 +1253,13 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       int cta = blockIdx.x, k = 0;
       uint32_t asked = 0;
       bool ok = true;
+      PtKeys more{};
       auto hand_over = [&](const PtItem& w) {
-        if (k >= 2) ok = ok && pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
+        if (k >= 2) ok = ok && pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&iempty_s[k & 1]), ((k >> 1) - 1) & 1, abort_flag, beat);
         if (!ok) return;
         if (lane == 0) {
           item_s[k & 1] = w;
+          if constexpr (KIND != kOverSelf) more_s.at[k & 1] = more;
           mbar_arrive(smem_u32(&ifull_s[k & 1]));
         }
         __syncwarp();
@@ -1243,14 +1268,14 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       PtItem w;
       while (ok) {
         int item = cta;
-        w.some = 1, w.share = 0;
-        if (SPLIT) w.share = cta % a.splits, item = cta / a.splits;
+        w.some = 1;
+        if (KIND == kOverShares) more.share = cta % a.splits, item = cta / a.splits;
         w.p = item % per, w.s = (item / per) % a.batch;
         const int tile = tiles - 1 - item / per / a.batch;
         w.tok0 = by_heads ? tile * kPtTile : tile * 2 * kPtTile;
         w.n = min(max(a.lens[w.s], 0), a.tokens);
         if (w.tok0 < w.n) {
-          w.keys = prompt_keys(a, w.s);
+          more.keys = KIND == kOverSelf ? PromptKeys{0, w.n} : prompt_keys(a, w.s);
           w.base = 0x7FFFFFFF;
           for (int t = 0; t < 2; ++t) {
             int first = 0x7FFFFFFF, end = -0x7FFFFFFF, all_lo = -0x7FFFFFFF, all_hi = 0x7FFFFFFF;  // what its rows see, any and all of them
@@ -1258,7 +1283,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             for (int r = 0; r < kPtTile / 32; ++r) {
               const int i = tok_of(w, t) + 32 * r + lane;
               int lo, hi;
-              prompt_interval(a, w.s, i, w.n, w.keys, lo, hi);
+              prompt_interval<KIND != kOverSelf>(a, w.s, i, w.n, more.keys, lo, hi);
               if (lo < hi) first = min(first, lo), end = max(end, hi);
               if (i < w.n) all_lo = max(all_lo, lo < hi ? lo : 0x7FFFFFFF), all_hi = min(all_hi, hi);
             }
@@ -1272,10 +1297,10 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             w.all_from[t] = w.je[t] - max(w.all_from[t] - w.base, 0) / kPtTile;
             w.all_to[t] = w.je[t] - (int)(((unsigned)w.all_to[t] - (unsigned)w.base + kPtTile - 1) / kPtTile);
           }
-          if (SPLIT) {  // this share's blocks, of those that either tile needs
+          if (KIND == kOverShares) {  // this share's blocks, of those that either tile needs
             const bool one = w.jb[0] < w.je[0], two = w.jb[1] < w.je[1];
             const int begin = one && two ? min(w.jb[0], w.jb[1]) : one ? w.jb[0] : w.jb[1], blocks = max(w.je[0], w.je[1]) - begin;
-            const int from = begin + (int)((long long)blocks * w.share / a.splits), to = begin + (int)((long long)blocks * (w.share + 1) / a.splits);
+            const int from = begin + (int)((long long)blocks * more.share / a.splits), to = begin + (int)((long long)blocks * (more.share + 1) / a.splits);
             for (int t = 0; t < 2; ++t) {
               const int end = min(w.je[t], to), less = w.je[t] - end;
               w.jb[t] = max(w.jb[t], from), w.je[t] = end;
@@ -1283,15 +1308,15 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
               if (w.jb[t] >= w.je[t]) w.jb[t] = w.je[t] = 0;
             }
           }
-          w.last_rows = w.keys.end - w.base - (max(w.je[0], w.je[1]) - 1) * kPtTile;
+          w.last_rows = more.keys.end - w.base - (max(w.je[0], w.je[1]) - 1) * kPtTile;
           hand_over(w);
           // not before this item is nearly done: a CTA that took the next one at once would be bound to it however long this one lasts
-          ok = ok && pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
+          ok = ok && pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&ask_s), (k - 1) & 1, abort_flag, beat);
         }
         if (!ok) break;
         if (lane == 0) pt_ask_work(answer, smem_u32(&work_s));
         ++asked;
-        if (!pt_wait_small<D, CAP, BIAS, SPLIT>(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
+        if (!pt_wait_small<D, CAP, BIAS, KIND>(smem_u32(&work_s), (asked - 1) & 1, abort_flag, beat)) break;
         const bool more = pt_read_work(answer, cta);
         __syncwarp();  // every lane has read the answer before the next one may be written
         if (!more) {

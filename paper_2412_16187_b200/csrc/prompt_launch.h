@@ -1,4 +1,4 @@
-// Host side of the attention of prompts and of rows over keys of another length that layer_ops.cu and cross_ops.cu share: tiles, tensor maps, launches.
+// Host side of the attention of prompts and of rows over keys of another length that layer_ops.cu, cross_ops.cu and cross_shares.cu share: tiles, tensor maps, launches.
 #pragma once
 #include "host_common.h"
 #include "prompt_attend_kernels.cuh"
@@ -7,7 +7,8 @@
 
 namespace he {
 
-// prompt_tc_kernel with the keys shared out (cross_ops.cu): HE_OK, an error, or -1: the caller's other kernel serves.
+// prompt_tc_kernel over keys of another length (cross_ops.cu), and with the keys shared out (cross_shares.cu): HE_OK, an error, or -1: the caller's other kernel serves.
+int launch_prompt_keys(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st);
 int launch_prompt_shares(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st);
 
 // Work items of prompt_tc_kernel: two query heads by 128 rows, or one head by 256.
@@ -51,9 +52,9 @@ int registers_suffice(K kernel, int* out) {
 }
 
 // HE_OK, an error, or -1: the caller's other kernel serves.
-template <int D, bool CAP, bool BIAS, bool SPLIT>
+template <int D, bool CAP, bool BIAS, int KIND>
 int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
-  auto kernel = prompt_tc_kernel<D, CAP, BIAS, SPLIT>;
+  auto kernel = prompt_tc_kernel<D, CAP, BIAS, KIND>;
   static DeviceTable<1> table;
   int dev = 0, enough = 0;
   HE_CUDA_CHECK(cudaGetDevice(&dev));
@@ -61,16 +62,16 @@ int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t s
   if (int rc = table.get(dev, 0, &enough, [&](int* got) { return registers_suffice(kernel, got); })) return rc;
   if (enough != 1) return -1;
   const PromptTiles t = prompt_tc_tiles(a);
-  const long long ctas = t.items * (SPLIT ? a.splits : 1);
+  const long long ctas = t.items * (KIND == kOverShares ? a.splits : 1);
   if (ctas > 0x7FFFFFFFLL) return fail(HE_ERR_UNSUPPORTED, "%lld tiles in one call", ctas);
   if (int rc = set_smem(kernel, PromptTc<D>::kSmem)) return rc;
   return launch_pdl(kernel, dim3((unsigned)ctas), kPtThreads, PromptTc<D>::kSmem, true, st, a, t.tiles, t.by_heads, maps);
 }
-template <int D, bool SPLIT>
+template <int D, int KIND>
 int launch_prompt_tc(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
   if (a.cap_log2 > 0.f)
-    return a.slopes != nullptr ? launch_prompt_tc<D, true, true, SPLIT>(a, maps, st) : launch_prompt_tc<D, true, false, SPLIT>(a, maps, st);
-  return a.slopes != nullptr ? launch_prompt_tc<D, false, true, SPLIT>(a, maps, st) : launch_prompt_tc<D, false, false, SPLIT>(a, maps, st);
+    return a.slopes != nullptr ? launch_prompt_tc<D, true, true, KIND>(a, maps, st) : launch_prompt_tc<D, true, false, KIND>(a, maps, st);
+  return a.slopes != nullptr ? launch_prompt_tc<D, false, true, KIND>(a, maps, st) : launch_prompt_tc<D, false, false, KIND>(a, maps, st);
 }
 
 }  // namespace he
