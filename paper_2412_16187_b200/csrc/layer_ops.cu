@@ -102,12 +102,12 @@ int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
   if (int rc = set_smem(kernel, smem)) return rc;
   return launch_pdl(kernel, dim3((unsigned)ctas), kPromptThreads, smem, true, st, a, tiles, stages);
 }
-// Tiles of 64 rows once there is one for every SM, else of 16.
+// Tiles of 64 rows once there is one for every SM, else of 16 (also for up to 16 rows over keys of another length).
 template <int NQ>
 int launch_prompt_fp32(const PromptArgs& a, cudaStream_t st) {
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
-  return prompt_fp32_tiles(a, 64) >= sms ? launch_prompt_fp32<NQ, 4>(a, st) : launch_prompt_fp32<NQ, 1>(a, st);
+  return prompt_fp32_tiles(a, 64) >= sms && (a.self || a.tokens > 16) ? launch_prompt_fp32<NQ, 4>(a, st) : launch_prompt_fp32<NQ, 1>(a, st);
 }
 
 bool on_tensor_cores(const PromptArgs& a) { return a.dtype == HE_DTYPE_BF16 && a.d <= 128 && getenv("HE_DISABLE_ATTEND_MMA") == nullptr; }
@@ -124,7 +124,7 @@ int prompt_splits(const PromptArgs& a, bool tc, int* out) {
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
   long long items = tc ? prompt_tc_tiles(a).items : prompt_fp32_tiles(a, 64);
-  if (!tc && items < sms) items = prompt_fp32_tiles(a, 16);
+  if (!tc && (items < sms || a.tokens <= 16)) items = prompt_fp32_tiles(a, 16);
   *out = 1;
   const long long blocks = ((long long)a.keys + (tc ? 127 : 63)) / (tc ? 128 : 64);
   double best = 0.0;
@@ -137,8 +137,8 @@ int prompt_splits(const PromptArgs& a, bool tc, int* out) {
 int launch_rows(const PromptArgs& a, bool tc, cudaStream_t st) {
   if (tc) {
     PromptMaps maps;
-    if (prompt_tmap(a.q, a, a.qs, a.n_kv_heads * a.group, a.tokens, &maps.q) && prompt_tmap(a.k, a, a.ks, a.n_kv_heads, a.keys, &maps.k) &&
-        prompt_tmap(a.v, a, a.ks, a.n_kv_heads, a.keys, &maps.v)) {
+    if (prompt_tmap(a.q, a, a.qs, a.n_kv_heads * a.group, a.tokens, 1 << a.pack, &maps.q) && prompt_tmap(a.k, a, a.ks, a.n_kv_heads, a.keys, 1, &maps.k) &&
+        prompt_tmap(a.v, a, a.ks, a.n_kv_heads, a.keys, 1, &maps.v)) {
       const int rc = a.splits > 1 ? launch_prompt_shares(a, maps, st) : !a.self ? launch_prompt_keys(a, maps, st)
                      : a.d <= 64  ? launch_prompt_tc<64, kOverSelf>(a, maps, st) : launch_prompt_tc<128, kOverSelf>(a, maps, st);
       if (rc >= 0) return rc;
@@ -175,6 +175,7 @@ int attend_rows(PromptArgs& a, const he_config* cfg, const he_score_mod* mod, co
   a.q = q, a.k = k, a.v = v, a.out = out;
   for (int i = 0; i < 3; ++i) a.qs[i] = q_strides[i], a.ks[i] = kv_strides[i], a.os[i] = out_strides[i];
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype;
+  prompt_pack(a);
   const bool tc = on_tensor_cores(a);
   if (workspace != nullptr) {
     // one row a sequence, or a few that see the same keys: K and V are read once for all of them
@@ -363,6 +364,7 @@ size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, 
   PromptArgs a{};
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_q_len, a.keys = max_kv_len;
   int splits = 1;
+  prompt_pack(a);
   if (prompt_splits(a, on_tensor_cores(a), &splits)) return 0;
   return std::max(prompt_part_bytes(a, splits), few_rows_workspace(cfg, max_q_len, max_kv_len));
 }

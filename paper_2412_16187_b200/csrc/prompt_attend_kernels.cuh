@@ -41,6 +41,7 @@ struct PromptArgs {
   const int32_t* q_pos;    // [B] or null: position of row 0
   int self;                // he_attend_prompt
   int all;                 // rows see every key, not only those up to their own position
+  int pack, packs;         // a tile holds 128 >> pack rows of 1 << pack query heads of a KV head, so a KV head's query heads make `packs` (0 and group for he_attend_prompt)
   int splits;              // > 1: the keys of a tile are shared out, and `part` takes what each share gives
   float* part;             // [splits][B][heads][tokens][d], then [splits][B][heads][tokens][2]: unnormalised outputs; maximum in log2 units and sum of the weights
 };
@@ -865,7 +866,8 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s, beat_s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int heads = a.n_kv_heads * a.group, per = by_heads ? heads / 2 : heads;
+  const int heads = a.n_kv_heads * (KIND == kOverSelf ? a.group : a.packs), per = by_heads ? heads / 2 : heads;
+  const int pack = KIND == kOverSelf ? 0 : a.pack, rows_of = kPtTile >> pack;  // rows of a head in a tile
   const uint32_t smem0 = (smem_u32(pt_smem_raw) + 1023u) & ~1023u;
   const uint32_t q_smem = smem0, ring = smem0 + 2 * T::kTileBytes;
   volatile int *abort_flag = &abort_s, *beat = &beat_s;
@@ -895,12 +897,15 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
   tc_fence_after();
   const uint32_t tmem = tmem_s;
   griddep_launch_dependents();
-  auto head_of = [&](const PtItem& w, int t) { return by_heads ? 2 * w.p + t : w.p; };
+  auto head_of = [&](const PtItem& w, int t) {  // the tile's first
+    const int q = by_heads ? 2 * w.p + t : w.p;
+    return KIND == kOverSelf ? q : q / a.packs * a.group + ((q % a.packs) << pack);
+  };
   auto keys_of = [&](const PtItem& w, int k) {
     if constexpr (KIND == kOverSelf) return PromptKeys{0, w.n};
     else return more_s.at[k & 1].keys;
   };
-  auto tok_of = [&](const PtItem& w, int t) { return by_heads ? w.tok0 : w.tok0 + t * kPtTile; };
+  auto tok_of = [&](const PtItem& w, int t) { return by_heads ? w.tok0 : w.tok0 + t * rows_of; };
   // Item k for a reader's warp (false: there is none, or the CTA has given up), and the end of the reading.
   auto take_item = [&](int k) -> bool { return pt_wait(smem_u32(&ifull_s[k & 1]), (k >> 1) & 1, abort_flag, beat) && item_s[k & 1].some != 0; };
   auto give_item = [&](int k) {
@@ -927,7 +932,13 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
     bool ok = true;
     for (int k = 0; ok && take_item(k); ++k) {
       const PtItem& w = item_s[k & 1];  // (read where it is used: registers are short here)
-      const int i = tok_of(w, t) + row, head = head_of(w, t), steps = w.je[t] - w.jb[t];
+      int i = tok_of(w, t) + row, head = head_of(w, t);
+      const int steps = w.je[t] - w.jb[t];
+      if (KIND != kOverSelf && pack > 0) {
+        const int last = (head / a.group + 1) * a.group - 1;
+        i = tok_of(w, t) + (row & (rows_of - 1)), head += row >> (7 - pack);
+        if (head > last) i = 0x3FFFFFFF, head = last;  // (a group that does not fill its last tile: rows behind the end)
+      }
       const int all_from = w.all_from[t], all_to = w.all_to[t];
       int lo, hi, j0 = w.base + w.je[t] * kPtTile;  // the block's first key
       prompt_interval<KIND != kOverSelf>(a, w.s, i, w.n, keys_of(w, k), lo, hi);
@@ -992,7 +1003,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         if (BIAS) {
           const float away = (float)(j0 - i);
           const pt2 sc(scale, scale);
-          if (a.prefix == nullptr || j0 + kPtTile - 1 <= i - row) {  // no row sees a key behind it
+          if (a.prefix == nullptr || j0 + kPtTile - 1 <= (KIND == kOverSelf ? i - row : tok_of(w, t))) {  // no row sees a key behind it
             const pt2 up(8.f * slope, 8.f * slope);
 #pragma unroll
             for (int q = 0; q < 128; q += 32) {
@@ -1272,7 +1283,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         if (KIND == kOverShares) more.share = cta % a.splits, item = cta / a.splits;
         w.p = item % per, w.s = (item / per) % a.batch;
         const int tile = tiles - 1 - item / per / a.batch;
-        w.tok0 = by_heads ? tile * kPtTile : tile * 2 * kPtTile;
+        w.tok0 = by_heads ? tile * rows_of : tile * 2 * rows_of;
         w.n = min(max(a.lens[w.s], 0), a.tokens);
         if (w.tok0 < w.n) {
           more.keys = KIND == kOverSelf ? PromptKeys{0, w.n} : prompt_keys(a, w.s);
@@ -1281,7 +1292,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
             int first = 0x7FFFFFFF, end = -0x7FFFFFFF, all_lo = -0x7FFFFFFF, all_hi = 0x7FFFFFFF;  // what its rows see, any and all of them
 #pragma unroll 1
             for (int r = 0; r < kPtTile / 32; ++r) {
-              const int i = tok_of(w, t) + 32 * r + lane;
+              const int i = tok_of(w, t) + ((32 * r + lane) & (rows_of - 1));
               int lo, hi;
               prompt_interval<KIND != kOverSelf>(a, w.s, i, w.n, more.keys, lo, hi);
               if (lo < hi) first = min(first, lo), end = max(end, hi);

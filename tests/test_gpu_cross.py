@@ -265,3 +265,21 @@ def test_few_rows(b, h, g, d, q_lens, n, kv_lens, opt, layout):
     again = torch.full_like(q, 7.0)
     cache.attend_cross(q, k, v, ql, kl, mod=mod, out=again, workspace=ws, **kw)
     assert torch.equal(out, again) and device_error_count() == 0
+
+
+# rows of several query heads in one tile: 32 rows of four heads, 64 of two, groups that do not fill their last tile
+PACKED = [(2, 2, 8, 128, BF16, [20, 29], [900, 300], "heads"), (1, 2, 7, 64, BF16, [5], [1400], "tokens"), (2, 1, 3, 80, BF16, [40, 61], [700, 500], "tokens"), (1, 3, 2, 128, BF16, [33], [600], "heads"),
+          (2, 2, 5, 128, BF16, [61, 0], [129, 40], "heads"), (3, 1, 6, 64, BF16, [2, 29, 1], [0, 5, 2000], "heads")]
+
+
+@pytest.mark.parametrize("opt", list(OPTIONS))
+@pytest.mark.parametrize("shape", PACKED, ids=[f"{'x'.join(map(str, s[:4]))}-{max(s[5])}-{max(s[6])}" for s in PACKED])
+@pytest.mark.parametrize("path", ["default", "whole"])
+def test_rows_of_several_heads_in_a_tile(shape, opt, path, monkeypatch):
+    test_attend_cross(shape, opt, path, monkeypatch)
+
+
+@pytest.mark.parametrize("whole", [True, False])
+def test_hidden_values_where_a_tile_holds_several_heads(whole):
+    for opt in ("causal, window", "all keys, first"):
+        test_hidden_infinities_and_nans_touch_nobody((1, 1, 4, 128, BF16, [30], [1500], "heads"), opt, whole)
