@@ -675,19 +675,33 @@ __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const std
       }
     };
     if constexpr (E == 1) {
-      for (; r < kScoredSlots; next()) {
-        const long long row = visible(r) ? row_of(j0 + r) : -1;
-        float kf[16] = {}, vf[16] = {};
-        if (row >= 0) {
-          const long long at = row / a.pages.page_size;
-          page_unpack(ldg_stream16(reinterpret_cast<const uint4*>(Kb + row * d + 16 * c)), __ldcg(a.pages.k_scale + at), kf);
-          page_unpack(ldg_stream16(reinterpret_cast<const uint4*>(Vb + row * d + 16 * c)), __ldcg(a.pages.v_scale + at), vf);
+      while (r < kScoredSlots) {  // four rows' codes at a time in registers
+        uint4 k4[4], v4[4];
+        float ks4[4], vs4[4];
+        int rr[4], cc[4];
+        long long row[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u, next()) rr[u] = r, cc[u] = c, row[u] = r < kScoredSlots && visible(r) ? row_of(j0 + r) : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          k4[u] = v4[u] = make_uint4(0u, 0u, 0u, 0u), ks4[u] = vs4[u] = 0.f;
+          if (row[u] >= 0) {
+            const long long at = row[u] / a.pages.page_size;
+            k4[u] = ldg_stream16(reinterpret_cast<const uint4*>(Kb + row[u] * d + 16 * cc[u])), v4[u] = ldg_stream16(reinterpret_cast<const uint4*>(Vb + row[u] * d + 16 * cc[u]));
+            ks4[u] = __ldcg(a.pages.k_scale + at), vs4[u] = __ldcg(a.pages.v_scale + at);
+          }
         }
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          *reinterpret_cast<float4*>(kt + r * pitch + 16 * c + e) = make_float4(kf[e], kf[e + 1], kf[e + 2], kf[e + 3]);
-          *reinterpret_cast<float4*>(vt + r * d + 16 * c + e) = make_float4(vf[e], vf[e + 1], vf[e + 2], vf[e + 3]);
-        }
+        for (int u = 0; u < 4; ++u)
+          if (rr[u] < kScoredSlots) {
+            float kf[16], vf[16];
+            page_unpack(k4[u], ks4[u], kf), page_unpack(v4[u], vs4[u], vf);
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              *reinterpret_cast<float4*>(kt + rr[u] * pitch + 16 * cc[u] + e) = make_float4(kf[e], kf[e + 1], kf[e + 2], kf[e + 3]);
+              *reinterpret_cast<float4*>(vt + rr[u] * d + 16 * cc[u] + e) = make_float4(vf[e], vf[e + 1], vf[e + 2], vf[e + 3]);
+            }
+          }
       }
     } else if (E == 4) {
       for (; r < kScoredSlots; next()) {

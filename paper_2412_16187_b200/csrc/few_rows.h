@@ -17,10 +17,15 @@ struct RowsOverCall {
   int window, rows, keys;
 };
 
+// Whether units, a sequence's groups of 32 keys and a CTA's share of all of them can be counted in 32 bits (page_attend_kernel).
+inline bool page_line_fits(const he_config* cfg, long long keys) {
+  const double units = (double)cfg->batch * cfg->n_kv_heads, groups = (double)(keys / 32 + 1);
+  return units < 2147483647.0 && (double)cfg->n_kv_heads * groups < 2147483647.0 && units * groups < 1e11;
+}
 // Whether `rows` rows of each query head over up to `keys` keys are few enough, where all rows of a sequence see the same keys.
 inline bool few_rows(const he_config* cfg, int rows, int keys) {
   return cfg->dtype == HE_DTYPE_BF16 && cfg->head_dim <= 128 && keys > 0 && (long long)rows * cfg->group_size <= kMaxGroup &&
-         (long long)cfg->n_kv_heads * ((long long)keys / 32 + 1) <= 0x7FFFFFFFLL && getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
+         page_line_fits(cfg, keys) && getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
 }
 // Bytes of `part` (0: not served).
 size_t few_rows_workspace(const he_config* cfg, int rows, int keys);

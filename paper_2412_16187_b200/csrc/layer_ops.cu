@@ -123,6 +123,7 @@ size_t prompt_part_bytes(const PromptArgs& a, int splits) {
 int prompt_splits(const PromptArgs& a, bool tc, int* out) {
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
+  if (!tc && a.d <= 128) sms *= 2;  // (CTAs of an SM)
   long long items = tc ? prompt_tc_tiles(a).items : prompt_fp32_tiles(a, 64);
   if (!tc && (items < sms || a.tokens <= 16)) items = prompt_fp32_tiles(a, 16);
   *out = 1;

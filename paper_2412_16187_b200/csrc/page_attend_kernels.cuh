@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
   const int groups = warp_begin(warp + 1) - warp_begin(warp), items = 2 * groups;
   PageCursor ask{};  // the group that is asked for next
   if (groups > 0) page_find<WARPS, ROWS>(a, each, table, begin + warp_begin(warp), ask);
-  __syncthreads();  // the table has been read
+  fence_proxy_async();  // the table has been read, and copies come into its place
+  __syncthreads();
   auto advance = [&](PageCursor& c) {
     if (++c.g < c.span.g1) return;
     if (++c.h == H) {

@@ -23,6 +23,7 @@ struct AppendArgs {
   int max_new, n_kv_heads, d;
   int tiles;  // pages that the new rows of a sequence may touch
   int units, heads_per_cta;
+  int turns;  // whether keys are rotated; else `rot` says where a thread's pieces lie and nothing more
 };
 
 constexpr int kAppendThreads = 1024;  // at most
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       sn[i] = 0.f, cs[i] = 1.f;
-      if (p.some && V * p.u + i < half) rotary_sincos(rot, V * p.u + i, at * P + p.row, sn[i], cs[i]);
+      if (a.turns && p.some && V * p.u + i < half) rotary_sincos(rot, V * p.u + i, at * P + p.row, sn[i], cs[i]);
     }
   };
   auto read = [&](const AppendPlace& p, int w, int h, Piece (&x)[2]) {
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
     // the rows of a place as they go into the page
     auto fetch = [&](const AppendPlace& p) {
       read(p, 0, h, x[0]), read(p, 1, h, x[1]);
-      if (p.some) {
+      if (a.turns && p.some) {
         sines(p, sn, cs);
         rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, p.u, half, p.turns);
       }
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
       for (int w = 0; w < 2; ++w)
 #pragma unroll
         for (int e = 0; e < 2; ++e) x[w][e].load(reinterpret_cast<const char*>(append_s + (size_t)(((h & 1) * 4 + 2 * w + e) * threads + tid)));
-      if (mine.some) rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, mine.u, half, mine.turns);
+      if (a.turns && mine.some) rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, mine.u, half, mine.turns);
       if (Q8) look(mine, 0, x[0], false), look(mine, 1, x[1], false);
       else write(mine, x[0], dst[0], 1.f, std::false_type()), write(mine, x[1], dst[1], 1.f, std::false_type());
     } else {

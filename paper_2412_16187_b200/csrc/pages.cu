@@ -143,8 +143,7 @@ int launch_page_attend(const TokenArgs& a, float* part, const PageMaps& maps, cu
 // Whether the tensor cores serve a call (where the driver makes tensor maps): rows of bf16 or of codes up to 128 channels, few enough for a map's coordinates.
 bool page_tensor_cores(const he_config* cfg, const he_pages* p) {
   return (p->eight_bit || cfg->dtype == HE_DTYPE_BF16) && cfg->head_dim <= 128 && (long long)p->n_pages * cfg->n_kv_heads * p->page_size < 0x7FFFFF00LL &&
-         (long long)cfg->n_kv_heads * (page_capacity(*p) / kPageGroup + 1) <= 0x7FFFFFFFLL &&
-         getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
+         page_line_fits(cfg, page_capacity(*p)) && getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
 }
 
 // Tensor map of keys or values: {channel, token, head, sequence} in boxes of 64 channels x 32 tokens. An axis of one entry may come with any stride.
@@ -191,7 +190,8 @@ int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary*
                    const int32_t* new_len, int32_t max_new, void* stream) {
   if (int rc = check_config(cfg, true)) return rc;
   if (int rc = check_pages(cfg, pages)) return rc;
-  he_rotary none{};
+  he_rotary none{};  // (halves of a row side by side in a warp write whole sectors: 512 MB of 8-bit pages 83 us, pieces next to each other 111)
+  none.channels = cfg != nullptr && cfg->head_dim % (2 * 16 / esize_of(cfg->dtype)) == 0 ? cfg->head_dim : 0;
   if (rotary != nullptr)
     if (int rc = check_rotary(rotary, cfg->head_dim)) return rc;
   if (max_new < 0) return fail(HE_ERR_INVALID_ARG, "max_new %d < 0", max_new);
@@ -204,7 +204,7 @@ int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary*
   a.pages = *pages, a.x[0] = k, a.x[1] = v, a.new_len = new_len, a.max_new = max_new, a.n_kv_heads = cfg->n_kv_heads, a.d = cfg->head_dim;
   for (int i = 0; i < 3; ++i) a.strides[i] = kv_strides[i];
   const int P = pages->page_size, V = rotary_piece(r, es);
-  a.units = rotary_units(r, cfg->head_dim, V);
+  a.units = rotary_units(r, cfg->head_dim, V), a.turns = rotary != nullptr;
   const long long most = ((long long)max_new + P - 2) / P + 1;  // (they may begin on a page's last row)
   a.tiles = (int)(most < pages->max_pages ? most : pages->max_pages);
   const long long ctas = (long long)cfg->batch * a.tiles;

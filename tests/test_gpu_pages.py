@@ -193,7 +193,7 @@ CACHES = [
     ((1, 8, 4, 128, 128, BF16, True), [2900]), ((2, 1, 8, 64, 32, BF16, True), [700, 64]), ((2, 2, 5, 96, 16, BF16, True), [333, 32]), ((200, 1, 2, 64, 16, BF16, False), list(range(200))),
     ((2, 2, 2, 24, 16, BF16, False), [100, 31]), ((2, 1, 1, 80, 64, BF16, True), [1300, 1]), ((4, 2, 4, 128, 32, BF16, False), [1, 4100, 0, 31]), ((2, 3, 8, 128, 16, BF16, True), [17, 1500]),
     ((1, 2, 2, 256, 128, F32, True), [700]), ((2, 2, 8, 128, 64, F32, True), [600, 63]), ((1, 1, 1, 8, 16, F32, False), [40]), ((300, 2, 4, 64, 32, BF16, True), [7 * i % 97 for i in range(300)]),
-    ((3, 2, 4, 64, 128, BF16, False), [2000, 129, 3]), ((2, 1, 6, 104, 16, BF16, False), [900, 15]),
+    ((3, 2, 4, 64, 128, BF16, False), [2000, 129, 3]), ((2, 1, 6, 104, 16, BF16, False), [900, 15]), ((2, 2, 3, 144, 32, BF16, True), [200, 70]), ((1, 1, 8, 240, 64, F32, True), [150]),
 ]
 NAMES = [f"{'x'.join(map(str, s[:4]))}-p{s[4]}-{'bf16' if s[5] == BF16 else 'fp32'}{'-8bit' if s[6] else ''}-{max(n)}" for s, n in CACHES]
 
