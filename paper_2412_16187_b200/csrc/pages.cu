@@ -191,7 +191,7 @@ int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary*
   if (int rc = check_config(cfg, true)) return rc;
   if (int rc = check_pages(cfg, pages)) return rc;
   he_rotary none{};  // (halves of a row side by side in a warp write whole sectors: 512 MB of 8-bit pages 83 us, pieces next to each other 111)
-  none.channels = cfg != nullptr && cfg->head_dim % (2 * 16 / esize_of(cfg->dtype)) == 0 ? cfg->head_dim : 0;
+  none.channels = cfg->head_dim % (2 * 16 / esize_of(cfg->dtype)) == 0 ? cfg->head_dim : 0;
   if (rotary != nullptr)
     if (int rc = check_rotary(rotary, cfg->head_dim)) return rc;
   if (max_new < 0) return fail(HE_ERR_INVALID_ARG, "max_new %d < 0", max_new);

@@ -1354,7 +1354,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
 // the weighted sum of their sums. A row whose output is a NaN that its sum does not explain is computed once more, as the kernels above do.
 constexpr int kJoinThreads = 128;
 __host__ __device__ inline int prompt_join_lanes(int d) { return d <= 16 ? 4 : d <= 32 ? 8 : d <= 64 ? 16 : 32; }  // of a row
-static __global__ void __launch_bounds__(kJoinThreads) prompt_join_kernel(const __grid_constant__ PromptArgs a) {
+static __global__ void __launch_bounds__(kJoinThreads, 8) prompt_join_kernel(const __grid_constant__ PromptArgs a) {
   const int lane = threadIdx.x & 31, heads = a.n_kv_heads * a.group, lanes = prompt_join_lanes(a.d), at_lane = lane % lanes;
   const long long item = ((long long)blockIdx.x * kJoinThreads + threadIdx.x) / lanes;
   griddep_wait();
