@@ -294,7 +294,8 @@ int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score
  * (layouts, strides, accuracy, what runs where) as for he_attend_prompt.
  * workspace (16-byte aligned; he_attend_cross_workspace_bytes(cfg, max_q_len, max_kv_len) bytes, 0 where none is of use) lets few rows over many keys fill the GPU: the
  * keys are then shared out and the shares' results joined in a fixed order. It holds nothing from one call to the next; calls that may run at the same time need one
- * each. NULL: a tile of rows walks over all its keys.
+ * each. NULL: a tile of rows walks over all its keys. With it, too, one bf16 row a sequence (d <= 128), or up to 8 rows of a KV head's query heads that all see the same keys, are
+ * computed as he_page_attend does (weights of about fp32's accuracy), without it as other rows are.
  */
 size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, int32_t max_kv_len);
 int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
@@ -346,7 +347,8 @@ int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary*
  * max(first_pos[s], len[s] - w, 0) <= j < len[s]. q: [B, Hkv*G, d] in the dtype of cfg (contiguous), out: [B, Hkv*G, d] fp32; mod and first_pos may be NULL, as there. Without
  * either it is also the single-token form of he_attend_cross over encoder states that were appended without a rotation. A sequence that holds nothing, or whose every token is
  * hidden, gives zeros; a token whose score is a NaN or +inf gives NaN; what hidden tokens hold reaches nobody. Pages that the query does not see are not read.
- * Accuracy as for he_attend_scored, over the values that the pages stand for.
+ * Accuracy as for he_attend_scored, over the values that the pages stand for. bf16 and 8-bit pages with head_dim <= 128 run on the tensor cores, whatever the lengths of the
+ * sequences are; fp32 pages and larger heads on the CUDA cores, several times as long.
  * workspace: 16-byte aligned, he_page_attend_workspace_bytes(cfg, pages) bytes (0: may be NULL; it depends on the shapes alone); it holds nothing from one call to the next;
  * calls that may run at the same time need one each.
  */

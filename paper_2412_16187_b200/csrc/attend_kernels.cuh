@@ -586,7 +586,8 @@ __device__ __forceinline__ void cp_async16_or_zero(void* smem_dst, const void* g
 }
 
 // With PAGED (he_page_attend) slot j is token j, from the tile that holds the first visible one on, and its rows lie in a page (E = 1: codes of 8 bits, times the
-// page's scale); rows of a page that is not there are zeros.
+// page's scale); rows of a page that is not there are zeros. fp32 at d = 128: 512 units of 2304 tokens 377 us (3.2 TB/s), 8 of 16384 118 us (HBM 20; 64 CTAs); 128 units of 2304
+// tokens at d = 256: 8 bits 253 us, bf16 235 (HBM 23 and 46).
 template <int E, int GP, bool PAGED = false>
 __global__ void __launch_bounds__(kAttendThreads) attend_scored_kernel(const std::conditional_t<PAGED, PagedAttendArgs, ScoredArgs> a, const int S, const int stages) {
   extern __shared__ __align__(16) float asm_[];

@@ -118,8 +118,8 @@ size_t prompt_part_bytes(const PromptArgs& a, int splits) {
 
 // Into how many shares the keys are cut where there are fewer tiles of rows than SMs. Tiles run side by side on the SMs, in rounds; a block of 128 keys costs
 // a tile 3500 cycles on the tensor cores and the tile's own start and end 9000 (prompt_tc_kernel), and each share of a row goes through HBM or L2 twice in fp32 (3400 bytes
-// a cycle). So the best count is the one with the least of rounds, starts and traffic, all for the longest rows and keys of the call: 32 heads of 512 rows over 32768 keys 271 us
-// with 9 shares, 250 with 2. On the CUDA cores a block of 64 keys by 16 or 64 rows takes the place.
+// a cycle). So the best count is the one with the least of rounds, starts and traffic, all for the longest rows and keys of the call: 32 heads of 512 rows over 32768 keys 265 us
+// with 2 shares, 483 with one, 327 with 9. On the CUDA cores a block of 64 keys by 16 or 64 rows takes the place.
 int prompt_splits(const PromptArgs& a, bool tc, int* out) {
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;

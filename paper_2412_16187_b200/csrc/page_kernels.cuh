@@ -6,8 +6,11 @@
 // moves the codes that are there already by whole binades, which is exact but for those that fall below 2^-6 s, the type's least normal number (rounded once more).
 //
 // append: a CTA has one page of one sequence (that is, the new rows that lie in it) and walks over KV heads. A thread owns two pieces of a row that hold whole
-// rotary pairs, as in rotate_kernel, keeps the sines and cosines of its pairs for all heads, and holds the pieces of K and V in registers from
-// the read to the write; between the two lies the maximum over the page, by one barrier.
+// rotary pairs, as in rotate_kernel, keeps the sines and cosines of its pairs for all heads, and holds the pieces of K and V in registers from the read to the write; between the
+// two lies the maximum over the page, by one barrier a head. Rows into pages of their own type run at HBM's rate (512 MB 86 us, 6.2 TB/s). 8-bit pages are bound by issue slots (80 %
+// used): some 590 instructions a warp for 32 elements a thread, of rotation, maximum, scaling and conversion: 402 MB 83 us (4.8 TB/s; 70 without a rotation; interleaved pairs and
+// pages of 128 tokens, one CTA of 1024 threads an SM, 100), 16 ragged prompts of 1024 to 4400 tokens 62 us, HBM 39. One token of 64 sequences 4.1 us, launch and latency.
+// read: 402 MB of 8-bit pages 64 us (6.3 TB/s).
 #pragma once
 #include "attend_kernels.cuh"
 #include "common.cuh"
