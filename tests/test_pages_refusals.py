@@ -2,10 +2,12 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2412_16187_b200 import Rotary, binding
 
-FAKE, FAR = 0x10000, 0x40000000  # never followed: every check below comes before the launch
+FAKE, FAR = 0x10000, 0x40000000  # never followed: every call below is one that a check ends before the launch, and none is made where a launch could succeed
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="pointers that are none: without a GPU only")
 three = ctypes.c_int64 * 3
 
 
@@ -19,13 +21,14 @@ def pages(**kw):
     return binding.he_pages(**f)
 
 
-def calls(cfg, pg, k=FAKE, v=FAR, strides=three(2 * 64 * 16, 64 * 16, 64), n=16, rotary=None, out=FAR, q=FAKE, workspace=None):
-    """The error code and text of each call that takes pages."""
+def calls(cfg, pg, k=FAKE, v=FAR, strides=three(2 * 64 * 16, 64 * 16, 64), n=16, rotary=None, out=FAR, q=FAKE, workspace=None, of=("append", "read", "attend")):
+    """The error code and text of each of the calls that take pages."""
     L, found = binding.lib(), []
     c, p = (None if cfg is None else ctypes.byref(cfg)), (None if pg is None else ctypes.byref(pg))
-    for rc in (lambda: L.he_page_append(c, p, rotary, k, v, strides, None, n, None), lambda: L.he_page_read(c, p, None, n, k, v, strides, None),
-               lambda: L.he_page_attend(c, p, None, q, None, out, workspace, 0, None)):
-        found.append((rc(), L.he_last_error().decode()))
+    made = {"append": lambda: L.he_page_append(c, p, rotary, k, v, strides, None, n, None), "read": lambda: L.he_page_read(c, p, None, n, k, v, strides, None),
+            "attend": lambda: L.he_page_attend(c, p, None, q, None, out, workspace, 0, None)}
+    for name in of:
+        found.append((made[name](), L.he_last_error().decode()))
     return found
 
 
@@ -46,20 +49,20 @@ def test_shapes_and_pointers():
         assert rc == 1 and "pages is null" in said
     for rc, said in calls(config(d=72), pages(eight_bit=1), strides=three(2 * 72 * 16, 72 * 16, 72)):
         assert rc == 2 and "multiple of 16" in said
-    append, read, _ = calls(config(), pages(), n=-1)
+    append, read = calls(config(), pages(), n=-1, of=("append", "read"))
     assert append[0] == read[0] == 1 and "max_new" in append[1] and "max_rows" in read[1]
     append, read, attend = calls(config(), pages(), k=None, v=None, q=None)
     assert append[0] == read[0] == attend[0] == 1 and "null" in append[1] and "neither" in read[1] and "null" in attend[1]
     append, read, attend = calls(config(), pages(), k=FAKE + 4, q=FAKE + 4)
     assert append[0] == read[0] == attend[0] == 1 and all("16-byte" in x[1] for x in (append, read, attend))
     for bad in (three(2 * 64 * 16, 64 * 16, 60), three(-64, 64, 64), None):
-        append, read, _ = calls(config(), pages(), strides=bad)
+        append, read = calls(config(), pages(), strides=bad, of=("append", "read"))
         assert append[0] == read[0] == 1 and "stride" in append[1] and "stride" in read[1]
-    assert "overlap" in calls(config(), pages(), strides=three(0, 64 * 16, 64))[1][1]
-    assert "overlap" in calls(config(), pages(), v=FAKE)[1][1]
-    assert calls(config(batch=70000), pages())[1][0] == 2
-    assert "out" in calls(config(), pages(), out=FAR + 8)[2][1]
-    assert "rotary channels 128" in calls(config(), pages(), rotary=Rotary(128).pointer)[0][1]
+    assert "overlap" in calls(config(), pages(), strides=three(0, 64 * 16, 64), of=("read",))[0][1]
+    assert "overlap" in calls(config(), pages(), v=FAKE, of=("read",))[0][1]
+    assert calls(config(batch=70000), pages(), of=("read",))[0][0] == 2
+    assert "out" in calls(config(), pages(), out=FAR + 8, of=("attend",))[0][1]
+    assert "rotary channels 128" in calls(config(), pages(), rotary=Rotary(128).pointer, of=("append",))[0][1]
 
 
 def test_calls_that_have_nothing_to_do_succeed_without_a_device():
