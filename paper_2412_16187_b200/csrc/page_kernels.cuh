@@ -6,10 +6,11 @@
 // moves the codes that are there already by whole binades, which is exact but for those that fall below 2^-6 s, the type's least normal number (rounded once more).
 //
 // append: a CTA has one page of one sequence (that is, the new rows that lie in it) and walks over KV heads. A thread owns two pieces of a row that hold whole
-// rotary pairs, as in rotate_kernel, keeps the sines and cosines of its pairs for all heads, and holds the pieces of K and V in registers from the read to the write; between the
-// two lies the maximum over the page, by one barrier a head. Rows into pages of their own type run at HBM's rate (512 MB 86 us, 6.2 TB/s). 8-bit pages are bound by issue slots (80 %
-// used): some 590 instructions a warp for 32 elements a thread, of rotation, maximum, scaling and conversion: 402 MB 83 us (4.8 TB/s; 70 without a rotation; interleaved pairs and
-// pages of 128 tokens, one CTA of 1024 threads an SM, 100), 16 ragged prompts of 1024 to 4400 tokens 62 us, HBM 39. One token of 64 sequences 4.1 us, launch and latency.
+// rotary pairs, as in rotate_kernel (interleaved pairs are whole in any piece: there the second lies as far on as the first ones of its row's threads reach, so that a warp reads
+// and writes whole sectors; 402 MB 69 us, two pieces side by side 100), keeps the sines and cosines of its pairs for all heads, and holds the pieces of K and V in registers from
+// the read to the write; between the two lies the maximum over the page, by one barrier a head. Rows into pages of their own type run at HBM's rate (537 MB 84 us, 6.4 TB/s). 8-bit
+// pages use 67 % of the issue slots: some 500 instructions a warp for 32 elements a thread, of rotation, maximum, scaling and conversion: 402 MB 68 us (6.0 TB/s; 63 without a
+// rotation; 81 for pages of 128 tokens, one CTA of 1024 threads an SM), 16 ragged prompts of 1024 to 4400 tokens 51 us, HBM 39. One token of 64 sequences 3.9 us, launch and latency.
 // read: 402 MB of 8-bit pages 64 us (6.3 TB/s).
 #pragma once
 #include "attend_kernels.cuh"
@@ -38,15 +39,22 @@ __host__ __device__ inline int page_scale_exponent(uint32_t top) {
   return e > -100 ? e : -100;
 }
 
-// V values over a scale as e4m3 codes; what is not finite becomes NaN (ODD: there may be infinities, which the conversion would saturate).
-template <int V, bool ODD>
-__device__ __forceinline__ void e4m3_store(uint8_t* dst, const float (&f)[V], float inv) {
+// A piece over a scale, times inv, as e4m3 codes; what is not finite becomes NaN. Pairs of bf16 values are multiplied as such, which is exact for a power of two but for
+// products that are zeros in e4m3 anyway. ANY: inv may be anything, and there may be infinities, which the conversion would saturate.
+template <int E, int V, bool ANY>
+__device__ __forceinline__ void e4m3_store(uint8_t* dst, RotaryPiece<E, V> p, float inv) {
   uint16_t two[(V + 1) / 2];
+  if constexpr (E == 2 && !ANY) {
+#pragma unroll
+    for (int i = 0; i < p.kWords; ++i) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(p.w[i]) : "r"(__byte_perm(__float_as_uint(inv), 0, 0x3232)));
+    inv = 1.f;
+  }
 #pragma unroll
   for (int i = 0; i < V; i += 2) {
-    float x = f[i], y = i + 1 < V ? f[(i + 1) % V] : 0.f;
-    if (ODD) x = fabsf(x) < INFINITY ? x : __int_as_float(0x7FC00000), y = fabsf(y) < INFINITY ? y : __int_as_float(0x7FC00000);
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two[i / 2]) : "f"(y * inv), "f"(x * inv));
+    float x = p.get(i), y = i + 1 < V ? p.get((i + 1) % V) : 0.f;
+    if (ANY) x = fabsf(x) < INFINITY ? x : __int_as_float(0x7FC00000), y = fabsf(y) < INFINITY ? y : __int_as_float(0x7FC00000);
+    if (E == 4 || ANY) x *= inv, y *= inv;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two[i / 2]) : "f"(y), "f"(x));
   }
   if constexpr (V == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(two[0] | (uint32_t)two[1] << 16, two[2] | (uint32_t)two[3] << 16);
   else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(dst) = two[0] | (uint32_t)two[1] << 16;
@@ -72,12 +80,12 @@ __device__ __forceinline__ void e4m3_rescale(uint8_t* codes, int bytes, float ra
   }
 }
 
-// The largest magnitudes seen so far: a pair of bf16 values, or an fp32 one; NaNs are passed over, infinities count.
+// The largest magnitudes seen so far: a pair of bf16 values (of any sign), or an fp32 one; NaNs are passed over, infinities count.
 template <int E, int V>
 __device__ __forceinline__ void page_top(uint32_t& top, const RotaryPiece<E, V>& p) {
 #pragma unroll
   for (int i = 0; i < RotaryPiece<E, V>::kWords; ++i) {
-    if constexpr (E == 2) asm("max.bf16x2 %0, %0, %1;" : "+r"(top) : "r"(p.w[i] & 0x7FFF7FFFu));
+    if constexpr (E == 2) asm("max.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(top) : "r"(p.w[i]));
     else top = __float_as_uint(fmaxf(__uint_as_float(top), fabsf(__uint_as_float(p.w[i]))));
   }
 }
@@ -97,6 +105,30 @@ struct AppendPlace {
   bool some, second, turns;  // whether there is such a row, a second piece, pairs in them
 };
 
+// Interleaved pairs of two pieces, turned: of the first piece by the sines that come first. pair0, pair1: the pieces' first pairs; those from `half` on stay.
+template <int E, int V>
+__device__ __forceinline__ void page_turn_neighbours(RotaryPiece<E, V>& p0, RotaryPiece<E, V>& p1, const float (&sn)[V], const float (&cs)[V], int pair0, int pair1, int half) {
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    RotaryPiece<E, V>& p = e ? p1 : p0;
+    const int left = half - (e ? pair1 : pair0);
+    float x[V];
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const int k = (e * V + i) / 2;
+      const float f = p.get(i), g = p.get(i + 1);
+      x[i] = f * cs[k] - g * sn[k], x[i + 1] = g * cs[k] + f * sn[k];
+    }
+    if (left >= V / 2) {
+      p.put(x);
+    } else if (left > 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = i / 2 < left ? x[i] : p.get(i);
+      p.put(x);
+    }
+  }
+}
+
 // grid.x: pages of sequences, grid.y: shares of the KV heads. With HOLD a thread owns one place of the page, whose pieces of 16 bytes it asks for a head ahead (into
 // shared memory that it alone reads) and holds until they are written; without (smaller pieces, pages of more than 1024 places) it walks over as many places as there are,
 // twice where the maximum has to be known first.
@@ -113,70 +145,80 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
   const int held = max(pg.len[s], 0), fresh = a.new_len != nullptr ? min(max(a.new_len[s], 0), a.max_new) : a.max_new;
   const int first = held - fresh;  // the position of row 0; rows ahead of position 0 or behind the table's end are dropped
   const int lo = max(first, 0), hi = (int)min((long long)held, page_capacity(pg));
-  const int at = lo / P + (int)(blockIdx.x % a.tiles);
-  if (lo >= hi || at > (hi - 1) / P) return;
+  const int log2 = __ffs(P) - 1, at = (lo >> log2) + (int)(blockIdx.x - s * a.tiles);
+  if (lo >= hi || at > (hi - 1) >> log2) return;
   const int page = page_of(pg, s, at * P);
   if (page < 0) return;
   const int r0 = max(lo - at * P, 0), r1 = min(hi - at * P, P), items = (r1 - r0) * a.units;
   const int half = rot.channels / 2;
   auto place = [&](int item) {
     AppendPlace p;
-    p.u = item % a.units, p.row = r0 + item / a.units, p.some = item < items, p.turns = V * p.u < half;
-    p.c0 = INTER ? 2 * V * p.u : p.turns ? V * p.u : rot.channels + 2 * V * (p.u - half / V);
-    p.c1 = !INTER && p.turns ? p.c0 + half : p.c0 + V;
+    const int row = (int)((unsigned)item / (unsigned)a.units);
+    p.u = item - row * a.units, p.row = r0 + row, p.some = item < items, p.turns = V * p.u < half;
+    p.c0 = INTER ? V * p.u : p.turns ? V * p.u : rot.channels + 2 * V * (p.u - half / V);
+    p.c1 = INTER ? p.c0 + V * a.units : p.turns ? p.c0 + half : p.c0 + V;
     p.second = p.some && p.c1 < a.d;
     return p;
   };
-  auto sines = [&](const AppendPlace& p, float (&sn)[V], float (&cs)[V]) {
+  float sn[V], cs[V];
+  auto sines = [&](const AppendPlace& p) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
+      const int pair = !INTER ? V * p.u + i : i < V / 2 ? p.c0 / 2 + i : p.c1 / 2 + i - V / 2;
       sn[i] = 0.f, cs[i] = 1.f;
-      if (a.turns && p.some && V * p.u + i < half) rotary_sincos(rot, V * p.u + i, at * P + p.row, sn[i], cs[i]);
+      if (a.turns && p.some && pair < half) rotary_sincos(rot, pair, at * P + p.row, sn[i], cs[i]);
     }
+  };
+  auto turn = [&](const AppendPlace& p, Piece (&x)[2]) {
+    if constexpr (INTER) page_turn_neighbours<E, V>(x[0], x[1], sn, cs, p.c0 / 2, p.c1 / 2, half);
+    else rotary_turn<E, V, false>(x[0], x[1], sn, cs, p.u, half, p.turns);
   };
   auto read = [&](const AppendPlace& p, int w, int h, Piece (&x)[2]) {
     const char* src = static_cast<const char*>(a.x[w]) + (s * a.strides[0] + h * a.strides[1] + (long long)(at * P + p.row - first) * a.strides[2]) * E;
     if (p.some) x[0].load(src + p.c0 * E);
     if (p.second) x[1].load(src + p.c1 * E);
   };
-  auto write = [&](const AppendPlace& p, const Piece (&x)[2], char* dst, float inv, auto odd) {  // dst: the page's rows of this head
+  auto write = [&](const AppendPlace& p, const Piece (&x)[2], char* to, float inv, auto any) {  // to: the first piece's place in the page
+    constexpr int kBytes = Q8 ? 1 : E;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       if (e ? p.second : p.some) {
-        const long long to = (long long)p.row * a.d + (e ? p.c1 : p.c0);
-        if constexpr (Q8) {
-          float f[V];
-#pragma unroll
-          for (int i = 0; i < V; ++i) f[i] = x[e].get(i);
-          e4m3_store<V, decltype(odd)::value>(reinterpret_cast<uint8_t*>(dst) + to, f, inv);
-        } else {
-          x[e].store(dst + to * E);
-        }
+        char* at = e ? to + (p.c1 - p.c0) * kBytes : to;
+        if constexpr (Q8) e4m3_store<E, V, decltype(any)::value>(reinterpret_cast<uint8_t*>(at), x[e], inv);
+        else x[e].store(at);
       }
   };
+  auto offset = [&](const AppendPlace& p) { return (p.row * a.d + p.c0) * (Q8 ? 1 : E); };
   const AppendPlace mine = place(tid);
-  float sn[V], cs[V];
-  if (HOLD) sines(mine, sn, cs);
   const int h_begin = blockIdx.y * a.heads_per_cta, h_end = min(h_begin + a.heads_per_cta, H);
-  auto ask = [&](int h) {  // (HOLD)
+  // HOLD: where the next head's pieces are asked from, and the places for them, by turns. (Kept from head to head: worked out anew they were a third of the instructions.)
+  const char* next[2];
+  const long long from = s * a.strides[0] + h_begin * a.strides[1] + (long long)(at * P + mine.row - first) * a.strides[2] + mine.c0;
+  next[0] = static_cast<const char*>(a.x[0]) + from * E, next[1] = static_cast<const char*>(a.x[1]) + from * E;
+  const long long head_bytes = a.strides[1] * E;
+  const int gap = (mine.c1 - mine.c0) * E;
+  uint4* const held_s = append_s + tid;
+  char* dst[2];  // the page's rows of this head, with HOLD the thread's first piece of them
+  const int page_bytes = P * a.d * (Q8 ? 1 : E);
+  {
+    const long long begin = ((long long)page * H + h_begin) * page_bytes + (HOLD ? offset(mine) : 0);
+    dst[0] = static_cast<char*>(pg.k_pages) + begin, dst[1] = static_cast<char*>(pg.v_pages) + begin;
+  }
+  auto ask = [&](int h) {
     if (h < h_end) {
-      const long long from = s * a.strides[0] + h * a.strides[1] + (long long)(at * P + mine.row - first) * a.strides[2];
+      uint4* to = held_s + ((h & 1) ? 4 * threads : 0);
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
-        const char* src = static_cast<const char*>(a.x[w]) + from * E;
-        uint4* to = append_s + (size_t)(((h & 1) * 4 + 2 * w) * threads + tid);
-        if (mine.some) cp_async16(to, src + mine.c0 * E);
-        if (mine.second) cp_async16(to + threads, src + mine.c1 * E);
+        if (mine.some) cp_async16(to + 2 * w * threads, next[w]);
+        if (mine.second) cp_async16(to + (2 * w + 1) * threads, next[w] + gap);
+        next[w] += head_bytes;
       }
     }
     cp_async_commit();
   };
-  if (HOLD) ask(h_begin);
-  for (int h = h_begin; h < h_end; ++h) {
+  if (HOLD) ask(h_begin), sines(mine);
+  for (int h = h_begin; h < h_end; ++h, dst[0] += page_bytes, dst[1] += page_bytes) {
     const long long block = (long long)page * H + h;  // of the pages' heads
-    char* dst[2];
-#pragma unroll
-    for (int w = 0; w < 2; ++w) dst[w] = static_cast<char*>(w ? pg.v_pages : pg.k_pages) + block * P * a.d * (Q8 ? 1 : E);
     float old[2] = {0.f, 0.f};
     if (Q8 && r0 > 0) old[0] = __ldcg(pg.k_scale + block), old[1] = __ldcg(pg.v_scale + block);
     Piece x[2][2];
@@ -189,8 +231,8 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
     auto fetch = [&](const AppendPlace& p) {
       read(p, 0, h, x[0]), read(p, 1, h, x[1]);
       if (a.turns && p.some) {
-        sines(p, sn, cs);
-        rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, p.u, half, p.turns);
+        sines(p);
+        turn(p, x[0]);
       }
     };
     if constexpr (HOLD) {
@@ -199,8 +241,8 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
 #pragma unroll
       for (int w = 0; w < 2; ++w)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[w][e].load(reinterpret_cast<const char*>(append_s + (size_t)(((h & 1) * 4 + 2 * w + e) * threads + tid)));
-      if (a.turns && mine.some) rotary_turn<E, V, INTER>(x[0][0], x[0][1], sn, cs, mine.u, half, mine.turns);
+        for (int e = 0; e < 2; ++e) x[w][e].load(reinterpret_cast<const char*>(held_s + ((h & 1) ? 4 * threads : 0) + (2 * w + e) * threads));
+      if (a.turns && mine.some) turn(mine, x[0]);
       if (Q8) look(mine, 0, x[0], false), look(mine, 1, x[1], false);
       else write(mine, x[0], dst[0], 1.f, std::false_type()), write(mine, x[1], dst[1], 1.f, std::false_type());
     } else {
@@ -208,7 +250,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
         const AppendPlace p = place(item);
         fetch(p);
         if (Q8) look(p, 0, x[0], false), look(p, 1, x[1], false);
-        else write(p, x[0], dst[0], 1.f, std::false_type()), write(p, x[1], dst[1], 1.f, std::false_type());
+        else write(p, x[0], dst[0] + offset(p), 1.f, std::false_type()), write(p, x[1], dst[1] + offset(p), 1.f, std::false_type());
       }
     }
     if constexpr (!Q8) continue;
@@ -223,7 +265,7 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
         for (int w = 0; w < 2; ++w) top[w] = __reduce_max_sync(0xFFFFFFFFu, lane < threads / 32 ? top_s[turn][w][lane] : 0u);
       }
     };
-    if (E == 2) top[0] = max(top[0] << 16, top[0] & 0xFFFF0000u), top[1] = max(top[1] << 16, top[1] & 0xFFFF0000u);
+    if (E == 2) top[0] = max(top[0] << 16 & 0x7FFF0000u, top[0] & 0x7FFF0000u), top[1] = max(top[1] << 16 & 0x7FFF0000u, top[1] & 0x7FFF0000u);
     gather(h & 1);
     const bool odd = max(top[0], top[1]) >= 0x7F800000u;  // an infinity (of the whole CTA): the largest of the others is to be found
     if (__builtin_expect(odd, 0)) {
@@ -241,25 +283,28 @@ __global__ void __launch_bounds__(kAppendThreads) page_append_kernel(const Appen
       if (threads > 32) __syncthreads();  // (the third place is used by any head)
     }
     float inv[2];
+    bool others = odd;  // or an earlier scale that is no power of two
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const float scale = fmaxf(__int_as_float((page_scale_exponent(top[w]) + 127) << 23), old[w]);
-      inv[w] = 1.f / scale;
-      if (r0 > 0 && old[w] != scale) e4m3_rescale(reinterpret_cast<uint8_t*>(dst[w]), r0 * a.d, old[w] / scale);
+      const int e = page_scale_exponent(top[w]);
+      float scale = __int_as_float((127 + e) << 23);
+      inv[w] = __int_as_float((127 - e) << 23);
+      if (old[w] > scale) scale = old[w], inv[w] = 1.f / scale, others |= (__float_as_uint(inv[w]) & 0x7FFFFFu) != 0u;
+      if (r0 > 0 && old[w] != scale) e4m3_rescale(reinterpret_cast<uint8_t*>(dst[w] - (HOLD ? offset(mine) : 0)), r0 * a.d, old[w] / scale);
       if (tid == 0 && (r0 == 0 || old[w] != scale)) (w ? pg.v_scale : pg.k_scale)[block] = scale;
     }
-    auto finish = [&](auto is_odd) {
+    auto finish = [&](auto any) {
       if constexpr (HOLD) {
-        write(mine, x[0], dst[0], inv[0], is_odd), write(mine, x[1], dst[1], inv[1], is_odd);
+        write(mine, x[0], dst[0], inv[0], any), write(mine, x[1], dst[1], inv[1], any);
       } else {
         for (int item = tid; item < items; item += threads) {
           const AppendPlace p = place(item);
           fetch(p);
-          write(p, x[0], dst[0], inv[0], is_odd), write(p, x[1], dst[1], inv[1], is_odd);
+          write(p, x[0], dst[0] + offset(p), inv[0], any), write(p, x[1], dst[1] + offset(p), inv[1], any);
         }
       }
     };
-    if (__builtin_expect(odd, 0)) finish(std::true_type());
+    if (__builtin_expect(others, 0)) finish(std::true_type());
     else finish(std::false_type());
   }
 }

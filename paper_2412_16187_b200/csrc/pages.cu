@@ -212,10 +212,11 @@ int he_page_append(const he_config* cfg, const he_pages* pages, const he_rotary*
   const int items = (max_new < P ? max_new : P) * a.units;  // of a page's new rows
   const bool hold = V == 16 / es && items <= kAppendThreads;
   const int threads = items < kAppendThreads ? (items + 31) / 32 * 32 : kAppendThreads;
-  // Heads are shared out until there are enough CTAs for every SM, but a thread that has worked out its sines keeps at least four heads of a whole page.
+  // Heads are shared out until there are enough CTAs for every SM, but a thread that has worked out its sines keeps at least four heads of a whole page. (16 prompts into pages of
+  // 64 tokens: 44 us so, 51 with twice as many CTAs; of 128 tokens, an SM has one CTA at a time: 43 with two for each SM, 56 with four.)
   int sms = 0;
   if (int rc = sm_count(&sms)) return rc;
-  const long long shares = (4LL * sms + ctas - 1) / ctas;
+  const long long shares = ((threads > 512 ? 2LL : 4LL) * sms + ctas - 1) / ctas;
   a.heads_per_cta = (int)((cfg->n_kv_heads + shares - 1) / shares);
   const int least = max_new < P ? 1 : 4;
   if (a.heads_per_cta < least) a.heads_per_cta = least;
