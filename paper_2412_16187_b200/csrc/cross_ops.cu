@@ -9,5 +9,9 @@ int he::cross_error_count() {
 }
 
 int he::launch_prompt_keys(const PromptArgs& a, const PromptMaps& maps, cudaStream_t st) {
-  return a.d <= 64 ? launch_prompt_tc<64, kOverKeys>(a, maps, st) : launch_prompt_tc<128, kOverKeys>(a, maps, st);
+  int sms = 0;
+  if (int rc = sm_count(&sms)) return rc;
+  PromptArgs b = a;
+  b.by_keys = a.batch > 1 && a.batch <= 32 && prompt_tc_tiles(a).items > sms;
+  return a.d <= 64 ? launch_prompt_tc<64, kOverKeys>(b, maps, st) : launch_prompt_tc<128, kOverKeys>(b, maps, st);
 }

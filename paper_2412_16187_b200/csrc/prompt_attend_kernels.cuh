@@ -44,6 +44,7 @@ struct PromptArgs {
   int pack, packs;         // a tile holds 128 >> pack rows of 1 << pack query heads of a KV head, so a KV head's query heads make `packs` (0 and group for he_attend_prompt)
   int splits;              // > 1: the keys of a tile are shared out, and `part` takes what each share gives
   float* part;             // [splits][B][heads][tokens][d], then [splits][B][heads][tokens][2]: unnormalised outputs; maximum in log2 units and sum of the weights
+  int by_keys;             // he_attend_cross on the tensor cores, 2 to 32 sequences, more items than SMs: the sequences with the most keys come first
 };
 
 // The keys of a sequence, numbered as its rows see them, are [-shift, end).
@@ -1276,6 +1277,15 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         __syncwarp();
         ++k;
       };
+      // Items end evenly when the long ones start first: those of the last rows, and here those of the sequences with the most keys. (16 heads of 100 to 448 rows over 700 to 1500
+      // keys, 8 sequences: 41 us so, 44 as they come; 16 of 50 to 900 rows over 300 to 4000: 144, 160.) `ranked`: of a lane, the sequence of that rank.
+      int ranked = lane;
+      if (KIND == kOverKeys && a.by_keys) {
+        const int mine = lane < a.batch ? min(max(a.kv_lens[lane], 0), a.keys) * 32 + 31 - lane : -1;  // (no two alike; at most 2^29)
+#pragma unroll 1
+        for (int z = 0; z < a.batch; ++z)
+          if (__popc(__ballot_sync(0xFFFFFFFFu, mine > __shfl_sync(0xFFFFFFFFu, mine, z))) == lane) ranked = z;
+      }
       PtItem w;
       while (ok) {
         int item = cta;
@@ -1283,6 +1293,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         if (KIND == kOverShares) more.share = cta % a.splits, item = cta / a.splits;
         w.p = item % per, w.s = (item / per) % a.batch;
         const int tile = tiles - 1 - item / per / a.batch;
+        if (KIND == kOverKeys && a.by_keys) w.s = __shfl_sync(0xFFFFFFFFu, ranked, w.s);
         w.tok0 = by_heads ? tile * rows_of : tile * 2 * rows_of;
         w.n = min(max(a.lens[w.s], 0), a.tokens);
         if (w.tok0 < w.n) {

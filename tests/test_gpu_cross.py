@@ -103,6 +103,19 @@ def test_attend_cross(shape, opt, path, monkeypatch):
     assert torch.equal(out, again) and device_error_count() == 0
 
 
+@pytest.mark.parametrize("opt", ["all keys, cap", "causal, all"])
+@pytest.mark.parametrize("shape", [(5, 32, 1, 64, BF16, [130, 300, 0, 1, 260], [5, 300, 40, 0, 300], "heads"), (33, 4, 2, 128, BF16, [40 + 3 * i for i in range(33)], [97 * i % 500 for i in range(33)], "tokens"),
+                                   (32, 4, 2, 128, BF16, [136 - 3 * i for i in range(32)], [61 * i % 7 * 80 for i in range(32)], "heads")], ids=["5", "33", "32"])
+def test_more_tiles_than_run_at_once(shape, opt):
+    """Sequences in the order of their keys (up to 32 of them), equal and empty ones among them."""
+    b, h, g, d, dtype, q_lens, kv_lens, _ = shape
+    o = OPTIONS[opt]
+    q, k, v, ql, kl, mod, kw, slopes = case(shape, o)
+    out = make_cache(b, h, g, d, dtype).attend_cross(q, k, v, ql, kl, mod=mod, out=torch.full_like(q, 7.0), workspace=torch.empty(0, dtype=torch.uint8, device="cuda"), **kw)
+    check(out, q, k, v, q_lens, kv_lens, o, kw, slopes, g, False)
+    assert device_error_count() == 0
+
+
 @pytest.mark.parametrize("dtype, d", [(BF16, 128), (F32, 64)])
 def test_a_prompt_over_itself_is_the_case_of_equal_lengths(dtype, d):
     gen = torch.Generator(device="cuda").manual_seed(3)
