@@ -64,6 +64,8 @@ APPENDS = [
     (1, 2, 256, 128, BF16, True, 256, False, [300, 1], "heads"), (1, 2, 256, 128, F32, True, 128, False, [130, 1, 5], "tokens"), (2, 2, 64, 64, F32, True, 64, True, [65, 1, 62, 1], "heads"),
     (1, 33, 128, 64, BF16, True, 128, False, [640], "tokens"), (1, 1, 128, 64, F32, False, 126, False, [66, 1], "heads"), (2, 2, 16, 16, BF16, True, 6, False, [17, 30, 1], "heads"),
     (1, 3, 128, 128, F32, False, 128, False, [129, 1, 300], "heads"), (1, 1, 8, 16, BF16, False, 8, False, [20], "heads"),
+    (2, 2, 128, 16, BF16, True, 100, True, [40, 1, 30], "tokens"), (1, 2, 72, 16, BF16, False, 72, True, [20, 1], "heads"), (1, 5, 80, 128, F32, True, 60, True, [130, 1], "heads"),
+    (1, 2, 256, 128, BF16, True, 200, True, [200, 2], "tokens"), (1, 9, 128, 128, BF16, True, 128, True, [300, 7], "tokens"),
 ]
 
 
@@ -142,6 +144,32 @@ def test_largest_and_smallest_values():
         cache.append(x, x.flip(2))
         ref.append(model, (x, x.flip(2)), None)
         same(cache, model)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d, p", [(128, 64), (256, 128)])
+def test_a_page_that_came_with_another_scale(dtype, d, p):
+    """Rows join a page whose scale is no power of two and large enough for them: it stays, as do the rows that are there, and each new entry is off by half a step at most."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    cache = paged(gen, 1, 2, 1, d, p, dtype, True, p)
+    k, v = (rows(gen, 1, 2, p, d, dtype) for _ in "kv")
+    k[0, 1, p - 1, 3], v[0, 0, 9, 0] = math.inf, math.nan
+    cache.length += 5
+    cache.append(k[:, :, :5], v[:, :, :5])
+    page = int(cache.page_table[0, 0])
+    for x in (cache.k_scale, cache.v_scale):
+        x[page] = 0.3
+    old = [x[page, :, :5].view(torch.uint8).clone() for x in (cache.k_pages, cache.v_pages)]
+    cache.length += p - 5
+    cache.append(k[:, :, 5:], v[:, :, 5:])
+    for x, pages, scale, was in ((k, cache.k_pages, cache.k_scale, old[0]), (v, cache.v_pages, cache.v_scale, old[1])):
+        assert bool((scale[page] == torch.tensor(0.3, device="cuda")).all()) and torch.equal(pages[page, :, :5].view(torch.uint8), was)
+        want, got = x[0, :, 5:].double(), pages[page, :, 5:].float().double() * scale[page].double()[:, None, None]
+        whole = torch.isfinite(want)
+        assert torch.equal(torch.isnan(got), ~whole)
+        # half a step of e4m3, and two roundings in fp32 (of 1 / s and of the product) ahead of it
+        most = torch.maximum(want.abs() * (2.0 ** -4 + 2.0 ** -20), torch.full_like(want, 0.3 * 2.0 ** -10 * (1 + 2.0 ** -20)))
+        assert bool(((got - want).abs() <= most)[whole].all())
 
 
 def filled(gen, b, h, g, d, p, dtype, eight, lens, missing=(), most=None):
