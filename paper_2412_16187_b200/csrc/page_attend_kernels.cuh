@@ -548,11 +548,10 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
         gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 8));
         gm = fmaxf(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, 16));
         const float mx = fmaxf(m[k], gm), mn = mx == -INFINITY ? 0.f : mx;
-        const float up = mn - 14.f;  // weights times 2^14: sums and outputs alike
         corr[k] = page_ex2(m[k] - mn);
         m[k] = mx;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i >> 1][i & 1][k] = page_ex2(x[i >> 1][i & 1][k] - up);
+        for (int i = 0; i < 4; ++i) x[i >> 1][i & 1][k] = page_ex2((x[i >> 1][i & 1][k] - mn) + 14.f);  // weights times 2^14: sums and outputs alike (mn - 14 would be rounded)
         l[k] = fmaf(l[k], corr[k], (x[0][0][k] + x[0][1][k]) + (x[1][0][k] + x[1][1][k]));
       }
       // the weights of 8 tokens by 8 heads at a time, turned round: rows of tokens become the products' columns of heads
