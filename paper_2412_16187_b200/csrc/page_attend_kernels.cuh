@@ -30,6 +30,7 @@
 namespace he {
 
 constexpr int kPageGroup = 32;            // tokens of a group
+constexpr float kPageFactorMax = 3.4028234e38f;  // the largest fp32 number
 // Warps of a CTA: as many as hold their state in registers (168 each with 12 of them, 128 with 16). The loop waits for its own instructions, so more warps are faster: codes of
 // 128 channels took 82 us with 10 warps and 69 with 12 at 512 units of 2304 tokens, and 65 with 16, which spill, where 12 took 60; codes of 64 channels 73 with 12 and 65 with 16.
 template <int D, bool Q8>
@@ -376,7 +377,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
       const int k = top == 0u ? 0 : min(13 - ((int)(top >> 23) - 127), 126);  // the row times 2^k is below 2^14
       const float up = __int_as_float((k + 127) << 23), down = __int_as_float((127 - k) << 23);
-      const float mine = (a.mod.cap_log2 > 0.f ? a.mod.inv_cap : a.mod.scale_log2) * down;  // of head gid
+      const float mine = fminf((a.mod.cap_log2 > 0.f ? a.mod.inv_cap : a.mod.scale_log2) * down, kPageFactorMax);  // of head gid
 #pragma unroll
       for (int k = 0; k < 2; ++k) by[k] = __shfl_sync(0xFFFFFFFFu, mine, 4 * (2 * tig + k));
 #pragma unroll
@@ -524,12 +525,13 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
 #pragma unroll
             for (int k = 0; k < 2; ++k) x[u][r][k] = c[u][2 * r + k];
       }
+      // (what makes a score of a product is finite, so that a product of zero is a score of zero)
       if (a.mod.cap_log2 > 0.f) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] = a.mod.cap_log2 * tanhf(x[i >> 2][(i >> 1) & 1][i & 1] * (by[i & 1] * ks[NBOX == 2 ? i >> 2 : 0]));
+        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] = a.mod.cap_log2 * tanhf(x[i >> 2][(i >> 1) & 1][i & 1] * fminf(by[i & 1] * ks[NBOX == 2 ? i >> 2 : 0], kPageFactorMax));
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] *= by[i & 1] * ks[NBOX == 2 ? i >> 2 : 0];
+        for (int i = 0; i < 8; ++i) x[i >> 2][(i >> 1) & 1][i & 1] *= fminf(by[i & 1] * ks[NBOX == 2 ? i >> 2 : 0], kPageFactorMax);
       }
       if (a.mod.slopes != nullptr) {
         const float away = (float)(now.away - gid);

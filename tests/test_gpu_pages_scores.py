@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from layer_reference import tolerance
 from paper_2412_16187_b200 import ScoreMod
 from test_gpu_layer_ops import BF16, F32
 from test_gpu_pages import filled, check_attend, paged
@@ -46,3 +47,23 @@ def test_a_steep_bias(h, g, d, p, dtype):
         got = cache.attend(q, ScoreMod(slopes=slopes))
         assert bool(torch.isfinite(got).all())
         check_attend(got, cache, q, {}, slopes, None)
+
+
+@pytest.mark.parametrize("h, g, d, p, dtype", SHAPES, ids=NAMES)
+def test_a_scale_and_a_query_whose_product_leaves_fp32(h, g, d, p, dtype):
+    """A page's scale comes from a row that is hidden; the visible rows' codes are zeros, and so are their scores, however large the query is: the mean of V."""
+    gen = torch.Generator(device="cuda").manual_seed(p)
+    n = 3 * p
+    cache = paged(gen, 2, h, g, d, p, dtype, True, n)
+    k, v = torch.zeros((2, h, n, d), device="cuda", dtype=dtype), torch.randn((2, h, n, d), generator=gen, device="cuda", dtype=dtype)
+    k[:, :, p, 1], k[:, :, p + 1:, 2] = 2.0 ** 70, 1.0
+    q = torch.full((2, h * g, d), 2.0 ** 100, device="cuda", dtype=dtype)
+    cache.length += n
+    cache.append(k, v)
+    first = torch.full((2,), p + 1, dtype=torch.int32, device="cuda")
+    cache.length.fill_(2 * p)  # (the scale of the third page is that of its own rows)
+    v = cache.read(2 * p)[1][:, :, p + 1:].double()
+    for cap in (0.0, 30.0):
+        got = cache.attend(q, ScoreMod(softcap=cap), first_pos=first).double().view(2, h, g, d)
+        want = v.mean(2)[:, :, None].expand_as(got)
+        assert bool(((got - want).abs() <= tolerance(want, v.abs().max(), F32, True)).all())
