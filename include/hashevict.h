@@ -292,9 +292,10 @@ int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score
  *   q_pos NULL: every row sees every key from first_key on, as a decoder's rows see an encoder's states; a window, slopes or a prefix is refused.
  * first_key (device int32 [B, max_q_len]), prefix_len and mod may be NULL. Rows i >= q_len of out are left as they were; a row that sees no key gives zeros. All else
  * (layouts, strides, accuracy, what runs where) as for he_attend_prompt.
- * workspace (16-byte aligned; he_attend_cross_workspace_bytes(cfg, max_q_len, max_kv_len) bytes, 0 where none is of use) lets few rows over many keys fill the GPU: the
- * keys are then shared out and the shares' results joined in a fixed order. It holds nothing from one call to the next; calls that may run at the same time need one
- * each. NULL: a tile of rows walks over all its keys. With it, too, one bf16 row a sequence (d <= 128), or up to 8 rows of a KV head's query heads that all see the same keys, are
+ * workspace (16-byte aligned; he_attend_cross_workspace_bytes(cfg, max_q_len, max_kv_len) bytes, which serve every call of up to these lengths, up to 160 MB at head_dim 128; 0 where none is of use) lets
+ * few rows over many keys fill the GPU: the keys are then shared out and the shares' results joined in a fixed order. What a call gives does not depend on how large it
+ * is beyond what the call needs; a smaller one is refused. It holds nothing from one call to the next; calls that may run at the same time need one each. NULL: a tile
+ * of rows walks over all its keys. With it, too, one bf16 row a sequence (d <= 128), or up to 8 rows of a KV head's query heads that all see the same keys, are
  * computed as he_page_attend does (weights of about fp32's accuracy), without it as other rows are.
  */
 size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, int32_t max_kv_len);

@@ -419,11 +419,13 @@ class _Layer:
         qs = self._rows("q", q, (self.B, self.H * self.G, n, self.d), self.dtype)
         return qs, ks, self._rows("out", out, q.shape, self.dtype)
 
+    def _cross_bytes(self, max_q_len, max_kv_len):
+        with torch.cuda.device(self.device):
+            return lib().he_attend_cross_workspace_bytes(self._cfg_p, max_q_len, max_kv_len)
+
     def cross_workspace(self, max_q_len, max_kv_len):
         """A workspace of he_attend_cross for calls of up to these lengths (uint8, perhaps empty). Calls that may run at the same time need one each."""
-        with torch.cuda.device(self.device):
-            need = lib().he_attend_cross_workspace_bytes(self._cfg_p, max_q_len, max_kv_len)
-        return torch.empty(need, dtype=torch.uint8, device=self.device)
+        return torch.empty(self._cross_bytes(max_q_len, max_kv_len), dtype=torch.uint8, device=self.device)
 
     def attend_cross(self, q, k, v, q_len, kv_len, q_pos=None, mod=None, first_key=None, prefix_len=None, out=None, workspace=None, stream=None):
         """he_attend_cross: attention of rows q [B, H*G, N, d] over keys of another length, k / v [B, H, M, d] (any strides on the first three axes), q_len and kv_len
@@ -437,7 +439,7 @@ class _Layer:
                                    _layout(prefix_len)), lambda: self._cross(q, k, v, out, (q_len, kv_len), q_pos, first_key, prefix_len))
         n, m = q.shape[-2], k.shape[-2]
         if workspace is None:
-            need = self._known(("cross workspace", n, m), lambda: self.cross_workspace(n, m).numel())
+            need = self._known(("cross workspace", n, m), lambda: self._cross_bytes(n, m))
             workspace = _empty((need,), torch.uint8, self.device, stream) if need else None
         else:
             self._workspace(workspace)
@@ -705,18 +707,20 @@ class PagedCache(_Layer):
             raise HashEvictError(f"rotary of head_dim {rotary.head_dim} for rows of {self.d}")
         self._call(lib().he_page_append, stream, self._cfg_p, self._pages_p, None if rotary is None else rotary.pointer, _ptr(k), _ptr(v), strides, _ptr(new_len), n)
 
+    def _attend_bytes(self):
+        with torch.cuda.device(self.device):
+            return lib().he_page_attend_workspace_bytes(self._cfg_p, self._pages_p)
+
     def workspace(self):
         """A workspace of he_page_attend (uint8, perhaps empty). Calls that may run at the same time need one each."""
-        with torch.cuda.device(self.device):
-            need = lib().he_page_attend_workspace_bytes(self._cfg_p, self._pages_p)
-        return torch.empty(need, dtype=torch.uint8, device=self.device)
+        return torch.empty(self._attend_bytes(), dtype=torch.uint8, device=self.device)
 
     def _attended(self, q, first_pos, out):
         self._tensor("q", q, (self.B, self.H * self.G, self.d), self.dtype)
         self._tensor("out", out, q.shape, torch.float32)
         if first_pos is not None:
             self._tensor("first_pos", first_pos, (self.B,), torch.int32)
-        return self.workspace().numel()
+        return self._attend_bytes()
 
     def attend(self, q, mod=None, first_pos=None, out=None, workspace=None, stream=None):
         """he_page_attend: q [B, H*G, d], the newest token of each sequence, over its pages -> fp32 [B, H*G, d]. mod a ScoreMod, first_pos int32 [B] the first position that

@@ -120,20 +120,45 @@ size_t prompt_part_bytes(const PromptArgs& a, int splits) {
 // a tile 3500 cycles on the tensor cores and the tile's own start and end 9000 (prompt_tc_kernel), and each share of a row goes through HBM or L2 twice in fp32 (3400 bytes
 // a cycle). So the best count is the one with the least of rounds, starts and traffic, all for the longest rows and keys of the call: 32 heads of 512 rows over 32768 keys 265 us
 // with 2 shares, 483 with one, 327 with 9. On the CUDA cores a block of 64 keys by 16 or 64 rows takes the place.
+constexpr int kMostShares = 64, kMostRounds = 8;  // of a tile; of tiles times shares, where there is more than one
+// Tiles of rows, as many as run at once, blocks of keys.
+struct PromptWork {
+  long long items, blocks;
+  int at_once;
+};
+int prompt_work(const PromptArgs& a, bool tc, PromptWork* w) {
+  if (int rc = sm_count(&w->at_once)) return rc;
+  if (!tc && a.d <= 128) w->at_once *= 2;  // (CTAs of an SM)
+  w->items = tc ? prompt_tc_tiles(a).items : prompt_fp32_tiles(a, 64);
+  if (!tc && (w->items < w->at_once || a.tokens <= 16)) w->items = prompt_fp32_tiles(a, 16);
+  w->blocks = ((long long)a.keys + (tc ? 127 : 63)) / (tc ? 128 : 64);
+  return HE_OK;
+}
 int prompt_splits(const PromptArgs& a, bool tc, int* out) {
-  int sms = 0;
-  if (int rc = sm_count(&sms)) return rc;
-  if (!tc && a.d <= 128) sms *= 2;  // (CTAs of an SM)
-  long long items = tc ? prompt_tc_tiles(a).items : prompt_fp32_tiles(a, 64);
-  if (!tc && (items < sms || a.tokens <= 16)) items = prompt_fp32_tiles(a, 16);
+  PromptWork w;
+  if (int rc = prompt_work(a, tc, &w)) return rc;
   *out = 1;
-  const long long blocks = ((long long)a.keys + (tc ? 127 : 63)) / (tc ? 128 : 64);
   double best = 0.0;
-  for (int z = 1; z <= 64 && 2 * z <= blocks && (z == 1 || items * z <= 8LL * sms); ++z) {
-    const double rounds = (double)((items * z + sms - 1) / sms), cost = rounds * ((double)((blocks + z - 1) / z) * 3500.0 + 9000.0) + (z > 1 ? 6000.0 + (double)prompt_part_bytes(a, z) * 2.0 / 3400.0 : 0.0);
+  for (int z = 1; z <= kMostShares && 2 * z <= w.blocks && (z == 1 || w.items * z <= (long long)kMostRounds * w.at_once); ++z) {
+    const double rounds = (double)((w.items * z + w.at_once - 1) / w.at_once), cost = rounds * ((double)((w.blocks + z - 1) / z) * 3500.0 + 9000.0) + (z > 1 ? 6000.0 + (double)prompt_part_bytes(a, z) * 2.0 / 3400.0 : 0.0);
     if (z == 1 || cost < 0.95 * best) best = cost, *out = z;
   }
   return HE_OK;
+}
+// Bytes that the shares of any call of up to a.tokens rows over up to a.keys keys fit in. Fewer rows may take more shares, and which of them a call takes is no simple function
+// of its sizes; so this is what its limits allow: as many as the blocks of keys and the rounds leave for each count of tiles, which changes at multiples of 16 rows.
+int prompt_most_bytes(PromptArgs a, bool tc, size_t* out) {
+  const int tokens = a.tokens;
+  *out = 0;
+  for (int n = 16;; n += 16) {
+    a.tokens = std::min(n, tokens);
+    prompt_pack(a);
+    PromptWork w;
+    if (int rc = prompt_work(a, tc, &w)) return rc;
+    const long long most = std::min<long long>({kMostShares, w.blocks / 2, (long long)kMostRounds * w.at_once / w.items});
+    if (most > 1) *out = std::max(*out, prompt_part_bytes(a, (int)most));
+    if (n >= tokens || (n > 64 && 2 * w.items > (long long)kMostRounds * w.at_once)) return HE_OK;  // (from 64 rows on tiles become more with the rows)
+  }
 }
 int launch_rows(const PromptArgs& a, bool tc, cudaStream_t st) {
   if (tc) {
@@ -364,10 +389,9 @@ size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, 
   if (check_config(cfg, true) || max_q_len < 1 || max_kv_len < 1 || max_q_len > kMaxTokens || max_kv_len > kMaxTokens) return 0;
   PromptArgs a{};
   a.batch = cfg->batch, a.n_kv_heads = cfg->n_kv_heads, a.group = cfg->group_size, a.d = cfg->head_dim, a.dtype = cfg->dtype, a.tokens = max_q_len, a.keys = max_kv_len;
-  int splits = 1;
-  prompt_pack(a);
-  if (prompt_splits(a, on_tensor_cores(a), &splits)) return 0;
-  return std::max(prompt_part_bytes(a, splits), few_rows_workspace(cfg, max_q_len, max_kv_len));
+  size_t most = 0;
+  if (prompt_most_bytes(a, on_tensor_cores(a), &most)) return 0;
+  return std::max(most, few_rows_workspace(cfg, std::min(max_q_len, kMaxGroup / cfg->group_size), 1));  // (of any number of keys the same)
 }
 
 int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
