@@ -314,6 +314,7 @@ int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q
  *                     behind a sequence's end, or behind which its window has passed, may hold anything.
  *   len               [B] int32, tokens that each sequence holds, those of the append under way included. The calls only read it (several layers may share one, and
  *                     one page_table); what exceeds max_pages * page_size counts as that, a negative one as 0.
+ * There may be no pages (n_pages 0: the arrays of pages may be NULL, all of them read as zeros) and no table (max_pages 0: page_table may be NULL, sequences hold nothing).
  * Sequences may share pages that are complete; a page that a sequence still appends to belongs to it alone. A sequence may be cut back by lowering len.
  */
 typedef struct he_pages {

@@ -23,7 +23,7 @@ namespace {
 
 int check_pages(const he_config* cfg, const he_pages* p) {
   if (p == nullptr) return fail(HE_ERR_INVALID_ARG, "pages is null");
-  if (!p->k_pages || !p->v_pages || !p->page_table || !p->len) return fail(HE_ERR_INVALID_ARG, "pages has a null pointer");
+  if (!p->len || (p->max_pages != 0 && !p->page_table) || (p->n_pages != 0 && (!p->k_pages || !p->v_pages))) return fail(HE_ERR_INVALID_ARG, "pages has a null pointer");
   if (!aligned16(p->k_pages) || !aligned16(p->v_pages)) return fail(HE_ERR_INVALID_ARG, "pages must be 16-byte aligned");
   if (p->page_size < 16 || p->page_size > 128 || (p->page_size & (p->page_size - 1)) != 0)
     return fail(HE_ERR_INVALID_ARG, "page_size %d is not 16, 32, 64 or 128", p->page_size);
@@ -31,7 +31,7 @@ int check_pages(const he_config* cfg, const he_pages* p) {
   if ((long long)p->max_pages * p->page_size > kMaxTokens) return fail(HE_ERR_UNSUPPORTED, "%d pages of %d tokens in a sequence: more than 2^24 tokens", p->max_pages, p->page_size);
   if (p->eight_bit != 0 && p->eight_bit != 1) return fail(HE_ERR_INVALID_ARG, "eight_bit %d is not 0 or 1", p->eight_bit);
   if (p->eight_bit) {
-    if (!p->k_scale || !p->v_scale) return fail(HE_ERR_INVALID_ARG, "8-bit pages without scales");
+    if (p->n_pages != 0 && (!p->k_scale || !p->v_scale)) return fail(HE_ERR_INVALID_ARG, "8-bit pages without scales");
     if (cfg->head_dim % 16 != 0) return fail(HE_ERR_UNSUPPORTED, "8-bit pages: head_dim %d is not a multiple of 16", cfg->head_dim);
   }
   return HE_OK;
@@ -142,7 +142,7 @@ int launch_page_attend(const TokenArgs& a, float* part, const PageMaps& maps, cu
 
 // Whether the tensor cores serve a call (where the driver makes tensor maps): rows of bf16 or of codes up to 128 channels, few enough for a map's coordinates.
 bool page_tensor_cores(const he_config* cfg, const he_pages* p) {
-  return (p->eight_bit || cfg->dtype == HE_DTYPE_BF16) && cfg->head_dim <= 128 && (long long)p->n_pages * cfg->n_kv_heads * p->page_size < 0x7FFFFF00LL &&
+  return p->n_pages > 0 && p->max_pages > 0 && (p->eight_bit || cfg->dtype == HE_DTYPE_BF16) && cfg->head_dim <= 128 && (long long)p->n_pages * cfg->n_kv_heads * p->page_size < 0x7FFFFF00LL &&
          page_line_fits(cfg, page_capacity(*p)) && getenv("HE_DISABLE_ATTEND_MMA") == nullptr;
 }
 
@@ -269,9 +269,9 @@ int he_page_attend(const he_config* cfg, const he_pages* pages, const he_score_m
   if (int rc = check_pages(cfg, pages)) return rc;
   if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(HE_ERR_INVALID_ARG, "q or out is null or not 16-byte aligned");
   if (cfg->batch > 65535) return fail(HE_ERR_UNSUPPORTED, "batch %d > 65535 in one call", cfg->batch);
-  if (pages->n_pages == 0 || pages->max_pages == 0) return fail(HE_ERR_INVALID_ARG, "no pages");
   TokenArgs a{};
   a.cfg = *cfg, a.pages = *pages, a.q = q, a.out = out;
+  if (pages->n_pages == 0) a.pages.k_pages = a.pages.v_pages = const_cast<void*>(q);  // (copies of no bytes are given an address all the same)
   if (int rc = check_mod(mod, cfg->head_dim, &a.mod.scale_log2, &a.mod.cap_log2, &a.mod.inv_cap, &a.mod.window, &a.mod.slopes)) return rc;
   a.mod.first_pos = first_pos;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
