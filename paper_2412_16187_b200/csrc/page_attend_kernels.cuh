@@ -35,8 +35,9 @@ constexpr float kPageFactorMax = 3.4028234e38f;  // the largest fp32 number
 // 128 channels took 82 us with 10 warps and 69 with 12 at 512 units of 2304 tokens, and 65 with 16, which spill, where 12 took 60; codes of 64 channels 73 with 12 and 65 with 16.
 template <int D, bool Q8>
 constexpr int kPageWarps = Q8 ? (D == 128 ? 12 : 16) : 8;
+constexpr int kPageBufs = 3;  // tiles of a warp's ring: K and V of a group by turns
 template <int D, bool Q8>
-constexpr int kPageRings = kPageWarps<D, Q8> * (Q8 ? (D == 128 ? 12 : 8) : 24) * 1024;  // bytes of a CTA's rings
+constexpr int kPageRings = kPageWarps<D, Q8> * kPageBufs * kPageGroup * (Q8 ? D : 2 * D);  // bytes of a CTA's rings
 
 struct PageMaps {
   alignas(64) CUtensorMap k, v;
@@ -44,7 +45,7 @@ struct PageMaps {
 
 template <int D, bool Q8>
 struct PageRing {
-  static constexpr int kRowBytes = Q8 ? D : 2 * D, kItemBytes = kPageGroup * kRowBytes, kBytes = kPageRings<D, Q8> / kPageWarps<D, Q8>, kBufs = kBytes / kItemBytes < 3 ? kBytes / kItemBytes : 3;
+  static constexpr int kRowBytes = Q8 ? D : 2 * D, kItemBytes = kPageGroup * kRowBytes, kBytes = kPageBufs * kItemBytes;
 };
 // Floats of a unit's piece: [G][d] outputs, [G] maxima in log2 units, [G] sums.
 __host__ __device__ inline int page_piece(int G, int d) { return G * d + (2 * G + 3) / 4 * 4; }
@@ -294,7 +295,7 @@ struct PageNow {
 template <int D, bool Q8, int NBOX, bool LO, bool FOLD, bool ROWS>
 __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(const __grid_constant__ TokenArgs a, float* part, const __grid_constant__ PageMaps maps) {
   using Ring = PageRing<D, Q8>;
-  constexpr int WARPS = kPageWarps<D, Q8>, THREADS = 32 * WARPS, NBUF = Ring::kBufs, ITEM = Ring::kItemBytes, GRP = kPageGroup, NH = Q8 ? 1 : D / 64;
+  constexpr int WARPS = kPageWarps<D, Q8>, THREADS = 32 * WARPS, NBUF = kPageBufs, ITEM = Ring::kItemBytes, GRP = kPageGroup, NH = Q8 ? 1 : D / 64;
   extern __shared__ __align__(16) unsigned char page_smem_raw[];
   __shared__ __align__(8) unsigned long long ring_bar[WARPS][NBUF];
   __shared__ int ent_unit[2 * WARPS], ent_flag[2 * WARPS];
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
   griddep_launch_dependents();
   // ---- the work: this CTA's part of the line, and where its warps begin
   PageTable<THREADS>& table = *reinterpret_cast<PageTable<THREADS>*>(smem);  // (the rings are not in use yet)
-  static_assert(sizeof(PageTable<THREADS>) <= kPageRings<D, Q8>, "the rings hold the table");
+  static_assert(sizeof(PageTable<THREADS>) <= kPageRings<D, Q8> && kMaxGroup * (D + 2) * sizeof(float) <= Ring::kBytes, "the rings hold the table, a ring the last piece");
   const int each = (a.cfg.batch + THREADS - 1) / THREADS;
   const PageLine line = page_line<WARPS, ROWS>(a, gridDim.x, each, scan_s, table, &empty_s);
   const bool empty = empty_s != 0;  // whether there are sequences that see nothing and whose outputs this CTA writes
@@ -514,8 +515,8 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
 #pragma unroll 1
   for (int t = 0; t < items && ok; t += 2) {
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
-    if constexpr (Q8) {  // (up to three items in a ring: the next group's have not been asked for yet)
-      static_assert(NBUF <= 3, "scales of one group at a time");
+    if constexpr (Q8) {  // (three items in a ring: the next group's have not been asked for yet)
+      static_assert(NBUF == 3, "scales of one group at a time");
 #pragma unroll
       for (int b = 0; b < NBOX; ++b) ks[b] = __shfl_sync(0xFFFFFFFFu, scale, b), vs[b] = __shfl_sync(0xFFFFFFFFu, scale, 2 + b);
     }
@@ -790,8 +791,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
       if (!whole && lane == 0) ent_unit[e] = now.unit, ent_flag[e] = (begins ? 1 : 0) | (ends ? 2 : 0);
       clear();
       fresh = true;
-      // (with two items in a ring the next group's V has not been asked for: it is the one that `ask` stands at)
-      if (t + 2 < items) ask_q(NBUF == 2 ? ask.s * H + ask.h : next.unit);
+      if (t + 2 < items) ask_q(next.unit);  // (its V has been asked for)
     }
   }
   if (!ok) {  // gave up on a copy: count it, and let what is in flight land (bounded) before the rings are reused
