@@ -413,12 +413,12 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
     }
   };
   if (groups > 0) ask_q(ask.s * H + ask.h);
-  // ---- copies. Lane i holds the page of box i & 1 of the group to be asked for, -1 where there is none, and fetches one of its scales.
+  // ---- copies. Lane i holds the page of box i & 1 of the group to be asked for, -1 where there is none or nothing of it is seen, and fetches one of its scales.
   int page = -1;
   float scale = 0.f;
   auto look_up = [&]() {
     const int j = ask.g * GRP + (NBOX == 2 ? 16 * (lane & 1) : 0);
-    if constexpr (!ROWS) page = j < ask.span.hi ? page_of(pg, ask.s, j) : -1;
+    if constexpr (!ROWS) page = j < ask.span.hi && (NBOX == 1 || j + 16 > ask.span.lo) ? page_of(pg, ask.s, j) : -1;
   };
   if (groups > 0) look_up();
   PageNow now{}, next{};  // the group that is worked on, the last one whose V has been asked for
@@ -599,12 +599,7 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
         for (int i = 0; i < NO; ++i) o[i][0] = pair_mul(o[i][0], both), o[i][1] = pair_mul(o[i][1], both);
       }
       tile = step(t + 1);
-      if (edge) {
-        hide(tile);
-#pragma unroll
-        for (int b = 0; b < NBOX; ++b)
-          if (NBOX == 2 && ((now.seen >> (16 * b)) & 0xFFFFu) == 0u) vs[b] = 0.f;  // (a page that is not seen has any scale)
-      }
+      if (edge) hide(tile);
       unsigned long long scales[NBOX];
 #pragma unroll
       for (int b = 0; b < NBOX; ++b) scales[b] = pair_of(vs[b], vs[b]);
