@@ -291,12 +291,13 @@ int he_attend_scored(const he_config* cfg, const he_cache* cache, const he_score
  *     A q_pos outside [-2^24, 2^24] counts as the nearer end.
  *   q_pos NULL: every row sees every key from first_key on, as a decoder's rows see an encoder's states; a window, slopes or a prefix is refused.
  * first_key (device int32 [B, max_q_len]), prefix_len and mod may be NULL. Rows i >= q_len of out are left as they were; a row that sees no key gives zeros. All else
- * (layouts, strides, accuracy, what runs where) as for he_attend_prompt.
- * workspace (16-byte aligned; he_attend_cross_workspace_bytes(cfg, max_q_len, max_kv_len) bytes, which serve every call of up to these lengths, up to 160 MB at head_dim 128; 0 where none is of use) lets
- * few rows over many keys fill the GPU: the keys are then shared out and the shares' results joined in a fixed order. What a call gives does not depend on how large it
- * is beyond what the call needs; a smaller one is refused. It holds nothing from one call to the next; calls that may run at the same time need one each. NULL: a tile
- * of rows walks over all its keys. With it, too, one bf16 row a sequence (d <= 128), or up to 8 rows of a KV head's query heads that all see the same keys, are
- * computed as he_page_attend does (weights of about fp32's accuracy), without it as other rows are.
+ * (layouts, strides, what runs where) as for he_attend_prompt, and so is the accuracy: on the tensor cores weights are rounded to bf16 (2^-8 of each at most) and some of the
+ * exponentials are within 7.5e-5, so that an output is off by up to about 2^-8 of the largest |V| entry, beside its own rounding.
+ * workspace (16-byte aligned; he_attend_cross_workspace_bytes(cfg, max_q_len, max_kv_len) bytes, which serve every call of up to these lengths: up to 160 MB at head_dim
+ * 128, 0 where none is of use) lets few rows over many keys fill the GPU: the keys are then shared out and the shares' results joined in a fixed order. A workspace that is
+ * smaller than a call needs is refused; what the call gives does not depend on how much larger it is. It holds nothing from one call to the next; calls that may run at the
+ * same time need one each. NULL: a tile of rows walks over all its keys. With it, too, one bf16 row a sequence (d <= 128), or up to 8 rows of a KV head's query heads that
+ * all see the same keys, are computed as he_page_attend does (weights of about fp32's accuracy), without it as other rows are.
  */
 size_t he_attend_cross_workspace_bytes(const he_config* cfg, int32_t max_q_len, int32_t max_kv_len);
 int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q, const void* k, const void* v, const int64_t q_strides[3],
@@ -313,7 +314,7 @@ int he_attend_cross(const he_config* cfg, const he_score_mod* mod, const void* q
  *   page_table        [B, max_pages] int32. An entry outside [0, n_pages) is never followed: rows for such a page are dropped, and it reads as zeros. Entries
  *                     behind a sequence's end, or behind which its window has passed, may hold anything.
  *   len               [B] int32, tokens that each sequence holds, those of the append under way included. The calls only read it (several layers may share one, and
- *                     one page_table); what exceeds max_pages * page_size counts as that, a negative one as 0.
+ *                     one page_table); what exceeds max_pages * page_size counts as that (an append drops the rows behind it), a negative one as 0.
  * There may be no pages (n_pages 0: the arrays of pages may be NULL, all of them read as zeros) and no table (max_pages 0: page_table may be NULL, sequences hold nothing).
  * Sequences may share pages that are complete; a page that a sequence still appends to belongs to it alone. A sequence may be cut back by lowering len.
  */

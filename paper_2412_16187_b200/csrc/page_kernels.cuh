@@ -9,8 +9,11 @@
 // rotary pairs, as in rotate_kernel (interleaved pairs are whole in any piece: there the second lies as far on as the first ones of its row's threads reach, so that a warp reads
 // and writes whole sectors; 402 MB 69 us, two pieces side by side 100), keeps the sines and cosines of its pairs for all heads, and holds the pieces of K and V in registers from
 // the read to the write; between the two lies the maximum over the page, by one barrier a head. Rows into pages of their own type run at HBM's rate (537 MB 84 us, 6.4 TB/s). 8-bit
-// pages use 67 % of the issue slots: some 500 instructions a warp for 32 elements a thread, of rotation, maximum, scaling and conversion: 402 MB 68 us (6.0 TB/s; 63 without a
-// rotation; 81 for pages of 128 tokens, one CTA of 1024 threads an SM), 16 ragged prompts of 1024 to 4400 tokens 51 us, HBM 39. One token of 64 sequences 3.9 us, launch and latency.
+// pages: some 500 instructions a warp for 32 elements a thread, of rotation, maximum, scaling and conversion, on 67 % of the issue slots: 402 MB 67 us (6.0 TB/s; 63 without a
+// rotation; 80 for pages of 128 tokens, one CTA of 1024 threads an SM). 16 ragged prompts of 1024 to 4400 tokens 51 to 53 us, HBM 39: CTAs' starts and the last of 2.3 rounds of them.
+// One token of 64 sequences 3.9 us, launch and latency. Where a thread does not hold its place, the sines and, in 8 bits, the rows are fetched and worked out anew for each head and
+// pass: 335 MB of fp32 rows into 8-bit pages of 128 tokens 177 us (HBM 51), 402 MB of bf16 at d = 256 327 (62), 402 MB of which 40 of 128 channels turn 235 (62), 537 MB of bf16 at
+// d = 256 into pages of their own type 153 (82).
 // read: 402 MB of 8-bit pages 64 us (6.3 TB/s).
 #pragma once
 #include "attend_kernels.cuh"
