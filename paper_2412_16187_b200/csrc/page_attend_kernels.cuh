@@ -407,8 +407,13 @@ __global__ void __launch_bounds__(32 * kPageWarps<D, Q8>, 1) page_attend_kernel(
       for (int k = 0; k < 2; ++k) by[k] = __shfl_sync(0xFFFFFFFFu, mine, 4 * (2 * tig + k));
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
-        if constexpr (LO) half_split(f[2 * i] * up, f[2 * i + 1] * up, qf[i], ql[i]);
-        else qf[i] = half_pair(f[2 * i] * up, f[2 * i + 1] * up);
+        if constexpr (LO) {
+          half_split(f[2 * i] * up, f[2 * i + 1] * up, qf[i], ql[i]);
+          if (fabsf(f[2 * i]) == INFINITY) ql[i] &= 0xFFFF0000u;  // (an infinity has no second term)
+          if (fabsf(f[2 * i + 1]) == INFINITY) ql[i] &= 0xFFFFu;
+        } else {
+          qf[i] = half_pair(f[2 * i] * up, f[2 * i + 1] * up);
+        }
       }
     }
   };

@@ -67,3 +67,23 @@ def test_a_scale_and_a_query_whose_product_leaves_fp32(h, g, d, p, dtype):
         got = cache.attend(q, ScoreMod(softcap=cap), first_pos=first).double().view(2, h, g, d)
         want = v.mean(2)[:, :, None].expand_as(got)
         assert bool(((got - want).abs() <= tolerance(want, v.abs().max(), F32, True)).all())
+
+
+@pytest.mark.parametrize("h, g, d, p, dtype", SHAPES, ids=NAMES)
+def test_queries_with_an_infinity(h, g, d, p, dtype):
+    """Scores of -inf alone give zeros, of +inf NaN; a cap makes both finite, here all equal: the mean of V."""
+    gen = torch.Generator(device="cuda").manual_seed(d * p)
+    n = 2 * p + 5
+    cache = paged(gen, 2, h, g, d, p, dtype, True, n)
+    k, v = (torch.randn((2, h, n, d), generator=gen, device="cuda", dtype=dtype) for _ in "kv")
+    k[..., 3] = k[..., 3].abs() + 1.0
+    q = torch.randn((2, h * g, d), generator=gen, device="cuda", dtype=dtype)
+    q[:, 0::2, 3], q[:, 1::2, 3] = torch.inf, -torch.inf
+    cache.length += n
+    cache.append(k, v)
+    got = cache.attend(q)
+    assert bool(torch.isnan(got[:, 0::2]).all()) and not got[:, 1::2].any()
+    got = cache.attend(q, ScoreMod(softcap=20.0)).double().view(2, h, g, d)
+    values = cache.read(n)[1].double()
+    want = values.mean(2)[:, :, None].expand_as(got)
+    assert bool(((got - want).abs() <= tolerance(want, values.abs().max(), F32, True)).all())
