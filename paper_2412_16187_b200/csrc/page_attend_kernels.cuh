@@ -18,7 +18,7 @@
 // are taken times 2^14 (below 2^-38 of the largest they are lost) and split into two half-precision terms, the second in the columns of heads 4..7 up to G = 4, else with
 // products of its own: 2^-22 of each is left out.
 //
-// Measured, d = 128 and G = 4 (HBM's copy rate in brackets): 512 units of 512 to 4096 tokens in 8 bits 59 us (47), of 2304 with fp32 queries 69 (46), 8 units of 32768 22 us (10), 8 of
+// Measured, d = 128 and G = 4 (HBM's copy rate in brackets): 512 units of 512 to 4096 tokens in 8 bits 59 us (47), of 2304 with fp32 queries 70 (46), 8 units of 32768 22 us (10), 8 of
 // 131072 53 us (41); 128 units of 1024 to 8192 tokens in bf16 with bias, a quarter hidden, 55 us (43); 128 rows of d = 64 over 1500 plain keys 15 us (5). A call spends 4 us before its
 // first copy has landed (lengths, the line, page numbers, each a trip to L2), 2 in a CTA's way out and 4 in page_join_kernel; the loop between them reads 5.8 to 6.3 TB/s. It issues 640
 // instructions a group of 8-bit codes on half of its slots (128 of them conversions), 250 of bf16 rows.
