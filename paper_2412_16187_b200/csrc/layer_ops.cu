@@ -219,7 +219,8 @@ int attend_rows(PromptArgs& a, const he_config* cfg, const he_score_mod* mod, co
     a.part = static_cast<float*>(workspace);
   }
   if (a.keys == 0) a.splits = 1;
-  if (int rc = launch_rows(a, tc && a.keys > 0, st)) return rc;
+  const bool far = a.cap_log2 >= kPtFar && a.slopes == nullptr;  // (scores that prompt_tc_kernel with a cap has no form for)
+  if (int rc = launch_rows(a, tc && a.keys > 0 && !far, st)) return rc;
   if (a.splits == 1) return HE_OK;
   const int rows = kJoinThreads / prompt_join_lanes(a.d);  // of a CTA
   const long long ctas = ((long long)a.batch * a.n_kv_heads * a.group * a.tokens + rows - 1) / rows;

@@ -285,6 +285,20 @@ static __device__ __noinline__ void prompt_rows_again(const PromptArgs& a, int s
   }
 }
 
+// The rows i0 + b of one head, b a bit of `rows`, computed anew. By a whole warp.
+static __device__ __noinline__ void prompt_rows_anew(const PromptArgs& a, int s, int head, int i0, uint32_t rows, int n, const PromptKeys keys, volatile int* beat = nullptr) {
+  while (rows != 0u) {
+    int row[kPromptAgain];
+#pragma unroll
+    for (int b = 0; b < kPromptAgain; ++b) {
+      row[b] = rows != 0u ? i0 + __ffs(rows) - 1 : row[b > 0 ? b - 1 : 0];  // (places that stay empty repeat the last row)
+      rows &= rows - 1u;
+    }
+    if (a.dtype == HE_DTYPE_BF16) prompt_compute_again<2>(a, s, head, row, n, keys, beat);
+    else prompt_compute_again<4>(a, s, head, row, n, keys, beat);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ CUDA cores
 //
 // 16 R rows of one query head per CTA, 64 keys at a time. Thread (ty, tx) of 16 x 16 holds the scores of rows R ty .. + R - 1 and keys
@@ -536,6 +550,9 @@ constexpr int kPtSoftRegs = 224, kPtOtherRegs = 56;
 constexpr int kPtAsk = 4;           // steps of an item that are still to be asked for when the next item is fetched
 constexpr int kPtReaders = 10;       // warps that read an item: softmax, products, copies
 constexpr float kPtSlack = 8.f;      // log2 of how far weights may exceed 1 before the output is rescaled
+// Scores are x scale - ref in one step, off from zero at the largest x by what ref = x scale was rounded by: from 2^31 in log2 units on more than an exponential can
+// take. Rows that had such a reference are computed anew. (Rounded products in the loop instead cost every call 1 to 4 %.)
+constexpr float kPtFar = 1073741824.f;  // 2^30
 constexpr float kPtTanhEnd = 7.f;    // see pt_tanh
 constexpr float kPtNearEnd = 0.7f;   // see pt_tanh_near
 constexpr float kPtNearInv = 1e-5f, kPtNearMost = 1e5f;  // the powers of a smaller or larger factor leave fp32: PromptArgs::near_end is -1 there
@@ -859,6 +876,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
                                                                    const __grid_constant__ PromptMaps maps) {
   using T = PromptTc<D>;
   constexpr int NS = T::kStages, NH = D / 64, BOX = kPtTile * 128, EMU = CAP && BIAS ? 2 : CAP || BIAS ? 8 : 12;
+  constexpr bool FAR = !CAP && !BIAS;  // (scores with a bias are rounded first; caps beyond kPtFar are not served here)
   extern __shared__ __align__(16) unsigned char pt_smem_raw[];
   __shared__ __align__(16) uint4 answer_s;
   __shared__ __align__(8) unsigned long long full_s[NS], empty_s[NS], qfull_s[2], qempty_s[2], sfull_s[2], pfull_s[2], odone_s[2], ifull_s[2], iempty_s[2], ask_s, work_s, drain_s;
@@ -866,6 +884,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
   __shared__ PtMore<KIND> more_s;
   __shared__ uint32_t tmem_s;
   __shared__ int abort_s, beat_s;
+  __shared__ bool far_s[2 * kPtTile];  // of each thread of the softmax
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int heads = a.n_kv_heads * (KIND == kOverSelf ? a.group : a.packs), per = by_heads ? heads / 2 : heads;
   const int pack = KIND == kOverSelf ? 0 : a.pack, rows_of = kPtTile >> pack;  // rows of a head in a tile
@@ -931,6 +950,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
     const uint32_t s_t = lane_base + t * kPtTile, o_t = lane_base + 2 * kPtTile + t * D;
     uint32_t blocks = 0, outputs = 0;  // done so far, over all items
     bool ok = true;
+    if (FAR) far_s[tid] = false;
     for (int k = 0; ok && take_item(k); ++k) {
       const PtItem& w = item_s[k & 1];  // (read where it is used: registers are short here)
       int i = tok_of(w, t) + row, head = head_of(w, t);
@@ -1040,6 +1060,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
         if (__any_sync(0xFFFFFFFFu, grown)) {
           const float corr = grown ? pt_ex2(m - mx) : 1.f;  // (a row does not depend on its neighbours)
           if (grown) m = mx;
+          if (FAR && grown && fabsf(mx) >= kPtFar && fabsf(mx) < INFINITY) far_s[tid] = true;
           l *= corr;
           if (it > 0) {  // the product of the block before is done: S of this one was issued behind it
 #pragma unroll
@@ -1094,7 +1115,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
       if (ok && steps > 0) ok = pt_wait(smem_u32(&odone_s[t]), outputs++ & 1, abort_flag, beat);
       if (!ok) break;
       tc_fence_after();
-      if constexpr (KIND == kOverShares) {  // what this share gives, relative to its own maximum
+      const bool far = FAR && far_s[tid];
+      if (far) far_s[tid] = false;
+      if constexpr (KIND == kOverShares) {  // what this share gives, relative to its own maximum; a sum below zero: the row is to be computed anew
         const long long at = prompt_part_row(a, more_s.at[k & 1].share, w.s, head, i);
         float* part = a.part + at * a.d;
 #pragma unroll
@@ -1108,7 +1131,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
           for (int e = 0; e < 32; e += 4)
             if (i < w.n && c + e < a.d) *reinterpret_cast<uint4*>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
-        if (i < w.n) *reinterpret_cast<float2*>(prompt_part_ml(a, at)) = make_float2(m, m != -INFINITY ? l : 0.f);
+        if (i < w.n) *reinterpret_cast<float2*>(prompt_part_ml(a, at)) = make_float2(m, far ? -1.f : m != -INFINITY ? l : 0.f);
         tc_fence_before();
         give_item(k);
         continue;
@@ -1137,8 +1160,9 @@ __global__ void __launch_bounds__(kPtThreads, 1) prompt_tc_kernel(const __grid_c
           if (i < w.n && c + 8 * e < a.d) *reinterpret_cast<uint4*>(out + c + 8 * e) = make_uint4(word[4 * e], word[4 * e + 1], word[4 * e + 2], word[4 * e + 3]);
       }
       const bool bad = !none && l == l && pt_max(nan[0], nan[1]) != pt_max(nan[0], nan[1]);
-      const uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && i < w.n);
+      const uint32_t again = __ballot_sync(0xFFFFFFFFu, bad && !far && i < w.n), anew = __ballot_sync(0xFFFFFFFFu, far);
       __syncwarp();
+      if (FAR && __builtin_expect(anew != 0u, 0)) prompt_rows_anew(a, w.s, head, i - lane, anew, w.n, keys_of(w, k), beat);
       if (again != 0u) prompt_rows_again(a, w.s, head, i - lane, again, w.n, keys_of(w, k), w.base + w.jb[t] * kPtTile, min(w.base + w.je[t] * kPtTile, keys_of(w, k).end), beat);
       tc_fence_before();
       give_item(k);
@@ -1375,6 +1399,7 @@ static __global__ void __launch_bounds__(kJoinThreads, 8) prompt_join_kernel(con
   const int s = (int)min(sequence, (long long)a.batch - 1), n = min(max(a.lens[s], 0), a.tokens);
   const bool some = sequence < a.batch && i < n;
   if (!__any_sync(0xFFFFFFFFu, some)) return;
+  bool far = false;
   float M = -INFINITY, L = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // channels 4 at_lane + e, 128 + 4 at_lane + e
   if (some)
 #pragma unroll 1
@@ -1393,7 +1418,7 @@ static __global__ void __launch_bounds__(kJoinThreads, 8) prompt_join_kernel(con
       for (int k = 0; k < 4; ++k)
         if (z0 + k < a.splits && ml[k].x != -INFINITY) {  // (a share that saw nothing holds anything)
           const float top = fmaxf(M, ml[k].x), ref = top == -INFINITY ? 0.f : top, f = exp2f(M - ref), g = exp2f(ml[k].x - ref);
-          M = top, L = fmaf(ml[k].y, g, L * f);
+          M = top, L = fmaf(ml[k].y, g, L * f), far |= ml[k].y < 0.f;
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
             o[4 * w] = fmaf(v[k][w].x, g, o[4 * w] * f), o[4 * w + 1] = fmaf(v[k][w].y, g, o[4 * w + 1] * f);
@@ -1420,13 +1445,15 @@ static __global__ void __launch_bounds__(kJoinThreads, 8) prompt_join_kernel(con
       *reinterpret_cast<float4*>(static_cast<char*>(a.out) + 4 * (o0 + c)) = make_float4(f[0], f[1], f[2], f[3]);
     }
   }
-  uint32_t odd = __ballot_sync(0xFFFFFFFFu, bad && L == L);
+  const uint32_t anew = __ballot_sync(0xFFFFFFFFu, far);
+  uint32_t odd = __ballot_sync(0xFFFFFFFFu, bad && L == L) | anew;
   __syncwarp();
   while (odd != 0u) {  // row by row, by the whole warp
     const int from = (__ffs(odd) - 1) / lanes * lanes;
     const int s1 = __shfl_sync(0xFFFFFFFFu, s, from), head1 = __shfl_sync(0xFFFFFFFFu, head, from), i1 = __shfl_sync(0xFFFFFFFFu, i, from), n1 = __shfl_sync(0xFFFFFFFFu, n, from);
     const PromptKeys keys = prompt_keys(a, s1);
-    prompt_rows_again(a, s1, head1, i1, 1u, n1, keys, -keys.shift, keys.end);
+    if ((anew >> from) & 1u) prompt_rows_anew(a, s1, head1, i1, 1u, n1, keys);
+    else prompt_rows_again(a, s1, head1, i1, 1u, n1, keys, -keys.shift, keys.end);
     odd &= ~((lanes == 32 ? 0xFFFFFFFFu : (1u << lanes) - 1u) << from);
   }
 }
